@@ -344,6 +344,148 @@ int tq_listing_get_info(tq_listing h, tq_listing_info *out);
 /* Frees the device memory; no work of the handle may be in flight.  NULL is a no-op. */
 int tq_listing_destroy(tq_listing h);
 
+/*
+ * What stands between the products of a decode step: the norm in front of them, the cache of keys and values, attention over
+ * it, and a cache that is kept at a budget.  The products give fp32 y and take bf16 x, and so do these calls.
+ *
+ * All of them run on the caller's stream and return: no synchronisation, no allocation, nothing kept between calls, so they may
+ * be captured in a HIP graph.  Argument structures are read during the call; zero-initialise them and set what you need.
+ * Strides count elements; 0 stands for rows without gaps.
+ */
+#define TQ_BF16 0u
+#define TQ_FP32 1u
+#define TQ_INT8 2u
+
+/*
+ * h = residual + delta, in fp32;  residual_out = h in the residual's type;  y = h / sqrt(mean(h^2) + eps) * weight, from the
+ * unrounded h;  out = y as bf16 (the x of the next product), or as int8 with one scale per row by the rule of the weights
+ * (tq_encode): scale = max|y| / 127, round half to even.  Sums in fp32.  A row with a NaN is NaN throughout, one with an infinity NaN there and zero elsewhere; as int8 its
+ * scale is NaN.
+ *   residual, residual_out: device, [rows][cols], TQ_FP32 or TQ_BF16 (residual_type); residual_out may be residual, or NULL.
+ *   delta: device, fp32 [rows][cols], a product's y, or NULL (nothing is added).
+ *   weight: device, [cols], TQ_FP32 or TQ_BF16 (weight_type).
+ *   out: device, [rows][cols], TQ_BF16 or TQ_INT8 (out_type); out_scale: device, fp32 [rows], with TQ_INT8.
+ * Pointers are aligned to their type; rows whose address and stride are a multiple of 4 values are read faster.  Apart from
+ * residual_out == residual (with equal strides) the buffers do not overlap.  rows may be 0 (nothing is done), cols is 1..2^20.
+ */
+typedef struct tq_norm_args {
+  const void *residual;
+  const float *delta;
+  const void *weight;
+  void *residual_out, *out;
+  float *out_scale;
+  uint32_t rows, cols;
+  uint64_t residual_stride, delta_stride, residual_out_stride, out_stride;
+  float eps;
+  uint32_t residual_type, weight_type, out_type;
+} tq_norm_args;
+int tq_add_rms_norm(const tq_norm_args *args, void *stream);
+
+/*
+ * A cache of keys and values in the caller's device memory, in pages of page_size tokens that sequences own through their
+ * page tables: the key of token slot t of sequence s and head h lies at
+ *   k + (tables[s][t / page_size] * page_stride + h * head_stride + (t % page_size) * slot_stride) elements, its head_dim values side by side.
+ * A page id outside 0..n_pages-1 stands for a page that is not there: nothing is read from it or written to it, and attention takes
+ * its tokens for masked.
+ *   type: TQ_BF16, or TQ_INT8 with fp32 scales k_scale, v_scale [n_pages][kv_heads][page_size] (one per token and head, symmetric).
+ *   page_size: a power of two, 16..1024.  head_dim: a multiple of 16 up to 256.
+ *   page_stride, head_stride, slot_stride: all 0 for pages [kv_heads][page_size][head_dim] without gaps, else multiples of 16
+ *   bytes; k, v and the scales 16-byte aligned.
+ *   tables: device, int32 [n_seqs][table_stride] (0: seq_pages), seq_pages of which are a sequence's: it holds up to seq_pages * page_size
+ *   tokens, its capacity (at most 2^30).
+ *   scores, positions: device, fp32 and int32 [n_seqs][kv_heads][capacity], or NULL: for every token slot the attention weight that
+ *   has gone to it so far, and the token's position.  For caches that are kept at a budget (tq_cache_evict).
+ */
+typedef struct tq_cache {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  const int32_t *tables;
+  float *scores;
+  int32_t *positions;
+  uint32_t type, n_pages, page_size, kv_heads, head_dim, n_seqs, seq_pages, reserved;
+  uint64_t table_stride, page_stride, head_stride, slot_stride;
+} tq_cache;
+
+/*
+ * New tokens: rotary positions on their queries and keys, keys and values into the cache.  Row r is a token of sequence seqs[r]
+ * (NULL: sequence r), goes to token slot slots[r] and has position positions[r] (NULL: its slot).
+ *   q: device, fp32 [rows][heads * head_dim], k, v: fp32 [rows][kv_heads * head_dim], the products' y.
+ *   q_out: device, [rows][heads * head_dim], TQ_FP32 (may be q, with equal strides) or TQ_BF16 (q_out_type).
+ *   cos, sin: device, fp32 [n_positions][rotary_dim / 2].  The first rotary_dim values of a head (a multiple of 8, 0: none) are
+ *   rotated in pairs (a, b) -> (a cos - b sin, a sin + b cos): value i with value i + rotary_dim / 2 (TQ_ROTARY_HALVES), or 2i with 2i + 1
+ *   (TQ_ROTARY_ADJACENT).
+ * Values go into a TQ_BF16 cache rounded to nearest even, into a TQ_INT8 cache by the rule of the weights (scale = absmax / 127;
+ * NaN, if a value is not finite).
+ * Where the cache has scores and positions, the slot's get 0 and positions[r].
+ * A row whose sequence, slot or position is outside the cache or the table of angles is padding: it writes nothing to the
+ * cache, and its q_out is zero.  No two rows may have the same slot of one sequence.
+ */
+#define TQ_ROTARY_HALVES 0u
+#define TQ_ROTARY_ADJACENT 1u
+typedef struct tq_append_args {
+  const float *q, *k, *v;
+  void *q_out;
+  const int32_t *seqs, *slots, *positions;
+  const float *cos, *sin;
+  uint32_t rows, heads, rotary_dim, n_positions;
+  uint64_t q_stride, k_stride, v_stride, q_out_stride;
+  uint32_t q_out_type, pairing;
+} tq_append_args;
+int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *stream);
+
+/*
+ * Attention of one new token per row over the pages of its sequence:
+ *   out[r][h] = sum_t p[t] v[t],  p = softmax over t < lengths[r] of scale * q[r][h] . k[t],  keys and values of head h / (heads / kv_heads).
+ * Row r belongs to sequence seqs[r] (NULL: sequence r).  Rows of one sequence with rising lengths are a prompt or a draft, causally masked.
+ *   q: device, TQ_FP32 or TQ_BF16 (q_type) [rows][heads * head_dim]; an fp32 q is used unrounded.
+ *   out: device, bf16 [rows][heads * head_dim]: the x of the output projection.
+ *   lengths: device, int32 [rows]; lengths beyond the capacity count as the capacity.  A row without tokens (length <= 0, a
+ *   sequence that is not there, only pages that are not there) gives zeros.
+ *   accumulate: 1 adds every token's weight, summed over the query heads of a key/value head, to cache->scores.
+ *   workspace: device, 16-byte aligned, of at least the size tq_attend_workspace gives for the same arguments, zero before the first
+ *   call with it; calls whose execution overlaps need one each.
+ * Logits, softmax statistics and sums are fp32; sums are made in an order that only the arguments and lengths decide, so results repeat.
+ * What lies in a cache beyond a row's length is not used, whatever it holds.  heads is a multiple of kv_heads.
+ */
+typedef struct tq_attend_args {
+  const void *q;
+  void *out;
+  const int32_t *seqs, *lengths;
+  void *workspace;
+  uint64_t workspace_bytes;
+  uint32_t rows, heads;
+  uint64_t q_stride, out_stride;
+  float scale;
+  uint32_t q_type, accumulate, reserved;
+} tq_attend_args;
+int tq_attend(const tq_cache *cache, const tq_attend_args *args, void *stream);
+int tq_attend_workspace(const tq_cache *cache, const tq_attend_args *args, uint64_t *bytes);
+
+/*
+ * Brings every sequence of a cache down to at most `keep` tokens per head.  Of a head's lengths[s] tokens those stay that have the
+ * largest scores (cache->scores); tokens with position >= since[s] (cache->positions; since NULL: none) rank above all others.  Equal ones: the
+ * lowest slots stay.  A NaN ranks below every number.
+ * A token that stays and lies in a slot below `keep` is not moved; those above go, in order, to the slots below that have become
+ * free, keys, values, scales, score and position with them.  (The order of tokens in a cache does not matter to attention: keys
+ * are rotated before they are stored.)  Sequences that have no more than `keep` tokens are left as they are.
+ *   lengths: device, int32 [n_seqs]; lengths_out: min(length, keep), NULL: written to lengths.
+ *   scores_out, positions_out: as cache->scores and cache->positions, which they replace as output (slots up to the new length are
+ *   written); NULL: in place.
+ *   workspace: as for tq_attend, but with any contents.
+ */
+typedef struct tq_evict_args {
+  int32_t *lengths;
+  int32_t *lengths_out;
+  const int32_t *since;
+  float *scores_out;
+  int32_t *positions_out;
+  void *workspace;
+  uint64_t workspace_bytes;
+  uint32_t keep, reserved;
+} tq_evict_args;
+int tq_cache_evict(const tq_cache *cache, const tq_evict_args *args, void *stream);
+int tq_cache_evict_workspace(const tq_cache *cache, const tq_evict_args *args, uint64_t *bytes);
+
 #ifdef __cplusplus
 }
 #endif

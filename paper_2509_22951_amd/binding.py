@@ -25,6 +25,7 @@ EXPORTS = [
     "tq_step_create", "tq_step_launch", "tq_step_get_info", "tq_step_destroy",
     "tq_listing_build_table", "tq_listing_compress", "tq_listing_create", "tq_listing_decompress", "tq_listing_get_info",
     "tq_listing_destroy",
+    "tq_add_rms_norm", "tq_cache_append", "tq_attend", "tq_attend_workspace", "tq_cache_evict", "tq_cache_evict_workspace",
 ]
 
 
@@ -64,6 +65,49 @@ class TqListingInfo(ctypes.Structure):
 
     def as_dict(self):
         return {n: int(getattr(self, n)) for n, _ in self._fields_ if n != "reserved"}
+
+
+_VP, _U32, _U64, _F32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float
+
+
+class _Args(ctypes.Structure):
+    """An argument structure of tq.h; fields that are not named are zero."""
+
+    def __init__(self, **fields):
+        unknown = set(fields) - {n for n, _ in self._fields_}
+        if unknown:
+            raise TypeError(f"{type(self).__name__} has no {', '.join(sorted(unknown))}")
+        super().__init__(**fields)
+
+
+class TqCache(_Args):
+    _fields_ = [("k", _VP), ("v", _VP), ("k_scale", _VP), ("v_scale", _VP), ("tables", _VP), ("scores", _VP), ("positions", _VP),
+                ("type", _U32), ("n_pages", _U32), ("page_size", _U32), ("kv_heads", _U32), ("head_dim", _U32), ("n_seqs", _U32),
+                ("seq_pages", _U32), ("reserved", _U32),
+                ("table_stride", _U64), ("page_stride", _U64), ("head_stride", _U64), ("slot_stride", _U64)]
+
+
+class TqNormArgs(_Args):
+    _fields_ = [("residual", _VP), ("delta", _VP), ("weight", _VP), ("residual_out", _VP), ("out", _VP), ("out_scale", _VP),
+                ("rows", _U32), ("cols", _U32), ("residual_stride", _U64), ("delta_stride", _U64), ("residual_out_stride", _U64),
+                ("out_stride", _U64), ("eps", _F32), ("residual_type", _U32), ("weight_type", _U32), ("out_type", _U32)]
+
+
+class TqAppendArgs(_Args):
+    _fields_ = [("q", _VP), ("k", _VP), ("v", _VP), ("q_out", _VP), ("seqs", _VP), ("slots", _VP), ("positions", _VP), ("cos", _VP),
+                ("sin", _VP), ("rows", _U32), ("heads", _U32), ("rotary_dim", _U32), ("n_positions", _U32), ("q_stride", _U64),
+                ("k_stride", _U64), ("v_stride", _U64), ("q_out_stride", _U64), ("q_out_type", _U32), ("pairing", _U32)]
+
+
+class TqAttendArgs(_Args):
+    _fields_ = [("q", _VP), ("out", _VP), ("seqs", _VP), ("lengths", _VP), ("workspace", _VP), ("workspace_bytes", _U64), ("rows", _U32),
+                ("heads", _U32), ("q_stride", _U64), ("out_stride", _U64), ("scale", _F32), ("q_type", _U32), ("accumulate", _U32),
+                ("reserved", _U32)]
+
+
+class TqEvictArgs(_Args):
+    _fields_ = [("lengths", _VP), ("lengths_out", _VP), ("since", _VP), ("scores_out", _VP), ("positions_out", _VP), ("workspace", _VP),
+                ("workspace_bytes", _U64), ("keep", _U32), ("reserved", _U32)]
 
 
 def lib_path() -> str:
@@ -141,6 +185,11 @@ def load() -> ctypes.CDLL:
     lib.tq_listing_get_info.argtypes = [vp, ctypes.POINTER(TqListingInfo)]
     lib.tq_listing_destroy.restype = ci
     lib.tq_listing_destroy.argtypes = [vp]
+    lib.tq_add_rms_norm.restype = ci
+    lib.tq_add_rms_norm.argtypes = [vp, vp]
+    for name in ("tq_cache_append", "tq_attend", "tq_attend_workspace", "tq_cache_evict", "tq_cache_evict_workspace"):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = [vp, vp, vp]
     _LIB = lib
     return lib
 
@@ -447,3 +496,73 @@ class Listing:
             self.close()
         except Exception:
             pass
+
+
+# ---- between the products of a decode step (marshalling only; fields as in tq.h, pointers as integers) ----
+
+TQ_BF16, TQ_FP32, TQ_INT8 = 0, 1, 2
+TQ_ROTARY_HALVES, TQ_ROTARY_ADJACENT = 0, 1
+
+
+class Cache:
+    """Description of a paged cache in the caller's memory, as tq_cache; the calls below keep it."""
+
+    def __init__(self, **fields):
+        self.args = TqCache(**fields)
+        self.address = ctypes.addressof(self.args)
+
+
+class _CacheCall:
+    """Arguments of a call on a cache, marshalled once and launched many times."""
+    _entry, _type = "", _Args
+
+    def __init__(self, cache: Cache, **fields):
+        self.cache, self.args = cache, self._type(**fields)
+        self._call, self._at = getattr(load(), self._entry), (cache.address, ctypes.addressof(self.args))
+
+    def launch(self, stream: int = 0) -> None:
+        rc = self._call(*self._at, stream)
+        if rc:
+            _check(rc)
+
+    @classmethod
+    def _workspace(cls, cache: Cache, fields: dict) -> int:
+        args, n = cls._type(**fields), _U64()
+        _check(getattr(load(), cls._entry + "_workspace")(cache.address, ctypes.addressof(args), ctypes.addressof(n)))
+        return n.value
+
+
+class AddNorm:
+    """tq_add_rms_norm with arguments marshalled once."""
+
+    def __init__(self, **fields):
+        self.args = TqNormArgs(**fields)
+        self._call, self._at = load().tq_add_rms_norm, ctypes.addressof(self.args)
+
+    def launch(self, stream: int = 0) -> None:
+        rc = self._call(self._at, stream)
+        if rc:
+            _check(rc)
+
+
+class CacheAppend(_CacheCall):
+    """tq_cache_append with arguments marshalled once."""
+    _entry, _type = "tq_cache_append", TqAppendArgs
+
+
+class Attend(_CacheCall):
+    """tq_attend with arguments marshalled once.  The workspace is zero before the first launch."""
+    _entry, _type = "tq_attend", TqAttendArgs
+
+    @classmethod
+    def workspace_bytes(cls, cache: Cache, **fields) -> int:
+        return cls._workspace(cache, fields)
+
+
+class CacheEvict(_CacheCall):
+    """tq_cache_evict with arguments marshalled once."""
+    _entry, _type = "tq_cache_evict", TqEvictArgs
+
+    @classmethod
+    def workspace_bytes(cls, cache: Cache, **fields) -> int:
+        return cls._workspace(cache, fields)

@@ -1,0 +1,226 @@
+"""tq_attend against the formula in 64 bits.
+
+Tolerances.  A logit in units of log 2 is a sum of fp32 products of exact operands: with dims of N(0, 1) keys and queries its terms
+add up to some 2^5 in magnitude, so it is off by at most 2^5 * 2^-22, and a weight relatively as much; a weight enters the second
+product with 16 bits (2^-17); the sums are fp32.  All in all 2^-15 of sum p |v| <= 2^-15 max |v|, taken twice; rounding the result
+to bf16 adds 2^-8 of it.  Scores: the weights' 2^-15, taken twice, of what is added, and fp32's rounding of the sum."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2509_22951_amd as tq
+from paged import Paged, attend_call, attend_reference, ptr, stream
+
+pytestmark = pytest.mark.gpu
+
+
+def queries(rows, heads, dim, seed=0, dtype=torch.float32):
+    return torch.randn((rows, heads, dim), generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def close(out, want, p):
+    vmax = p.values("v").nan_to_num(0, 0, 0).abs().max()
+    off = (out.cpu().double() - want).abs()
+    assert (off <= want.abs() * 2.0 ** -8 + vmax * 2.0 ** -14).all(), float((off - want.abs() * 2.0 ** -8).max() / vmax)
+
+
+def run(p, q, lengths, **more):
+    call, out = attend_call(p.describe(), p, q, lengths, **more)
+    call.launch(stream())
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 31, 33, 100, 127, 128, 129, 500, 1023, 1024, 1025, 2000, 4100])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_lengths(length, kind):
+    p = Paged(2, -(-length // 16) + 1, kind=kind, seed=length)
+    q = queries(2, 8, 64, length)
+    lengths = ints([length, max(1, length - 7)])
+    close(run(p, q, lengths), attend_reference(p, q, lengths)[0], p)
+
+
+@pytest.mark.parametrize("dim", [16, 32, 48, 64, 80, 96, 112, 128, 144, 192, 240, 256])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_head_dims(dim, kind):
+    p = Paged(3, 5, dim=dim, page=32, kind=kind, seed=dim)
+    q = queries(3, 6, dim, dim)
+    lengths = ints([150, 7, 64])
+    close(run(p, q, lengths), attend_reference(p, q, lengths)[0], p)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (2, 2), (3, 1), (8, 1), (9, 1), (16, 1), (24, 8), (20, 4), (34, 2), (71, 1)])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_groups_of_query_heads(heads, kv_heads, kind):
+    p = Paged(2, 5, kv_heads=kv_heads, dim=64, kind=kind, seed=heads)
+    q = queries(2, heads, 64, heads)
+    lengths = ints([70, 33])
+    close(run(p, q, lengths), attend_reference(p, q, lengths)[0], p)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 1024])
+def test_pages(page):
+    for kind in ("bf16", "int8"):
+        p = Paged(3, -(-1500 // page), page=page, kind=kind, seed=page)
+        q = queries(3, 4, 64, page)
+        lengths = ints([1500, 1, 777])
+        close(run(p, q, lengths), attend_reference(p, q, lengths)[0], p)
+
+
+@pytest.mark.parametrize("order", ["pthd", "hptd", "tphd"])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_pools_in_another_order_with_gaps(order, kind):
+    p = Paged(2, 6, kv_heads=3, dim=80, kind=kind, order=order, table_stride=11)
+    q = queries(2, 6, 80)
+    lengths = ints([90, 41])
+    close(run(p, q, lengths), attend_reference(p, q, lengths)[0], p)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_query_types_strides_and_addresses(dtype):
+    p = Paged(3, 4, dim=64)
+    buf = queries(3, 9, 64, dtype=dtype).view(3, -1)
+    q = buf.as_strided((3, 8, 64), (buf.stride(0), 64, 1), 3)
+    out = torch.full((3, 700), 7, dtype=torch.bfloat16, device="cuda")
+    lengths = ints([60, 3, 17])
+    o = out.as_strided((3, 8, 64), (700, 64, 1), 1)
+    run(p, q, lengths, out=o, q_stride=buf.stride(0), out_stride=700)
+    close(o, attend_reference(p, q, lengths)[0], p)
+    assert (out[:, 0] == 7).all() and (out[:, 513:] == 7).all()
+
+
+def test_rows_without_tokens_and_sequences_that_are_not_there():
+    p = Paged(4, 3)
+    q = queries(6, 4, 64)
+    lengths, seqs = ints([0, -5, 20, 20, 48, 99999]), ints([0, 1, -1, 4, 3, 2])
+    out = run(p, q, lengths, seqs=seqs)
+    assert (out[:4] == 0).all()
+    close(out, attend_reference(p, q, lengths, seqs)[0], p)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_what_lies_beyond_a_length_is_not_used(kind):
+    p = Paged(3, 4, kind=kind)
+    q = queries(3, 4, 64)
+    lengths = ints([0, 21, 33])
+    want = attend_reference(p, q, lengths)[0]
+    for s, n in enumerate([0, 21, 33]):
+        for t in range(n, p.capacity):
+            p.set_slot(s, t, [float("nan"), float("inf"), float("-inf"), torch.finfo(torch.bfloat16).min][t % 4])
+    close(run(p, q, lengths), want, p)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_pages_that_are_not_there_are_masked(kind):
+    p = Paged(3, 80, kind=kind)
+    p.tables[0, ::2] = -1
+    p.tables[1] = p.n_pages
+    p.tables[2, 0], p.tables[2, 1], p.tables[2, 70:] = -1, 2 ** 31 - 1, -7
+    q = queries(3, 4, 64)
+    lengths = ints([1280, 1280, 1279])
+    out = run(p, q, lengths)
+    assert (out[1] == 0).all()
+    close(out, attend_reference(p, q, lengths)[0], p)
+
+
+def test_large_logits_and_equal_ones():
+    p = Paged(2, 70)
+    p.k[:] = p.k * 30
+    q = queries(2, 4, 64) * 20
+    q[1] = 0
+    lengths = ints([1100, 1100])
+    want, _ = attend_reference(p, q, lengths)
+    out = run(p, q, lengths)
+    # logits in the thousands: their fp32 error, 2^13 * 2^-22, is what their weights are off
+    vmax = p.values("v").abs().max()
+    assert ((out[0].cpu().double() - want[0]).abs() <= want[0].abs() * 2.0 ** -8 + vmax * 2.0 ** -8).all()
+    close(out[1], want[1], p)
+
+
+def test_a_nan_within_the_length_reaches_the_result():
+    p = Paged(2, 70)
+    p.set_slot(0, 1050, float("nan"))
+    q = queries(2, 4, 64)
+    lengths = ints([1060, 1060])
+    out = run(p, q, lengths)
+    assert torch.isnan(out[0]).all() and torch.isfinite(out[1]).all()
+
+
+def test_rows_of_one_sequence_are_a_causal_prompt():
+    p = Paged(2, 10, kv_heads=2)
+    q = queries(40, 4, 64)
+    lengths, seqs = ints(list(range(100, 140))), ints([1] * 40)
+    close(run(p, q, lengths, seqs=seqs), attend_reference(p, q, lengths, seqs)[0], p)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 64), (24, 8, 128), (18, 2, 96), (4, 4, 256)])
+def test_weights_are_added_to_the_scores(kind, heads, kv_heads, dim):
+    p = Paged(4, 90, kv_heads=kv_heads, dim=dim, kind=kind, marks=True)
+    before = p.scores.cpu().double()
+    q = queries(4, heads, dim)
+    lengths = ints([1333, 0, 17, 1440])
+    out = run(p, q, lengths, accumulate=True)
+    want, added = attend_reference(p, q, lengths)
+    close(out, want, p)
+    off = (p.scores.cpu().double() - before - added).abs()
+    assert (off <= added * 2.0 ** -14 + (before + added) * 2.0 ** -23).all(), float(off.max())
+    untouched = added == 0
+    assert torch.equal(p.scores.cpu()[untouched], before.float()[untouched])
+
+
+def test_scores_of_several_rows_of_one_sequence_and_again():
+    p = Paged(3, 6, marks=True)
+    before = p.scores.cpu().double()
+    q = queries(5, 4, 64)
+    lengths, seqs = ints([50, 51, 20, 52, 9]), ints([2, 2, 0, 2, 7])
+    call, out = attend_call(p.describe(), p, q, lengths, seqs=seqs, accumulate=True)
+    for _ in range(3):
+        call.launch(stream())
+    torch.cuda.synchronize()
+    want, added = attend_reference(p, q, lengths, seqs)
+    close(out, want, p)
+    off = (p.scores.cpu().double() - before - 3 * added).abs()
+    assert (off <= added * 2.0 ** -12 + (before + 3 * added) * 2.0 ** -21).all()
+
+
+def test_results_repeat_and_the_workspace_serves_calls_of_any_lengths():
+    p = Paged(5, 130, kv_heads=2, dim=128, page=32, marks=True)
+    q = queries(5, 6, 128)
+    lengths = ints([1, 1, 1, 1, 1])
+    call, out = attend_call(p.describe(), p, q, lengths, accumulate=True)
+    seen = {}
+    for n in ([4000, 3, 0, 2047, 1024], [1, 1, 1, 1, 1], [4160, 4160, 4160, 4160, 4160], [4000, 3, 0, 2047, 1024], [0, 0, 0, 0, 0], [4000, 3, 0, 2047, 1024]):
+        lengths.copy_(ints(n))
+        p.scores.zero_()
+        call.launch(stream())
+        torch.cuda.synchronize()
+        close(out, attend_reference(p, q, lengths)[0], p)
+        key = tuple(n)
+        if key in seen:
+            assert torch.equal(seen[key][0], out) and torch.equal(seen[key][1], p.scores)
+        seen[key] = (out.clone(), p.scores.clone())
+
+
+def test_a_pool_beyond_32_bits_of_offset():
+    """Pages more than 2^31 elements into the pool."""
+    p = Paged(1, 4, kv_heads=2, dim=64)
+    base = 2 ** 31 // (2 * 16 * 64) + 5
+    far = p.n_pages + base
+    for name in ("k", "v"):
+        pool = torch.empty((far, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+        pool[base:] = getattr(p, name)
+        setattr(p, name, pool)
+    q = queries(1, 4, 64)
+    lengths = ints([60])
+    p.tables += base
+    p.n_pages = far
+    out = run(p, q, lengths)
+    p.k, p.v = p.k[base:].clone(), p.v[base:].clone()
+    p.tables -= base
+    p.n_pages -= base
+    close(out, attend_reference(p, q, lengths)[0], p)
