@@ -17,9 +17,9 @@
 namespace tq {
 namespace {
 
-constexpr int kAttendWaves = 4, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
+constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
-constexpr uint32_t kMaxGroups = 512, kMinShare = 2;                       // workgroups of a launch; units of one
+constexpr uint32_t kMaxGroups = 256, kMinShare = 1;                       // workgroups of a launch; units of one
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttendView {
@@ -50,10 +50,10 @@ typedef __attribute__((address_space(4))) const int32_t constant_i32;
 template <int DIM, bool INT8>
 struct Tile {
   static constexpr int kSteps = DIM / 32, kVals = DIM / 16;   // contraction steps of the logits; a lane's dims of a value
-  static constexpr int kKeyWords = INT8 ? kSteps * 2 : kSteps * 4, kValWords = INT8 ? kVals / 4 : kVals / 2;
-  uint32_t k[2][kKeyWords], v[8][kValWords];
+  static constexpr int kLoads = INT8 ? kSteps / 2 : kSteps;   // 16-byte loads of a key
+  static constexpr int kValWords = INT8 ? kVals / 4 : kVals / 2;
+  uint32_t k[2][4 * kLoads], v[8][kValWords];
   float4 ks[2], vs[2];
-  uint32_t limit[2];   // tokens of a 16-token block that take part
 };
 
 template <int WORDS>
@@ -90,297 +90,336 @@ __device__ __forceinline__ uint32_t prefix_sum(uint32_t v) {
 // workgroup leaves its maximum, total and weighted sum in memory and counts itself in, and the last one joins them, in the order
 // of the line.  Nobody waits for anybody.
 //
-// A wavefront always has the next tile's loads on their way while it works on one: they are requested without a condition, so
-// that the wait for a tile counts the loads behind it (the last tile is requested again in place of one that is not there, and a page
-// that is not there is read as page 0 and masked).
+// A wavefront asks for the next tile's keys as soon as the logits of this one are made, and for its values when they are multiplied
+// in: the loads are requested without a condition, so that a wait counts the loads behind those it is for (the last tile is
+// requested again in place of one that is not there, and a page that is not there is read as page 0 and masked).
 template <int DIM, bool INT8, bool TRACK>
-__global__ __launch_bounds__(kAttendThreads, DIM == 256 ? 1 : 2) void k_attend(CacheView c, AttendView a) {
+__global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, AttendView a) {
   using T = Tile<DIM, INT8>;
   __shared__ __attribute__((aligned(16))) float lds_sum[kAttendWaves * kHeads * (DIM + 4)];   // [wave][head][DIM + 4]: heads in other banks
-  __shared__ float lds_max[16 * kHeads], lds_total[16 * kHeads];                        // [wave or group][head]
+  __shared__ bf16x8 lds_q[T::kSteps][2][64];                // [step][0]: upper (columns 0..7) and middle 8 bits of q, [1]: lower ones, beside zeros
+  __shared__ float lds_max[kAttendWaves * kHeads], lds_total[kAttendWaves * kHeads];            // [wave or group][head]
   __shared__ uint32_t lds_before;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, n = lane % 16, head = n % 8, part = n / 8;
   const uint32_t D = c.head_dim, per_kv = a.chunks / c.kv_heads;
   auto scalar = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
 
   // this workgroup's share, and the row it begins in
-  auto row_units = [&](uint32_t r) {
-    uint32_t seq;
-    return r < a.rows ? units_of(row_length(c, a, r, &seq)) : 0u;
+  uint32_t lane_length = 0, lane_seq = 0;   // of row (r & ~63) + lane
+  auto look_at = [&](uint32_t first) {
+    if (first + lane < a.rows) lane_length = row_length(c, a, first + lane, &lane_seq);
+    return prefix_sum(first + lane < a.rows ? units_of(lane_length) : 0u);
   };
-  uint32_t all = 0;
-  for (uint32_t r = 0; r < a.rows; r += 64) all += scalar(__shfl(prefix_sum(row_units(r + lane)), 63));
+  uint32_t upto = 0, all = 0;
+  for (uint32_t first = (a.rows - 1) & ~63u;; first -= 64) {   // (the first rows last: they stay in the lanes)
+    upto = look_at(first);
+    all += scalar(__shfl(upto, 63));
+    if (first == 0) break;
+  }
   all *= a.chunks;
   const uint32_t share = max(kMinShare, (all + gridDim.x - 1) / gridDim.x);
   uint32_t pos = blockIdx.x * share;
   const uint32_t stop = min(pos + share, all);
   if (pos >= stop) return;
   uint32_t r = 0, row_first = 0;
-  for (uint32_t base = 0;; base += 64) {   // (all > pos: the row is found)
-    const uint32_t upto = prefix_sum(row_units(base + lane));
+  for (;;) {   // (all > pos: the row is found)
     const uint64_t beyond = __ballot(row_first + upto * a.chunks > pos);
     if (beyond) {
       const uint32_t at = (uint32_t)__builtin_ctzll(beyond);
-      r = base + at;
+      r += at;
       if (at) row_first += scalar(__shfl(upto, at - 1)) * a.chunks;
       break;
     }
     row_first += scalar(__shfl(upto, 63)) * a.chunks;
+    r += 64;
+    upto = look_at(r);
   }
 
-  while (pos < stop) {
-  uint32_t seq;
-  const uint32_t length = scalar(row_length(c, a, r, &seq)), units = units_of(length);
-  seq = scalar(seq);
-  const uint32_t pair = (pos - row_first) / units, unit = (pos - row_first) % units, unit_end = min(units, unit + (stop - pos));
-  const uint32_t kv = pair / per_kv, chunk = pair % per_kv;
-  const uint32_t begin = unit * kUnit, end = min(length, unit_end * kUnit);
-  const uint32_t first_head = kv * a.group + chunk * kHeads, n_heads = min((uint32_t)kHeads, a.group - chunk * kHeads);
-  constant_i32* table = (constant_i32*)(c.tables + (uint64_t)seq * c.table_stride);
-
-  // the query's parts: [step][0]: upper (columns 0..7) and middle 8 bits, [1]: lower ones, beside zeros
-  bf16x8 q[T::kSteps][2];
-#pragma unroll
-  for (int s = 0; s < T::kSteps; ++s) {
-    const uint32_t d0 = INT8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float x = 0.f;
-      if (head < n_heads && d0 < D) {
-        const uint64_t at = r * a.q_stride + (first_head + head) * D + d0 + j;
-        x = (a.q16 ? bf16_value(((const uint16_t*)a.q)[at]) : ((const float*)a.q)[at]) * a.scale;
-      }
-      const __bf16 hi = (__bf16)x, mid = (__bf16)(x - (float)hi), lo = (__bf16)(x - (float)hi - (float)mid);
-      q[s][0][j] = part ? mid : hi;
-      q[s][1][j] = part ? (__bf16)0.f : lo;
-    }
-  }
-
-  f32x4 o[T::kVals];
-#pragma unroll
-  for (int b = 0; b < T::kVals; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float top = -INFINITY, total = 0.f;
-
-  struct Pages {
-    uint32_t id[2];
-  };
-  auto pages_of = [&](uint32_t t) {
-    Pages p;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) p.id[b] = (uint32_t)table[min(t + 16 * b, end - 1) >> c.page_shift];
-    return p;
-  };
   // a lane's places in a block of 16 tokens: dims that a head does not have are read as its first ones, against zeros of q, and dropped
   constexpr uint32_t kSize = INT8 ? 1 : 2;
-  uint32_t key_at[INT8 ? T::kSteps / 2 : T::kSteps];
+  const uint32_t slot_bytes = kSize * (uint32_t)c.slot_stride;
+  uint32_t key_at[T::kLoads];
 #pragma unroll
-  for (int s = 0; s < (INT8 ? T::kSteps / 2 : T::kSteps); ++s) {
+  for (int s = 0; s < T::kLoads; ++s) {
     const uint32_t d0 = INT8 ? 64 * s + 16 * g : 32 * s + 8 * g;
-    key_at[s] = kSize * (d0 < D ? d0 : 0);
+    key_at[s] = n * slot_bytes + kSize * (d0 < D ? d0 : 0);
   }
-  const uint32_t val_at = kSize * (n * T::kVals < D ? n * T::kVals : 0);
-  auto fetch = [&](T& x, uint32_t t, const Pages& p) {
+  const uint32_t val_at = 4 * g * slot_bytes + kSize * (n * T::kVals < D ? n * T::kVals : 0);
+
+  while (pos < stop) {
+    const uint32_t length = (uint32_t)__builtin_amdgcn_readlane((int)lane_length, r & 63), seq = (uint32_t)__builtin_amdgcn_readlane((int)lane_seq, r & 63);
+    const uint32_t units = units_of(length);
+    const uint32_t pair = (pos - row_first) / units, unit = (pos - row_first) % units, unit_end = min(units, unit + (stop - pos));
+    const uint32_t kv = pair / per_kv, chunk = pair % per_kv;
+    const uint32_t begin = unit * kUnit, end = min(length, unit_end * kUnit);
+    const uint32_t first_head = kv * a.group + chunk * kHeads, n_heads = min((uint32_t)kHeads, a.group - chunk * kHeads);
+    constant_i32* table = (constant_i32*)(c.tables + (uint64_t)seq * c.table_stride);
+
+    T x;
+    f32x4 o[T::kVals];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint32_t at = t + 16 * b;
-      x.limit[b] = p.id[b] < c.n_pages && at < end ? min(end - at, 16u) : 0u;
-      const uint32_t page = p.id[b] < c.n_pages ? p.id[b] : 0, slot = at & ((1u << c.page_shift) - 1);
-      const uint64_t block = kSize * ((uint64_t)page * c.page_stride + kv * c.head_stride + slot * c.slot_stride);
-      const char* key = c.k + block + kSize * (n * c.slot_stride);
+    for (int b = 0; b < T::kVals; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, total = 0.f;
+    const uint32_t rounds = end > begin ? unit_end - unit : 0;   // rounds of kUnit tokens, the same for every wavefront
+    struct Pages {
+      uint32_t id[2];
+    };
+    struct Blocks {         // two blocks of 16 tokens: their first byte in a pool, their first scale, how many tokens take part
+      uint64_t at[2], mark[2];
+      uint32_t limit[2];
+    };
+    auto tile_of = [&](uint32_t i) { return begin + i * kUnit + wave * kTile; };
+    auto held = [&](uint32_t i) { return min(tile_of(min(i, rounds - 1)), (end - 1) & ~(kTile - 1u)); };   // a tile that is there
+    auto pages_of = [&](uint32_t i) {
+      Pages p;
 #pragma unroll
-      for (int s = 0; s < (INT8 ? T::kSteps / 2 : T::kSteps); ++s) load_words<4>(&x.k[b][4 * s], key + key_at[s]);
+      for (int b = 0; b < 2; ++b) p.id[b] = (uint32_t)table[min(held(i) + 16 * b, end - 1) >> c.page_shift];
+      return p;
+    };
+    auto blocks_of = [&](uint32_t i, const Pages& p) {
+      Blocks w;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + block + (kSize * ((4 * g + j) * c.slot_stride) + val_at));
-      if constexpr (INT8) {
-        const uint64_t mark = (((uint64_t)page * c.kv_heads + kv) << c.page_shift) + slot + 4 * g;
-        x.ks[b] = *(const float4*)(c.k_scale + mark);
-        x.vs[b] = *(const float4*)(c.v_scale + mark);
+      for (int b = 0; b < 2; ++b) {
+        const uint32_t at = held(i) + 16 * b, want = tile_of(i) + 16 * b, id = p.id[b];
+        w.limit[b] = id < c.n_pages && want < end ? min(end - want, 16u) : 0u;
+        const uint32_t page = id < c.n_pages ? id : 0, slot = at & ((1u << c.page_shift) - 1);
+        w.at[b] = kSize * ((uint64_t)page * c.page_stride + kv * c.head_stride + slot * c.slot_stride);
+        w.mark[b] = INT8 ? (((uint64_t)page * c.kv_heads + kv) << c.page_shift) + slot : 0;
+      }
+      return w;
+    };
+    auto fetch_keys = [&](const Blocks& w) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const char* from = c.k + w.at[b];
+#pragma unroll
+        for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + key_at[s]);
+        if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
+      }
+    };
+    auto fetch_values = [&](const Blocks& w) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + val_at);
+        if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
+      }
+    };
+    Blocks now;
+    Pages ahead;
+    if (rounds) {
+      now = blocks_of(0, pages_of(0));
+      ahead = pages_of(1);
+      fetch_keys(now);
+      fetch_values(now);
+    }
+    // the query's parts, for all wavefronts
+    for (uint32_t i = threadIdx.x; i < T::kSteps * 64; i += kAttendThreads) {
+      const uint32_t s = i / 64, qg = i % 64 / 16, qn = i % 16, qh = qn % 8;
+      const uint32_t d0 = INT8 ? 64 * (s / 2) + 16 * qg + 8 * (s % 2) : 32 * s + 8 * qg;
+      bf16x8 q0, q1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v = 0.f;
+        if (qh < n_heads && d0 < D) {
+          const uint64_t at = r * a.q_stride + (first_head + qh) * D + d0 + j;
+          v = (a.q16 ? bf16_value(((const uint16_t*)a.q)[at]) : ((const float*)a.q)[at]) * a.scale;
+        }
+        const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
+        q0[j] = qn / 8 ? mid : hi;
+        q1[j] = qn / 8 ? (__bf16)0.f : lo;
+      }
+      lds_q[s][0][i % 64] = q0;
+      lds_q[s][1][i % 64] = q1;
+    }
+    __syncthreads();
+
+    if (rounds) {
+      for (uint32_t round = 0;; ++round) {
+        const uint32_t t = tile_of(round);
+        const Blocks next = blocks_of(round + 1, ahead);
+        ahead = pages_of(round + 2);
+        if constexpr (DIM == 256) asm volatile("" ::: "memory");   // q is read from LDS for every tile: registers are for what is on its way
+        f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < T::kSteps; ++s) {
+          const bf16x8 q0 = lds_q[s][0][lane], q1 = lds_q[s][1][lane];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            bf16x8 key;
+            if constexpr (INT8) key = i8x8_to_bf16x8(make_uint2(x.k[b][2 * s], x.k[b][2 * s + 1]));
+            else key = __builtin_bit_cast(bf16x8, make_uint4(x.k[b][4 * s], x.k[b][4 * s + 1], x.k[b][4 * s + 2], x.k[b][4 * s + 3]));
+            l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q0, l[b], 0, 0, 0);
+            l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q1, l[b], 0, 0, 0);
+          }
+        }
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = ror8_sum(l[i / 4][i % 4]);
+          if constexpr (INT8) p[i] *= (&x.ks[i / 4].x)[i % 4];
+        }
+        fetch_keys(next);
+        if (now.limit[0] < 16 || now.limit[1] < 16) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (4 * g + i % 4 >= now.limit[i / 4]) p[i] = -INFINITY;
+        }
+        if constexpr (TRACK) {
+          if (part == 0 && head < n_heads) {
+            float* to = a.logits + ((uint64_t)r * a.heads + first_head + head) * c.capacity + t + 4 * g;
+            if (t < end) *(float4*)to = make_float4(p[0], p[1], p[2], p[3]);
+            if (t + 16 < end) *(float4*)(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
+          }
+        }
+        float m = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i]);
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float base = m == -INFINITY ? 0.f : m;   // nothing here takes part
+        const float shrink = __builtin_amdgcn_exp2f(top - base);
+        top = m;
+        total *= shrink;
+#pragma unroll
+        for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
+        if (now.limit[0] < 16 || now.limit[1] < 16) {   // whatever lies there is not used
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (4 * g + i % 4 >= now.limit[i / 4]) {
+              if constexpr (INT8) (&x.vs[i / 4].x)[i % 4] = 0.f;
+#pragma unroll
+              for (int w = 0; w < T::kValWords; ++w) x.v[i][w] = 0;
+            }
+        }
+        bf16x8 pb;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float w = __builtin_amdgcn_exp2f(p[i] - base);
+          total += w;
+          if constexpr (INT8) w *= (&x.vs[i / 4].x)[i % 4];
+          const __bf16 hi = (__bf16)w;
+          pb[i] = part ? (__bf16)(w - (float)hi) : hi;
+        }
+#pragma unroll
+        for (int b = 0; b < T::kVals; ++b) {
+          uint32_t vt[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (INT8) {
+              const float lo = (float)(int8_t)(x.v[2 * i][b / 4] >> (8 * (b % 4))), hi = (float)(int8_t)(x.v[2 * i + 1][b / 4] >> (8 * (b % 4)));
+              vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+            } else {
+              vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u);
+            }
+          }
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
+        }
+        if (round + 1 == rounds) break;
+        fetch_values(next);
+        __builtin_amdgcn_s_barrier();   // (older wavefronts are served first: without it they end early and leave the others alone)
+        now = next;
       }
     }
-  };
-  auto take = [&](T& x, uint32_t t) {
-    float p[8];
+
+    // join the wavefronts: lane (g, head) holds dims (4 g + j) * kVals + b of the head, halves of p beside each other
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    if (lane < kHeads) lds_max[wave * kHeads + lane] = top, lds_total[wave * kHeads + lane] = total;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x4 l = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < T::kSteps; ++s) {
-        bf16x8 key;
-        if constexpr (INT8) key = i8x8_to_bf16x8(make_uint2(x.k[b][2 * s], x.k[b][2 * s + 1]));
-        else key = __builtin_bit_cast(bf16x8, make_uint4(x.k[b][4 * s], x.k[b][4 * s + 1], x.k[b][4 * s + 2], x.k[b][4 * s + 3]));
-        l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[s][0], l, 0, 0, 0);
-        l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[s][1], l, 0, 0, 0);
-      }
+    for (int b = 0; b < T::kVals; b += 4)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float v = ror8_sum(l[j]);
-        if constexpr (INT8) v *= (&x.ks[b].x)[j];
-        p[4 * b + j] = v;
+        const float4 v = make_float4(ror8_sum(o[b][j]), ror8_sum(o[b + 1][j]), ror8_sum(o[b + 2][j]), ror8_sum(o[b + 3][j]));
+        if (part == 0) *(float4*)&lds_sum[(wave * kHeads + head) * (DIM + 4) + (4 * g + j) * T::kVals + b] = v;
       }
-    }
-    if (x.limit[0] < 16 || x.limit[1] < 16) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (4 * g + i % 4 >= x.limit[i / 4]) {
-          p[i] = -INFINITY;
-          if constexpr (INT8) (&x.vs[i / 4].x)[i % 4] = 0.f;
-#pragma unroll
-          for (int w = 0; w < T::kValWords; ++w) x.v[i][w] = 0;
-        }
-    }
-    if constexpr (TRACK) {
-      if (part == 0 && head < n_heads) {
-        float* to = a.logits + ((uint64_t)r * a.heads + first_head + head) * c.capacity + t + 4 * g;
-        *(float4*)to = make_float4(p[0], p[1], p[2], p[3]);
-        if (t + 16 < end) *(float4*)(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
-      }
-    }
-    float m = top;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i]);
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float base = m == -INFINITY ? 0.f : m;   // nothing here takes part
-    const float shrink = __builtin_amdgcn_exp2f(top - base);
-    top = m;
-    total *= shrink;
-#pragma unroll
-    for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
-    bf16x8 pb;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float w = __builtin_amdgcn_exp2f(p[i] - base);
-      total += w;
-      if constexpr (INT8) w *= (&x.vs[i / 4].x)[i % 4];
-      const __bf16 hi = (__bf16)w;
-      pb[i] = part ? (__bf16)(w - (float)hi) : hi;
-    }
-#pragma unroll
-    for (int b = 0; b < T::kVals; ++b) {
-      uint32_t vt[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (INT8) {
-          const float lo = (float)(int8_t)(x.v[2 * i][b / 4] >> (8 * (b % 4))), hi = (float)(int8_t)(x.v[2 * i + 1][b / 4] >> (8 * (b % 4)));
-          vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-        } else {
-          vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u);
-        }
-      }
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
-    }
-  };
-  const uint32_t first = begin + wave * kTile;
-  if (first < end) {
-    const uint32_t last = first + (end - 1 - first) / kUnit * kUnit;
-    T x, y;
-    fetch(x, first, pages_of(first));
-    Pages next = pages_of(min(first + kUnit, last));
-    for (uint32_t t = first;; t += 2 * kUnit) {
-      fetch(y, min(t + kUnit, last), next);
-      next = pages_of(min(t + 2 * kUnit, last));
-      take(x, t);
-      if (t == last) break;
-      fetch(x, min(t + 2 * kUnit, last), next);
-      next = pages_of(min(t + 3 * kUnit, last));
-      take(y, t + kUnit);
-      if (t + kUnit == last) break;
-    }
-  }
-
-  // join the wavefronts: lane (g, head) holds dims (4 g + j) * kVals + b of the head, halves of p beside each other
-  total += __shfl_xor(total, 16);
-  total += __shfl_xor(total, 32);
-  if (lane < kHeads) lds_max[wave * kHeads + lane] = top, lds_total[wave * kHeads + lane] = total;
-#pragma unroll
-  for (int b = 0; b < T::kVals; b += 4)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 v = make_float4(ror8_sum(o[b][j]), ror8_sum(o[b + 1][j]), ror8_sum(o[b + 2][j]), ror8_sum(o[b + 3][j]));
-      if (part == 0) *(float4*)&lds_sum[(wave * kHeads + head) * (DIM + 4) + (4 * g + j) * T::kVals + b] = v;
-    }
-  __syncthreads();
-  // the workgroups among which this (row, chunk) is cut
-  const uint32_t pair_first = row_first + pair * units, group0 = pair_first / share, parts = (pair_first + units - 1) / share - group0 + 1;
-  const uint64_t slot_floats = kHeads * (D + 2);
-  auto slot_of = [&](uint32_t group) { return a.partials + (2 * (uint64_t)group + (group * share >= pair_first ? 0 : 1)) * slot_floats; };
-  auto finish = [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
-    const float inv = sum_p == 0.f ? 0.f : 1.f / sum_p;
-    a.out[r * a.out_stride + (first_head + h) * D + d] = (uint16_t)pack_bf16(sum * inv, 0.f);
-    if (TRACK && d == 0) a.stats[(uint64_t)r * a.heads + first_head + h] = make_float2(m == -INFINITY ? 0.f : m, inv);
-  };
-  // one of n parts' sums, maxima and totals in LDS, [part][head][DIM + 4] from head h0 on -> the whole
-  auto joined = [&](uint32_t parts_n, uint32_t h_n, uint32_t h0, uint32_t i, auto&& put) {
-    const uint32_t h = i / D, d = i % D;
-    float m = -INFINITY, sum = 0.f, sum_p = 0.f;
-    for (uint32_t w = 0; w < parts_n; ++w) m = fmaxf(m, lds_max[w * kHeads + h0 + h]);
-    const float base = m == -INFINITY ? 0.f : m;
-    for (uint32_t w = 0; w < parts_n; ++w) {
-      const float f = __builtin_amdgcn_exp2f(lds_max[w * kHeads + h0 + h] - base);
-      sum = fmaf(f, lds_sum[(w * h_n + h) * (DIM + 4) + d], sum);
-      sum_p = fmaf(f, lds_total[w * kHeads + h0 + h], sum_p);
-    }
-    put(h0 + h, d, sum, m, sum_p);
-  };
-  if (parts == 1) {
-    for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads) joined(kAttendWaves, kHeads, 0, i, finish);
-  } else {
-    typedef __attribute__((address_space(1))) float global_f32;
-    typedef __attribute__((address_space(1))) uint32_t global_u32;
-    float* mine = slot_of(blockIdx.x);
-    auto leave = [&](float* p, float v) { __hip_atomic_store((global_f32*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-    for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads)
-      joined(kAttendWaves, kHeads, 0, i, [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
-        leave(mine + h * D + d, sum);
-        if (d == 0) leave(mine + kHeads * D + 2 * h, m), leave(mine + kHeads * D + 2 * h + 1, sum_p);
-      });
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
     __syncthreads();
-    global_u32* arrived = (global_u32*)(a.arrived + (uint64_t)r * a.chunks + pair);
-    if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (lds_before == parts - 1) {   // the others' parts are in
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-      if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // groups of DIM / 4 lanes take every kGroups-th part, four dims a lane, all heads
-      constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes, kBatch = kAttendWaves * kHeads / kGroups;
-      const uint32_t mine_of = threadIdx.x / kLanes, d0 = threadIdx.x % kLanes * 4;
-      float4 sum[kHeads];
-      float m[kHeads], sum_p[kHeads];
+    // the workgroups among which this (row, chunk) is cut
+    const uint32_t pair_first = row_first + pair * units, group0 = pair_first / share, parts = (pair_first + units - 1) / share - group0 + 1;
+    const uint64_t slot_floats = kHeads * (D + 2);
+    auto slot_of = [&](uint32_t group) { return a.partials + (2 * (uint64_t)group + (group * share >= pair_first ? 0 : 1)) * slot_floats; };
+    auto finish = [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
+      const float inv = sum_p == 0.f ? 0.f : 1.f / sum_p;
+      a.out[r * a.out_stride + (first_head + h) * D + d] = (uint16_t)pack_bf16(sum * inv, 0.f);
+      if (TRACK && d == 0) a.stats[(uint64_t)r * a.heads + first_head + h] = make_float2(m == -INFINITY ? 0.f : m, inv);
+    };
+    // n parts' sums, maxima and totals in LDS, [part][heads_n][DIM + 4] -> the whole
+    auto joined = [&](uint32_t n, uint32_t heads_n, uint32_t i, auto&& put) {
+      const uint32_t h = i / D, d = i % D;
+      float m = -INFINITY, sum = 0.f, sum_p = 0.f;
+      for (uint32_t w = 0; w < n; ++w) m = fmaxf(m, lds_max[w * heads_n + h]);
+      const float base = m == -INFINITY ? 0.f : m;
+      for (uint32_t w = 0; w < n; ++w) {
+        const float f = __builtin_amdgcn_exp2f(lds_max[w * heads_n + h] - base);
+        sum = fmaf(f, lds_sum[(w * heads_n + h) * (DIM + 4) + d], sum);
+        sum_p = fmaf(f, lds_total[w * heads_n + h], sum_p);
+      }
+      put(h, d, sum, m, sum_p);
+    };
+    if (parts == 1) {
+      for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads) joined(kAttendWaves, kHeads, i, finish);
+    } else {
+      typedef __attribute__((address_space(1))) float global_f32;
+      typedef __attribute__((address_space(1))) uint32_t global_u32;
+      typedef __attribute__((address_space(1))) const uint64_t global_cu64;
+      float* mine = slot_of(blockIdx.x);
+      // stored to and loaded from the level that the device shares (an acquire fence would empty an L2 that the others read through)
+      auto left_by = [&](const float* p) {
+        return __builtin_bit_cast(float2, __hip_atomic_load((global_cu64*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+      };
+      auto leave = [&](float* p, float v) { __hip_atomic_store((global_f32*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+      for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads)
+        joined(kAttendWaves, kHeads, i, [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
+          leave(mine + h * D + d, sum);
+          if (d == 0) leave(mine + kHeads * D + 2 * h, m), leave(mine + kHeads * D + 2 * h + 1, sum_p);
+        });
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
+      __syncthreads();
+      global_u32* arrived = (global_u32*)(a.arrived + (uint64_t)r * a.chunks + pair);
+      if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      if (lds_before == parts - 1) {   // the others' parts are in, and what was joined above is no longer needed
+        if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // a head and every per_head-th part for each group of DIM / 4 lanes, four dims a lane, kAhead parts at a time
+        constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes, kAhead = 8;
+        const uint32_t heads_n = n_heads > 4 ? 8 : n_heads > 2 ? 4 : n_heads, per_head = kGroups / heads_n;
+        const uint32_t mine_of = threadIdx.x / kLanes, h = mine_of % heads_n, part0 = mine_of / heads_n, d0 = threadIdx.x % kLanes * 4;
+        if (h < n_heads) {
+          float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+          float m = -INFINITY, sum_p = 0.f;
+          for (uint32_t v = part0; v < parts; v += kAhead * per_head) {
+            float2 s[kAhead][2], st[kAhead];
 #pragma unroll
-      for (int h = 0; h < kHeads; ++h) sum[h] = make_float4(0.f, 0.f, 0.f, 0.f), m[h] = -INFINITY, sum_p[h] = 0.f;
-      for (uint32_t v = mine_of; v < parts; v += kGroups) {
-        const float* from = slot_of(group0 + v);
+            for (uint32_t i = 0; i < kAhead; ++i) {
+              const float* from = slot_of(group0 + min(v + i * per_head, parts - 1));
+              const float* at = from + h * D + (d0 < D ? d0 : 0);
+              s[i][0] = left_by(at), s[i][1] = left_by(at + 2);
+              st[i] = left_by(from + kHeads * D + 2 * h);
+            }
 #pragma unroll
-        for (uint32_t h = 0; h < kHeads; ++h)
-          if (h < n_heads) {
-            const float4 s = d0 < D ? *(const float4*)(from + h * D + d0) : make_float4(0.f, 0.f, 0.f, 0.f);
-            const float2 st = *(const float2*)(from + kHeads * D + 2 * h);
-            const float to = fmaxf(m[h], st.x), base = to == -INFINITY ? 0.f : to;
-            const float f = __builtin_amdgcn_exp2f(m[h] - base), e = __builtin_amdgcn_exp2f(st.x - base);
-            m[h] = to;
-            sum_p[h] = sum_p[h] * f + st.y * e;
-            sum[h].x = sum[h].x * f + s.x * e, sum[h].y = sum[h].y * f + s.y * e;
-            sum[h].z = sum[h].z * f + s.z * e, sum[h].w = sum[h].w * f + s.w * e;
+            for (uint32_t i = 0; i < kAhead; ++i) {
+              if (v + i * per_head >= parts) continue;
+              const float to = fmaxf(m, st[i].x), base = to == -INFINITY ? 0.f : to;
+              const float f = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(st[i].x - base);
+              m = to;
+              sum_p = sum_p * f + st[i].y * e;
+              sum.x = sum.x * f + s[i][0].x * e, sum.y = sum.y * f + s[i][0].y * e;
+              sum.z = sum.z * f + s[i][1].x * e, sum.w = sum.w * f + s[i][1].y * e;
+            }
           }
-      }
-      if (threadIdx.x % kLanes == 0)
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h) lds_max[mine_of * kHeads + h] = m[h], lds_total[mine_of * kHeads + h] = sum_p[h];
-      for (uint32_t h0 = 0; h0 < n_heads; h0 += kBatch) {
+          if (d0 == 0) lds_max[mine_of] = m, lds_total[mine_of] = sum_p;
+          *(float4*)&lds_sum[mine_of * (DIM + 4) + d0] = sum;
+        }
         __syncthreads();
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h)
-          if (h >= (int)h0 && h < (int)(h0 + kBatch)) *(float4*)&lds_sum[(mine_of * kBatch + h - h0) * (DIM + 4) + d0] = sum[h];
-        __syncthreads();
-        const uint32_t some = min(kBatch, n_heads - h0);
-        for (uint32_t i = threadIdx.x; i < some * D; i += kAttendThreads) joined(kGroups, kBatch, h0, i, finish);
+        for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads) joined(per_head, heads_n, i, finish);
       }
     }
-  }
-  __syncthreads();   // LDS is free again
-  pos += unit_end - unit;
-  if (pos == row_first + units * a.chunks) row_first = pos, ++r;
+    __syncthreads();   // LDS is free again
+    pos += unit_end - unit;
+    if (pos == row_first + units * a.chunks) {
+      row_first = pos;
+      if ((++r & 63) == 0 && pos < stop) look_at(r);
+    }
   }
 }
 
