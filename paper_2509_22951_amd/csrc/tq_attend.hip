@@ -91,8 +91,9 @@ __device__ __forceinline__ uint32_t prefix_sum(uint32_t v) {
 // of the line.  Nobody waits for anybody.
 //
 // A wavefront asks for the next tile's keys as soon as the logits of this one are made, and for its values when they are multiplied
-// in: the loads are requested without a condition, so that a wait counts the loads behind those it is for (the last tile is
-// requested again in place of one that is not there, and a page that is not there is read as page 0 and masked).
+// in, also where the next tile is another row's: a row's end is worked on while the next one's first tile is on its way.  The keys are
+// requested without a condition, so that a wait counts the loads behind those it is for (in place of a tile that is not there the
+// last one is requested again, and a page that is not there is read as page 0 and masked).
 template <int DIM, bool INT8, bool TRACK>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, AttendView a) {
   using T = Tile<DIM, INT8>;
@@ -146,180 +147,201 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   }
   const uint32_t val_at = 4 * g * slot_bytes + kSize * (n * T::kVals < D ? n * T::kVals : 0);
 
-  while (pos < stop) {
-    const uint32_t length = (uint32_t)__builtin_amdgcn_readlane((int)lane_length, r & 63), seq = (uint32_t)__builtin_amdgcn_readlane((int)lane_seq, r & 63);
-    const uint32_t units = units_of(length);
-    const uint32_t pair = (pos - row_first) / units, unit = (pos - row_first) % units, unit_end = min(units, unit + (stop - pos));
-    const uint32_t kv = pair / per_kv, chunk = pair % per_kv;
-    const uint32_t begin = unit * kUnit, end = min(length, unit_end * kUnit);
-    const uint32_t first_head = kv * a.group + chunk * kHeads, n_heads = min((uint32_t)kHeads, a.group - chunk * kHeads);
-    constant_i32* table = (constant_i32*)(c.tables + (uint64_t)seq * c.table_stride);
+  struct Segment {   // the part of a (row, chunk) that lies in this share
+    uint32_t r, seq, kv, first_head, n_heads, pair, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
+  };
+  auto next_segment = [&] {
+    Segment s;
+    s.r = r;
+    const uint32_t length = (uint32_t)__builtin_amdgcn_readlane((int)lane_length, r & 63);
+    s.seq = (uint32_t)__builtin_amdgcn_readlane((int)lane_seq, r & 63);
+    s.units = units_of(length);
+    s.pair = (pos - row_first) / s.units;
+    s.pair_first = row_first + s.pair * s.units;
+    s.kv = s.pair / per_kv;
+    const uint32_t chunk = s.pair % per_kv, unit = pos - s.pair_first, unit_end = min(s.units, unit + (stop - pos));
+    s.first_head = s.kv * a.group + chunk * kHeads;
+    s.n_heads = min((uint32_t)kHeads, a.group - chunk * kHeads);
+    s.begin = unit * kUnit;
+    s.end = min(length, unit_end * kUnit);
+    s.rounds = unit_end - unit;
+    pos += unit_end - unit;
+    if (pos == row_first + s.units * a.chunks) {
+      row_first = pos;
+      if ((++r & 63) == 0 && pos < stop) look_at(r);
+    }
+    return s;
+  };
+  struct Blocks {   // two blocks of 16 tokens: their first byte in a pool, their first scale, how many tokens take part
+    uint64_t at[2], mark[2];
+    uint32_t limit[2];
+  };
+  auto blocks_of = [&](const Segment& s, uint32_t round) {
+    constant_i32* table = (constant_i32*)(c.tables + (uint64_t)s.seq * c.table_stride);
+    const uint32_t tile = s.begin + round * kUnit + wave * kTile, newest = max(s.end, 1u) - 1, there = min(tile, newest & ~(kTile - 1u));
+    Blocks w;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const uint32_t at = there + 16 * b, want = tile + 16 * b, id = (uint32_t)table[min(at, newest) >> c.page_shift];
+      w.limit[b] = id < c.n_pages && want < s.end ? min(s.end - want, 16u) : 0u;
+      const uint32_t page = id < c.n_pages ? id : 0, slot = at & ((1u << c.page_shift) - 1);
+      w.at[b] = kSize * ((uint64_t)page * c.page_stride + s.kv * c.head_stride + slot * c.slot_stride);
+      w.mark[b] = INT8 ? (((uint64_t)page * c.kv_heads + s.kv) << c.page_shift) + slot : 0;
+    }
+    return w;
+  };
+  T x;
+  auto fetch_keys = [&](const Blocks& w) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const char* from = c.k + w.at[b];
+#pragma unroll
+      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + key_at[s]);
+      if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
+    }
+  };
+  auto fetch_values = [&](const Blocks& w) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + val_at);
+      if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
+    }
+  };
+  // 8 values of a segment's q: lane threadIdx.x % 64 of contraction step threadIdx.x / 64
+  const uint32_t q_dim = INT8 ? 64 * (wave / 2) + 16 * g + 8 * (wave % 2) : 32 * wave + 8 * g;
+  float q8[8];
+  auto fetch_q = [&](const Segment& s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q8[j] = 0.f;
+    if (head < s.n_heads && q_dim < D) {
+      const uint64_t at = s.r * a.q_stride + (s.first_head + head) * D + q_dim;
+      if (a.q16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q8[j] = bf16_value(((const uint16_t*)a.q)[at + j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q8[j] = ((const float*)a.q)[at + j];
+      }
+    }
+  };
 
-    T x;
+  Segment s = next_segment();
+  fetch_q(s);
+  Blocks now = blocks_of(s, 0);
+  fetch_keys(now);
+  fetch_values(now);
+  for (;;) {
+    static_assert(T::kSteps <= kAttendWaves, "a wavefront per step of q");
+    if (wave < T::kSteps) {
+      bf16x8 q0, q1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = q8[j] * a.scale;
+        const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
+        q0[j] = part ? mid : hi;
+        q1[j] = part ? (__bf16)0.f : lo;
+      }
+      lds_q[wave][0][lane] = q0;
+      lds_q[wave][1][lane] = q1;
+    }
+    __syncthreads();
+
     f32x4 o[T::kVals];
 #pragma unroll
     for (int b = 0; b < T::kVals; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, total = 0.f;
-    const uint32_t rounds = end > begin ? unit_end - unit : 0;   // rounds of kUnit tokens, the same for every wavefront
-    struct Pages {
-      uint32_t id[2];
-    };
-    struct Blocks {         // two blocks of 16 tokens: their first byte in a pool, their first scale, how many tokens take part
-      uint64_t at[2], mark[2];
-      uint32_t limit[2];
-    };
-    auto tile_of = [&](uint32_t i) { return begin + i * kUnit + wave * kTile; };
-    auto held = [&](uint32_t i) { return min(tile_of(min(i, rounds - 1)), (end - 1) & ~(kTile - 1u)); };   // a tile that is there
-    auto pages_of = [&](uint32_t i) {
-      Pages p;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) p.id[b] = (uint32_t)table[min(held(i) + 16 * b, end - 1) >> c.page_shift];
-      return p;
-    };
-    auto blocks_of = [&](uint32_t i, const Pages& p) {
-      Blocks w;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint32_t at = held(i) + 16 * b, want = tile_of(i) + 16 * b, id = p.id[b];
-        w.limit[b] = id < c.n_pages && want < end ? min(end - want, 16u) : 0u;
-        const uint32_t page = id < c.n_pages ? id : 0, slot = at & ((1u << c.page_shift) - 1);
-        w.at[b] = kSize * ((uint64_t)page * c.page_stride + kv * c.head_stride + slot * c.slot_stride);
-        w.mark[b] = INT8 ? (((uint64_t)page * c.kv_heads + kv) << c.page_shift) + slot : 0;
+    const bool more = pos < stop;
+    Segment next_s = s;
+    for (uint32_t round = 0;; ++round) {
+      const bool last = round + 1 == s.rounds;
+      const uint32_t t = s.begin + round * kUnit + wave * kTile;
+      if (last && more) {
+        next_s = next_segment();
+        fetch_q(next_s);
       }
-      return w;
-    };
-    auto fetch_keys = [&](const Blocks& w) {
+      const Blocks next = blocks_of(next_s, !last ? round + 1 : more ? 0 : round);
+      asm volatile("" ::: "memory");   // q is read from LDS for every tile: registers are for what is on its way
+      f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const char* from = c.k + w.at[b];
+      for (int s = 0; s < T::kSteps; ++s) {
+        const bf16x8 q0 = lds_q[s][0][lane], q1 = lds_q[s][1][lane];
 #pragma unroll
-        for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + key_at[s]);
-        if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
-      }
-    };
-    auto fetch_values = [&](const Blocks& w) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + val_at);
-        if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
-      }
-    };
-    Blocks now;
-    Pages ahead;
-    if (rounds) {
-      now = blocks_of(0, pages_of(0));
-      ahead = pages_of(1);
-      fetch_keys(now);
-      fetch_values(now);
-    }
-    // the query's parts, for all wavefronts
-    for (uint32_t i = threadIdx.x; i < T::kSteps * 64; i += kAttendThreads) {
-      const uint32_t s = i / 64, qg = i % 64 / 16, qn = i % 16, qh = qn % 8;
-      const uint32_t d0 = INT8 ? 64 * (s / 2) + 16 * qg + 8 * (s % 2) : 32 * s + 8 * qg;
-      bf16x8 q0, q1;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float v = 0.f;
-        if (qh < n_heads && d0 < D) {
-          const uint64_t at = r * a.q_stride + (first_head + qh) * D + d0 + j;
-          v = (a.q16 ? bf16_value(((const uint16_t*)a.q)[at]) : ((const float*)a.q)[at]) * a.scale;
+        for (int b = 0; b < 2; ++b) {
+          bf16x8 key;
+          if constexpr (INT8) key = i8x8_to_bf16x8(make_uint2(x.k[b][2 * s], x.k[b][2 * s + 1]));
+          else key = __builtin_bit_cast(bf16x8, make_uint4(x.k[b][4 * s], x.k[b][4 * s + 1], x.k[b][4 * s + 2], x.k[b][4 * s + 3]));
+          l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q0, l[b], 0, 0, 0);
+          l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q1, l[b], 0, 0, 0);
         }
-        const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
-        q0[j] = qn / 8 ? mid : hi;
-        q1[j] = qn / 8 ? (__bf16)0.f : lo;
       }
-      lds_q[s][0][i % 64] = q0;
-      lds_q[s][1][i % 64] = q1;
-    }
-    __syncthreads();
-
-    if (rounds) {
-      for (uint32_t round = 0;; ++round) {
-        const uint32_t t = tile_of(round);
-        const Blocks next = blocks_of(round + 1, ahead);
-        ahead = pages_of(round + 2);
-        if constexpr (DIM == 256) asm volatile("" ::: "memory");   // q is read from LDS for every tile: registers are for what is on its way
-        f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      float p[8];
 #pragma unroll
-        for (int s = 0; s < T::kSteps; ++s) {
-          const bf16x8 q0 = lds_q[s][0][lane], q1 = lds_q[s][1][lane];
+      for (int i = 0; i < 8; ++i) {
+        p[i] = ror8_sum(l[i / 4][i % 4]);
+        if constexpr (INT8) p[i] *= (&x.ks[i / 4].x)[i % 4];
+      }
+      fetch_keys(next);
+      if (now.limit[0] < 16 || now.limit[1] < 16) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            bf16x8 key;
-            if constexpr (INT8) key = i8x8_to_bf16x8(make_uint2(x.k[b][2 * s], x.k[b][2 * s + 1]));
-            else key = __builtin_bit_cast(bf16x8, make_uint4(x.k[b][4 * s], x.k[b][4 * s + 1], x.k[b][4 * s + 2], x.k[b][4 * s + 3]));
-            l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q0, l[b], 0, 0, 0);
-            l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q1, l[b], 0, 0, 0);
+        for (int i = 0; i < 8; ++i)
+          if (4 * g + i % 4 >= now.limit[i / 4]) p[i] = -INFINITY;
+      }
+      if constexpr (TRACK) {
+        if (part == 0 && head < s.n_heads) {
+          float* to = a.logits + ((uint64_t)s.r * a.heads + s.first_head + head) * c.capacity + t + 4 * g;
+          if (t < s.end) *(float4*)to = make_float4(p[0], p[1], p[2], p[3]);
+          if (t + 16 < s.end) *(float4*)(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
+        }
+      }
+      float m = top;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i]);
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float base = m == -INFINITY ? 0.f : m;   // nothing here takes part
+      const float shrink = __builtin_amdgcn_exp2f(top - base);
+      top = m;
+      total *= shrink;
+#pragma unroll
+      for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
+      if (now.limit[0] < 16 || now.limit[1] < 16) {   // whatever lies there is not used
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (4 * g + i % 4 >= now.limit[i / 4]) {
+            if constexpr (INT8) (&x.vs[i / 4].x)[i % 4] = 0.f;
+#pragma unroll
+            for (int w = 0; w < T::kValWords; ++w) x.v[i][w] = 0;
+          }
+      }
+      bf16x8 pb;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float w = __builtin_amdgcn_exp2f(p[i] - base);
+        total += w;
+        if constexpr (INT8) w *= (&x.vs[i / 4].x)[i % 4];
+        const __bf16 hi = (__bf16)w;
+        pb[i] = part ? (__bf16)(w - (float)hi) : hi;
+      }
+#pragma unroll
+      for (int b = 0; b < T::kVals; ++b) {
+        uint32_t vt[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (INT8) {
+            const float lo = (float)(int8_t)(x.v[2 * i][b / 4] >> (8 * (b % 4))), hi = (float)(int8_t)(x.v[2 * i + 1][b / 4] >> (8 * (b % 4)));
+            vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+          } else {
+            vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u);
           }
         }
-        float p[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = ror8_sum(l[i / 4][i % 4]);
-          if constexpr (INT8) p[i] *= (&x.ks[i / 4].x)[i % 4];
-        }
-        fetch_keys(next);
-        if (now.limit[0] < 16 || now.limit[1] < 16) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (4 * g + i % 4 >= now.limit[i / 4]) p[i] = -INFINITY;
-        }
-        if constexpr (TRACK) {
-          if (part == 0 && head < n_heads) {
-            float* to = a.logits + ((uint64_t)r * a.heads + first_head + head) * c.capacity + t + 4 * g;
-            if (t < end) *(float4*)to = make_float4(p[0], p[1], p[2], p[3]);
-            if (t + 16 < end) *(float4*)(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
-          }
-        }
-        float m = top;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, p[i]);
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float base = m == -INFINITY ? 0.f : m;   // nothing here takes part
-        const float shrink = __builtin_amdgcn_exp2f(top - base);
-        top = m;
-        total *= shrink;
-#pragma unroll
-        for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
-        if (now.limit[0] < 16 || now.limit[1] < 16) {   // whatever lies there is not used
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (4 * g + i % 4 >= now.limit[i / 4]) {
-              if constexpr (INT8) (&x.vs[i / 4].x)[i % 4] = 0.f;
-#pragma unroll
-              for (int w = 0; w < T::kValWords; ++w) x.v[i][w] = 0;
-            }
-        }
-        bf16x8 pb;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float w = __builtin_amdgcn_exp2f(p[i] - base);
-          total += w;
-          if constexpr (INT8) w *= (&x.vs[i / 4].x)[i % 4];
-          const __bf16 hi = (__bf16)w;
-          pb[i] = part ? (__bf16)(w - (float)hi) : hi;
-        }
-#pragma unroll
-        for (int b = 0; b < T::kVals; ++b) {
-          uint32_t vt[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (INT8) {
-              const float lo = (float)(int8_t)(x.v[2 * i][b / 4] >> (8 * (b % 4))), hi = (float)(int8_t)(x.v[2 * i + 1][b / 4] >> (8 * (b % 4)));
-              vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-            } else {
-              vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u);
-            }
-          }
-          o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
-        }
-        if (round + 1 == rounds) break;
-        fetch_values(next);
-        __builtin_amdgcn_s_barrier();   // (older wavefronts are served first: without it they end early and leave the others alone)
-        now = next;
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
       }
+      if (last && !more) break;
+      fetch_values(next);
+      now = next;
+      if (last) break;
+      __builtin_amdgcn_s_barrier();   // (older wavefronts are served first: without it they end early and leave the others alone)
     }
 
     // join the wavefronts: lane (g, head) holds dims (4 g + j) * kVals + b of the head, halves of p beside each other
@@ -335,13 +357,13 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       }
     __syncthreads();
     // the workgroups among which this (row, chunk) is cut
-    const uint32_t pair_first = row_first + pair * units, group0 = pair_first / share, parts = (pair_first + units - 1) / share - group0 + 1;
+    const uint32_t n_heads = s.n_heads, group0 = s.pair_first / share, parts = (s.pair_first + s.units - 1) / share - group0 + 1;
     const uint64_t slot_floats = kHeads * (D + 2);
-    auto slot_of = [&](uint32_t group) { return a.partials + (2 * (uint64_t)group + (group * share >= pair_first ? 0 : 1)) * slot_floats; };
+    auto slot_of = [&](uint32_t group) { return a.partials + (2 * (uint64_t)group + (group * share >= s.pair_first ? 0 : 1)) * slot_floats; };
     auto finish = [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
       const float inv = sum_p == 0.f ? 0.f : 1.f / sum_p;
-      a.out[r * a.out_stride + (first_head + h) * D + d] = (uint16_t)pack_bf16(sum * inv, 0.f);
-      if (TRACK && d == 0) a.stats[(uint64_t)r * a.heads + first_head + h] = make_float2(m == -INFINITY ? 0.f : m, inv);
+      a.out[s.r * a.out_stride + (s.first_head + h) * D + d] = (uint16_t)pack_bf16(sum * inv, 0.f);
+      if (TRACK && d == 0) a.stats[(uint64_t)s.r * a.heads + s.first_head + h] = make_float2(m == -INFINITY ? 0.f : m, inv);
     };
     // n parts' sums, maxima and totals in LDS, [part][heads_n][DIM + 4] -> the whole
     auto joined = [&](uint32_t n, uint32_t heads_n, uint32_t i, auto&& put) {
@@ -375,25 +397,25 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         });
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
       __syncthreads();
-      global_u32* arrived = (global_u32*)(a.arrived + (uint64_t)r * a.chunks + pair);
+      global_u32* arrived = (global_u32*)(a.arrived + (uint64_t)s.r * a.chunks + s.pair);
       if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __syncthreads();
       if (lds_before == parts - 1) {   // the others' parts are in, and what was joined above is no longer needed
         if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         // a head and every per_head-th part for each group of DIM / 4 lanes, four dims a lane, kAhead parts at a time
-        constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes, kAhead = 8;
+        constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes, kAhead = 4;
         const uint32_t heads_n = n_heads > 4 ? 8 : n_heads > 2 ? 4 : n_heads, per_head = kGroups / heads_n;
         const uint32_t mine_of = threadIdx.x / kLanes, h = mine_of % heads_n, part0 = mine_of / heads_n, d0 = threadIdx.x % kLanes * 4;
         if (h < n_heads) {
           float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
           float m = -INFINITY, sum_p = 0.f;
           for (uint32_t v = part0; v < parts; v += kAhead * per_head) {
-            float2 s[kAhead][2], st[kAhead];
+            float2 sums[kAhead][2], st[kAhead];
 #pragma unroll
             for (uint32_t i = 0; i < kAhead; ++i) {
               const float* from = slot_of(group0 + min(v + i * per_head, parts - 1));
               const float* at = from + h * D + (d0 < D ? d0 : 0);
-              s[i][0] = left_by(at), s[i][1] = left_by(at + 2);
+              sums[i][0] = left_by(at), sums[i][1] = left_by(at + 2);
               st[i] = left_by(from + kHeads * D + 2 * h);
             }
 #pragma unroll
@@ -403,8 +425,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
               const float f = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(st[i].x - base);
               m = to;
               sum_p = sum_p * f + st[i].y * e;
-              sum.x = sum.x * f + s[i][0].x * e, sum.y = sum.y * f + s[i][0].y * e;
-              sum.z = sum.z * f + s[i][1].x * e, sum.w = sum.w * f + s[i][1].y * e;
+              sum.x = sum.x * f + sums[i][0].x * e, sum.y = sum.y * f + sums[i][0].y * e;
+              sum.z = sum.z * f + sums[i][1].x * e, sum.w = sum.w * f + sums[i][1].y * e;
             }
           }
           if (d0 == 0) lds_max[mine_of] = m, lds_total[mine_of] = sum_p;
@@ -414,12 +436,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads) joined(per_head, heads_n, i, finish);
       }
     }
+    if (!more) break;
     __syncthreads();   // LDS is free again
-    pos += unit_end - unit;
-    if (pos == row_first + units * a.chunks) {
-      row_first = pos;
-      if ((++r & 63) == 0 && pos < stop) look_at(r);
-    }
+    s = next_s;
   }
 }
 
