@@ -19,14 +19,14 @@ namespace {
 
 constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
-constexpr uint32_t kMaxGroups = 256, kMinShare = 1;                       // workgroups of a launch; units of one
+constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;                       // workgroups of a launch; units of one; parts that are joined at a time
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttendView {
   const void* q;
   uint16_t* out;
   const int32_t *seqs, *lengths;
-  uint32_t* arrived;   // [row][chunk]: workgroups whose part is in the partials; zero between calls
+  uint32_t* arrived;   // [cluster][2], then [row][chunk]: workgroups whose part is in the partials; zero between calls
   float* partials;     // [workgroup][2]: kHeads x head_dim sums, then maximum and total of every head
   float* logits;       // [row][head][capacity], in units of log 2 (accumulate)
   float2* stats;       // [row][head]: maximum and 1 / total of the whole row (accumulate)
@@ -88,7 +88,7 @@ __device__ __forceinline__ uint32_t prefix_sum(uint32_t v) {
 // All (row, chunk, unit of kUnit tokens) in this order are one line, cut into equal shares, one per workgroup: whatever the
 // lengths, every workgroup has as much to do.  A (row, chunk) that lies in one share is finished there; of one that is cut every
 // workgroup leaves its maximum, total and weighted sum in memory and counts itself in, and the last one joins them, in the order
-// of the line.  Nobody waits for anybody.
+// of the line; more than kCluster parts are joined by clusters first.  Nobody waits for anybody.
 //
 // A wavefront asks for the next tile's keys as soon as the logits of this one are made, and for its values when they are multiplied
 // in, also where the next tile is another row's: a row's end is worked on while the next one's first tile is on its way.  The keys are
@@ -384,43 +384,55 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       typedef __attribute__((address_space(1))) float global_f32;
       typedef __attribute__((address_space(1))) uint32_t global_u32;
       typedef __attribute__((address_space(1))) const uint64_t global_cu64;
-      float* mine = slot_of(blockIdx.x);
       // stored to and loaded from the level that the device shares (an acquire fence would empty an L2 that the others read through)
       auto left_by = [&](const float* p) {
         return __builtin_bit_cast(float2, __hip_atomic_load((global_cu64*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
       };
       auto leave = [&](float* p, float v) { __hip_atomic_store((global_f32*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-      for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads)
-        joined(kAttendWaves, kHeads, i, [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
-          leave(mine + h * D + d, sum);
-          if (d == 0) leave(mine + kHeads * D + 2 * h, m), leave(mine + kHeads * D + 2 * h + 1, sum_p);
-        });
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
-      __syncthreads();
-      global_u32* arrived = (global_u32*)(a.arrived + (uint64_t)s.r * a.chunks + s.pair);
-      if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __syncthreads();
-      if (lds_before == parts - 1) {   // the others' parts are in, and what was joined above is no longer needed
+      // what is joined first: this workgroup's wavefronts; then, if there are many parts, those of a cluster; then all, or the clusters'
+      const uint32_t cluster = blockIdx.x / kCluster, last_group = group0 + parts - 1;
+      bool whole = parts <= kCluster;
+      uint32_t first_part = whole ? group0 : max(group0, cluster * kCluster), n = whole ? parts : min(last_group, cluster * kCluster + kCluster - 1) - first_part + 1;
+      float* mine = slot_of(blockIdx.x);
+      uint32_t joins = kAttendWaves, joins_heads = kHeads;
+      for (;;) {
+        for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads)
+          joined(joins, joins_heads, i, [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
+            if (n == 0) return finish(h, d, sum, m, sum_p);
+            leave(mine + h * D + d, sum);
+            if (d == 0) leave(mine + kHeads * D + 2 * h, m), leave(mine + kHeads * D + 2 * h + 1, sum_p);
+          });
+        if (n == 0) break;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
+        __syncthreads();
+        // (a cluster has parts of at most two rows that reach beyond it: one that begins before it, one that begins in it)
+        global_u32* arrived = (global_u32*)(whole ? a.arrived + 2 * (kMaxGroups / kCluster) + (uint64_t)s.r * a.chunks + s.pair
+                                                  : a.arrived + 2 * cluster + (group0 >= cluster * kCluster ? 1 : 0));
+        if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (lds_before != n - 1) break;   // the last one joins: the others' parts are in
         if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         // a head and every per_head-th part for each group of DIM / 4 lanes, four dims a lane, kAhead parts at a time
         constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes, kAhead = 4;
         const uint32_t heads_n = n_heads > 4 ? 8 : n_heads > 2 ? 4 : n_heads, per_head = kGroups / heads_n;
         const uint32_t mine_of = threadIdx.x / kLanes, h = mine_of % heads_n, part0 = mine_of / heads_n, d0 = threadIdx.x % kLanes * 4;
+        const bool of_clusters = whole && parts > kCluster;
         if (h < n_heads) {
           float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
           float m = -INFINITY, sum_p = 0.f;
-          for (uint32_t v = part0; v < parts; v += kAhead * per_head) {
+          for (uint32_t v = part0; v < n; v += kAhead * per_head) {
             float2 sums[kAhead][2], st[kAhead];
 #pragma unroll
             for (uint32_t i = 0; i < kAhead; ++i) {
-              const float* from = slot_of(group0 + min(v + i * per_head, parts - 1));
+              const uint32_t w = min(v + i * per_head, n - 1);
+              const float* from = slot_of(of_clusters ? max(group0, (group0 / kCluster + w) * kCluster) : first_part + w);
               const float* at = from + h * D + (d0 < D ? d0 : 0);
               sums[i][0] = left_by(at), sums[i][1] = left_by(at + 2);
               st[i] = left_by(from + kHeads * D + 2 * h);
             }
 #pragma unroll
             for (uint32_t i = 0; i < kAhead; ++i) {
-              if (v + i * per_head >= parts) continue;
+              if (v + i * per_head >= n) continue;
               const float to = fmaxf(m, st[i].x), base = to == -INFINITY ? 0.f : to;
               const float f = __builtin_amdgcn_exp2f(m - base), e = __builtin_amdgcn_exp2f(st[i].x - base);
               m = to;
@@ -433,7 +445,13 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
           *(float4*)&lds_sum[mine_of * (DIM + 4) + d0] = sum;
         }
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads) joined(per_head, heads_n, i, finish);
+        joins = per_head, joins_heads = heads_n;
+        if (whole) {
+          n = 0;
+        } else {   // the cluster's parts become one, in the first one's place
+          mine = slot_of(first_part);
+          whole = true, n = last_group / kCluster - group0 / kCluster + 1;
+        }
       }
     }
     if (!more) break;
@@ -488,7 +506,7 @@ int check_attend(const std::string& who, const tq_cache* cache, const tq_attend_
     return at;
   };
   l->bytes = 0;
-  l->arrived = place((uint64_t)a->rows * l->chunks * 4);
+  l->arrived = place(((uint64_t)a->rows * l->chunks + 2 * (kMaxGroups / kCluster)) * 4);
   l->partials = place((uint64_t)l->groups * 2 * kHeads * (c->head_dim + 2) * 4);
   l->logits = a->accumulate ? place((uint64_t)a->rows * a->heads * c->capacity * 4) : 0;
   l->stats = a->accumulate ? place((uint64_t)a->rows * a->heads * 8) : 0;
