@@ -32,7 +32,7 @@ struct AttendView {
   float2* stats;       // [row][head]: maximum and 1 / total of the whole row (accumulate)
   uint64_t q_stride, out_stride;
   float scale;         // times log2(e)
-  uint32_t rows, heads, group, chunks, q16;   // chunks: of up to kHeads query heads that share a key/value head, of all of these
+  uint32_t rows, heads, group, chunks, q16, out_by4;   // chunks: of up to kHeads query heads that share a key/value head, of all of these
 };
 
 __device__ __forceinline__ float ror8_sum(float v) {   // v of this lane + v of the lane 8 columns on
@@ -360,48 +360,66 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     const uint32_t n_heads = s.n_heads, group0 = s.pair_first / share, parts = (s.pair_first + s.units - 1) / share - group0 + 1;
     const uint64_t slot_floats = kHeads * (D + 2);
     auto slot_of = [&](uint32_t group) { return a.partials + (2 * (uint64_t)group + (group * share >= s.pair_first ? 0 : 1)) * slot_floats; };
-    auto finish = [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
-      const float inv = sum_p == 0.f ? 0.f : 1.f / sum_p;
-      a.out[s.r * a.out_stride + (s.first_head + h) * D + d] = (uint16_t)pack_bf16(sum * inv, 0.f);
-      if (TRACK && d == 0) a.stats[(uint64_t)s.r * a.heads + s.first_head + h] = make_float2(m == -INFINITY ? 0.f : m, inv);
+    // a group of DIM / 4 lanes per head, four dims a lane
+    constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes;
+    static_assert(kGroups >= kHeads && kGroups <= kAttendWaves * kHeads, "a group per head; lds_max");
+    const uint32_t of_group = threadIdx.x / kLanes, d0 = threadIdx.x % kLanes * 4;
+    const bool joins = of_group < n_heads && d0 < D;
+    struct Joined {
+      float4 sum;
+      float m, sum_p;
     };
-    // n parts' sums, maxima and totals in LDS, [part][heads_n][DIM + 4] -> the whole
-    auto joined = [&](uint32_t n, uint32_t heads_n, uint32_t i, auto&& put) {
-      const uint32_t h = i / D, d = i % D;
-      float m = -INFINITY, sum = 0.f, sum_p = 0.f;
-      for (uint32_t w = 0; w < n; ++w) m = fmaxf(m, lds_max[w * heads_n + h]);
-      const float base = m == -INFINITY ? 0.f : m;
+    auto joined = [&](uint32_t n, uint32_t heads_n) {   // n parts in LDS, [part][heads_n][DIM + 4] -> the whole
+      Joined j = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+#pragma unroll 4
+      for (uint32_t w = 0; w < n; ++w) j.m = fmaxf(j.m, lds_max[w * heads_n + of_group]);
+      const float base = j.m == -INFINITY ? 0.f : j.m;
+#pragma unroll 4
       for (uint32_t w = 0; w < n; ++w) {
-        const float f = __builtin_amdgcn_exp2f(lds_max[w * heads_n + h] - base);
-        sum = fmaf(f, lds_sum[(w * heads_n + h) * (DIM + 4) + d], sum);
-        sum_p = fmaf(f, lds_total[w * heads_n + h], sum_p);
+        const float f = __builtin_amdgcn_exp2f(lds_max[w * heads_n + of_group] - base);
+        const float4 v = *(const float4*)&lds_sum[(w * heads_n + of_group) * (DIM + 4) + d0];
+        j.sum.x = fmaf(f, v.x, j.sum.x), j.sum.y = fmaf(f, v.y, j.sum.y), j.sum.z = fmaf(f, v.z, j.sum.z), j.sum.w = fmaf(f, v.w, j.sum.w);
+        j.sum_p = fmaf(f, lds_total[w * heads_n + of_group], j.sum_p);
       }
-      put(h, d, sum, m, sum_p);
+      return j;
+    };
+    auto finish = [&](const Joined& j) {
+      const float inv = j.sum_p == 0.f ? 0.f : 1.f / j.sum_p;
+      uint16_t* to = a.out + s.r * a.out_stride + (s.first_head + of_group) * D + d0;
+      const uint32_t lo = pack_bf16(j.sum.x * inv, j.sum.y * inv), hi = pack_bf16(j.sum.z * inv, j.sum.w * inv);
+      if (a.out_by4) *(uint2*)to = make_uint2(lo, hi);
+      else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
+      if (TRACK && d0 == 0) a.stats[(uint64_t)s.r * a.heads + s.first_head + of_group] = make_float2(j.m == -INFINITY ? 0.f : j.m, inv);
     };
     if (parts == 1) {
-      for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads) joined(kAttendWaves, kHeads, i, finish);
+      if (joins) finish(joined(kAttendWaves, kHeads));
     } else {
-      typedef __attribute__((address_space(1))) float global_f32;
       typedef __attribute__((address_space(1))) uint32_t global_u32;
-      typedef __attribute__((address_space(1))) const uint64_t global_cu64;
+      typedef __attribute__((address_space(1))) uint64_t global_u64;
       // stored to and loaded from the level that the device shares (an acquire fence would empty an L2 that the others read through)
       auto left_by = [&](const float* p) {
-        return __builtin_bit_cast(float2, __hip_atomic_load((global_cu64*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        return __builtin_bit_cast(float2, __hip_atomic_load((global_u64*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
       };
-      auto leave = [&](float* p, float v) { __hip_atomic_store((global_f32*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+      auto leave = [&](float* p, float x, float y) {
+        __hip_atomic_store((global_u64*)p, __builtin_bit_cast(uint64_t, make_float2(x, y)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      };
       // what is joined first: this workgroup's wavefronts; then, if there are many parts, those of a cluster; then all, or the clusters'
       const uint32_t cluster = blockIdx.x / kCluster, last_group = group0 + parts - 1;
       bool whole = parts <= kCluster;
       uint32_t first_part = whole ? group0 : max(group0, cluster * kCluster), n = whole ? parts : min(last_group, cluster * kCluster + kCluster - 1) - first_part + 1;
       float* mine = slot_of(blockIdx.x);
-      uint32_t joins = kAttendWaves, joins_heads = kHeads;
+      uint32_t in_lds = kAttendWaves, in_lds_heads = kHeads;
       for (;;) {
-        for (uint32_t i = threadIdx.x; i < n_heads * D; i += kAttendThreads)
-          joined(joins, joins_heads, i, [&](uint32_t h, uint32_t d, float sum, float m, float sum_p) {
-            if (n == 0) return finish(h, d, sum, m, sum_p);
-            leave(mine + h * D + d, sum);
-            if (d == 0) leave(mine + kHeads * D + 2 * h, m), leave(mine + kHeads * D + 2 * h + 1, sum_p);
-          });
+        if (joins) {
+          const Joined j = joined(in_lds, in_lds_heads);
+          if (n == 0) {
+            finish(j);
+          } else {
+            leave(mine + of_group * D + d0, j.sum.x, j.sum.y);
+            leave(mine + of_group * D + d0 + 2, j.sum.z, j.sum.w);
+            if (d0 == 0) leave(mine + kHeads * D + 2 * of_group, j.m, j.sum_p);
+          }
+        }
         if (n == 0) break;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
         __syncthreads();
@@ -412,10 +430,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         __syncthreads();
         if (lds_before != n - 1) break;   // the last one joins: the others' parts are in
         if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        // a head and every per_head-th part for each group of DIM / 4 lanes, four dims a lane, kAhead parts at a time
-        constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes, kAhead = 4;
-        const uint32_t heads_n = n_heads > 4 ? 8 : n_heads > 2 ? 4 : n_heads, per_head = kGroups / heads_n;
-        const uint32_t mine_of = threadIdx.x / kLanes, h = mine_of % heads_n, part0 = mine_of / heads_n, d0 = threadIdx.x % kLanes * 4;
+        // every group takes a head and every per_head-th part, kAhead parts at a time
+        constexpr uint32_t kAhead = 4;
+        const uint32_t heads_n = n_heads > 4 ? 8 : n_heads > 2 ? 4 : n_heads, per_head = kGroups / heads_n, h = of_group % heads_n, part0 = of_group / heads_n;
         const bool of_clusters = whole && parts > kCluster;
         if (h < n_heads) {
           float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -441,11 +458,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
               sum.z = sum.z * f + sums[i][1].x * e, sum.w = sum.w * f + sums[i][1].y * e;
             }
           }
-          if (d0 == 0) lds_max[mine_of] = m, lds_total[mine_of] = sum_p;
-          *(float4*)&lds_sum[mine_of * (DIM + 4) + d0] = sum;
+          if (d0 == 0) lds_max[of_group] = m, lds_total[of_group] = sum_p;
+          *(float4*)&lds_sum[of_group * (DIM + 4) + d0] = sum;
         }
         __syncthreads();
-        joins = per_head, joins_heads = heads_n;
+        in_lds = per_head, in_lds_heads = heads_n;
         if (whole) {
           n = 0;
         } else {   // the cluster's parts become one, in the first one's place
@@ -537,7 +554,8 @@ int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
   char* ws = (char*)a->workspace;
   const AttendView v{a->q, (uint16_t*)a->out, a->seqs, a->lengths, (uint32_t*)(ws + l.arrived), (float*)(ws + l.partials), (float*)(ws + l.logits),
                      (float2*)(ws + l.stats), a->q_stride ? a->q_stride : row, a->out_stride ? a->out_stride : row,
-                     a->scale * kLog2e, a->rows, a->heads, a->heads / c.kv_heads, l.chunks, q16};
+                     a->scale * kLog2e, a->rows, a->heads, a->heads / c.kv_heads, l.chunks, q16,
+                     (a->out_stride ? a->out_stride : row) % 4 == 0 && aligned_to(a->out, 8)};
   const bool int8 = cache->type == TQ_INT8;
   hipStream_t s = (hipStream_t)stream;
   if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, s);
