@@ -163,12 +163,15 @@ struct EvictView {
   float* scores_out;
   int32_t* positions_out;
   uint32_t* counts;   // [seq][head]: tokens to move
-  uint2* moves;       // [seq][head][keep]: slot to fill, slot it is filled from
+  uint32_t *to, *from;   // [seq][head][keep]: slots to fill, and the slots they are filled from
   uint32_t keep;
+  bool by4;           // scores and positions start on 16 bytes, in and out
 };
 
-constexpr int kSelectThreads = 1024, kMoveThreads = 256;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kMoveThreads = 256, kCopies = 16;
+constexpr uint32_t kMovesInSelect = 512;
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Numbers that compare as the scores do: NaN lowest, the two zeros equal, protected tokens above +infinity.
 __device__ __forceinline__ uint32_t rank_of(float score, bool is_protected) {
@@ -178,117 +181,250 @@ __device__ __forceinline__ uint32_t rank_of(float score, bool is_protected) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Sum over lower threads of the workgroup, and over all of them; totals: one word per wavefront.
-__device__ __forceinline__ uint32_t sum_below(bool v, uint32_t* totals, uint32_t* all) {
-  const uint64_t ballot = __ballot(v);
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  __syncthreads();
-  if (lane == 0) totals[wave] = __popcll(ballot);
-  __syncthreads();
-  uint32_t below = __popcll(ballot & ((1ull << lane) - 1)), sum = 0;
-  for (uint32_t w = 0; w < kSelectThreads / 64; ++w) {
-    below += w < wave ? totals[w] : 0;
-    sum += totals[w];
-  }
-  *all = sum;
-  return below;
+__device__ __forceinline__ uint32_t wave_prefix_sum(uint32_t v) {   // inclusive
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next one
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
+  return v;
 }
 
-// Which tokens of a (sequence, head) stay: the `keep` highest ranks, found 8 bits at a time from the top (a histogram of the
-// next 8 bits over those that agree with the bits found), then one pass in the order of the slots that numbers the equal ones at
-// the limit, the free slots below `keep` and the kept ones above.
+// Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., kAhead of them
+// together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.
+template <bool INT8>
+__device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, uint32_t n, uint32_t first, uint32_t step) {
+  constexpr uint32_t kAhead = 4;
+  const uint32_t list = s * c.kv_heads + h, lane = threadIdx.x % 16, bytes = c.head_dim * (INT8 ? 1 : 2), mask = (1u << c.page_shift) - 1;
+  const uint64_t row = (uint64_t)list * c.capacity, size = INT8 ? 1 : 2;
+  const uint32_t *slots_to = e.to + (uint64_t)list * e.keep, *slots_from = e.from + (uint64_t)list * e.keep;
+  const int32_t* table = c.tables + (uint64_t)s * c.table_stride;
+  for (uint32_t m = first; m < n; m += kAhead * step) {
+    uint32_t to[kAhead], of[kAhead], to_page[kAhead], of_page[kAhead];
+    bool there[kAhead];
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      const uint32_t at = min(m + i * step, n - 1);
+      to[i] = slots_to[at], of[i] = slots_from[at];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      to_page[i] = (uint32_t)table[to[i] >> c.page_shift], of_page[i] = (uint32_t)table[of[i] >> c.page_shift];
+      there[i] = m + i * step < n && to_page[i] < c.n_pages && of_page[i] < c.n_pages;
+    }
+    auto place = [&](uint32_t page, uint32_t slot) { return size * (page * c.page_stride + h * c.head_stride + (slot & mask) * c.slot_stride); };
+    auto mark = [&](uint32_t page, uint32_t slot) { return (((uint64_t)page * c.kv_heads + h) << c.page_shift) + (slot & mask); };
+    for (uint32_t b = lane * 16; b < bytes; b += 256) {
+      u32x4 k[kAhead], v[kAhead];
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) {   // (in place of a token that is not moved, one of page 0)
+        const uint64_t at = place(there[i] ? of_page[i] : 0, of[i]) + b;
+        k[i] = *(const u32x4*)(c.k + at), v[i] = *(const u32x4*)(c.v + at);
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i)
+        if (there[i]) {
+          const uint64_t at = place(to_page[i], to[i]) + b;
+          *(u32x4*)(c.k + at) = k[i], *(u32x4*)(c.v + at) = v[i];
+        }
+    }
+    if (lane < kAhead && m + lane * step < n) {   // a lane per token
+      uint32_t t = to[0], f = of[0], tp = to_page[0], fp = of_page[0];
+#pragma unroll
+      for (uint32_t i = 1; i < kAhead; ++i)
+        if (lane == i) t = to[i], f = of[i], tp = to_page[i], fp = of_page[i];
+      e.scores_out[row + t] = c.scores[row + f];
+      if (c.positions) e.positions_out[row + t] = c.positions[row + f];
+      if (INT8 && tp < c.n_pages && fp < c.n_pages) {
+        c.k_scale[mark(tp, t)] = c.k_scale[mark(fp, f)];
+        c.v_scale[mark(tp, t)] = c.v_scale[mark(fp, f)];
+      }
+    }
+  }
+}
+
+// Which tokens of a (sequence, head) stay: the `keep` highest ranks, found 8 bits at a time from the top (a histogram of the next
+// 8 bits over those that agree with the bits found), then one look in the order of the slots that numbers the equal ones at the
+// limit, the free slots below `keep` and the kept ones above.
+//
+// A workgroup per list; a thread has 4 neighbouring slots of every kStride, and the ranks of STRIDES of them in registers.  Where
+// that is not the whole list the ranks are made again from the scores, which the L2 holds by then, for every 8 bits.  Scores share
+// few exponents, so that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there
+// are kCopies of it.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
+template <int STRIDES, bool INT8, bool MOVES>
 __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, EvictView e) {
-  __shared__ uint32_t bins[256], totals[kSelectThreads / 64], found[2];
-  const uint32_t h = blockIdx.x, s = blockIdx.y, list = s * c.kv_heads + h;
+  __shared__ __attribute__((aligned(16))) uint32_t bins[256 * kCopies], sums[256], totals[2][64];
+  constexpr uint32_t kStride = kSelectThreads * 4, kRound = kStride * STRIDES;
+  const uint32_t h = blockIdx.x, s = blockIdx.y, list = s * c.kv_heads + h, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint64_t row = (uint64_t)list * c.capacity;
   const uint32_t length = (uint32_t)min(max(e.lengths[s], 0), (int32_t)c.capacity);
   const int32_t since = e.since ? e.since[s] : 0;
-  const bool out_of_place = e.scores_out != c.scores, positions_too = e.positions_out != c.positions;
-  auto stay = [&](uint32_t slot) {
-    if (out_of_place) e.scores_out[row + slot] = c.scores[row + slot];
-    if (positions_too) e.positions_out[row + slot] = c.positions[row + slot];
+  const uint32_t stay = min(length, e.keep);
+  const uint32_t rounds = (length + kRound - 1) / kRound;
+  uint32_t rank[STRIDES][4];
+  auto slot_of = [&](uint32_t round, int k) { return round * kRound + k * kStride + threadIdx.x * 4; };
+  auto look = [&](uint32_t round, bool copies) {   // the ranks of this thread's slots of a round
+#pragma unroll
+    for (int k = 0; k < STRIDES; ++k) {
+      if (k % 4 == 0 && k) asm volatile("" ::: "memory");   // (no more than four strides' loads at a time: registers)
+      const uint32_t i = slot_of(round, k);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      int4 p = make_int4(0, 0, 0, 0);
+      if (i < length) {   // (a list's room is a multiple of 16 slots)
+        if (e.by4) {
+          v = *(const float4*)(c.scores + row + i);
+          if (c.positions) p = *(const int4*)(c.positions + row + i);
+        } else {
+          const float* sc = c.scores + row + i;
+          v = make_float4(sc[0], sc[1], sc[2], sc[3]);
+          if (c.positions) p = make_int4(c.positions[row + i], c.positions[row + i + 1], c.positions[row + i + 2], c.positions[row + i + 3]);
+        }
+        if (copies) {   // what stays in its place, and what will be written over by a token that is moved
+          if (e.by4 && i + 4 <= stay) {
+            if (e.scores_out != c.scores) *(float4*)(e.scores_out + row + i) = v;
+            if (e.positions_out != c.positions) *(int4*)(e.positions_out + row + i) = p;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (i + j < stay) {
+                if (e.scores_out != c.scores) e.scores_out[row + i + j] = (&v.x)[j];
+                if (e.positions_out != c.positions) e.positions_out[row + i + j] = (&p.x)[j];
+              }
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rank[k][j] = rank_of((&v.x)[j], e.since && (&p.x)[j] >= since);
+    }
   };
+  const bool copies = e.scores_out != c.scores || e.positions_out != c.positions;
+  if (MOVES && h == 0 && threadIdx.x == 0) e.lengths_out[s] = min(e.lengths[s], (int32_t)min(e.keep, 0x7FFFFFFFu));
   if (length <= e.keep) {
     if (threadIdx.x == 0) e.counts[list] = 0;
-    for (uint32_t i = threadIdx.x; i < length; i += kSelectThreads) stay(i);
+    if (copies)
+      for (uint32_t round = 0; round < rounds; ++round) look(round, true);
     return;
   }
-  auto rank_at = [&](uint32_t i) { return rank_of(c.scores[row + i], e.since && c.positions[row + i] >= since); };
+  *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
+  static_assert(256 * kCopies == kSelectThreads * 4, "a thread clears four words");
+  if (rounds == 1) look(0, copies);
+  __syncthreads();
   uint32_t prefix = 0, left = e.keep;   // `left` of those that agree with the prefix stay
   for (int shift = 24; shift >= 0; shift -= 8) {
-    if (threadIdx.x < 256) bins[threadIdx.x] = 0;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < length; i += kSelectThreads) {
-      const uint32_t k = rank_at(i);
-      if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&bins[k >> shift & 255], 1u);
+    for (uint32_t round = 0; round < rounds; ++round) {
+      if (rounds > 1) look(round, copies && shift == 24);
+#pragma unroll
+      for (int k = 0; k < STRIDES; ++k) {
+        const uint32_t i = slot_of(round, k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (i + j < length && (shift == 24 || (rank[k][j] ^ prefix) >> ((shift + 8) & 31) == 0))
+            atomicAdd(&bins[(rank[k][j] >> shift & 255) * kCopies + (lane & (kCopies - 1))], 1u);
+      }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      uint32_t b = 255, over = 0;
-      while (over + bins[b] < left) over += bins[b--];
-      found[0] = b, found[1] = over;
+    {   // four lanes per bin
+      const uint4 v = *(const uint4*)&bins[threadIdx.x * 4];
+      *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
+      uint32_t n = v.x + v.y + v.z + v.w;
+      n += __shfl_xor(n, 1);
+      n += __shfl_xor(n, 2);
+      if ((threadIdx.x & 3) == 0) sums[255 - threadIdx.x / 4] = n;   // from the top
     }
     __syncthreads();
-    prefix |= found[0] << shift;
-    left -= found[1];
+    const uint4 v = *(const uint4*)&sums[4 * lane];   // every wavefront looks for itself
+    const uint32_t n = v.x + v.y + v.z + v.w, upto = wave_prefix_sum(n), before = upto - n;
+    const uint64_t at = __ballot(before < left && left <= upto);
+    uint32_t over = before, b = 4 * lane, in = v.x;
+    if (over + in < left) over += in, in = v.y, ++b;
+    if (over + in < left) over += in, in = v.z, ++b;
+    if (over + in < left) over += in, in = v.w, ++b;
+    const int one = __builtin_ctzll(at);
+    prefix |= (255 - (uint32_t)__builtin_amdgcn_readlane((int)b, one)) << shift;
+    left -= (uint32_t)__builtin_amdgcn_readlane((int)over, one);
+    if ((uint32_t)__builtin_amdgcn_readlane((int)in, one) == left) break;   // all of these stay
   }
+  // The numbering, up to four strides at a time.  Sums over all wavefronts and strides before this wavefront's: totals has a word
+  // for each, in that order.
+  constexpr int kSome = STRIDES < 4 ? STRIDES : 4;
+  static_assert(4 * kSelectWaves == 64, "a lane per word");
+  auto before_each = [&](uint32_t word, uint32_t (&at)[kSome]) {
+    const uint32_t upto = wave_prefix_sum(word), below = upto - word;
+#pragma unroll
+    for (int k = 0; k < kSome; ++k) at[k] = (uint32_t)__builtin_amdgcn_readlane((int)below, k * kSelectWaves + wave);
+    return (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  };
   uint32_t equal = 0, freed = 0, taken = 0;   // numbered so far
-  uint2* moves = e.moves + (uint64_t)list * e.keep;
-  for (uint32_t first = 0; first < length; first += kSelectThreads) {
-    const uint32_t i = first + threadIdx.x;
-    const uint32_t k = i < length ? rank_at(i) : 0;
-    uint32_t all;
-    const bool at_limit = i < length && k == prefix;
-    const uint32_t before = equal + sum_below(at_limit, totals, &all);
-    equal += all;
-    const bool kept = i < length && (k > prefix || (at_limit && before < left));
-    const bool frees = i < e.keep && !kept, takes = i >= e.keep && kept;
-    const uint32_t f = freed + sum_below(frees, totals, &all);
-    freed += all;
-    const uint32_t t = taken + sum_below(takes, totals, &all);
-    taken += all;
-    if (frees) moves[f].x = i;
-    if (takes) moves[t].y = i;
-    if (kept && i < e.keep) stay(i);
+  uint32_t *to = e.to + (uint64_t)list * e.keep, *from = e.from + (uint64_t)list * e.keep;
+  if (threadIdx.x < 64) totals[0][threadIdx.x] = totals[1][threadIdx.x] = 0;   // (more than there are of them with one stride)
+  __syncthreads();
+  for (uint32_t round = 0; round < rounds; ++round) {
+    if (rounds > 1) look(round, false);
+    uint64_t above = 0, ties = 0;   // a bit per slot of this thread: its rank is above the limit, or at it
+#pragma unroll
+    for (int k = 0; k < STRIDES; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool here = slot_of(round, k) + j < length;
+        above |= (uint64_t)(here && rank[k][j] > prefix) << (4 * k + j);
+        ties |= (uint64_t)(here && rank[k][j] == prefix) << (4 * k + j);
+      }
+    for (int k0 = 0; k0 < STRIDES && slot_of(round, k0) - threadIdx.x * 4 < length; k0 += kSome, above >>= 16, ties >>= 16) {
+      uint32_t eq[kSome], at[kSome];
+#pragma unroll
+      for (int k = 0; k < kSome; ++k) {
+        const uint32_t n = (uint32_t)__builtin_popcount((uint32_t)ties >> (4 * k) & 15), upto = wave_prefix_sum(n);
+        if (lane == 63) totals[0][k * kSelectWaves + wave] = upto;
+        eq[k] = upto - n;
+      }
+      __syncthreads();
+      const uint32_t all = before_each(totals[0][lane], at);
+      uint32_t packed[kSome], upto[kSome];   // a bit per slot: 0..3 it becomes free, 4..7 its token moves; both counts, up to and with this lane
+#pragma unroll
+      for (int k = 0; k < kSome; ++k) {
+        const uint32_t i = slot_of(round, k0 + k);
+        uint32_t before = equal + at[k] + eq[k];
+        packed[k] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool tie = (uint32_t)ties >> (4 * k + j) & 1, kept = ((uint32_t)above >> (4 * k + j) & 1) || (tie && before < left);
+          before += tie;
+          packed[k] |= (uint32_t)(i + j < stay && !kept) << j | (uint32_t)(i + j >= e.keep && kept) << (4 + j);
+        }
+        upto[k] = wave_prefix_sum((uint32_t)__builtin_popcount(packed[k] & 15) << 16 | (uint32_t)__builtin_popcount(packed[k] >> 4));
+        if (lane == 63) totals[1][k * kSelectWaves + wave] = upto[k];
+      }
+      equal += all;
+      __syncthreads();
+      // (four strides have at most 2^14 of each)
+      const uint32_t both = before_each(totals[1][lane], at);
+#pragma unroll
+      for (int k = 0; k < kSome; ++k) {
+        const uint32_t i = slot_of(round, k0 + k), frees = packed[k] & 15, takes = packed[k] >> 4, below = at[k] + upto[k];
+        uint32_t f = freed + (below >> 16) - (uint32_t)__builtin_popcount(frees), t = taken + (below & 0xFFFF) - (uint32_t)__builtin_popcount(takes);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (frees >> j & 1) to[f++] = i + j;
+          if (takes >> j & 1) from[t++] = i + j;
+        }
+      }
+      freed += both >> 16, taken += both & 0xFFFF;
+    }
+    __syncthreads();
   }
-  if (threadIdx.x == 0) e.counts[list] = freed;
+  if constexpr (MOVES) move_tokens<INT8>(c, e, s, h, freed, threadIdx.x / 16, kSelectThreads / 16);   // (the list is this workgroup's: the barrier suffices)
+  else if (threadIdx.x == 0) e.counts[list] = freed;
 }
 
-// Moves keys, values, scales and marks: a group of 16 lanes per token.  No slot is both written and read.
 template <bool INT8>
 __global__ __launch_bounds__(kMoveThreads) void k_evict_move(CacheView c, EvictView e) {
-  const uint32_t h = blockIdx.y, s = blockIdx.z, list = s * c.kv_heads + h;
+  const uint32_t h = blockIdx.y, s = blockIdx.z;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) {
     const int32_t length = e.lengths[s];
     e.lengths_out[s] = min(length, (int32_t)min(e.keep, 0x7FFFFFFFu));
   }
-  const uint32_t n = e.counts[list];
-  const uint64_t row = (uint64_t)list * c.capacity;
-  const uint2* moves = e.moves + (uint64_t)list * e.keep;
-  const uint32_t lane = threadIdx.x % 16, bytes = c.head_dim * (INT8 ? 1 : 2), mask = (1u << c.page_shift) - 1;
-  const int32_t* table = c.tables + (uint64_t)s * c.table_stride;
-  for (uint32_t m = (blockIdx.x * kMoveThreads + threadIdx.x) / 16; m < n; m += gridDim.x * (kMoveThreads / 16)) {
-    const uint2 mv = moves[m];
-    if (lane == 0) {
-      e.scores_out[row + mv.x] = c.scores[row + mv.y];
-      if (c.positions) e.positions_out[row + mv.x] = c.positions[row + mv.y];
-    }
-    const uint32_t to = (uint32_t)table[mv.x >> c.page_shift], of = (uint32_t)table[mv.y >> c.page_shift];
-    if (to >= c.n_pages || of >= c.n_pages) continue;
-    const uint64_t size = INT8 ? 1 : 2;
-    const uint64_t d = size * (to * c.page_stride + h * c.head_stride + (mv.x & mask) * c.slot_stride);
-    const uint64_t f = size * (of * c.page_stride + h * c.head_stride + (mv.y & mask) * c.slot_stride);
-    for (uint32_t b = lane * 16; b < bytes; b += 256) {
-      const uint4 k = *(const uint4*)(c.k + f + b), v = *(const uint4*)(c.v + f + b);
-      *(uint4*)(c.k + d + b) = k;
-      *(uint4*)(c.v + d + b) = v;
-    }
-    if (INT8 && lane == 0) {
-      const uint64_t sd = (((uint64_t)to * c.kv_heads + h) << c.page_shift) + (mv.x & mask), sf = (((uint64_t)of * c.kv_heads + h) << c.page_shift) + (mv.y & mask);
-      c.k_scale[sd] = c.k_scale[sf];
-      c.v_scale[sd] = c.v_scale[sf];
-    }
-  }
+  move_tokens<INT8>(c, e, s, h, e.counts[s * c.kv_heads + h], (blockIdx.x * kMoveThreads + threadIdx.x) / 16, gridDim.x * (kMoveThreads / 16));
 }
 
 uint64_t evict_counts_bytes(const CacheView& c) { return ((uint64_t)c.n_seqs * c.kv_heads * 4 + 255) / 256 * 256; }
@@ -316,13 +452,31 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
     return refuse(TQ_E_INVALID_ARG, who + ": a pointer is not aligned to its type (workspace: 16 bytes)");
   const uint32_t keep = std::min(a->keep, c.capacity);
   EvictView e{a->lengths, a->since, a->lengths_out ? a->lengths_out : a->lengths, a->scores_out ? a->scores_out : c.scores,
-              a->positions_out ? a->positions_out : c.positions, (uint32_t*)a->workspace, (uint2*)((char*)a->workspace + evict_counts_bytes(c)), keep};
-  hipLaunchKernelGGL(k_evict_select, dim3(c.kv_heads, c.n_seqs), dim3(kSelectThreads), 0, (hipStream_t)stream, c, e);
-  const uint32_t most = std::min(keep, c.capacity - keep), groups = kMoveThreads / 16;
-  const uint32_t parts = std::max(1u, std::min((most + groups - 1) / groups, std::max(1u, 4096u / (c.kv_heads * c.n_seqs))));
-  const dim3 grid(parts, c.kv_heads, c.n_seqs);
-  if (cache->type == TQ_INT8) hipLaunchKernelGGL(k_evict_move<true>, grid, dim3(kMoveThreads), 0, (hipStream_t)stream, c, e);
-  else hipLaunchKernelGGL(k_evict_move<false>, grid, dim3(kMoveThreads), 0, (hipStream_t)stream, c, e);
+              a->positions_out ? a->positions_out : c.positions, (uint32_t*)a->workspace, (uint32_t*)((char*)a->workspace + evict_counts_bytes(c)), nullptr, keep,
+              aligned_to(c.scores, 16) && aligned_to(c.positions, 16) && aligned_to(a->scores_out, 16) && aligned_to(a->positions_out, 16)};
+  e.from = e.to + (uint64_t)c.n_seqs * c.kv_heads * keep;
+  const bool int8 = cache->type == TQ_INT8;
+  const uint32_t most = std::min(keep, c.capacity - keep);   // tokens to move, of a list
+  // Few of them are moved by the workgroup that has found them, unless others may still have to read the lengths that it writes.
+  const bool moves = e.lengths_out != e.lengths && most <= kMovesInSelect;
+  const dim3 lists(c.kv_heads, c.n_seqs);
+  hipStream_t st = (hipStream_t)stream;
+  auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, lists, dim3(kSelectThreads), 0, st, c, e); };
+  auto of = [&](auto n) {
+    constexpr int S = decltype(n)::value;
+    if (moves) int8 ? select(k_evict_select<S, true, true>) : select(k_evict_select<S, false, true>);
+    else select(k_evict_select<S, false, false>);
+  };
+  if (c.capacity <= 4 * kSelectThreads) of(std::integral_constant<int, 1>());
+  else if (c.capacity <= 16 * kSelectThreads) of(std::integral_constant<int, 4>());
+  else of(std::integral_constant<int, 16>());
+  if (!moves) {
+    const uint32_t groups = kMoveThreads / 16;
+    const uint32_t parts = std::max(1u, std::min((most + groups - 1) / groups, std::max(1u, 4096u / (c.kv_heads * c.n_seqs))));
+    const dim3 grid(parts, c.kv_heads, c.n_seqs);
+    if (int8) hipLaunchKernelGGL(k_evict_move<true>, grid, dim3(kMoveThreads), 0, st, c, e);
+    else hipLaunchKernelGGL(k_evict_move<false>, grid, dim3(kMoveThreads), 0, st, c, e);
+  }
   return launched("tq_cache_evict");
 }
 
