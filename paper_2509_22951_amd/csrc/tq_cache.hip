@@ -6,6 +6,8 @@
 namespace tq {
 namespace {
 
+constexpr int kAppendThreads = 256;
+
 struct AppendView {
   const float *q, *k, *v;
   void* q_out;
@@ -13,101 +15,120 @@ struct AppendView {
   const float *cos, *sin;
   uint64_t q_stride, k_stride, v_stride, q_out_stride;
   uint32_t heads, rotary_dim, n_positions, adjacent;
-  bool by4;   // every row starts on 16 bytes
+  bool by4, angles_by4;   // every row starts on 16 bytes, and those of the angles
 };
 
-// One workgroup takes some of the heads (query, key and value heads in this order) of one row; LANES lanes of a wavefront take a
-// head, 4 values each.  A pair of the halves rotation lies head_dim / 2 values apart: its other half comes from another lane of
-// the same group, so a wavefront has read all of its values before it writes any (q_out may be q), and 8 bits' absmax is a
-// maximum over the group.
+// One workgroup takes ITEMS * kAppendThreads / LANES of the heads (query, key and value heads in this order) of one row; LANES lanes of a
+// wavefront take a head, 4 values each, and ITEMS heads one after another, all of them requested ahead.  A pair of the halves
+// rotation lies rotary_dim / 2 values apart: its other half comes from another lane of the same group, so a wavefront has read all
+// of a head before it writes any (q_out may be q), and 8 bits' absmax is a maximum over the group.
 //
 // Bound: device memory for prompts; for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
-template <int LANES, bool INT8, bool Q16>
-__global__ __launch_bounds__(256) void k_cache_append(CacheView c, AppendView a) {
+template <int LANES, int ITEMS, bool INT8, bool Q16>
+__global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
+  typedef __attribute__((address_space(4))) const int32_t constant_i32;
+  constexpr uint32_t kGroups = kAppendThreads / LANES;
   const uint32_t r = blockIdx.x, D = c.head_dim;
-  const uint32_t t = threadIdx.x % LANES, head = (blockIdx.y * 256 + threadIdx.x) / LANES;
+  const uint32_t t = threadIdx.x % LANES, i = 4 * t, first_head = blockIdx.y * (ITEMS * kGroups) + threadIdx.x / LANES;
   const uint32_t n_heads = a.heads + 2 * c.kv_heads;
-  const int32_t seq = a.seqs ? a.seqs[r] : (int32_t)r, slot = a.slots[r], pos = a.positions ? a.positions[r] : slot;
+  const int32_t seq = a.seqs ? ((constant_i32*)a.seqs)[r] : (int32_t)r, slot = ((constant_i32*)a.slots)[r], pos = a.positions ? ((constant_i32*)a.positions)[r] : slot;
   const bool there = (uint32_t)seq < c.n_seqs && (uint32_t)slot < c.capacity && (a.rotary_dim == 0 || (uint32_t)pos < a.n_positions);
-  const uint32_t i = 4 * t;
-  const bool mine = head < n_heads && i < D;
-  const bool is_q = head < a.heads, is_v = head >= a.heads + c.kv_heads;
-  const uint32_t h = is_q ? head : is_v ? head - a.heads - c.kv_heads : head - a.heads;
-  float x[4] = {0.f, 0.f, 0.f, 0.f};
-  if (mine && there) {
-    const float* from = (is_q ? a.q + r * a.q_stride : is_v ? a.v + r * a.v_stride : a.k + r * a.k_stride) + h * D + i;
-    if (a.by4) {
-      const float4 d = *(const float4*)from;
-      x[0] = d.x, x[1] = d.y, x[2] = d.z, x[3] = d.w;
-    } else {
+  float x[ITEMS][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = from[j];
+  for (int k = 0; k < ITEMS; ++k) {
+    const uint32_t head = first_head + k * kGroups;
+    const bool is_q = head < a.heads, is_v = head >= a.heads + c.kv_heads;
+    const uint32_t h = is_q ? head : is_v ? head - a.heads - c.kv_heads : head - a.heads;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[k][j] = 0.f;
+    if (head < n_heads && i < D && there) {
+      const float* from = (is_q ? a.q + r * a.q_stride : is_v ? a.v + r * a.v_stride : a.k + r * a.k_stride) + h * D + i;
+      if (a.by4) {
+        const float4 d = *(const float4*)from;
+        x[k][0] = d.x, x[k][1] = d.y, x[k][2] = d.z, x[k][3] = d.w;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[k][j] = from[j];
+      }
     }
   }
-  if (a.rotary_dim && there) {   // the same for the whole workgroup
-    const uint32_t half = a.rotary_dim / 2;
-    const bool turned = mine && !is_v && i < a.rotary_dim;
-    const float *cs = a.cos + (uint64_t)(uint32_t)pos * half, *sn = a.sin + (uint64_t)(uint32_t)pos * half;
+  uint32_t page = c.n_pages;
+  if (there) page = (uint32_t)((constant_i32*)c.tables)[(uint64_t)(uint32_t)seq * c.table_stride + ((uint32_t)slot >> c.page_shift)];
+  const uint32_t half = a.rotary_dim / 2, in_page = (uint32_t)slot & ((1u << c.page_shift) - 1);
+  const bool turned = i < a.rotary_dim, second = !a.adjacent && i >= half;
+  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};   // of this lane's values (adjacent pairs: of pairs 0 and 1)
+  if (turned && there) {
+    const uint64_t at = (uint64_t)(uint32_t)pos * half + (a.adjacent ? i / 2 : second ? i - half : i);
     if (a.adjacent) {
-      if (turned) {
-        const float c0 = cs[i / 2], s0 = sn[i / 2], c1 = cs[i / 2 + 1], s1 = sn[i / 2 + 1];
-        const float y[4] = {x[0] * c0 - x[1] * s0, x[0] * s0 + x[1] * c0, x[2] * c1 - x[3] * s1, x[2] * s1 + x[3] * c1};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = y[j];
-      }
+      cs[0] = a.cos[at], cs[1] = a.cos[at + 1], sn[0] = a.sin[at], sn[1] = a.sin[at + 1];
+    } else if (a.angles_by4) {
+      const float4 d = *(const float4*)(a.cos + at), e = *(const float4*)(a.sin + at);
+      cs[0] = d.x, cs[1] = d.y, cs[2] = d.z, cs[3] = d.w, sn[0] = e.x, sn[1] = e.y, sn[2] = e.z, sn[3] = e.w;
     } else {
-      const bool second = i >= half;
-      const int other = (int)(threadIdx.x & 63) + (second ? -(int)(half / 4) : (int)(half / 4));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) cs[j] = a.cos[at + j], sn[j] = a.sin[at + j];
+    }
+  }
+  const int other = ((int)(threadIdx.x & 63) + (second ? -(int)(half / 4) : (int)(half / 4))) & 63;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const uint32_t head = first_head + k * kGroups;
+    const bool is_q = head < a.heads, is_v = head >= a.heads + c.kv_heads, mine = head < n_heads && i < D;
+    const uint32_t h = is_q ? head : is_v ? head - a.heads - c.kv_heads : head - a.heads;
+    float (&y)[4] = x[k];
+    if (a.adjacent) {
+      if (turned && !is_v) {
+        const float z[4] = {y[0] * cs[0] - y[1] * sn[0], y[0] * sn[0] + y[1] * cs[0], y[2] * cs[1] - y[3] * sn[1], y[2] * sn[1] + y[3] * cs[1]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = z[j];
+      }
+    } else if (half) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float y = __shfl(x[j], other & 63);
-        const uint32_t at = second ? i + j - half : i + j;
-        if (turned) x[j] = second ? y * sn[at] + x[j] * cs[at] : x[j] * cs[at] - y * sn[at];
+        const float z = __shfl(y[j], other);
+        if (turned && !is_v) y[j] = second ? z * sn[j] + y[j] * cs[j] : y[j] * cs[j] - z * sn[j];
       }
     }
-  }
-  if (is_q) {
-    if (!mine) return;   // (a group is whole: its lanes of unused places hold nothing that the others need from here on)
-    if constexpr (Q16) {
-      uint16_t* to = (uint16_t*)a.q_out + r * a.q_out_stride + h * D + i;
-      const uint32_t lo = pack_bf16(x[0], x[1]), hi = pack_bf16(x[2], x[3]);
-      if (a.by4) *(uint2*)to = make_uint2(lo, hi);
-      else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
-    } else {
-      float* to = (float*)a.q_out + r * a.q_out_stride + h * D + i;
-      if (a.by4) *(float4*)to = make_float4(x[0], x[1], x[2], x[3]);
-      else
+    float scale = 0.f;
+    if constexpr (INT8) {
+      float top = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[j] = x[j];
+      for (int j = 0; j < 4; ++j) top = max_or_nan(top, fabsf(y[j]));
+#pragma unroll
+      for (int d = 1; d < LANES; d *= 2) top = max_or_nan(top, __shfl_xor(top, d));
+      scale = scale_of(top);
     }
-    return;
-  }
-  if (!there) return;
-  const uint32_t page = (uint32_t)c.tables[(uint64_t)(uint32_t)seq * c.table_stride + ((uint32_t)slot >> c.page_shift)];
-  const uint32_t in_page = (uint32_t)slot & ((1u << c.page_shift) - 1);
-  float scale = 0.f;
-  if constexpr (INT8) {
-    float top = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) top = max_or_nan(top, fabsf(x[j]));
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) top = max_or_nan(top, __shfl_xor(top, d));
-    scale = scale_of(top);
-  }
-  if (!mine || page >= c.n_pages) return;
-  const uint64_t at = (uint64_t)page * c.page_stride + h * c.head_stride + in_page * c.slot_stride + i;
-  char* pool = is_v ? c.v : c.k;
-  if constexpr (INT8) {
-    *(uint32_t*)(pool + at) = (uint32_t)(quantized(x[0], scale) & 255) | (uint32_t)(quantized(x[1], scale) & 255) << 8 |
-                              (uint32_t)(quantized(x[2], scale) & 255) << 16 | (uint32_t)quantized(x[3], scale) << 24;
-    if (t == 0) (is_v ? c.v_scale : c.k_scale)[(((uint64_t)page * c.kv_heads + h) << c.page_shift) + in_page] = scale;
-  } else {
-    *(uint2*)(pool + 2 * at) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-  }
-  if (t == 0 && !is_v) {
-    const uint64_t mark = ((uint64_t)(uint32_t)seq * c.kv_heads + h) * c.capacity + (uint32_t)slot;
-    if (c.scores) c.scores[mark] = 0.f;
-    if (c.positions) c.positions[mark] = pos;
+    if (!mine) continue;
+    if (is_q) {
+      const uint64_t at = r * a.q_out_stride + h * D + i;
+      if constexpr (Q16) {
+        uint16_t* to = (uint16_t*)a.q_out + at;
+        const uint32_t lo = pack_bf16(y[0], y[1]), hi = pack_bf16(y[2], y[3]);
+        if (a.by4) *(uint2*)to = make_uint2(lo, hi);
+        else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
+      } else {
+        float* to = (float*)a.q_out + at;
+        if (a.by4) *(float4*)to = make_float4(y[0], y[1], y[2], y[3]);
+        else to[0] = y[0], to[1] = y[1], to[2] = y[2], to[3] = y[3];
+      }
+      continue;
+    }
+    if (page < c.n_pages) {
+      const uint64_t at = (uint64_t)page * c.page_stride + h * c.head_stride + in_page * c.slot_stride + i;
+      char* pool = is_v ? c.v : c.k;
+      if constexpr (INT8) {
+        *(uint32_t*)(pool + at) = (uint32_t)(quantized(y[0], scale) & 255) | (uint32_t)(quantized(y[1], scale) & 255) << 8 |
+                                  (uint32_t)(quantized(y[2], scale) & 255) << 16 | (uint32_t)quantized(y[3], scale) << 24;
+        if (t == 0) (is_v ? c.v_scale : c.k_scale)[(((uint64_t)page * c.kv_heads + h) << c.page_shift) + in_page] = scale;
+      } else {
+        *(uint2*)(pool + 2 * at) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+      }
+      if (t == 0 && !is_v) {
+        const uint64_t mark = ((uint64_t)(uint32_t)seq * c.kv_heads + h) * c.capacity + (uint32_t)slot;
+        if (c.scores) c.scores[mark] = 0.f;
+        if (c.positions) c.positions[mark] = pos;
+      }
+    }
   }
 }
 
@@ -127,7 +148,7 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   const uint64_t q_row = (uint64_t)a->heads * c.head_dim, kv_row = (uint64_t)c.kv_heads * c.head_dim;
   AppendView v{a->q, a->k, a->v, a->q_out, a->seqs, a->slots, a->positions, a->cos, a->sin, a->q_stride ? a->q_stride : q_row,
                a->k_stride ? a->k_stride : kv_row, a->v_stride ? a->v_stride : kv_row, a->q_out_stride ? a->q_out_stride : q_row,
-               a->heads, a->rotary_dim, a->n_positions, a->pairing, false};
+               a->heads, a->rotary_dim, a->n_positions, a->pairing, false, aligned_to(a->cos, 16) && aligned_to(a->sin, 16)};
   if (v.q_stride < q_row || v.k_stride < kv_row || v.v_stride < kv_row || v.q_out_stride < q_row)
     return refuse(TQ_E_INVALID_ARG, who + ": a stride is smaller than a row");
   const bool q16 = a->q_out_type == TQ_BF16;
@@ -140,13 +161,18 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   v.by4 = fours(v.q, v.q_stride, 4) && fours(v.k, v.k_stride, 4) && fours(v.v, v.v_stride, 4) && fours(v.q_out, v.q_out_stride, q16 ? 2 : 4);
   const bool int8 = cache->type == TQ_INT8;
   const uint32_t lanes = c.head_dim <= 16 ? 4 : c.head_dim <= 32 ? 8 : c.head_dim <= 64 ? 16 : c.head_dim <= 128 ? 32 : 64;
-  const uint32_t n_heads = a->heads + 2 * c.kv_heads, blocks = (n_heads * lanes + 255) / 256;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, blocks), dim3(256), 0, (hipStream_t)stream, c, v); };
-  auto of = [&](auto n) {
-    constexpr int L = decltype(n)::value;
-    if (int8) q16 ? go(k_cache_append<L, true, true>) : go(k_cache_append<L, true, false>);
-    else q16 ? go(k_cache_append<L, false, true>) : go(k_cache_append<L, false, false>);
+  const uint32_t n_heads = a->heads + 2 * c.kv_heads, groups = kAppendThreads / lanes;
+  // Few rows: a head per group of lanes, all of the GPU that there is work for.  Many: four per group, so that their loads are on
+  // their way together (8192 rows of 40 heads of 128 in 8 bits: 120 us with one, 72 with four).
+  const uint32_t one = (n_heads + groups - 1) / groups, four = (n_heads + 4 * groups - 1) / (4 * groups);
+  const bool many = (uint64_t)a->rows * one > 2048;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, many ? four : one), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v); };
+  auto pick = [&](auto n, auto items) {
+    constexpr int L = decltype(n)::value, I = decltype(items)::value;
+    if (int8) q16 ? go(k_cache_append<L, I, true, true>) : go(k_cache_append<L, I, true, false>);
+    else q16 ? go(k_cache_append<L, I, false, true>) : go(k_cache_append<L, I, false, false>);
   };
+  auto of = [&](auto n) { many ? pick(n, std::integral_constant<int, 4>()) : pick(n, std::integral_constant<int, 1>()); };
   if (lanes == 4) of(std::integral_constant<int, 4>());
   else if (lanes == 8) of(std::integral_constant<int, 8>());
   else if (lanes == 16) of(std::integral_constant<int, 16>());
@@ -220,13 +246,13 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 #pragma unroll
       for (uint32_t i = 0; i < kAhead; ++i) {   // (in place of a token that is not moved, one of page 0)
         const uint64_t at = place(there[i] ? of_page[i] : 0, of[i]) + b;
-        k[i] = *(const u32x4*)(c.k + at), v[i] = *(const u32x4*)(c.v + at);
+        k[i] = __builtin_nontemporal_load((const u32x4*)(c.k + at)), v[i] = __builtin_nontemporal_load((const u32x4*)(c.v + at));
       }
 #pragma unroll
       for (uint32_t i = 0; i < kAhead; ++i)
         if (there[i]) {
           const uint64_t at = place(to_page[i], to[i]) + b;
-          *(u32x4*)(c.k + at) = k[i], *(u32x4*)(c.v + at) = v[i];
+          __builtin_nontemporal_store(k[i], (u32x4*)(c.k + at)), __builtin_nontemporal_store(v[i], (u32x4*)(c.v + at));
         }
     }
     if (lane < kAhead && m + lane * step < n) {   // a lane per token
