@@ -441,7 +441,8 @@ int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *str
  *   out: device, bf16 [rows][heads * head_dim]: the x of the output projection.
  *   lengths: device, int32 [rows]; lengths beyond the capacity count as the capacity.  A row without tokens (length <= 0, a
  *   sequence that is not there, only pages that are not there) gives zeros.
- *   accumulate: 1 adds every token's weight, summed over the query heads of a key/value head, to cache->scores.
+ *   accumulate: 1 adds every token's weight, summed over the query heads of a key/value head, to cache->scores (capacity: at most
+ *   2^25 tokens).
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_workspace gives for the same arguments, zero before the first
  *   call with it; calls whose execution overlaps need one each.
  * Logits, softmax statistics and sums are fp32; sums are made in an order that only the arguments and lengths decide, so results repeat.

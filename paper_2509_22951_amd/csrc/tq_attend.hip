@@ -46,6 +46,7 @@ __device__ __forceinline__ uint32_t row_length(const CacheView& c, const AttendV
 }
 
 typedef __attribute__((address_space(4))) const int32_t constant_i32;
+typedef __attribute__((address_space(1))) const uint32_t global_cu32;
 
 template <int DIM, bool INT8>
 struct Tile {
@@ -91,9 +92,10 @@ __device__ __forceinline__ uint32_t prefix_sum(uint32_t v) {
 // of the line; more than kCluster parts are joined by clusters first.  Nobody waits for anybody.
 //
 // A wavefront asks for the next tile's keys as soon as the logits of this one are made, and for its values when they are multiplied
-// in, also where the next tile is another row's: a row's end is worked on while the next one's first tile is on its way.  The keys are
-// requested without a condition, so that a wait counts the loads behind those it is for (in place of a tile that is not there the
-// last one is requested again, and a page that is not there is read as page 0 and masked).
+// in, also where the next tile is another row's: a row's end is worked on while the next one's first tile is on its way.  All of
+// them are requested without a condition, keys ahead of values, and nothing else that is loaded is left unused: only then do the
+// compiler's waits count the loads behind those they are for.  (In place of a tile that is not there all lanes read one word of
+// the last one, and a page that is not there is read as page 0 and masked.)
 template <int DIM, bool INT8, bool TRACK>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, AttendView a) {
   using T = Tile<DIM, INT8>;
@@ -191,60 +193,54 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     return w;
   };
   T x;
-  auto fetch_keys = [&](const Blocks& w) {
+  auto fetch_keys = [&](const Blocks& w, uint32_t lanes) {   // lanes 0: all of them the same words
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const char* from = c.k + w.at[b];
 #pragma unroll
-      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + key_at[s]);
+      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + (key_at[s] & lanes));
       if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
     }
   };
-  auto fetch_values = [&](const Blocks& w) {
+  auto fetch_values = [&](const Blocks& w, uint32_t lanes) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + val_at);
+      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + (val_at & lanes));
       if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
     }
   };
-  // 8 values of a segment's q: lane threadIdx.x % 64 of contraction step threadIdx.x / 64
-  const uint32_t q_dim = INT8 ? 64 * (wave / 2) + 16 * g + 8 * (wave % 2) : 32 * wave + 8 * g;
-  float q8[8];
+  // 8 values of a segment's q: lane threadIdx.x % 64 of contraction step threadIdx.x / 64.  They are requested as the words they lie
+  // in, without a condition, so that nothing waits for them here (a lane without values reads the first ones).
+  const uint32_t q_dim = INT8 ? 64 * (wave / 2) + 16 * g + 8 * (wave % 2) : 32 * wave + 8 * g, q_size = a.q16 ? 2 : 4;
+  uint32_t q8[8];
   auto fetch_q = [&](const Segment& s) {
+    const uint64_t row = (uint64_t)a.q + q_size * (s.r * a.q_stride + s.first_head * D);
+    const uint32_t lane_at = head < s.n_heads && q_dim < D ? q_size * (head * D + q_dim) : 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q8[j] = 0.f;
-    if (head < s.n_heads && q_dim < D) {
-      const uint64_t at = s.r * a.q_stride + (s.first_head + head) * D + q_dim;
-      if (a.q16) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q8[j] = bf16_value(((const uint16_t*)a.q)[at + j]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q8[j] = ((const float*)a.q)[at + j];
-      }
-    }
+    for (uint32_t j = 0; j < 8; ++j) q8[j] = *(global_cu32*)(((row + q_size * j) & ~(uint64_t)3) + lane_at);   // (lane_at: a multiple of 16)
   };
-
   Segment s = next_segment();
   fetch_q(s);
   Blocks now = blocks_of(s, 0);
-  fetch_keys(now);
-  fetch_values(now);
+  __builtin_amdgcn_sched_barrier(0);   // keys ahead of values, here too: the waits in the loop go by the worst order there is
+  fetch_keys(now, ~0u);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_values(now, ~0u);
+  __builtin_amdgcn_sched_barrier(0);
   for (;;) {
     static_assert(T::kSteps <= kAttendWaves, "a wavefront per step of q");
-    if (wave < T::kSteps) {
-      bf16x8 q0, q1;
+    bf16x8 q0, q1;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = q8[j] * a.scale;
-        const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
-        q0[j] = part ? mid : hi;
-        q1[j] = part ? (__bf16)0.f : lo;
-      }
-      lds_q[wave][0][lane] = q0;
-      lds_q[wave][1][lane] = q1;
+    for (int j = 0; j < 8; ++j) {   // (by all wavefronts: a load that some of them never use would be waited for in the loop, and with it those behind it)
+      const uint32_t upper = ((uint32_t)(uint64_t)a.q + 2 * (uint32_t)(s.r * a.q_stride + j)) & 2;   // (of a bf16 value: the half of its word)
+      const float one = __uint_as_float((q8[j] << (a.q16 && !upper ? 16 : 0)) & (a.q16 ? 0xFFFF0000u : ~0u));
+      const float v = head < s.n_heads && q_dim < D ? one * a.scale : 0.f;
+      const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
+      q0[j] = part ? mid : hi;
+      q1[j] = part ? (__bf16)0.f : lo;
     }
+    if (wave < T::kSteps) lds_q[wave][0][lane] = q0, lds_q[wave][1][lane] = q1;
     __syncthreads();
 
     f32x4 o[T::kVals];
@@ -253,14 +249,16 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     float top = -INFINITY, total = 0.f;
     const bool more = pos < stop;
     Segment next_s = s;
+#pragma clang loop unroll(disable)   // (nor peeled: the copies between the two forms would wait for what is on its way)
     for (uint32_t round = 0;; ++round) {
       const bool last = round + 1 == s.rounds;
-      const uint32_t t = s.begin + round * kUnit + wave * kTile;
       if (last && more) {
         next_s = next_segment();
         fetch_q(next_s);
       }
-      const Blocks next = blocks_of(next_s, !last ? round + 1 : more ? 0 : round);
+      const uint32_t lanes = last && !more ? 0u : ~0u;
+      Blocks next = now;
+      if (lanes) next = blocks_of(next_s, last ? 0 : round + 1);
       asm volatile("" ::: "memory");   // q is read from LDS for every tile: registers are for what is on its way
       f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -281,18 +279,30 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         p[i] = ror8_sum(l[i / 4][i % 4]);
         if constexpr (INT8) p[i] *= (&x.ks[i / 4].x)[i % 4];
       }
-      fetch_keys(next);
+      __builtin_amdgcn_sched_barrier(0);
+      fetch_keys(next, lanes);
+      __builtin_amdgcn_sched_barrier(0);
+      // Tokens that take no part: their weight is 0, and the bits of their values are masked out, whatever lies there.  (The masks, and not the
+      // loaded words, are what the branch changes: a word that it changed would be waited for there.)
+      uint32_t value_bits[4] = {~0u, ~0u, ~0u, ~0u};   // of two neighbouring tokens
       if (now.limit[0] < 16 || now.limit[1] < 16) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (4 * g + i % 4 >= now.limit[i / 4]) p[i] = -INFINITY;
+        for (int i = 0; i < 8; i += 2) {
+          const uint32_t at = 4 * g + i % 4, limit = now.limit[i / 4];
+          if (at >= limit) p[i] = -INFINITY;
+          if (at + 1 >= limit) p[i + 1] = -INFINITY;
+          value_bits[i / 2] = at >= limit ? 0u : at + 1 >= limit ? 0xFFFFu : ~0u;
+        }
       }
       if constexpr (TRACK) {
-        if (part == 0 && head < s.n_heads) {
-          float* to = a.logits + ((uint64_t)s.r * a.heads + s.first_head + head) * c.capacity + t + 4 * g;
-          if (t < s.end) *(float4*)to = make_float4(p[0], p[1], p[2], p[3]);
-          if (t + 16 < s.end) *(float4*)(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
-        }
+        // Both halves of the columns hold the same logits: one stores the first block, the other the second.  Lanes without a head or
+        // a token store beyond the buffer's end, which drops it: no branch, so that the waits below still count.
+        const uint32_t t = s.begin + round * kUnit + wave * kTile;
+        const bool stores = head < s.n_heads && t + 16 * part < s.end;
+        float* to = a.logits + ((uint64_t)s.r * a.heads + s.first_head) * c.capacity + t;
+        const auto rows = __builtin_amdgcn_make_buffer_rsrc(to, 0, 0x7FFFFFFF, 0x00020000);
+        const u32x4 four = {__float_as_uint(part ? p[4] : p[0]), __float_as_uint(part ? p[5] : p[1]), __float_as_uint(part ? p[6] : p[2]), __float_as_uint(part ? p[7] : p[3])};
+        __builtin_amdgcn_raw_buffer_store_b128(four, rows, stores ? (int)(4 * (head * c.capacity + 16 * part + 4 * g)) : -16, 0, 0);
       }
       float m = top;
 #pragma unroll
@@ -305,21 +315,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       total *= shrink;
 #pragma unroll
       for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
-      if (now.limit[0] < 16 || now.limit[1] < 16) {   // whatever lies there is not used
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (4 * g + i % 4 >= now.limit[i / 4]) {
-            if constexpr (INT8) (&x.vs[i / 4].x)[i % 4] = 0.f;
-#pragma unroll
-            for (int w = 0; w < T::kValWords; ++w) x.v[i][w] = 0;
-          }
-      }
       bf16x8 pb;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float w = __builtin_amdgcn_exp2f(p[i] - base);
         total += w;
-        if constexpr (INT8) w *= (&x.vs[i / 4].x)[i % 4];
+        if constexpr (INT8) w = w > 0.f ? w * (&x.vs[i / 4].x)[i % 4] : 0.f;   // (a masked token's scale may be anything; a NaN weight is in the total)
         const __bf16 hi = (__bf16)w;
         pb[i] = part ? (__bf16)(w - (float)hi) : hi;
       }
@@ -330,18 +331,18 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         for (int i = 0; i < 4; ++i) {
           if constexpr (INT8) {
             const float lo = (float)(int8_t)(x.v[2 * i][b / 4] >> (8 * (b % 4))), hi = (float)(int8_t)(x.v[2 * i + 1][b / 4] >> (8 * (b % 4)));
-            vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+            vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u) & value_bits[i];
           } else {
-            vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u);
+            vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u) & value_bits[i];
           }
         }
         o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
       }
-      if (last && !more) break;
-      fetch_values(next);
+      __builtin_amdgcn_sched_barrier(0);
+      fetch_values(next, lanes);
+      __builtin_amdgcn_sched_barrier(0);
       now = next;
       if (last) break;
-      __builtin_amdgcn_s_barrier();   // (older wavefronts are served first: without it they end early and leave the others alone)
     }
 
     // join the wavefronts: lane (g, head) holds dims (4 g + j) * kVals + b of the head, halves of p beside each other
@@ -458,6 +459,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
               sum.z = sum.z * f + sums[i][1].x * e, sum.w = sum.w * f + sums[i][1].y * e;
             }
           }
+          __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): none of these loads is left for the loop to wait for
           if (d0 == 0) lds_max[of_group] = m, lds_total[of_group] = sum_p;
           *(float4*)&lds_sum[of_group * (DIM + 4) + d0] = sum;
         }
@@ -477,24 +479,30 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   }
 }
 
-// Adds the weights of all rows of a sequence to its slots' scores, rows and heads in order.
+// Adds the weights of all rows of a sequence to its slots' scores, rows and heads in order; four slots a thread.
 __global__ __launch_bounds__(256) void k_attend_scores(CacheView c, AttendView a) {
-  const uint32_t slot = blockIdx.x * 256 + threadIdx.x, kv = blockIdx.y, s = blockIdx.z;
-  if (slot >= c.capacity) return;
-  const uint64_t at = ((uint64_t)s * c.kv_heads + kv) * c.capacity + slot;
-  float sum = 0.f;
-  bool any = false;
+  const uint32_t slot = (blockIdx.x * 256 + threadIdx.x) * 4, kv = blockIdx.y, s = blockIdx.z;
+  if (slot >= c.capacity) return;   // (a multiple of 16)
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  int32_t longest = 0;
   const uint32_t r0 = a.seqs ? 0 : s, r1 = a.seqs ? a.rows : min(a.rows, s + 1);
   for (uint32_t r = r0; r < r1; ++r) {
     if (a.seqs && a.seqs[r] != (int32_t)s) continue;
-    if ((int64_t)slot >= (int64_t)a.lengths[r]) continue;
-    any = true;
+    const int32_t length = a.lengths[r];
+    if ((int64_t)slot >= (int64_t)length) continue;
+    longest = max(longest, length);
     for (uint32_t h = kv * a.group; h < (kv + 1) * a.group; ++h) {
       const float2 st = a.stats[(uint64_t)r * a.heads + h];
-      sum += __builtin_amdgcn_exp2f(a.logits[((uint64_t)r * a.heads + h) * c.capacity + slot] - st.x) * st.y;
+      const float4 l = *(const float4*)(a.logits + ((uint64_t)r * a.heads + h) * c.capacity + slot);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if ((int64_t)slot + j < (int64_t)length) sum[j] += __builtin_amdgcn_exp2f((&l.x)[j] - st.x) * st.y;
     }
   }
-  if (any) c.scores[at] += sum;
+  float* to = c.scores + ((uint64_t)s * c.kv_heads + kv) * c.capacity + slot;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if ((int64_t)slot + j < (int64_t)longest) to[j] += sum[j];
 }
 
 struct Layout {
@@ -510,6 +518,7 @@ int check_attend(const std::string& who, const tq_cache* cache, const tq_attend_
   if (a->rows > 65535) return refuse(TQ_E_UNSUPPORTED, who + ": more than 65535 rows");
   if (!a->seqs && a->rows > c->n_seqs) return refuse(TQ_E_INVALID_ARG, who + ": more rows than sequences, and no seqs");
   if (a->accumulate > 1) return refuse(TQ_E_INVALID_ARG, who + ": accumulate is 0 or 1");
+  if (a->accumulate && c->capacity > (1u << 25)) return refuse(TQ_E_UNSUPPORTED, who + ": accumulate needs a capacity of at most 2^25 tokens");
   if (a->accumulate && !c->scores) return refuse(TQ_E_INVALID_ARG, who + ": the cache has no scores to add to");
   if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return refuse(TQ_E_INVALID_ARG, who + ": scale must be positive");
   const uint32_t group = a->heads / c->kv_heads;
@@ -561,7 +570,7 @@ int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
   if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, s);
   else if (c.head_dim <= 128) launch_attend<128>(c, v, l.groups, int8, a->accumulate, s);
   else launch_attend<256>(c, v, l.groups, int8, a->accumulate, s);
-  if (a->accumulate) hipLaunchKernelGGL(k_attend_scores, dim3((c.capacity + 255) / 256, c.kv_heads, c.n_seqs), dim3(256), 0, s, c, v);
+  if (a->accumulate) hipLaunchKernelGGL(k_attend_scores, dim3((c.capacity + 1023) / 1024, c.kv_heads, c.n_seqs), dim3(256), 0, s, c, v);
   return launched("tq_attend");
 }
 

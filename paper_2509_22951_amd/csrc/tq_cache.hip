@@ -195,7 +195,7 @@ struct EvictView {
 };
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kMoveThreads = 256, kCopies = 16;
-constexpr uint32_t kMovesInSelect = 512;
+constexpr uint32_t kMovesInSelect = 512;   // tokens of a list
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -220,11 +220,11 @@ __device__ __forceinline__ uint32_t wave_prefix_sum(uint32_t v) {   // inclusive
 // Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., kAhead of them
 // together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.
 template <bool INT8>
-__device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, uint32_t n, uint32_t first, uint32_t step) {
+__device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, const uint32_t* slots_to, const uint32_t* slots_from, uint32_t n,
+                                            uint32_t first, uint32_t step) {
   constexpr uint32_t kAhead = 4;
   const uint32_t list = s * c.kv_heads + h, lane = threadIdx.x % 16, bytes = c.head_dim * (INT8 ? 1 : 2), mask = (1u << c.page_shift) - 1;
   const uint64_t row = (uint64_t)list * c.capacity, size = INT8 ? 1 : 2;
-  const uint32_t *slots_to = e.to + (uint64_t)list * e.keep, *slots_from = e.from + (uint64_t)list * e.keep;
   const int32_t* table = c.tables + (uint64_t)s * c.table_stride;
   for (uint32_t m = first; m < n; m += kAhead * step) {
     uint32_t to[kAhead], of[kAhead], to_page[kAhead], of_page[kAhead];
@@ -382,7 +382,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
     return (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   };
   uint32_t equal = 0, freed = 0, taken = 0;   // numbered so far
-  uint32_t *to = e.to + (uint64_t)list * e.keep, *from = e.from + (uint64_t)list * e.keep;
+  __shared__ uint32_t few[2][MOVES ? kMovesInSelect : 1];   // the list, where it is used here
+  uint32_t *to = MOVES ? few[0] : e.to + (uint64_t)list * e.keep, *from = MOVES ? few[1] : e.from + (uint64_t)list * e.keep;
   if (threadIdx.x < 64) totals[0][threadIdx.x] = totals[1][threadIdx.x] = 0;   // (more than there are of them with one stride)
   __syncthreads();
   for (uint32_t round = 0; round < rounds; ++round) {
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
     }
     __syncthreads();
   }
-  if constexpr (MOVES) move_tokens<INT8>(c, e, s, h, freed, threadIdx.x / 16, kSelectThreads / 16);   // (the list is this workgroup's: the barrier suffices)
+  if constexpr (MOVES) move_tokens<INT8>(c, e, s, h, few[0], few[1], freed, threadIdx.x / 16, kSelectThreads / 16);
   else if (threadIdx.x == 0) e.counts[list] = freed;
 }
 
@@ -450,7 +451,8 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(CacheView c, EvictV
     const int32_t length = e.lengths[s];
     e.lengths_out[s] = min(length, (int32_t)min(e.keep, 0x7FFFFFFFu));
   }
-  move_tokens<INT8>(c, e, s, h, e.counts[s * c.kv_heads + h], (blockIdx.x * kMoveThreads + threadIdx.x) / 16, gridDim.x * (kMoveThreads / 16));
+  const uint32_t list = s * c.kv_heads + h;
+  move_tokens<INT8>(c, e, s, h, e.to + (uint64_t)list * e.keep, e.from + (uint64_t)list * e.keep, e.counts[list], (blockIdx.x * kMoveThreads + threadIdx.x) / 16, gridDim.x * (kMoveThreads / 16));
 }
 
 uint64_t evict_counts_bytes(const CacheView& c) { return ((uint64_t)c.n_seqs * c.kv_heads * 4 + 255) / 256 * 256; }
