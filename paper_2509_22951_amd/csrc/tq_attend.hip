@@ -122,10 +122,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   all *= a.chunks;
   const uint32_t share = max(kMinShare, (all + gridDim.x - 1) / gridDim.x);
   uint32_t pos = blockIdx.x * share;
-  const uint32_t stop = min(pos + share, all);
+  uint32_t stop = min(pos + share, all);
   if (pos >= stop) return;
   uint32_t r = 0, row_first = 0;
-  for (;;) {   // (all > pos: the row is found)
+  while (r < a.rows) {   // (all > pos: the row is found)
     const uint64_t beyond = __ballot(row_first + upto * a.chunks > pos);
     if (beyond) {
       const uint32_t at = (uint32_t)__builtin_ctzll(beyond);
@@ -137,6 +137,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     r += 64;
     upto = look_at(r);
   }
+  if (r >= a.rows) return;   // (lengths that change under the call)
 
   // a lane's places in a block of 16 tokens: dims that a head does not have are read as its first ones, against zeros of q, and dropped
   constexpr uint32_t kSize = INT8 ? 1 : 2;
@@ -170,7 +171,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     pos += unit_end - unit;
     if (pos == row_first + s.units * a.chunks) {
       row_first = pos;
-      if ((++r & 63) == 0 && pos < stop) look_at(r);
+      if (++r >= a.rows) stop = pos;
+      else if ((r & 63) == 0 && pos < stop) look_at(r);
     }
     return s;
   };
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       }
     __syncthreads();
     // the workgroups among which this (row, chunk) is cut
-    const uint32_t n_heads = s.n_heads, group0 = s.pair_first / share, parts = (s.pair_first + s.units - 1) / share - group0 + 1;
+    const uint32_t n_heads = s.n_heads, group0 = s.pair_first / share, parts = min((s.pair_first + s.units - 1) / share, gridDim.x - 1) - group0 + 1;
     const uint64_t slot_floats = kHeads * (D + 2);
     auto slot_of = [&](uint32_t group) { return a.partials + (2 * (uint64_t)group + (group * share >= s.pair_first ? 0 : 1)) * slot_floats; };
     // a group of DIM / 4 lanes per head, four dims a lane

@@ -51,6 +51,7 @@ inline int view_cache(const std::string& who, const tq_cache* c, CacheView* view
   if ((slot * size) % 16 || (head * size) % 16 || (page * size) % 16 || !aligned_to(c->k, 16) || !aligned_to(c->v, 16) ||
       !aligned_to(c->k_scale, 16) || !aligned_to(c->v_scale, 16))
     return refuse(TQ_E_INVALID_ARG, who + ": k, v, their scales and strides must be multiples of 16 bytes");
+  if (slot * size > (1u << 26)) return refuse(TQ_E_UNSUPPORTED, who + ": slot_stride is more than 2^26 bytes");   // (16 slots are within 32 bits)
   if (!aligned_to(c->tables, 4) || !aligned_to(c->scores, 4) || !aligned_to(c->positions, 4))
     return refuse(TQ_E_INVALID_ARG, who + ": tables, scores and positions must be 4-byte aligned");
   const uint64_t table = c->table_stride ? c->table_stride : c->seq_pages;
@@ -70,11 +71,19 @@ inline int launched(const char* who) {
 // Runs the body of an entry point; no C++ exception leaves the library.
 template <typename F>
 int contained(const char* who, F&& body) {
+  auto say = [&](const char* what) {
+    try {
+      set_error(std::string(who) + what);
+    } catch (...) {   // (no memory for the message either)
+    }
+  };
   try {
     return body();
   } catch (const std::bad_alloc&) {
+    say(": out of host memory");
     return TQ_E_OOM;
   } catch (...) {
+    say(": unexpected internal error");
     return TQ_E_HIP;
   }
 }

@@ -224,3 +224,31 @@ def test_a_pool_beyond_32_bits_of_offset():
     p.tables -= base
     p.n_pages -= base
     close(out, attend_reference(p, q, lengths)[0], p)
+
+
+def test_many_rows_and_another_stream():
+    """More rows than a wavefront has lanes, some without tokens, on a stream of their own."""
+    p = Paged(150, 3, kv_heads=2, dim=32)
+    q = queries(150, 2, 32)
+    lengths = ints([(7 * r) % 49 if r % 5 else 0 for r in range(150)])
+    want = attend_reference(p, q, lengths)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = run(p, q, lengths)
+    close(out, want, p)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,rows", [(8, 1, 256, 1), (5, 1, 128, 2), (2, 1, 64, 1), (16, 1, 64, 3)])
+def test_rows_that_many_workgroups_share(heads, kv_heads, dim, rows):
+    """Up to 160 parts of one row: joined by clusters first; rows that begin and end inside a cluster."""
+    p = Paged(rows, 2600, kv_heads=kv_heads, dim=dim)
+    q = queries(rows, heads, dim)
+    for n in ([41600, 9000, 41500], [4096, 41600, 300], [20000, 0, 30001]):
+        lengths = ints(n[:rows])
+        call, out = attend_call(p.describe(), p, q, lengths)
+        want = attend_reference(p, q, lengths)[0]
+        for _ in range(2):
+            call.launch(stream())
+            torch.cuda.synchronize()
+            close(out, want, p)

@@ -166,6 +166,37 @@ def test_rows_that_are_not_finite_read_back_as_nan_in_8_bits():
     assert torch.isfinite(got[page[0], 0, 1]).all()
 
 
+def far_pool(p):
+    """The same cache at the end of a pool of more than 2^31 values -> (the cache with that pool, what takes it back)."""
+    base = 2 ** 31 // (p.kv_heads * p.page * p.dim) + 3
+    for name in ("k", "v"):
+        small = getattr(p, name)
+        pool = torch.empty((base + p.n_pages, *small.shape[1:]), dtype=small.dtype, device="cuda")
+        pool[base:] = small
+        setattr(p, name, pool)
+    p.tables += base
+    p.n_pages += base
+
+    def back():
+        p.n_pages -= base
+        p.tables -= base
+        for name in ("k", "v"):
+            setattr(p, name, getattr(p, name)[base:].clone())
+
+    return back
+
+
+def test_append_beyond_32_bits_of_offset():
+    p = Paged(2, 3, kv_heads=2, dim=64)
+    q, k, v = new_tokens(2, 4, 2, 64)
+    cos, sin = angles(50, 64)
+    slots, before = ints([17, 40]), snapshot(p)
+    back = far_pool(p)
+    got = append(p, q, k, v, None, slots, None, cos, sin, 64)
+    back()
+    check_append(p, before, got, q, k, v, None, slots, None, cos, sin, 64)
+
+
 # ---- eviction ----
 
 def evict(p, lengths, keep, since=None, in_place=True):
@@ -259,6 +290,16 @@ def test_evict_without_positions_and_with_pages_that_are_not_there():
     p.positions = None
     p.tables[0, 2], p.tables[1, 8] = -1, p.n_pages
     check_evict(p, ints([160, 160]), 70)
+
+
+def test_evict_beyond_32_bits_of_offset():
+    p, same = (Paged(2, 5, kv_heads=2, dim=32, marks=True, seed=9) for _ in range(2))
+    check_evict(same, ints([80, 77]), 50)
+    back = far_pool(p)
+    evict(p, ints([80, 77]), 50)
+    back()
+    for name in ("k", "v", "scores", "positions"):
+        assert torch.equal(getattr(p, name), getattr(same, name)), name
 
 
 def test_evict_more_than_there_is_changes_nothing():

@@ -35,7 +35,7 @@ def test_norm_refuses(code, change):
     (UNSUPPORTED, dict(page_size=48)), (UNSUPPORTED, dict(page_size=2048)), (UNSUPPORTED, dict(head_dim=72)), (UNSUPPORTED, dict(head_dim=272)),
     (UNSUPPORTED, dict(head_dim=0)), (INVALID, dict(n_pages=0)), (INVALID, dict(n_seqs=0)), (INVALID, dict(seq_pages=0)), (INVALID, dict(kv_heads=0)),
     (UNSUPPORTED, dict(seq_pages=1 << 27)), (INVALID, dict(k=A + 8)), (INVALID, dict(page_stride=4096)), (INVALID, dict(page_stride=4096, head_stride=64, slot_stride=4)),
-    (INVALID, dict(table_stride=1)), (INVALID, dict(scores=A + 1)),
+    (UNSUPPORTED, dict(page_stride=1 << 30, head_stride=64, slot_stride=1 << 26)), (INVALID, dict(table_stride=1)), (INVALID, dict(scores=A + 1)),
 ])
 def test_every_call_refuses_a_cache_that_is_not_one(code, change):
     cache = tq.Cache(**{**CACHE, "scores": A, **change})
