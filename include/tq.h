@@ -365,7 +365,7 @@ int tq_listing_destroy(tq_listing h);
  *   delta: device, fp32 [rows][cols], a product's y, or NULL (nothing is added).
  *   weight: device, [cols], TQ_FP32 or TQ_BF16 (weight_type).
  *   out: device, [rows][cols], TQ_BF16 or TQ_INT8 (out_type); out_scale: device, fp32 [rows], with TQ_INT8.
- * Pointers are aligned to their type; rows whose address and stride are a multiple of 4 values are read faster.  Apart from
+ * Pointers are aligned to their type.  Apart from
  * residual_out == residual (with equal strides) the buffers do not overlap.  rows may be 0 (nothing is done), cols is 1..2^20.
  */
 typedef struct tq_norm_args {

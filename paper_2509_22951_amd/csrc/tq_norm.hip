@@ -18,32 +18,51 @@ struct NormView {
   float eps;
 };
 
-// VEC values at element i (a multiple of VEC) of a row of fp32 or bf16.
-template <int VEC, bool BF16>
-__device__ __forceinline__ void load_values(const void* row, uint32_t i, float (&v)[VEC]) {
-  if constexpr (VEC == 4 && BF16) {
-    const uint2 d = *(const uint2*)((const uint16_t*)row + i);
-    v[0] = bf16_value(d.x), v[1] = __uint_as_float(d.x & 0xFFFF0000u), v[2] = bf16_value(d.y), v[3] = __uint_as_float(d.y & 0xFFFF0000u);
-  } else if constexpr (VEC == 4) {
-    const float4 d = *(const float4*)((const float*)row + i);
-    v[0] = d.x, v[1] = d.y, v[2] = d.z, v[3] = d.w;
-  } else if constexpr (BF16) {
-    v[0] = bf16_value(((const uint16_t*)row)[i]);
+// Four values at a time, at any address that their type allows: the memory unit takes 16 bytes from a 4-byte boundary as it
+// does from a 16-byte one.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
+// Values i..i+3 of a row of n, fp32 or bf16; those beyond it are zero.  WHOLE: n is a multiple of 4.
+template <bool WHOLE, bool BF16>
+__device__ __forceinline__ void load_values(const void* row, uint32_t i, uint32_t n, float (&v)[4]) {
+  if (WHOLE || i + 4 <= n) {
+    if constexpr (BF16) {
+      const u16x4_any d = *(const u16x4_any*)((const uint16_t*)row + i);
+      v[0] = bf16_value(d.x), v[1] = bf16_value(d.y), v[2] = bf16_value(d.z), v[3] = bf16_value(d.w);
+    } else {
+      const f32x4_any d = *(const f32x4_any*)((const float*)row + i);
+      v[0] = d.x, v[1] = d.y, v[2] = d.z, v[3] = d.w;
+    }
   } else {
-    v[0] = ((const float*)row)[i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = i + k >= n ? 0.f : BF16 ? bf16_value(((const uint16_t*)row)[i + k]) : ((const float*)row)[i + k];
   }
 }
 
-template <int VEC, bool BF16>
-__device__ __forceinline__ void store_values(void* row, uint32_t i, const float (&v)[VEC]) {
-  if constexpr (VEC == 4 && BF16)
-    *(uint2*)((uint16_t*)row + i) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-  else if constexpr (VEC == 4)
-    *(float4*)((float*)row + i) = make_float4(v[0], v[1], v[2], v[3]);
-  else if constexpr (BF16)
-    ((uint16_t*)row)[i] = (uint16_t)pack_bf16(v[0], 0.f);
-  else
-    ((float*)row)[i] = v[0];
+template <bool WHOLE, bool BF16>
+__device__ __forceinline__ void store_values(void* row, uint32_t i, uint32_t n, const float (&v)[4]) {
+  if constexpr (BF16) {
+    uint16_t* to = (uint16_t*)row + i;
+    const uint32_t lo = pack_bf16(v[0], v[1]), hi = pack_bf16(v[2], v[3]);
+    if (WHOLE || i + 4 <= n) {
+      *(u16x4_any*)to = __builtin_bit_cast(u16x4_any, make_uint2(lo, hi));
+    } else {
+      if (i < n) to[0] = (uint16_t)lo;
+      if (i + 1 < n) to[1] = (uint16_t)(lo >> 16);
+      if (i + 2 < n) to[2] = (uint16_t)hi;
+    }
+  } else {
+    float* to = (float*)row + i;
+    if (WHOLE || i + 4 <= n) {
+      *(f32x4_any*)to = f32x4_any{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (i + k < n) to[k] = v[k];
+    }
+  }
 }
 
 // One value of every wavefront -> the combined one in all threads.  slots: one per wavefront, unused since the last barrier.
@@ -62,67 +81,67 @@ __device__ __forceinline__ float wave_max_or_nan(float v) {
   return v;
 }
 
-// CHUNKS pieces of VEC values per thread (0: any number, read again for the output).
-template <int VEC, int CHUNKS, bool RES16, bool W16, bool OUT8>
+// CHUNKS pieces of four values per thread (0: any number, read again for the output).
+template <int CHUNKS, bool WHOLE, bool RES16, bool W16, bool OUT8>
 __global__ __launch_bounds__(1024) void k_add_rms_norm(NormView a) {
   __shared__ float sums[16], tops[16];
   const uint64_t r = blockIdx.x;
   const char* res = (const char*)a.residual + r * a.residual_stride * (RES16 ? 2 : 4);
   const float* delta = a.delta ? a.delta + r * a.delta_stride : nullptr;
   char* res_out = a.residual_out ? (char*)a.residual_out + r * a.residual_out_stride * (RES16 ? 2 : 4) : nullptr;
-  const uint32_t step = blockDim.x * VEC;
+  const uint32_t step = blockDim.x * 4;
   constexpr int KEEP = CHUNKS ? CHUNKS : 1;
-  float h[KEEP][VEC];
-  auto sum_of = [&](uint32_t i, float (&x)[VEC]) {
-    load_values<VEC, RES16>(res, i, x);
+  float h[KEEP][4];
+  auto sum_of = [&](uint32_t i, float (&x)[4]) {
+    load_values<WHOLE, RES16>(res, i, a.cols, x);
     if (delta) {
-      float d[VEC];
-      load_values<VEC, false>(delta, i, d);
+      float d[4];
+      load_values<WHOLE, false>(delta, i, a.cols, d);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) x[k] += d[k];
+      for (int k = 0; k < 4; ++k) x[k] += d[k];
     }
   };
   const float share = 1.f / (float)a.cols;   // of a value in the mean, taken before it is squared: a sum of squares overflows sooner
   float square = 0.f;
-  auto take = [&](uint32_t i, float (&x)[VEC]) {
+  auto take = [&](uint32_t i, float (&x)[4]) {
     sum_of(i, x);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) square = fmaf(x[k] * share, x[k], square);
-    if (CHUNKS && res_out) store_values<VEC, RES16>(res_out, i, x);
+    for (int k = 0; k < 4; ++k) square = fmaf(x[k] * share, x[k], square);
+    if (CHUNKS && res_out) store_values<WHOLE, RES16>(res_out, i, a.cols, x);
   };
   if constexpr (CHUNKS) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      const uint32_t i = threadIdx.x * VEC + c * step;
+      const uint32_t i = threadIdx.x * 4 + c * step;
       if (i < a.cols) take(i, h[c]);
     }
   } else {
-    for (uint32_t i = threadIdx.x * VEC; i < a.cols; i += step) take(i, h[0]);
+    for (uint32_t i = threadIdx.x * 4; i < a.cols; i += step) take(i, h[0]);
   }
   square = over_waves(group_sum<64>(square), sums, [](float x, float y) { return x + y; });
   const float inv = 1.f / sqrtf(square + a.eps);
-  auto normed = [&](uint32_t i, float (&x)[VEC]) {
-    float w[VEC];
-    load_values<VEC, W16>(a.weight, i, w);
+  auto normed = [&](uint32_t i, float (&x)[4]) {
+    float w[4];
+    load_values<WHOLE, W16>(a.weight, i, a.cols, w);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] = x[k] * inv * w[k];
+    for (int k = 0; k < 4; ++k) x[k] = x[k] * inv * w[k];
   };
   float scale = 0.f;
   if constexpr (OUT8) {
     float top = 0.f;
-    auto see = [&](uint32_t i, float (&x)[VEC]) {
+    auto see = [&](uint32_t i, float (&x)[4]) {
       normed(i, x);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) top = max_or_nan(top, fabsf(x[k]));
+      for (int k = 0; k < 4; ++k) top = max_or_nan(top, fabsf(x[k]));
     };
     if constexpr (CHUNKS) {
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
-        const uint32_t i = threadIdx.x * VEC + c * step;
+        const uint32_t i = threadIdx.x * 4 + c * step;
         if (i < a.cols) see(i, h[c]);
       }
     } else {
-      for (uint32_t i = threadIdx.x * VEC; i < a.cols; i += step) {
+      for (uint32_t i = threadIdx.x * 4; i < a.cols; i += step) {
         sum_of(i, h[0]);
         see(i, h[0]);
       }
@@ -131,46 +150,50 @@ __global__ __launch_bounds__(1024) void k_add_rms_norm(NormView a) {
     scale = scale_of(top);
     if (threadIdx.x == 0) a.out_scale[r] = scale;
   }
-  auto put = [&](uint32_t i, float (&x)[VEC]) {
+  auto put = [&](uint32_t i, float (&x)[4]) {
     if constexpr (OUT8) {
       int8_t* out = (int8_t*)a.out + r * a.out_stride + i;
-      if constexpr (VEC == 4)
-        *(uint32_t*)out = (uint32_t)(quantized(x[0], scale) & 255) | (uint32_t)(quantized(x[1], scale) & 255) << 8 |
-                          (uint32_t)(quantized(x[2], scale) & 255) << 16 | (uint32_t)quantized(x[3], scale) << 24;
-      else
-        *out = (int8_t)quantized(x[0], scale);
+      const uint32_t bytes = (uint32_t)(quantized(x[0], scale) & 255) | (uint32_t)(quantized(x[1], scale) & 255) << 8 |
+                             (uint32_t)(quantized(x[2], scale) & 255) << 16 | (uint32_t)quantized(x[3], scale) << 24;
+      if (WHOLE || i + 4 <= a.cols) {
+        *(u32_any*)out = bytes;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          if (i + k < a.cols) out[k] = (int8_t)(bytes >> (8 * k));
+      }
     } else {
-      store_values<VEC, true>((uint16_t*)a.out + r * a.out_stride, i, x);
+      store_values<WHOLE, true>((uint16_t*)a.out + r * a.out_stride, i, a.cols, x);
     }
   };
   if constexpr (CHUNKS) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      const uint32_t i = threadIdx.x * VEC + c * step;
+      const uint32_t i = threadIdx.x * 4 + c * step;
       if (i < a.cols) {
         if constexpr (!OUT8) normed(i, h[c]);
         put(i, h[c]);
       }
     }
   } else {
-    for (uint32_t i = threadIdx.x * VEC; i < a.cols; i += step) {   // (residual_out may be residual: it is written after its last use)
+    for (uint32_t i = threadIdx.x * 4; i < a.cols; i += step) {   // (residual_out may be residual: it is written after its last use)
       sum_of(i, h[0]);
-      if (res_out) store_values<VEC, RES16>(res_out, i, h[0]);
+      if (res_out) store_values<WHOLE, RES16>(res_out, i, a.cols, h[0]);
       normed(i, h[0]);
       put(i, h[0]);
     }
   }
 }
 
-template <int VEC, int CHUNKS>
+template <int CHUNKS, bool WHOLE>
 void launch_norm(const NormView& v, uint32_t threads, bool res16, bool w16, bool out8, hipStream_t stream) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(v.rows), dim3(threads), 0, stream, v); };
   if (res16) {
-    if (w16) out8 ? go(k_add_rms_norm<VEC, CHUNKS, true, true, true>) : go(k_add_rms_norm<VEC, CHUNKS, true, true, false>);
-    else out8 ? go(k_add_rms_norm<VEC, CHUNKS, true, false, true>) : go(k_add_rms_norm<VEC, CHUNKS, true, false, false>);
+    if (w16) out8 ? go(k_add_rms_norm<CHUNKS, WHOLE, true, true, true>) : go(k_add_rms_norm<CHUNKS, WHOLE, true, true, false>);
+    else out8 ? go(k_add_rms_norm<CHUNKS, WHOLE, true, false, true>) : go(k_add_rms_norm<CHUNKS, WHOLE, true, false, false>);
   } else {
-    if (w16) out8 ? go(k_add_rms_norm<VEC, CHUNKS, false, true, true>) : go(k_add_rms_norm<VEC, CHUNKS, false, true, false>);
-    else out8 ? go(k_add_rms_norm<VEC, CHUNKS, false, false, true>) : go(k_add_rms_norm<VEC, CHUNKS, false, false, false>);
+    if (w16) out8 ? go(k_add_rms_norm<CHUNKS, WHOLE, false, true, true>) : go(k_add_rms_norm<CHUNKS, WHOLE, false, true, false>);
+    else out8 ? go(k_add_rms_norm<CHUNKS, WHOLE, false, false, true>) : go(k_add_rms_norm<CHUNKS, WHOLE, false, false, false>);
   }
 }
 
@@ -196,24 +219,19 @@ int add_rms_norm(const tq_norm_args* a, void* stream) {
   if (!aligned_to(a->residual, res_size) || !aligned_to(a->residual_out, res_size) || !aligned_to(a->delta, 4) ||
       !aligned_to(a->weight, w16 ? 2 : 4) || !aligned_to(a->out, out_size) || !aligned_to(a->out_scale, 4))
     return refuse(TQ_E_INVALID_ARG, who + ": a pointer is not aligned to its type");
-  auto fours = [](const void* p, uint64_t stride, size_t size) { return stride % 4 == 0 && aligned_to(p, 4 * size); };
-  const bool by4 = a->cols % 4 == 0 && fours(a->residual, v.residual_stride, res_size) && fours(a->delta, v.delta_stride, 4) &&
-                   fours(a->residual_out, v.residual_out_stride, res_size) && fours(a->out, v.out_stride, out_size) && aligned_to(a->weight, w16 ? 8 : 16);
-  const uint32_t pieces = a->cols / (by4 ? 4 : 1);
-  const uint32_t chunks = pieces > 4096 ? 0 : pieces > 2048 ? 4 : pieces > 1024 ? 2 : 1;
-  const uint32_t threads = chunks ? ((pieces + chunks - 1) / chunks + 63) / 64 * 64 : 1024;
+  const uint32_t pieces = (a->cols + 3) / 4;
+  const uint32_t chunks = pieces > 8192 ? 0 : pieces > 4096 ? 8 : pieces > 2048 ? 4 : pieces > 1024 ? 2 : 1;
+  const uint32_t threads = chunks && chunks < 8 ? ((pieces + chunks - 1) / chunks + 63) / 64 * 64 : 1024;
   hipStream_t s = (hipStream_t)stream;
-  if (by4) {
-    if (chunks == 1) launch_norm<4, 1>(v, threads, res16, w16, out8, s);
-    else if (chunks == 2) launch_norm<4, 2>(v, threads, res16, w16, out8, s);
-    else if (chunks == 4) launch_norm<4, 4>(v, threads, res16, w16, out8, s);
-    else launch_norm<4, 0>(v, threads, res16, w16, out8, s);
-  } else {
-    if (chunks == 1) launch_norm<1, 1>(v, threads, res16, w16, out8, s);
-    else if (chunks == 2) launch_norm<1, 2>(v, threads, res16, w16, out8, s);
-    else if (chunks == 4) launch_norm<1, 4>(v, threads, res16, w16, out8, s);
-    else launch_norm<1, 0>(v, threads, res16, w16, out8, s);
-  }
+  auto go = [&](auto whole) {
+    constexpr bool W = decltype(whole)::value;
+    if (chunks == 1) launch_norm<1, W>(v, threads, res16, w16, out8, s);
+    else if (chunks == 2) launch_norm<2, W>(v, threads, res16, w16, out8, s);
+    else if (chunks == 4) launch_norm<4, W>(v, threads, res16, w16, out8, s);
+    else if (chunks == 8) launch_norm<8, W>(v, threads, res16, w16, out8, s);
+    else launch_norm<0, W>(v, threads, res16, w16, out8, s);
+  };
+  a->cols % 4 ? go(std::false_type()) : go(std::true_type());
   return launched("tq_add_rms_norm");
 }
 
