@@ -485,6 +485,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
 __global__ __launch_bounds__(256) void k_attend_scores(CacheView c, AttendView a) {
   const uint32_t slot = (blockIdx.x * 256 + threadIdx.x) * 4, kv = blockIdx.y, s = blockIdx.z;
   if (slot >= c.capacity) return;   // (a multiple of 16)
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+  float* to = c.scores + ((uint64_t)s * c.kv_heads + kv) * c.capacity + slot;
+  const f32x4_any were = *(const f32x4_any*)to;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   int32_t longest = 0;
   const uint32_t r0 = a.seqs ? 0 : s, r1 = a.seqs ? a.rows : min(a.rows, s + 1);
@@ -493,6 +496,7 @@ __global__ __launch_bounds__(256) void k_attend_scores(CacheView c, AttendView a
     const int32_t length = a.lengths[r];
     if ((int64_t)slot >= (int64_t)length) continue;
     longest = max(longest, length);
+#pragma unroll 4
     for (uint32_t h = kv * a.group; h < (kv + 1) * a.group; ++h) {
       const float2 st = a.stats[(uint64_t)r * a.heads + h];
       const float4 l = *(const float4*)(a.logits + ((uint64_t)r * a.heads + h) * c.capacity + slot);
@@ -501,10 +505,13 @@ __global__ __launch_bounds__(256) void k_attend_scores(CacheView c, AttendView a
         if ((int64_t)slot + j < (int64_t)length) sum[j] += __builtin_amdgcn_exp2f((&l.x)[j] - st.x) * st.y;
     }
   }
-  float* to = c.scores + ((uint64_t)s * c.kv_heads + kv) * c.capacity + slot;
+  if ((int64_t)slot + 4 <= (int64_t)longest) {
+    *(f32x4_any*)to = were + f32x4_any{sum[0], sum[1], sum[2], sum[3]};
+  } else {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if ((int64_t)slot + j < (int64_t)longest) to[j] += sum[j];
+    for (int j = 0; j < 3; ++j)
+      if ((int64_t)slot + j < (int64_t)longest) to[j] = were[j] + sum[j];
+  }
 }
 
 struct Layout {
