@@ -194,7 +194,7 @@ struct EvictView {
   bool by4;           // scores and positions start on 16 bytes, in and out
 };
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kMoveThreads = 256, kCopies = 16;
+constexpr int kMoveThreads = 256;
 constexpr uint32_t kMovesInSelect = 512;   // tokens of a list
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -277,11 +277,12 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 // A workgroup per list; a thread has 4 neighbouring slots of every kStride, and the ranks of STRIDES of them in registers.  Where
 // that is not the whole list the ranks are made again from the scores, which the L2 holds by then, for every 8 bits.  Scores share
 // few exponents, so that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there
-// are kCopies of it.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
-template <int STRIDES, bool INT8, bool MOVES>
-__global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, EvictView e) {
+// are several copies of it.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
+template <int THREADS, int STRIDES, bool INT8, bool MOVES>
+__global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView e) {
+  constexpr int kWaves = THREADS / 64, kCopies = THREADS / 64;
   __shared__ __attribute__((aligned(16))) uint32_t bins[256 * kCopies], sums[256], totals[2][64];
-  constexpr uint32_t kStride = kSelectThreads * 4, kRound = kStride * STRIDES;
+  constexpr uint32_t kStride = THREADS * 4, kRound = kStride * STRIDES;
   const uint32_t h = blockIdx.x, s = blockIdx.y, list = s * c.kv_heads + h, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint64_t row = (uint64_t)list * c.capacity;
   const uint32_t length = (uint32_t)min(max(e.lengths[s], 0), (int32_t)c.capacity);
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
     return;
   }
   *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
-  static_assert(256 * kCopies == kSelectThreads * 4, "a thread clears four words");
+  static_assert(256 * kCopies == THREADS * 4 && kCopies % 4 == 0, "a thread clears four words, of one bin");
   if (rounds == 1) look(0, copies);
   __syncthreads();
   uint32_t prefix = 0, left = e.keep;   // `left` of those that agree with the prefix stay
@@ -350,13 +351,13 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
       }
     }
     __syncthreads();
-    {   // four lanes per bin
+    {   // kCopies / 4 lanes per bin
       const uint4 v = *(const uint4*)&bins[threadIdx.x * 4];
       *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
       uint32_t n = v.x + v.y + v.z + v.w;
-      n += __shfl_xor(n, 1);
-      n += __shfl_xor(n, 2);
-      if ((threadIdx.x & 3) == 0) sums[255 - threadIdx.x / 4] = n;   // from the top
+#pragma unroll
+      for (int d = 1; d < kCopies / 4; d *= 2) n += __shfl_xor(n, d);
+      if (threadIdx.x % (kCopies / 4) == 0) sums[255 - threadIdx.x / (kCopies / 4)] = n;   // from the top
     }
     __syncthreads();
     const uint4 v = *(const uint4*)&sums[4 * lane];   // every wavefront looks for itself
@@ -374,11 +375,11 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
   // The numbering, up to four strides at a time.  Sums over all wavefronts and strides before this wavefront's: totals has a word
   // for each, in that order.
   constexpr int kSome = STRIDES < 4 ? STRIDES : 4;
-  static_assert(4 * kSelectWaves == 64, "a lane per word");
+  static_assert(4 * kWaves <= 64, "a lane per word");
   auto before_each = [&](uint32_t word, uint32_t (&at)[kSome]) {
     const uint32_t upto = wave_prefix_sum(word), below = upto - word;
 #pragma unroll
-    for (int k = 0; k < kSome; ++k) at[k] = (uint32_t)__builtin_amdgcn_readlane((int)below, k * kSelectWaves + wave);
+    for (int k = 0; k < kSome; ++k) at[k] = (uint32_t)__builtin_amdgcn_readlane((int)below, k * kWaves + wave);
     return (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   };
   uint32_t equal = 0, freed = 0, taken = 0;   // numbered so far
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
 #pragma unroll
       for (int k = 0; k < kSome; ++k) {
         const uint32_t n = (uint32_t)__builtin_popcount((uint32_t)ties >> (4 * k) & 15), upto = wave_prefix_sum(n);
-        if (lane == 63) totals[0][k * kSelectWaves + wave] = upto;
+        if (lane == 63) totals[0][k * kWaves + wave] = upto;
         eq[k] = upto - n;
       }
       __syncthreads();
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
           packed[k] |= (uint32_t)(i + j < stay && !kept) << j | (uint32_t)(i + j >= e.keep && kept) << (4 + j);
         }
         upto[k] = wave_prefix_sum((uint32_t)__builtin_popcount(packed[k] & 15) << 16 | (uint32_t)__builtin_popcount(packed[k] >> 4));
-        if (lane == 63) totals[1][k * kSelectWaves + wave] = upto[k];
+        if (lane == 63) totals[1][k * kWaves + wave] = upto[k];
       }
       equal += all;
       __syncthreads();
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(CacheView c, Ev
     }
     __syncthreads();
   }
-  if constexpr (MOVES) move_tokens<INT8>(c, e, s, h, few[0], few[1], freed, threadIdx.x / 16, kSelectThreads / 16);
+  if constexpr (MOVES) move_tokens<INT8>(c, e, s, h, few[0], few[1], freed, threadIdx.x / 16, THREADS / 16);
   else if (threadIdx.x == 0) e.counts[list] = freed;
 }
 
@@ -489,15 +490,18 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
   const bool moves = e.lengths_out != e.lengths && most <= kMovesInSelect;
   const dim3 lists(c.kv_heads, c.n_seqs);
   hipStream_t st = (hipStream_t)stream;
-  auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, lists, dim3(kSelectThreads), 0, st, c, e); };
-  auto of = [&](auto n) {
-    constexpr int S = decltype(n)::value;
-    if (moves) int8 ? select(k_evict_select<S, true, true>) : select(k_evict_select<S, false, true>);
-    else select(k_evict_select<S, false, false>);
+  auto select = [&](auto threads, auto strides) {
+    constexpr int T = decltype(threads)::value, S = decltype(strides)::value;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, lists, dim3(T), 0, st, c, e); };
+    if (moves) int8 ? go(k_evict_select<T, S, true, true>) : go(k_evict_select<T, S, false, true>);
+    else go(k_evict_select<T, S, false, false>);
   };
-  if (c.capacity <= 4 * kSelectThreads) of(std::integral_constant<int, 1>());
-  else if (c.capacity <= 16 * kSelectThreads) of(std::integral_constant<int, 4>());
-  else of(std::integral_constant<int, 16>());
+  // As many threads as a list has fours of slots, as far as there are: a barrier among fewer wavefronts is shorter (1152 slots: 512 threads 7.7 us, 1024 9.4).
+  if (c.capacity <= 1024) select(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+  else if (c.capacity <= 2048) select(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+  else if (c.capacity <= 4096) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+  else if (c.capacity <= 16384) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+  else select(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
   if (!moves) {
     const uint32_t groups = kMoveThreads / 16;
     const uint32_t parts = std::max(1u, std::min((most + groups - 1) / groups, std::max(1u, 4096u / (c.kv_heads * c.n_seqs))));
