@@ -194,13 +194,18 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     }
     return w;
   };
+  // (kept from being widened ahead of the loop: a 32-bit offset beside a scalar base takes one register and no addition)
+  auto offset_of = [](uint32_t v) {
+    asm("" : "+v"(v));
+    return v;
+  };
   T x;
   auto fetch_keys = [&](const Blocks& w, uint32_t lanes) {   // lanes 0: all of them the same words
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const char* from = c.k + w.at[b];
 #pragma unroll
-      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + (key_at[s] & lanes));
+      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + offset_of(key_at[s] & lanes));
       if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
     }
   };
@@ -208,7 +213,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + (val_at & lanes));
+      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + offset_of(val_at & lanes));
       if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
     }
   };
