@@ -35,9 +35,8 @@ struct AttendView {
   uint32_t rows, heads, group, chunks, q16, out_by4;   // chunks: of up to kHeads query heads that share a key/value head, of all of these
 };
 
-__device__ __forceinline__ float ror8_sum(float v) {   // v of this lane + v of the lane 8 columns on
-  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128, 0xf, 0xf, true));
-}
+__device__ __forceinline__ uint32_t ror8(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true); }   // v of the lane 8 columns on
+__device__ __forceinline__ float ror8_sum(float v) { return v + __uint_as_float(ror8(__float_as_uint(v))); }
 
 __device__ __forceinline__ uint32_t row_length(const CacheView& c, const AttendView& a, uint32_t r, uint32_t* seq) {
   const int32_t s = a.seqs ? a.seqs[r] : (int32_t)r;
@@ -139,15 +138,17 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   }
   if (r >= a.rows) return;   // (lengths that change under the call)
 
-  // a lane's places in a block of 16 tokens: dims that a head does not have are read as its first ones, against zeros of q, and dropped
-  constexpr uint32_t kSize = INT8 ? 1 : 2;
+  // a lane's places in a block of 16 tokens: dims that a head does not have are read as its first ones, against zeros of q, and dropped.
+  // With 256 dims of bf16 the tiles alone take 192 registers of the 256, and what spills waits for all that is on its way: there one
+  // offset serves all loads of keys (where a head ends before a load's dims, it has the head's last ones once more), and the
+  // two halves of the columns fetch half of q each: 4 x 32768 tokens 110 -> 99 us.  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
+  constexpr bool kTight = DIM == 256 && !INT8;
+  constexpr uint32_t kSize = INT8 ? 1 : 2, kSpan = INT8 ? 64 : 32, kOffsets = kTight ? 1 : T::kLoads, kFetched = kTight ? 4 : 8;
   const uint32_t slot_bytes = kSize * (uint32_t)c.slot_stride;
-  uint32_t key_at[T::kLoads];
+  auto first_dim = [&](uint32_t s) { return !kTight ? kSpan * s : D >= kSpan ? min(kSpan * s, D - kSpan) : 0u; };
+  uint32_t key_at[kOffsets];
 #pragma unroll
-  for (int s = 0; s < T::kLoads; ++s) {
-    const uint32_t d0 = INT8 ? 64 * s + 16 * g : 32 * s + 8 * g;
-    key_at[s] = n * slot_bytes + kSize * (d0 < D ? d0 : 0);
-  }
+  for (uint32_t s = 0; s < kOffsets; ++s) key_at[s] = n * slot_bytes + (kSpan * kSize * s + 16 * g < kSize * D ? kSpan * kSize * s + 16 * g : 0);
   const uint32_t val_at = 4 * g * slot_bytes + kSize * (n * T::kVals < D ? n * T::kVals : 0);
 
   struct Segment {   // the part of a (row, chunk) that lies in this share
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     for (int b = 0; b < 2; ++b) {
       const char* from = c.k + w.at[b];
 #pragma unroll
-      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + offset_of(key_at[s] & lanes));
+      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + (kTight ? kSize * first_dim(s) : 0) + offset_of(key_at[kTight ? 0 : s] & lanes));
       if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
     }
   };
@@ -219,13 +220,14 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   };
   // 8 values of a segment's q: lane threadIdx.x % 64 of contraction step threadIdx.x / 64.  They are requested as the words they lie
   // in, without a condition, so that nothing waits for them here (a lane without values reads the first ones).
-  const uint32_t q_dim = INT8 ? 64 * (wave / 2) + 16 * g + 8 * (wave % 2) : 32 * wave + 8 * g, q_size = a.q16 ? 2 : 4;
-  uint32_t q8[8];
+  const uint32_t q_load = INT8 ? wave / 2 : wave, q_dim = first_dim(q_load) + (INT8 ? 16 * g + 8 * (wave % 2) : 8 * g), q_size = a.q16 ? 2 : 4;
+  const bool has_q = q_dim >= kSpan * q_load && q_dim < D;
+  uint32_t q_words[kFetched];
   auto fetch_q = [&](const Segment& s) {
     const uint64_t row = (uint64_t)a.q + q_size * (s.r * a.q_stride + s.first_head * D);
-    const uint32_t lane_at = head < s.n_heads && q_dim < D ? q_size * (head * D + q_dim) : 0;
+    const uint32_t lane_at = head < s.n_heads && has_q ? q_size * (head * D + q_dim + (kTight ? 4 * part : 0)) : 0;
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) q8[j] = *(global_cu32*)(((row + q_size * j) & ~(uint64_t)3) + lane_at);   // (lane_at: a multiple of 16)
+    for (uint32_t j = 0; j < kFetched; ++j) q_words[j] = *(global_cu32*)(((row + q_size * j) & ~(uint64_t)3) + lane_at);   // (lane_at: a multiple of 8)
   };
   Segment s = next_segment();
   fetch_q(s);
@@ -241,8 +243,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
 #pragma unroll
     for (int j = 0; j < 8; ++j) {   // (by all wavefronts: a load that some of them never use would be waited for in the loop, and with it those behind it)
       const uint32_t upper = ((uint32_t)(uint64_t)a.q + 2 * (uint32_t)(s.r * a.q_stride + j)) & 2;   // (of a bf16 value: the half of its word)
-      const float one = __uint_as_float((q8[j] << (a.q16 && !upper ? 16 : 0)) & (a.q16 ? 0xFFFF0000u : ~0u));
-      const float v = head < s.n_heads && q_dim < D ? one * a.scale : 0.f;
+      const uint32_t own = q_words[j % kFetched], other = kTight ? ror8(own) : own, word = (j < 4) == (part == 0) ? own : other;
+      const float one = __uint_as_float((word << (a.q16 && !upper ? 16 : 0)) & (a.q16 ? 0xFFFF0000u : ~0u));
+      const float v = head < s.n_heads && has_q ? one * a.scale : 0.f;
       const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
       q0[j] = part ? mid : hi;
       q1[j] = part ? (__bf16)0.f : lo;
