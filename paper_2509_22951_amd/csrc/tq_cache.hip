@@ -189,15 +189,23 @@ struct EvictView {
   float* scores_out;
   int32_t* positions_out;
   uint32_t* counts;   // [seq][head]: tokens to move
-  uint32_t *to, *from;   // [seq][head][keep]: slots to fill, and the slots they are filled from
+  uint32_t *to, *from;   // [seq][head][keep]: slots to fill, and the slots they are filled from (slices: the last one first)
   uint32_t keep;
-  bool by4;           // scores and positions start on 16 bytes, in and out
+  // lists that are cut into slices
+  uint32_t slices;         // of a list; 0: not cut
+  uint32_t* histograms;    // [round % 2][seq][head][slice][256]
+  uint32_t* above;         // [seq][head][slice]: tokens above what is found of the limit
+  uint2* found;            // [round][seq][head]: upper bits of the limit, tokens with these bits that stay
 };
 
 constexpr int kMoveThreads = 256;
 constexpr uint32_t kMovesInSelect = 512;   // tokens of a list
+constexpr uint32_t kSlicesTogether = 512;      // workgroups
+constexpr uint32_t kListInWorkgroup = 16384;   // slots: one workgroup takes 8 lists of 16384 in 20 us, slices 29; of 20000 it took 44, slices 28
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // (16 bytes from any 4-byte boundary are one load)
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Numbers that compare as the scores do: NaN lowest, the two zeros equal, protected tokens above +infinity.
 __device__ __forceinline__ uint32_t rank_of(float score, bool is_protected) {
@@ -217,6 +225,63 @@ __device__ __forceinline__ uint32_t wave_prefix_sum(uint32_t v) {   // inclusive
   return v;
 }
 
+// The ranks of slots first + k * stride .. + 3 of a list, whose slots begin at `row`; those from `length` on are read as the list's first ones.  All
+// loads are requested before any of them is used, and without a condition: behind one they would come one after another (8 lists
+// of 16384 slots, all of the call: 24.1 us in place of 19.9).  copies: what stays in its place goes to scores_out and positions_out, with what will be written over there
+// by a token that is moved.
+template <int STRIDES>
+__device__ __forceinline__ void ranks_at(const CacheView& c, const EvictView& e, uint64_t row, uint32_t first, uint32_t stride, uint32_t length, int32_t since, bool copies,
+                                         uint32_t (&rank)[STRIDES][4]) {
+  f32x4_any v[STRIDES];
+  i32x4_any p[STRIDES];
+  const float* scores = c.scores + row;
+  const int32_t* positions = (c.positions ? c.positions : (const int32_t*)c.scores) + row;   // (no use is made of them without positions)
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    const uint32_t i = first + k * stride, at = i < length ? i : 0;   // (a list's room is a multiple of 16 slots)
+    v[k] = *(const f32x4_any*)(scores + at), p[k] = *(const i32x4_any*)(positions + at);
+  }
+  if (copies) {
+    const uint32_t stay = min(length, e.keep);
+#pragma unroll
+    for (int k = 0; k < STRIDES; ++k) {
+      const uint32_t i = first + k * stride;
+      if (i + 4 <= stay) {
+        if (e.scores_out != c.scores) *(f32x4_any*)(e.scores_out + row + i) = v[k];
+        if (e.positions_out != c.positions) *(i32x4_any*)(e.positions_out + row + i) = p[k];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (i + j < stay) {
+            if (e.scores_out != c.scores) e.scores_out[row + i + j] = v[k][j];
+            if (e.positions_out != c.positions) e.positions_out[row + i + j] = p[k][j];
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) rank[k][j] = rank_of(v[k][j], e.since && p[k][j] >= since);
+}
+
+// The bin, from the top, in which the `left`-th token lies; `over` lie above it.  sums: of 256 bins, the highest first.
+struct Bin {
+  uint32_t bin, over, in;
+};
+__device__ __forceinline__ Bin find_bin(const uint32_t* sums, uint32_t left) {   // every wavefront for itself
+  const uint32_t lane = threadIdx.x & 63;
+  const uint4 v = *(const uint4*)&sums[4 * lane];
+  const uint32_t n = v.x + v.y + v.z + v.w, upto = wave_prefix_sum(n), before = upto - n;
+  const uint64_t at = __ballot(before < left && left <= upto);
+  uint32_t over = before, b = 4 * lane, in = v.x;
+  if (over + in < left) over += in, in = v.y, ++b;
+  if (over + in < left) over += in, in = v.z, ++b;
+  if (over + in < left) over += in, in = v.w, ++b;
+  const int one = at ? __builtin_ctzll(at) : 63;   // (there is one)
+  return {255 - (uint32_t)__builtin_amdgcn_readlane((int)b, one), (uint32_t)__builtin_amdgcn_readlane((int)over, one), (uint32_t)__builtin_amdgcn_readlane((int)in, one)};
+}
+
 // Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., kAhead of them
 // together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.
 template <bool INT8>
@@ -232,7 +297,7 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 #pragma unroll
     for (uint32_t i = 0; i < kAhead; ++i) {
       const uint32_t at = min(m + i * step, n - 1);
-      to[i] = slots_to[at], of[i] = slots_from[at];
+      to[i] = min(slots_to[at], c.capacity - 1), of[i] = min(slots_from[e.slices ? n - 1 - at : at], c.capacity - 1);   // (lengths that change under the call)
     }
 #pragma unroll
     for (uint32_t i = 0; i < kAhead; ++i) {
@@ -274,81 +339,40 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 // 8 bits over those that agree with the bits found), then one look in the order of the slots that numbers the equal ones at the
 // limit, the free slots below `keep` and the kept ones above.
 //
-// A workgroup per list; a thread has 4 neighbouring slots of every kStride, and the ranks of STRIDES of them in registers.  Where
-// that is not the whole list the ranks are made again from the scores, which the L2 holds by then, for every 8 bits.  Scores share
-// few exponents, so that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there
+// A workgroup per list; a thread has 4 neighbouring slots of every kStride, and their ranks in registers.  Scores share few exponents, so that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there
 // are several copies of it.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
 template <int THREADS, int STRIDES, bool INT8, bool MOVES>
 __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView e) {
   constexpr int kWaves = THREADS / 64, kCopies = THREADS / 64;
   __shared__ __attribute__((aligned(16))) uint32_t bins[256 * kCopies], sums[256], totals[2][64];
-  constexpr uint32_t kStride = THREADS * 4, kRound = kStride * STRIDES;
+  constexpr uint32_t kStride = THREADS * 4;
   const uint32_t h = blockIdx.x, s = blockIdx.y, list = s * c.kv_heads + h, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint64_t row = (uint64_t)list * c.capacity;
   const uint32_t length = (uint32_t)min(max(e.lengths[s], 0), (int32_t)c.capacity);
   const int32_t since = e.since ? e.since[s] : 0;
   const uint32_t stay = min(length, e.keep);
-  const uint32_t rounds = (length + kRound - 1) / kRound;
   uint32_t rank[STRIDES][4];
-  auto slot_of = [&](uint32_t round, int k) { return round * kRound + k * kStride + threadIdx.x * 4; };
-  auto look = [&](uint32_t round, bool copies) {   // the ranks of this thread's slots of a round
-#pragma unroll
-    for (int k = 0; k < STRIDES; ++k) {
-      if (k % 4 == 0 && k) asm volatile("" ::: "memory");   // (no more than four strides' loads at a time: registers)
-      const uint32_t i = slot_of(round, k);
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      int4 p = make_int4(0, 0, 0, 0);
-      if (i < length) {   // (a list's room is a multiple of 16 slots)
-        if (e.by4) {
-          v = *(const float4*)(c.scores + row + i);
-          if (c.positions) p = *(const int4*)(c.positions + row + i);
-        } else {
-          const float* sc = c.scores + row + i;
-          v = make_float4(sc[0], sc[1], sc[2], sc[3]);
-          if (c.positions) p = make_int4(c.positions[row + i], c.positions[row + i + 1], c.positions[row + i + 2], c.positions[row + i + 3]);
-        }
-        if (copies) {   // what stays in its place, and what will be written over by a token that is moved
-          if (e.by4 && i + 4 <= stay) {
-            if (e.scores_out != c.scores) *(float4*)(e.scores_out + row + i) = v;
-            if (e.positions_out != c.positions) *(int4*)(e.positions_out + row + i) = p;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (i + j < stay) {
-                if (e.scores_out != c.scores) e.scores_out[row + i + j] = (&v.x)[j];
-                if (e.positions_out != c.positions) e.positions_out[row + i + j] = (&p.x)[j];
-              }
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) rank[k][j] = rank_of((&v.x)[j], e.since && (&p.x)[j] >= since);
-    }
-  };
+  auto slot_of = [&](int k) { return k * kStride + threadIdx.x * 4; };
   const bool copies = e.scores_out != c.scores || e.positions_out != c.positions;
   if (MOVES && h == 0 && threadIdx.x == 0) e.lengths_out[s] = min(e.lengths[s], (int32_t)min(e.keep, 0x7FFFFFFFu));
   if (length <= e.keep) {
     if (threadIdx.x == 0) e.counts[list] = 0;
-    if (copies)
-      for (uint32_t round = 0; round < rounds; ++round) look(round, true);
+    if (copies) ranks_at<STRIDES>(c, e, row, slot_of(0), kStride, length, since, true, rank);
     return;
   }
   *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
   static_assert(256 * kCopies == THREADS * 4 && kCopies % 4 == 0, "a thread clears four words, of one bin");
-  if (rounds == 1) look(0, copies);
+  ranks_at<STRIDES>(c, e, row, slot_of(0), kStride, length, since, copies, rank);
   __syncthreads();
   uint32_t prefix = 0, left = e.keep;   // `left` of those that agree with the prefix stay
   for (int shift = 24; shift >= 0; shift -= 8) {
-    for (uint32_t round = 0; round < rounds; ++round) {
-      if (rounds > 1) look(round, copies && shift == 24);
 #pragma unroll
-      for (int k = 0; k < STRIDES; ++k) {
-        const uint32_t i = slot_of(round, k);
+    for (int k = 0; k < STRIDES; ++k) {
+      const uint32_t i = slot_of(k);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (i + j < length && (shift == 24 || (rank[k][j] ^ prefix) >> ((shift + 8) & 31) == 0))
-            atomicAdd(&bins[(rank[k][j] >> shift & 255) * kCopies + (lane & (kCopies - 1))], 1u);
-      }
+      for (int j = 0; j < 4; ++j)
+        if (i + j < length && (shift == 24 || (rank[k][j] ^ prefix) >> ((shift + 8) & 31) == 0))
+          atomicAdd(&bins[(rank[k][j] >> shift & 255) * kCopies + (lane & (kCopies - 1))], 1u);
     }
     __syncthreads();
     {   // kCopies / 4 lanes per bin
@@ -360,89 +384,207 @@ __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView
       if (threadIdx.x % (kCopies / 4) == 0) sums[255 - threadIdx.x / (kCopies / 4)] = n;   // from the top
     }
     __syncthreads();
-    const uint4 v = *(const uint4*)&sums[4 * lane];   // every wavefront looks for itself
-    const uint32_t n = v.x + v.y + v.z + v.w, upto = wave_prefix_sum(n), before = upto - n;
-    const uint64_t at = __ballot(before < left && left <= upto);
-    uint32_t over = before, b = 4 * lane, in = v.x;
-    if (over + in < left) over += in, in = v.y, ++b;
-    if (over + in < left) over += in, in = v.z, ++b;
-    if (over + in < left) over += in, in = v.w, ++b;
-    const int one = __builtin_ctzll(at);
-    prefix |= (255 - (uint32_t)__builtin_amdgcn_readlane((int)b, one)) << shift;
-    left -= (uint32_t)__builtin_amdgcn_readlane((int)over, one);
-    if ((uint32_t)__builtin_amdgcn_readlane((int)in, one) == left) break;   // all of these stay
+    const Bin found = find_bin(sums, left);
+    prefix |= found.bin << shift;
+    left -= found.over;
+    if (found.in == left) break;   // all of these stay
   }
-  // The numbering, up to four strides at a time.  Sums over all wavefronts and strides before this wavefront's: totals has a word
-  // for each, in that order.
-  constexpr int kSome = STRIDES < 4 ? STRIDES : 4;
-  static_assert(4 * kWaves <= 64, "a lane per word");
-  auto before_each = [&](uint32_t word, uint32_t (&at)[kSome]) {
+  // The numbering.  Sums over all wavefronts and strides before this wavefront's: totals has a word for each, in that order.
+  static_assert(STRIDES * kWaves <= 64, "a lane per word");
+  auto before_each = [&](uint32_t word, uint32_t (&at)[STRIDES]) {
     const uint32_t upto = wave_prefix_sum(word), below = upto - word;
 #pragma unroll
-    for (int k = 0; k < kSome; ++k) at[k] = (uint32_t)__builtin_amdgcn_readlane((int)below, k * kWaves + wave);
+    for (int k = 0; k < STRIDES; ++k) at[k] = (uint32_t)__builtin_amdgcn_readlane((int)below, k * kWaves + wave);
     return (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   };
-  uint32_t equal = 0, freed = 0, taken = 0;   // numbered so far
   __shared__ uint32_t few[2][MOVES ? kMovesInSelect : 1];   // the list, where it is used here
   uint32_t *to = MOVES ? few[0] : e.to + (uint64_t)list * e.keep, *from = MOVES ? few[1] : e.from + (uint64_t)list * e.keep;
   if (threadIdx.x < 64) totals[0][threadIdx.x] = totals[1][threadIdx.x] = 0;   // (more than there are of them with one stride)
   __syncthreads();
-  for (uint32_t round = 0; round < rounds; ++round) {
-    if (rounds > 1) look(round, false);
-    uint64_t above = 0, ties = 0;   // a bit per slot of this thread: its rank is above the limit, or at it
+  uint32_t eq[STRIDES], at[STRIDES];
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n += slot_of(k) + j < length && rank[k][j] == prefix;
+    const uint32_t upto = wave_prefix_sum(n);
+    if (lane == 63) totals[0][k * kWaves + wave] = upto;
+    eq[k] = upto - n;
+  }
+  __syncthreads();
+  before_each(totals[0][lane], at);
+  uint32_t packed[STRIDES], upto[STRIDES];   // a bit per slot: 0..3 it becomes free, 4..7 its token moves; both counts, up to and with this lane
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    const uint32_t i = slot_of(k);
+    uint32_t before = at[k] + eq[k];
+    packed[k] = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool here = i + j < length, tie = here && rank[k][j] == prefix, kept = here && (rank[k][j] > prefix || (tie && before < left));
+      before += tie;
+      packed[k] |= (uint32_t)(i + j < stay && !kept) << j | (uint32_t)(i + j >= e.keep && kept) << (4 + j);
+    }
+    upto[k] = wave_prefix_sum((uint32_t)__builtin_popcount(packed[k] & 15) << 16 | (uint32_t)__builtin_popcount(packed[k] >> 4));
+    if (lane == 63) totals[1][k * kWaves + wave] = upto[k];
+  }
+  __syncthreads();
+  static_assert(kStride * STRIDES <= 1u << 15, "either count in 16 bits: at most half of the slots move");
+  const uint32_t moves = before_each(totals[1][lane], at) & 0xFFFF;
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    const uint32_t i = slot_of(k), frees = packed[k] & 15, takes = packed[k] >> 4, below = at[k] + upto[k];
+    uint32_t f = (below >> 16) - (uint32_t)__builtin_popcount(frees), t = (below & 0xFFFF) - (uint32_t)__builtin_popcount(takes);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (frees >> j & 1) to[f++] = i + j;
+      if (takes >> j & 1) from[t++] = i + j;
+    }
+  }
+  if constexpr (MOVES) {
+    __syncthreads();
+    move_tokens<INT8>(c, e, s, h, few[0], few[1], moves, threadIdx.x / 16, THREADS / 16);
+  } else if (threadIdx.x == 0) {
+    e.counts[list] = moves;
+  }
+}
+
+// The same for lists that are more than a workgroup has registers for: a workgroup per slice, a launch per 8 bits of the limit (rounds
+// 0..3: the slice's histogram of these bits) and one that numbers (round 4).  Each begins with the sum of the slices' histograms of the
+// launch before.  With K kept tokens before it, a free slot i below `keep` is the list's (i - K)-th, and a kept one at or above `keep` the
+// (keep - 1 - K)-th from the end of those that move, so that K is all a slice has to know of the others.
+constexpr int kSliceThreads = 1024;
+template <int STRIDES>
+__global__ __launch_bounds__(kSliceThreads) void k_evict_slice(CacheView c, EvictView e, uint32_t round) {
+  constexpr int kWaves = kSliceThreads / 64, kCopies = 16;
+  constexpr uint32_t kStride = kSliceThreads * 4, kSlice = kStride * STRIDES;
+  __shared__ __attribute__((aligned(16))) uint32_t bins[256 * kCopies], sums[256], totals[4][64];
+  const uint32_t slice = blockIdx.x, h = blockIdx.y, s = blockIdx.z, list = s * c.kv_heads + h, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lists = c.n_seqs * c.kv_heads, length = (uint32_t)min(max(e.lengths[s], 0), (int32_t)c.capacity);
+  if (length <= e.keep && slice == 0 && threadIdx.x == 0) e.counts[list] = 0;
+  if (slice * kSlice >= length || (length <= e.keep && round)) return;
+  auto slot_of = [&](int k) { return slice * kSlice + k * kStride + threadIdx.x * 4; };
+  uint32_t rank[STRIDES][4];
+  ranks_at<STRIDES>(c, e, (uint64_t)list * c.capacity, slot_of(0), kStride, length, e.since ? e.since[s] : 0, round == 0 && (e.scores_out != c.scores || e.positions_out != c.positions), rank);
+  if (length <= e.keep) return;
+  const uint32_t slices = (length + kSlice - 1) / kSlice;
+  auto histogram_of = [&](uint32_t r, uint32_t q) { return (uint4*)(e.histograms + (((uint64_t)(r % 2) * lists + list) * e.slices + q) * 256); };
+  uint32_t prefix = 0, left = e.keep, above = 0;   // `left` of those that agree with the prefix stay; the slice's tokens above it
+  uint32_t bin = 0;
+  if (round) {
+    if (round > 1) {
+      const uint2 f = e.found[(uint64_t)(round - 1) * lists + list];
+      prefix = f.x, left = f.y;
+    }
+    uint4 n = make_uint4(0, 0, 0, 0);
+    for (uint32_t q = wave; q < slices; q += kWaves) {
+      const uint4 v = histogram_of(round - 1, q)[lane];
+      n.x += v.x, n.y += v.y, n.z += v.z, n.w += v.w;
+    }
+    *(uint4*)&bins[wave * 256 + 4 * lane] = n;
+    __syncthreads();
+    if (threadIdx.x < 256) {
+      uint32_t sum = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) sum += bins[w * 256 + threadIdx.x];
+      sums[255 - threadIdx.x] = sum;
+    }
+    __syncthreads();
+    const Bin found = find_bin(sums, left);
+    bin = found.bin;
+    prefix |= bin << (32 - 8 * round);
+    left -= found.over;
+  }
+  auto above_in = [&](uint4 v) { return (4 * lane > bin ? v.x : 0u) + (4 * lane + 1 > bin ? v.y : 0u) + (4 * lane + 2 > bin ? v.z : 0u) + (4 * lane + 3 > bin ? v.w : 0u); };
+  if (round < 4) {
+    *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
+    static_assert(256 * kCopies == kSliceThreads * 4 && kWaves <= kCopies, "a thread clears four words, of one bin; a wavefront's sums fit");
+    if (round && wave == 0) {
+      above = above_in(histogram_of(round - 1, slice)[lane]);
+      above = (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(above), 63);
+      if (lane == 0) {
+        uint32_t* to = e.above + (uint64_t)list * e.slices + slice;
+        *to = above + (round > 1 ? *to : 0);
+        if (slice == 0) e.found[(uint64_t)round * lists + list] = make_uint2(prefix, left);
+      }
+    }
+    __syncthreads();
+    const uint32_t shift = 24 - 8 * round;
 #pragma unroll
     for (int k = 0; k < STRIDES; ++k)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool here = slot_of(round, k) + j < length;
-        above |= (uint64_t)(here && rank[k][j] > prefix) << (4 * k + j);
-        ties |= (uint64_t)(here && rank[k][j] == prefix) << (4 * k + j);
-      }
-    for (int k0 = 0; k0 < STRIDES && slot_of(round, k0) - threadIdx.x * 4 < length; k0 += kSome, above >>= 16, ties >>= 16) {
-      uint32_t eq[kSome], at[kSome];
-#pragma unroll
-      for (int k = 0; k < kSome; ++k) {
-        const uint32_t n = (uint32_t)__builtin_popcount((uint32_t)ties >> (4 * k) & 15), upto = wave_prefix_sum(n);
-        if (lane == 63) totals[0][k * kWaves + wave] = upto;
-        eq[k] = upto - n;
-      }
-      __syncthreads();
-      const uint32_t all = before_each(totals[0][lane], at);
-      uint32_t packed[kSome], upto[kSome];   // a bit per slot: 0..3 it becomes free, 4..7 its token moves; both counts, up to and with this lane
-#pragma unroll
-      for (int k = 0; k < kSome; ++k) {
-        const uint32_t i = slot_of(round, k0 + k);
-        uint32_t before = equal + at[k] + eq[k];
-        packed[k] = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool tie = (uint32_t)ties >> (4 * k + j) & 1, kept = ((uint32_t)above >> (4 * k + j) & 1) || (tie && before < left);
-          before += tie;
-          packed[k] |= (uint32_t)(i + j < stay && !kept) << j | (uint32_t)(i + j >= e.keep && kept) << (4 + j);
-        }
-        upto[k] = wave_prefix_sum((uint32_t)__builtin_popcount(packed[k] & 15) << 16 | (uint32_t)__builtin_popcount(packed[k] >> 4));
-        if (lane == 63) totals[1][k * kWaves + wave] = upto[k];
-      }
-      equal += all;
-      __syncthreads();
-      // (four strides have at most 2^14 of each)
-      const uint32_t both = before_each(totals[1][lane], at);
-#pragma unroll
-      for (int k = 0; k < kSome; ++k) {
-        const uint32_t i = slot_of(round, k0 + k), frees = packed[k] & 15, takes = packed[k] >> 4, below = at[k] + upto[k];
-        uint32_t f = freed + (below >> 16) - (uint32_t)__builtin_popcount(frees), t = taken + (below & 0xFFFF) - (uint32_t)__builtin_popcount(takes);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (frees >> j & 1) to[f++] = i + j;
-          if (takes >> j & 1) from[t++] = i + j;
-        }
-      }
-      freed += both >> 16, taken += both & 0xFFFF;
-    }
+      for (int j = 0; j < 4; ++j)
+        if (slot_of(k) + j < length && (round == 0 || (rank[k][j] ^ prefix) >> ((shift + 8) & 31) == 0))
+          atomicAdd(&bins[(rank[k][j] >> shift & 255) * kCopies + (lane & (kCopies - 1))], 1u);
     __syncthreads();
+    const uint4 v = *(const uint4*)&bins[threadIdx.x * 4];
+    uint32_t n = v.x + v.y + v.z + v.w;
+#pragma unroll
+    for (int d = 1; d < kCopies / 4; d *= 2) n += __shfl_xor(n, d);
+    if (threadIdx.x % (kCopies / 4) == 0) ((uint32_t*)histogram_of(round, slice))[threadIdx.x / (kCopies / 4)] = n;
+    return;
   }
-  if constexpr (MOVES) move_tokens<INT8>(c, e, s, h, few[0], few[1], freed, threadIdx.x / 16, THREADS / 16);
-  else if (threadIdx.x == 0) e.counts[list] = freed;
+  // what the slices before this one have above the limit and at it
+  uint32_t over = 0, equal = 0;
+  for (uint32_t q = wave; q < slice; q += kWaves) {
+    const uint4 v = histogram_of(3, q)[lane];
+    over += above_in(v) + (lane == 0 ? e.above[(uint64_t)list * e.slices + q] : 0);
+    equal += 4 * lane == (bin & ~3u) ? (bin & 2 ? bin & 1 ? v.w : v.z : bin & 1 ? v.y : v.x) : 0;
+  }
+  over = wave_prefix_sum(over), equal = wave_prefix_sum(equal);
+  if (threadIdx.x < 4 * 64) totals[threadIdx.x / 64][lane] = 0;   // (with fewer strides there are fewer of them)
+  __syncthreads();
+  if (lane == 63) totals[0][wave] = over, totals[1][wave] = equal;
+  static_assert(STRIDES * kWaves <= 64, "a lane per word");
+  auto before_each = [&](uint32_t word, uint32_t (&at)[STRIDES]) {   // over all wavefronts and strides before this wavefront's
+    const uint32_t below = wave_prefix_sum(word) - word;
+#pragma unroll
+    for (int k = 0; k < STRIDES; ++k) at[k] = (uint32_t)__builtin_amdgcn_readlane((int)below, k * kWaves + wave);
+  };
+  uint32_t tie[STRIDES], kept[STRIDES], before[STRIDES], at[STRIDES];
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n += slot_of(k) + j < length && rank[k][j] == prefix;
+    const uint32_t upto = wave_prefix_sum(n);
+    if (lane == 63) totals[2][k * kWaves + wave] = upto;
+    tie[k] = upto - n;
+  }
+  __syncthreads();
+  const uint32_t over_before = (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(totals[0][lane]), 63);
+  const uint32_t equal_before = (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(totals[1][lane]), 63);
+  before_each(totals[2][lane], at);
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    uint32_t order = equal_before + at[k] + tie[k];
+    kept[k] = 0;   // a bit per slot
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool here = slot_of(k) + j < length, same = here && rank[k][j] == prefix;
+      kept[k] |= (uint32_t)(here && (rank[k][j] > prefix || (same && order < left))) << j;
+      order += same;
+    }
+    const uint32_t n = (uint32_t)__builtin_popcount(kept[k]), upto = wave_prefix_sum(n);
+    if (lane == 63) totals[3][k * kWaves + wave] = upto;
+    before[k] = upto - n;
+  }
+  __syncthreads();
+  before_each(totals[3][lane], at);
+  uint32_t *to = e.to + (uint64_t)list * e.keep, *from = e.from + (uint64_t)list * e.keep;
+#pragma unroll
+  for (int k = 0; k < STRIDES; ++k) {
+    uint32_t n = over_before + min(equal_before, left) + at[k] + before[k];   // kept tokens before slot i
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t i = slot_of(k) + j;
+      const bool stays = kept[k] >> j & 1;
+      if (i < e.keep && !stays && n <= i) to[i - n] = i;   // (the bounds: lengths that change under the call)
+      if (i >= e.keep && stays && n < e.keep) from[e.keep - 1 - n] = i;
+      n += stays;
+      if (i + 1 == e.keep) e.counts[list] = e.keep - min(n, e.keep);
+    }
+  }
 }
 
 template <bool INT8>
@@ -458,6 +600,23 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(CacheView c, EvictV
 
 uint64_t evict_counts_bytes(const CacheView& c) { return ((uint64_t)c.n_seqs * c.kv_heads * 4 + 255) / 256 * 256; }
 
+uint64_t evict_moves_bytes(const CacheView& c, uint32_t keep) { return ((uint64_t)c.n_seqs * c.kv_heads * std::min(keep, c.capacity) * sizeof(uint2) + 255) / 256 * 256; }
+// A slice has as few strides as let all workgroups be on the GPU together (two per compute unit): 8 lists of 20000 slots 28 us with one stride
+// and 32 with two, 128 of them 80 and 68.
+uint32_t evict_strides(const CacheView& c) {
+  const uint64_t pieces = (uint64_t)c.n_seqs * c.kv_heads * ((c.capacity + 4 * kSliceThreads - 1) / (4 * kSliceThreads));
+  return pieces <= kSlicesTogether ? 1 : pieces <= 2 * kSlicesTogether ? 2 : 4;
+}
+// Slices of a list, or 0 where a workgroup takes the whole of it
+uint32_t evict_slices(const CacheView& c) {
+  const uint32_t slots = 4 * kSliceThreads * evict_strides(c);
+  return c.capacity <= kListInWorkgroup ? 0 : (c.capacity + slots - 1) / slots;
+}
+uint64_t evict_slices_bytes(const CacheView& c) {   // histograms of two rounds, above, found
+  const uint64_t lists = (uint64_t)c.n_seqs * c.kv_heads, slices = evict_slices(c);
+  return slices ? lists * (slices * (2 * 256 + 1) * sizeof(uint32_t) + 4 * sizeof(uint2)) : 0;
+}
+
 int check_evict(const std::string& who, const tq_cache* cache, const tq_evict_args* a, CacheView* c, uint64_t* bytes) {
   if (int rc = view_cache(who, cache, c)) return rc;
   if (!a) return refuse(TQ_E_INVALID_ARG, who + ": null argument");
@@ -465,7 +624,7 @@ int check_evict(const std::string& who, const tq_cache* cache, const tq_evict_ar
   if (!c->scores) return refuse(TQ_E_INVALID_ARG, who + ": the cache has no scores");
   if (a->since && !c->positions) return refuse(TQ_E_INVALID_ARG, who + ": since needs the cache's positions");
   if ((a->positions_out && !c->positions)) return refuse(TQ_E_INVALID_ARG, who + ": positions_out needs the cache's positions");
-  *bytes = evict_counts_bytes(*c) + (uint64_t)c->n_seqs * c->kv_heads * std::min(a->keep, c->capacity) * sizeof(uint2);
+  *bytes = evict_counts_bytes(*c) + evict_moves_bytes(*c, a->keep) + evict_slices_bytes(*c);
   return TQ_OK;
 }
 
@@ -481,13 +640,17 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
     return refuse(TQ_E_INVALID_ARG, who + ": a pointer is not aligned to its type (workspace: 16 bytes)");
   const uint32_t keep = std::min(a->keep, c.capacity);
   EvictView e{a->lengths, a->since, a->lengths_out ? a->lengths_out : a->lengths, a->scores_out ? a->scores_out : c.scores,
-              a->positions_out ? a->positions_out : c.positions, (uint32_t*)a->workspace, (uint32_t*)((char*)a->workspace + evict_counts_bytes(c)), nullptr, keep,
-              aligned_to(c.scores, 16) && aligned_to(c.positions, 16) && aligned_to(a->scores_out, 16) && aligned_to(a->positions_out, 16)};
-  e.from = e.to + (uint64_t)c.n_seqs * c.kv_heads * keep;
+              a->positions_out ? a->positions_out : c.positions, (uint32_t*)a->workspace, (uint32_t*)((char*)a->workspace + evict_counts_bytes(c)), nullptr, keep};
+  const uint64_t n_lists = (uint64_t)c.n_seqs * c.kv_heads;
+  e.from = e.to + n_lists * keep;
+  e.slices = evict_slices(c);
+  e.found = (uint2*)((char*)a->workspace + evict_counts_bytes(c) + evict_moves_bytes(c, keep));
+  e.histograms = (uint32_t*)(e.found + 4 * n_lists);
+  e.above = e.histograms + 2 * n_lists * e.slices * 256;
   const bool int8 = cache->type == TQ_INT8;
   const uint32_t most = std::min(keep, c.capacity - keep);   // tokens to move, of a list
   // Few of them are moved by the workgroup that has found them, unless others may still have to read the lengths that it writes.
-  const bool moves = e.lengths_out != e.lengths && most <= kMovesInSelect;
+  const bool moves = !e.slices && e.lengths_out != e.lengths && most <= kMovesInSelect;
   const dim3 lists(c.kv_heads, c.n_seqs);
   hipStream_t st = (hipStream_t)stream;
   auto select = [&](auto threads, auto strides) {
@@ -500,8 +663,13 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
   if (c.capacity <= 1024) select(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 2048) select(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 4096) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
-  else if (c.capacity <= 16384) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
-  else select(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
+  else if (!e.slices) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+  else
+    for (uint32_t round = 0; round <= 4; ++round) {
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(e.slices, c.kv_heads, c.n_seqs), dim3(kSliceThreads), 0, st, c, e, round); };
+      const uint32_t strides = evict_strides(c);
+      strides == 1 ? go(k_evict_slice<1>) : strides == 2 ? go(k_evict_slice<2>) : go(k_evict_slice<4>);
+    }
   if (!moves) {
     const uint32_t groups = kMoveThreads / 16;
     const uint32_t parts = std::max(1u, std::min((most + groups - 1) / groups, std::max(1u, 4096u / (c.kv_heads * c.n_seqs))));

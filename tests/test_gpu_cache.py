@@ -277,6 +277,18 @@ def test_evict_equal_scores_zeros_infinities_and_nan():
         check_evict(p, ints([1280, 1280, 1280, 1280]), keep, in_place=False)
 
 
+@pytest.mark.parametrize("keep,kind,in_place", [(1, "bf16", True), (4095, "int8", False), (4096, "bf16", True), (4098, "bf16", False), (12289, "int8", True), (20477, "bf16", False)])
+def test_evict_long_lists_of_equal_scores(keep, kind, in_place):
+    p = Paged(5, 1280, kv_heads=1, dim=16, kind=kind, marks=True, seed=keep)
+    g = torch.Generator().manual_seed(keep)
+    few = torch.tensor([0.0, 0.5, 0.5000001, 1.0, float("nan"), float("-inf"), -2.0])
+    p.scores.copy_(few[torch.randint(0, len(few), p.scores.shape, generator=g)])
+    p.scores[1] = 0.25
+    p.scores[1, :, 8192:12288] = 0.75   # more than the others, all in one stretch
+    p.positions.copy_(torch.arange(p.positions[0].numel(), dtype=torch.int32).flip(0).expand_as(p.positions))   # the newest first
+    check_evict(p, ints([20480, 20479, 0, 4096, 16400]), keep, since=ints([20480 - 700, 20481, 0, 0, 20475]), in_place=in_place)
+
+
 @pytest.mark.parametrize("recent", [0, 1, 30, 99, 100, 150])
 def test_evict_protects_by_position(recent):
     p = Paged(3, 20, kv_heads=2, dim=32, marks=True)
