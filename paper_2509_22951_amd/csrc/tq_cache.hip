@@ -199,7 +199,8 @@ struct EvictView {
 };
 
 constexpr int kMoveThreads = 256;
-constexpr uint32_t kMovesInSelect = 512;   // tokens of a list
+constexpr uint32_t kMovesInSelect = 512;   // tokens of a list, half of it with fewer than kManyLists lists
+constexpr uint32_t kManyLists = 64;
 constexpr uint32_t kSlicesTogether = 512;      // workgroups
 constexpr uint32_t kListInWorkgroup = 16384;   // slots: one workgroup takes 8 lists of 16384 in 20 us, slices 29; of 20000 it took 44, slices 28
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
@@ -343,7 +344,7 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 // are several copies of it.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
 template <int THREADS, int STRIDES, bool INT8, bool MOVES>
 __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView e) {
-  constexpr int kWaves = THREADS / 64, kCopies = THREADS / 64;
+  constexpr int kWaves = THREADS / 64, kCopies = kWaves < 8 ? kWaves : 8;   // (a copy per lane costs more to clear and add up than it saves: 16384 slots 19.9 -> 22.8 us)
   __shared__ __attribute__((aligned(16))) uint32_t bins[256 * kCopies], sums[256], totals[2][64];
   constexpr uint32_t kStride = THREADS * 4;
   const uint32_t h = blockIdx.x, s = blockIdx.y, list = s * c.kv_heads + h, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -360,8 +361,8 @@ __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView
     if (copies) ranks_at<STRIDES>(c, e, row, slot_of(0), kStride, length, since, true, rank);
     return;
   }
-  *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
-  static_assert(256 * kCopies == THREADS * 4 && kCopies % 4 == 0, "a thread clears four words, of one bin");
+  if (threadIdx.x < 64 * kCopies) *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
+  static_assert(64 * kCopies <= THREADS && kCopies % 4 == 0, "a thread clears four words, of one bin");
   ranks_at<STRIDES>(c, e, row, slot_of(0), kStride, length, since, copies, rank);
   __syncthreads();
   uint32_t prefix = 0, left = e.keep;   // `left` of those that agree with the prefix stay
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView
           atomicAdd(&bins[(rank[k][j] >> shift & 255) * kCopies + (lane & (kCopies - 1))], 1u);
     }
     __syncthreads();
-    {   // kCopies / 4 lanes per bin
+    if (threadIdx.x < 64 * kCopies) {   // kCopies / 4 lanes per bin
       const uint4 v = *(const uint4*)&bins[threadIdx.x * 4];
       *(uint4*)&bins[threadIdx.x * 4] = make_uint4(0, 0, 0, 0);
       uint32_t n = v.x + v.y + v.z + v.w;
@@ -602,7 +603,7 @@ uint64_t evict_counts_bytes(const CacheView& c) { return ((uint64_t)c.n_seqs * c
 
 uint64_t evict_moves_bytes(const CacheView& c, uint32_t keep) { return ((uint64_t)c.n_seqs * c.kv_heads * std::min(keep, c.capacity) * sizeof(uint2) + 255) / 256 * 256; }
 // A slice has as few strides as let all workgroups be on the GPU together (two per compute unit): 8 lists of 20000 slots 28 us with one stride
-// and 32 with two, 128 of them 80 and 68.
+// and 32 with two, 128 of them 74 and 69, of 32768 95 and 81.
 uint32_t evict_strides(const CacheView& c) {
   const uint64_t pieces = (uint64_t)c.n_seqs * c.kv_heads * ((c.capacity + 4 * kSliceThreads - 1) / (4 * kSliceThreads));
   return pieces <= kSlicesTogether ? 1 : pieces <= 2 * kSlicesTogether ? 2 : 4;
@@ -649,8 +650,9 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
   e.above = e.histograms + 2 * n_lists * e.slices * 256;
   const bool int8 = cache->type == TQ_INT8;
   const uint32_t most = std::min(keep, c.capacity - keep);   // tokens to move, of a list
-  // Few of them are moved by the workgroup that has found them, unless others may still have to read the lengths that it writes.
-  const bool moves = !e.slices && e.lengths_out != e.lengths && most <= kMovesInSelect;
+  // Few of them are moved by the workgroup that has found them, unless others may still have to read the lengths that it writes: 8 lists of
+  // 1152 slots, 128 moves 6.7 us in place of 8.7, 400 moves 10.4 in place of 9.0; 128 lists of them 8.6 in place of 12.6, 13.2 in place of 17.8.
+  const bool moves = !e.slices && e.lengths_out != e.lengths && most <= (c.n_seqs * c.kv_heads < kManyLists ? kMovesInSelect / 2 : kMovesInSelect);
   const dim3 lists(c.kv_heads, c.n_seqs);
   hipStream_t st = (hipStream_t)stream;
   auto select = [&](auto threads, auto strides) {
@@ -659,7 +661,7 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
     if (moves) int8 ? go(k_evict_select<T, S, true, true>) : go(k_evict_select<T, S, false, true>);
     else go(k_evict_select<T, S, false, false>);
   };
-  // As many threads as a list has fours of slots, as far as there are: a barrier among fewer wavefronts is shorter (1152 slots: 512 threads 7.7 us, 1024 9.4).
+  // As many threads as a list has fours of slots, as far as there are: a barrier among fewer wavefronts is shorter (8 lists of 1152 slots: 512 threads 7.7 us, 1024 9.4).
   if (c.capacity <= 1024) select(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 2048) select(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 4096) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
