@@ -665,6 +665,7 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
   if (c.capacity <= 1024) select(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 2048) select(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 4096) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+  else if (c.capacity <= 8192) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());   // (with four strides, two of them empty: 8000 slots 16.4 us in place of 12.5)
   else if (!e.slices) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
   else
     for (uint32_t round = 0; round <= 4; ++round) {
