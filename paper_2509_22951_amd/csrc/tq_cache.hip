@@ -6,7 +6,12 @@
 namespace tq {
 namespace {
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 256, kMostItems = 6;
+
+// (the memory unit takes 16 bytes from any 4-byte boundary, 8 from any 2-byte one)
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 struct AppendView {
   const float *q, *k, *v;
@@ -14,43 +19,32 @@ struct AppendView {
   const int32_t *seqs, *slots, *positions;
   const float *cos, *sin;
   uint64_t q_stride, k_stride, v_stride, q_out_stride;
-  uint32_t heads, rotary_dim, n_positions, adjacent;
-  bool by4, angles_by4;   // every row starts on 16 bytes, and those of the angles
+  uint32_t heads, rotary_dim, n_positions, adjacent, items;
 };
 
-// One workgroup takes ITEMS * kAppendThreads / LANES of the heads (query, key and value heads in this order) of one row; LANES lanes of a
-// wavefront take a head, 4 values each, and ITEMS heads one after another, all of them requested ahead.  A pair of the halves
+// One workgroup takes a.items * kAppendThreads / LANES of the heads (query, key and value heads in this order) of one row; LANES lanes of a
+// wavefront take a head, 4 values each, and a.items heads one after another, all of them requested ahead.  A pair of the halves
 // rotation lies rotary_dim / 2 values apart: its other half comes from another lane of the same group, so a wavefront has read all
 // of a head before it writes any (q_out may be q), and 8 bits' absmax is a maximum over the group.
 //
 // Bound: device memory for prompts; for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
-template <int LANES, int ITEMS, bool INT8, bool Q16>
+template <int LANES, bool INT8, bool Q16>
 __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
   typedef __attribute__((address_space(4))) const int32_t constant_i32;
   constexpr uint32_t kGroups = kAppendThreads / LANES;
   const uint32_t r = blockIdx.x, D = c.head_dim;
-  const uint32_t t = threadIdx.x % LANES, i = 4 * t, first_head = blockIdx.y * (ITEMS * kGroups) + threadIdx.x / LANES;
+  const uint32_t t = threadIdx.x % LANES, i = 4 * t, first_head = blockIdx.y * (a.items * kGroups) + threadIdx.x / LANES;
   const uint32_t n_heads = a.heads + 2 * c.kv_heads;
   const int32_t seq = a.seqs ? ((constant_i32*)a.seqs)[r] : (int32_t)r, slot = ((constant_i32*)a.slots)[r], pos = a.positions ? ((constant_i32*)a.positions)[r] : slot;
   const bool there = (uint32_t)seq < c.n_seqs && (uint32_t)slot < c.capacity && (a.rotary_dim == 0 || (uint32_t)pos < a.n_positions);
-  float x[ITEMS][4];
+  f32x4_any x[kMostItems];   // requested ahead of what decides whether the row is there
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k) {
-    const uint32_t head = first_head + k * kGroups;
+  for (int k = 0; k < kMostItems; ++k) {
+    if (k && k >= (int)a.items) break;
+    const uint32_t head = first_head + k * kGroups < n_heads ? first_head + k * kGroups : 0;
     const bool is_q = head < a.heads, is_v = head >= a.heads + c.kv_heads;
     const uint32_t h = is_q ? head : is_v ? head - a.heads - c.kv_heads : head - a.heads;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[k][j] = 0.f;
-    if (head < n_heads && i < D && there) {
-      const float* from = (is_q ? a.q + r * a.q_stride : is_v ? a.v + r * a.v_stride : a.k + r * a.k_stride) + h * D + i;
-      if (a.by4) {
-        const float4 d = *(const float4*)from;
-        x[k][0] = d.x, x[k][1] = d.y, x[k][2] = d.z, x[k][3] = d.w;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[k][j] = from[j];
-      }
-    }
+    x[k] = *(const f32x4_any*)((is_q ? a.q + r * a.q_stride : is_v ? a.v + r * a.v_stride : a.k + r * a.k_stride) + h * D + (i < D ? i : 0));
   }
   uint32_t page = c.n_pages;
   if (there) page = (uint32_t)((constant_i32*)c.tables)[(uint64_t)(uint32_t)seq * c.table_stride + ((uint32_t)slot >> c.page_shift)];
@@ -61,21 +55,22 @@ __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, Ap
     const uint64_t at = (uint64_t)(uint32_t)pos * half + (a.adjacent ? i / 2 : second ? i - half : i);
     if (a.adjacent) {
       cs[0] = a.cos[at], cs[1] = a.cos[at + 1], sn[0] = a.sin[at], sn[1] = a.sin[at + 1];
-    } else if (a.angles_by4) {
-      const float4 d = *(const float4*)(a.cos + at), e = *(const float4*)(a.sin + at);
-      cs[0] = d.x, cs[1] = d.y, cs[2] = d.z, cs[3] = d.w, sn[0] = e.x, sn[1] = e.y, sn[2] = e.z, sn[3] = e.w;
     } else {
+      const f32x4_any d = *(const f32x4_any*)(a.cos + at), e = *(const f32x4_any*)(a.sin + at);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) cs[j] = a.cos[at + j], sn[j] = a.sin[at + j];
+      for (int j = 0; j < 4; ++j) cs[j] = d[j], sn[j] = e[j];
     }
   }
   const int other = ((int)(threadIdx.x & 63) + (second ? -(int)(half / 4) : (int)(half / 4))) & 63;
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k) {
+  for (int k = 0; k < kMostItems; ++k) {
+    if (k && k >= (int)a.items) break;
     const uint32_t head = first_head + k * kGroups;
     const bool is_q = head < a.heads, is_v = head >= a.heads + c.kv_heads, mine = head < n_heads && i < D;
     const uint32_t h = is_q ? head : is_v ? head - a.heads - c.kv_heads : head - a.heads;
-    float (&y)[4] = x[k];
+    float y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = mine && there ? x[k][j] : 0.f;
     if (a.adjacent) {
       if (turned && !is_v) {
         const float z[4] = {y[0] * cs[0] - y[1] * sn[0], y[0] * sn[0] + y[1] * cs[0], y[2] * cs[1] - y[3] * sn[1], y[2] * sn[1] + y[3] * cs[1]};
@@ -104,12 +99,10 @@ __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, Ap
       if constexpr (Q16) {
         uint16_t* to = (uint16_t*)a.q_out + at;
         const uint32_t lo = pack_bf16(y[0], y[1]), hi = pack_bf16(y[2], y[3]);
-        if (a.by4) *(uint2*)to = make_uint2(lo, hi);
-        else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
+        *(u32x2_any*)to = u32x2_any{lo, hi};
       } else {
         float* to = (float*)a.q_out + at;
-        if (a.by4) *(float4*)to = make_float4(y[0], y[1], y[2], y[3]);
-        else to[0] = y[0], to[1] = y[1], to[2] = y[2], to[3] = y[3];
+        *(f32x4_any*)to = f32x4_any{y[0], y[1], y[2], y[3]};
       }
       continue;
     }
@@ -148,7 +141,7 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   const uint64_t q_row = (uint64_t)a->heads * c.head_dim, kv_row = (uint64_t)c.kv_heads * c.head_dim;
   AppendView v{a->q, a->k, a->v, a->q_out, a->seqs, a->slots, a->positions, a->cos, a->sin, a->q_stride ? a->q_stride : q_row,
                a->k_stride ? a->k_stride : kv_row, a->v_stride ? a->v_stride : kv_row, a->q_out_stride ? a->q_out_stride : q_row,
-               a->heads, a->rotary_dim, a->n_positions, a->pairing, false, aligned_to(a->cos, 16) && aligned_to(a->sin, 16)};
+               a->heads, a->rotary_dim, a->n_positions, a->pairing};
   if (v.q_stride < q_row || v.k_stride < kv_row || v.v_stride < kv_row || v.q_out_stride < q_row)
     return refuse(TQ_E_INVALID_ARG, who + ": a stride is smaller than a row");
   const bool q16 = a->q_out_type == TQ_BF16;
@@ -157,22 +150,20 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   if (!aligned_to(a->q, 4) || !aligned_to(a->k, 4) || !aligned_to(a->v, 4) || !aligned_to(a->q_out, q16 ? 2 : 4) || !aligned_to(a->seqs, 4) ||
       !aligned_to(a->slots, 4) || !aligned_to(a->positions, 4) || !aligned_to(a->cos, 4) || !aligned_to(a->sin, 4))
     return refuse(TQ_E_INVALID_ARG, who + ": a pointer is not aligned to its type");
-  auto fours = [](const void* p, uint64_t stride, size_t size) { return stride % 4 == 0 && aligned_to(p, 4 * size); };
-  v.by4 = fours(v.q, v.q_stride, 4) && fours(v.k, v.k_stride, 4) && fours(v.v, v.v_stride, 4) && fours(v.q_out, v.q_out_stride, q16 ? 2 : 4);
   const bool int8 = cache->type == TQ_INT8;
   const uint32_t lanes = c.head_dim <= 16 ? 4 : c.head_dim <= 32 ? 8 : c.head_dim <= 64 ? 16 : c.head_dim <= 128 ? 32 : 64;
-  const uint32_t n_heads = a->heads + 2 * c.kv_heads, groups = kAppendThreads / lanes;
-  // Few rows: a head per group of lanes, all of the GPU that there is work for.  Many: four per group, so that their loads are on
-  // their way together (8192 rows of 40 heads of 128 in 8 bits: 120 us with one, 72 with four).
-  const uint32_t one = (n_heads + groups - 1) / groups, four = (n_heads + 4 * groups - 1) / (4 * groups);
-  const bool many = (uint64_t)a->rows * one > 2048;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, many ? four : one), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v); };
-  auto pick = [&](auto n, auto items) {
-    constexpr int L = decltype(n)::value, I = decltype(items)::value;
-    if (int8) q16 ? go(k_cache_append<L, I, true, true>) : go(k_cache_append<L, I, true, false>);
-    else q16 ? go(k_cache_append<L, I, false, true>) : go(k_cache_append<L, I, false, false>);
+  const uint32_t n_heads = a->heads + 2 * c.kv_heads, groups = kAppendThreads / lanes, rounds = (n_heads + groups - 1) / groups;
+  // A head per group of lanes, until there are many more workgroups than the GPU holds; then several per group, so that their loads are on their way
+  // together, and as evenly as they divide, since a group without a head waits with the others (40 heads of 128 in 8 bits: 8192 rows 75 us with one, 68 with
+  // four and one in turn, 62 with five; 1024 rows 12.6 with one, 13.7 with five).
+  const uint32_t most = (uint64_t)a->rows * rounds > 16384 ? kMostItems : 1, parts = (rounds + most - 1) / most;
+  v.items = (rounds + parts - 1) / parts;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, parts), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v); };
+  auto of = [&](auto n) {
+    constexpr int L = decltype(n)::value;
+    if (int8) q16 ? go(k_cache_append<L, true, true>) : go(k_cache_append<L, true, false>);
+    else q16 ? go(k_cache_append<L, false, true>) : go(k_cache_append<L, false, false>);
   };
-  auto of = [&](auto n) { many ? pick(n, std::integral_constant<int, 4>()) : pick(n, std::integral_constant<int, 1>()); };
   if (lanes == 4) of(std::integral_constant<int, 4>());
   else if (lanes == 8) of(std::integral_constant<int, 8>());
   else if (lanes == 16) of(std::integral_constant<int, 16>());
@@ -205,8 +196,6 @@ constexpr uint32_t kSlicesTogether = 512;      // workgroups
 constexpr uint32_t kListInWorkgroup = 16384;   // slots: one workgroup takes 8 lists of 16384 in 20 us, slices 29; of 20000 it took 44, slices 28
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // (16 bytes from any 4-byte boundary are one load)
-typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Numbers that compare as the scores do: NaN lowest, the two zeros equal, protected tokens above +infinity.
 __device__ __forceinline__ uint32_t rank_of(float score, bool is_protected) {
