@@ -20,6 +20,7 @@ namespace {
 constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
 constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;                       // workgroups of a launch; units of one; parts that are joined at a time
+constexpr uint32_t kMostAligned = 16;   // units of a share
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttendView {
@@ -85,6 +86,17 @@ __device__ __forceinline__ uint32_t prefix_sum(uint32_t v) {
   return v;
 }
 
+// The largest of 64 lanes, in the last one.
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+  return v;
+}
+
 // All (row, chunk, unit of kUnit tokens) in this order are one line, cut into equal shares, one per workgroup: whatever the
 // lengths, every workgroup has as much to do.  A (row, chunk) that lies in one share is finished there; of one that is cut every
 // workgroup leaves its maximum, total and weighted sum in memory and counts itself in, and the last one joins them, in the order
@@ -112,14 +124,29 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     if (first + lane < a.rows) lane_length = row_length(c, a, first + lane, &lane_seq);
     return prefix_sum(first + lane < a.rows ? units_of(lane_length) : 0u);
   };
-  uint32_t upto = 0, all = 0;
+  uint32_t upto = 0, all = 0, longest = 0;   // longest: units of a row
   for (uint32_t first = (a.rows - 1) & ~63u;; first -= 64) {   // (the first rows last: they stay in the lanes)
     upto = look_at(first);
     all += scalar(__shfl(upto, 63));
+    longest = max(longest, units_of((uint32_t)__builtin_amdgcn_readlane((int)max_of_lanes(first + lane < a.rows ? lane_length : 0u), 63)));
     if (first == 0) break;
   }
   all *= a.chunks;
-  const uint32_t share = max(kMinShare, (all + gridDim.x - 1) / gridDim.x);
+  const uint32_t even = max(kMinShare, (all + gridDim.x - 1) / gridDim.x);
+  uint32_t share = even, quantum = 1;
+  if (a.rows <= 64 && even <= kMostAligned && longest > 1 && (even > 1 || (DIM <= 64 && longest == 2))) {
+    const uint32_t units = lane < a.rows ? units_of(lane_length) : 0;
+    auto attempt = [&](uint32_t q, uint32_t most) {
+      const uint32_t quanta = prefix_sum((uint32_t)(((float)(units + q - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)q)));   // (exact: far fewer than 2^20 units)
+      const uint32_t total = scalar(__shfl(quanta, 63)) * a.chunks, mine = total <= gridDim.x ? q : (total + gridDim.x - 1) / gridDim.x * q;
+      if (mine > most) return false;
+      upto = quanta * q, all = total * q, share = mine, quantum = q;
+      return true;
+    };
+    bool done = longest <= (DIM <= 64 ? 4 : 3) && attempt(longest, even + (even > 1 ? 2 : 1));
+    const uint32_t most = even + (even > 4 ? even / 4 : even / 2);
+    for (uint32_t q = even; q <= most && !done; ++q) done = attempt(q, most);
+  }
   uint32_t pos = blockIdx.x * share;
   uint32_t stop = min(pos + share, all);
   if (pos >= stop) return;
@@ -159,7 +186,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     s.r = r;
     const uint32_t length = (uint32_t)__builtin_amdgcn_readlane((int)lane_length, r & 63);
     s.seq = (uint32_t)__builtin_amdgcn_readlane((int)lane_seq, r & 63);
-    s.units = units_of(length);
+    const uint32_t units = units_of(length);
+    s.units = quantum == 1 ? units : (uint32_t)(((float)(units + quantum - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)quantum)) * quantum;
     s.pair = (pos - row_first) / s.units;
     s.pair_first = row_first + s.pair * s.units;
     s.kv = s.pair / per_kv;
@@ -168,7 +196,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     s.n_heads = min((uint32_t)kHeads, a.group - chunk * kHeads);
     s.begin = unit * kUnit;
     s.end = min(length, unit_end * kUnit);
-    s.rounds = unit_end - unit;
+    s.rounds = min(unit_end, units) - unit;
     pos += unit_end - unit;
     if (pos == row_first + s.units * a.chunks) {
       row_first = pos;
