@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
-constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;                       // workgroups of a launch; units of one; parts that are joined at a time
+constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;   // workgroups of a launch (one per compute unit); units of one; parts that are joined at a time
 constexpr uint32_t kMostAligned = 16;   // units of a share
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -97,8 +97,12 @@ __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
   return v;
 }
 
+// Bound: reading the cache.  16 x 32768 tokens, 8 heads of 64 in bf16: 190 us, 5.65 TB/s; 1 x 131072 of 128: 96, 5.6; in 8 bits 16 x 32768 of 128: 192, 5.7, with the
+// vector units at about 90 % (conversion to bf16); 4 x 32768, 4 heads of 256: 99, 5.4.  Few tokens: launch, lengths, page table, keys and values, join, 5.7 us for 200 tokens.
+//
 // All (row, chunk, unit of kUnit tokens) in this order are one line, cut into equal shares, one per workgroup: whatever the
-// lengths, every workgroup has as much to do.  A (row, chunk) that lies in one share is finished there; of one that is cut every
+// lengths, every workgroup has as much to do.  Eight wavefronts (one workgroup per compute unit) hold as much on its way as the memory needs: twelve and sixteen,
+// or two workgroups per unit, leave too few registers for a tile ahead (16 x 16384 of 128: 188, 198, 281, 191 us).  A (row, chunk) that lies in one share is finished there; of one that is cut every
 // workgroup leaves its maximum, total and weighted sum in memory and counts itself in, and the last one joins them, in the order
 // of the line; more than kCluster parts are joined by clusters first.  Nobody waits for anybody.
 //
@@ -134,6 +138,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   all *= a.chunks;
   const uint32_t even = max(kMinShare, (all + gridDim.x - 1) / gridDim.x);
   uint32_t share = even, quantum = 1;
+  // Where the shares are small, a share that has the end of one row and the start of another is joined twice, one after the other, and a row is in
+  // more parts than it need be.  So every (row, chunk) is rounded up to whole quanta, and a share is whole quanta: the longest row's units, and no row is
+  // cut, or the fewest from an even share on with which every part has a workgroup.  A compute unit alone draws 41 bytes per ns, among all of them 24, so that
+  // shares that differ by a half do not take longer by as much; a join takes about 4 us.  Of 64 dims, 16 x 700 tokens: 15.3 -> 11.1 us, 16 ragged ones up to 1000
+  // 14.6 -> 12.2; of 128, 16 x 1250 24.9 -> 22.8, 2 x 20000 37.8 -> 36.0; where rows were cut evenly before, 0.1 to 0.4 us more.  Longer shares take their next row's
+  // loads while they join, and are cut anywhere.
   if (a.rows <= 64 && even <= kMostAligned && longest > 1 && (even > 1 || (DIM <= 64 && longest == 2))) {
     const uint32_t units = lane < a.rows ? units_of(lane_length) : 0;
     auto attempt = [&](uint32_t q, uint32_t most) {
@@ -517,7 +527,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   }
 }
 
-// Adds the weights of all rows of a sequence to its slots' scores, rows and heads in order; four slots a thread.
+// Adds the weights of all rows of a sequence to its slots' scores, rows and heads in order; four slots a thread.  Bound: a launch and, for long
+// lists, reading the logits (8 x 8179 tokens of 32 heads, 8 MB: 4.9 us).
 __global__ __launch_bounds__(256) void k_attend_scores(CacheView c, AttendView a) {
   const uint32_t slot = (blockIdx.x * 256 + threadIdx.x) * 4, kv = blockIdx.y, s = blockIdx.z;
   if (slot >= c.capacity) return;   // (a multiple of 16)

@@ -27,7 +27,7 @@ struct AppendView {
 // rotation lies rotary_dim / 2 values apart: its other half comes from another lane of the same group, so a wavefront has read all
 // of a head before it writes any (q_out may be q), and 8 bits' absmax is a maximum over the group.
 //
-// Bound: device memory for prompts; for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
+// Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits: 62 us); for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
 template <int LANES, bool INT8, bool Q16>
 __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
   typedef __attribute__((address_space(4))) const int32_t constant_i32;
@@ -273,7 +273,8 @@ __device__ __forceinline__ Bin find_bin(const uint32_t* sums, uint32_t left) {  
 }
 
 // Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., kAhead of them
-// together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.
+// together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.  Bound: memory, for many tokens (16 x 8 lists, 4096
+// rows of 256 bytes of keys and of values each: 120 us, 4.5 TB/s read and written).
 template <bool INT8>
 __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, const uint32_t* slots_to, const uint32_t* slots_from, uint32_t n,
                                             uint32_t first, uint32_t step) {
@@ -330,7 +331,8 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 // limit, the free slots below `keep` and the kept ones above.
 //
 // A workgroup per list; a thread has 4 neighbouring slots of every kStride, and their ranks in registers.  Scores share few exponents, so that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there
-// are several copies of it.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
+// are several copies of it.  Bound: one workgroup's chain of loads, four rounds of histogram and look, numbering: 8 lists of 1152 slots 6.7 us with their
+// 128 moves, of 16384 18.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
 template <int THREADS, int STRIDES, bool INT8, bool MOVES>
 __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView e) {
   constexpr int kWaves = THREADS / 64, kCopies = kWaves < 8 ? kWaves : 8;   // (a copy per lane costs more to clear and add up than it saves: 16384 slots 19.9 -> 22.8 us)

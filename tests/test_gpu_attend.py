@@ -239,6 +239,25 @@ def test_many_rows_and_another_stream():
     close(out, want, p)
 
 
+@pytest.mark.parametrize("kind,track", [("bf16", False), ("int8", True)])
+@pytest.mark.parametrize("rows,longest,heads,kv_heads,dim", [
+    (16, 500, 8, 8, 64), (16, 700, 16, 8, 64), (17, 1000, 8, 8, 64), (40, 1000, 20, 10, 64), (16, 700, 8, 8, 128), (64, 760, 8, 8, 96), (33, 400, 12, 6, 256),
+    (16, 1270, 8, 8, 64), (4, 5100, 34, 2, 64), (11, 2900, 8, 8, 128), (2, 20000, 3, 3, 64), (65, 1100, 4, 4, 64)])
+def test_how_rows_are_cut(rows, longest, heads, kv_heads, dim, kind, track):
+    """Rows that are as long as each other, spread, and with one of them far longer: not cut, cut at whole shares, cut anywhere; twice with one workspace."""
+    p = Paged(rows, -(-longest // 16), kv_heads=kv_heads, dim=dim, kind=kind, marks=track, seed=rows)
+    q = queries(rows, heads, dim, longest)
+    for lengths in ([longest] * rows, [(r * 619 + 5) % (longest + 1) for r in range(rows)], [longest if r == rows // 2 else r for r in range(rows)]):
+        lengths = ints(lengths)
+        call, out = attend_call(p.describe(), p, q, lengths, accumulate=track)
+        want = attend_reference(p, q, lengths)[0]
+        for _ in range(2):
+            out.fill_(float("nan"))
+            call.launch(stream())
+            torch.cuda.synchronize()
+            close(out, want, p)
+
+
 @pytest.mark.parametrize("heads,kv_heads,dim,rows", [(8, 1, 256, 1), (5, 1, 128, 2), (2, 1, 64, 1), (16, 1, 64, 3)])
 def test_rows_that_many_workgroups_share(heads, kv_heads, dim, rows):
     """Up to 160 parts of one row: joined by clusters first; rows that begin and end inside a cluster."""
