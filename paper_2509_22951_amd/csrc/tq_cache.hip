@@ -189,7 +189,7 @@ struct EvictView {
   uint2* found;            // [round][seq][head]: upper bits of the limit, tokens with these bits that stay
 };
 
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 256, kMoveAhead = 2;   // (64 lists, 3000 rows of 128 bytes each: 25.6 us; with four together 26.1, one 28.6)
 constexpr uint32_t kMovesInSelect = 512;   // tokens of a list, half of it with fewer than kManyLists lists
 constexpr uint32_t kManyLists = 64;
 constexpr uint32_t kSlicesTogether = 512;      // workgroups
@@ -272,49 +272,57 @@ __device__ __forceinline__ Bin find_bin(const uint32_t* sums, uint32_t left) {  
   return {255 - (uint32_t)__builtin_amdgcn_readlane((int)b, one), (uint32_t)__builtin_amdgcn_readlane((int)over, one), (uint32_t)__builtin_amdgcn_readlane((int)in, one)};
 }
 
-// Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., kAhead of them
+// Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., AHEAD of them
 // together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.  Bound: memory, for many tokens (16 x 8 lists, 4096
 // rows of 256 bytes of keys and of values each: 120 us, 4.5 TB/s read and written).
-template <bool INT8>
+template <bool INT8, uint32_t AHEAD>
 __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, const uint32_t* slots_to, const uint32_t* slots_from, uint32_t n,
                                             uint32_t first, uint32_t step) {
-  constexpr uint32_t kAhead = 4;
-  const uint32_t list = s * c.kv_heads + h, lane = threadIdx.x % 16, bytes = c.head_dim * (INT8 ? 1 : 2), mask = (1u << c.page_shift) - 1;
+  const uint32_t list = s * c.kv_heads + h, lane = threadIdx.x % 16, pieces = c.head_dim * (INT8 ? 1 : 2) / 16, mask = (1u << c.page_shift) - 1;
   const uint64_t row = (uint64_t)list * c.capacity, size = INT8 ? 1 : 2;
   const int32_t* table = c.tables + (uint64_t)s * c.table_stride;
-  for (uint32_t m = first; m < n; m += kAhead * step) {
-    uint32_t to[kAhead], of[kAhead], to_page[kAhead], of_page[kAhead];
-    bool there[kAhead];
+  for (uint32_t m = first; m < n; m += AHEAD * step) {
+    uint32_t to[AHEAD], of[AHEAD], to_page[AHEAD], of_page[AHEAD];
+    bool there[AHEAD];
 #pragma unroll
-    for (uint32_t i = 0; i < kAhead; ++i) {
+    for (uint32_t i = 0; i < AHEAD; ++i) {
       const uint32_t at = min(m + i * step, n - 1);
       to[i] = min(slots_to[at], c.capacity - 1), of[i] = min(slots_from[e.slices ? n - 1 - at : at], c.capacity - 1);   // (lengths that change under the call)
     }
 #pragma unroll
-    for (uint32_t i = 0; i < kAhead; ++i) {
+    for (uint32_t i = 0; i < AHEAD; ++i) {
       to_page[i] = (uint32_t)table[to[i] >> c.page_shift], of_page[i] = (uint32_t)table[of[i] >> c.page_shift];
       there[i] = m + i * step < n && to_page[i] < c.n_pages && of_page[i] < c.n_pages;
     }
     auto place = [&](uint32_t page, uint32_t slot) { return size * (page * c.page_stride + h * c.head_stride + (slot & mask) * c.slot_stride); };
     auto mark = [&](uint32_t page, uint32_t slot) { return (((uint64_t)page * c.kv_heads + h) << c.page_shift) + (slot & mask); };
-    for (uint32_t b = lane * 16; b < bytes; b += 256) {
-      u32x4 k[kAhead], v[kAhead];
+    // a lane's pieces of 16 bytes: of the key's, then of the value's
+    for (uint32_t p0 = lane; p0 - lane < 2 * pieces; p0 += 32) {
+      u32x4 x[AHEAD][2];
+      const bool more = p0 - lane + 16 < 2 * pieces;
+      auto piece = [&](uint32_t p) { return p < pieces ? c.k + 16 * p : c.v + 16 * (p - pieces); };
+      auto load = [&](int half) {
+        const uint32_t p = p0 + 16 * half;
+        const char* from = piece(p < 2 * pieces ? p : 0);
 #pragma unroll
-      for (uint32_t i = 0; i < kAhead; ++i) {   // (in place of a token that is not moved, one of page 0)
-        const uint64_t at = place(there[i] ? of_page[i] : 0, of[i]) + b;
-        k[i] = __builtin_nontemporal_load((const u32x4*)(c.k + at)), v[i] = __builtin_nontemporal_load((const u32x4*)(c.v + at));
-      }
+        for (uint32_t i = 0; i < AHEAD; ++i) x[i][half] = __builtin_nontemporal_load((const u32x4*)(from + place(there[i] ? of_page[i] : 0, of[i])));   // (in place of a token that is not moved, one of page 0)
+      };
+      auto store = [&](int half) {
+        const uint32_t p = p0 + 16 * half;
+        char* to_piece = piece(p);
 #pragma unroll
-      for (uint32_t i = 0; i < kAhead; ++i)
-        if (there[i]) {
-          const uint64_t at = place(to_page[i], to[i]) + b;
-          __builtin_nontemporal_store(k[i], (u32x4*)(c.k + at)), __builtin_nontemporal_store(v[i], (u32x4*)(c.v + at));
-        }
+        for (uint32_t i = 0; i < AHEAD; ++i)
+          if (there[i] && p < 2 * pieces) __builtin_nontemporal_store(x[i][half], (u32x4*)(to_piece + place(to_page[i], to[i])));
+      };
+      load(0);
+      if (more) load(1);
+      store(0);
+      if (more) store(1);
     }
-    if (lane < kAhead && m + lane * step < n) {   // a lane per token
+    if (lane < AHEAD && m + lane * step < n) {   // a lane per token
       uint32_t t = to[0], f = of[0], tp = to_page[0], fp = of_page[0];
 #pragma unroll
-      for (uint32_t i = 1; i < kAhead; ++i)
+      for (uint32_t i = 1; i < AHEAD; ++i)
         if (lane == i) t = to[i], f = of[i], tp = to_page[i], fp = of_page[i];
       e.scores_out[row + t] = c.scores[row + f];
       if (c.positions) e.positions_out[row + t] = c.positions[row + f];
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView
   }
   if constexpr (MOVES) {
     __syncthreads();
-    move_tokens<INT8>(c, e, s, h, few[0], few[1], moves, threadIdx.x / 16, THREADS / 16);
+    move_tokens<INT8, 4>(c, e, s, h, few[0], few[1], moves, threadIdx.x / 16, THREADS / 16);
   } else if (threadIdx.x == 0) {
     e.counts[list] = moves;
   }
@@ -587,7 +595,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(CacheView c, EvictV
     e.lengths_out[s] = min(length, (int32_t)min(e.keep, 0x7FFFFFFFu));
   }
   const uint32_t list = s * c.kv_heads + h;
-  move_tokens<INT8>(c, e, s, h, e.to + (uint64_t)list * e.keep, e.from + (uint64_t)list * e.keep, e.counts[list], (blockIdx.x * kMoveThreads + threadIdx.x) / 16, gridDim.x * (kMoveThreads / 16));
+  move_tokens<INT8, kMoveAhead>(c, e, s, h, e.to + (uint64_t)list * e.keep, e.from + (uint64_t)list * e.keep, e.counts[list], (blockIdx.x * kMoveThreads + threadIdx.x) / 16, gridDim.x * (kMoveThreads / 16));
 }
 
 uint64_t evict_counts_bytes(const CacheView& c) { return ((uint64_t)c.n_seqs * c.kv_heads * 4 + 255) / 256 * 256; }
@@ -665,7 +673,7 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
       strides == 1 ? go(k_evict_slice<1>) : strides == 2 ? go(k_evict_slice<2>) : go(k_evict_slice<4>);
     }
   if (!moves) {
-    const uint32_t groups = kMoveThreads / 16;
+    const uint32_t groups = kMoveThreads / 16 * kMoveAhead;
     const uint32_t parts = std::max(1u, std::min((most + groups - 1) / groups, std::max(1u, 4096u / (c.kv_heads * c.n_seqs))));
     const dim3 grid(parts, c.kv_heads, c.n_seqs);
     if (int8) hipLaunchKernelGGL(k_evict_move<true>, grid, dim3(kMoveThreads), 0, st, c, e);
