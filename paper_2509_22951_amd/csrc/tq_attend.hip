@@ -20,6 +20,7 @@ namespace {
 constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
 constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;   // workgroups of a launch (one per compute unit); units of one; parts that are joined at a time
+constexpr uint64_t kPassing = 8 << 20;   // bytes of keys and values
 constexpr uint32_t kMostAligned = 16;   // units of a share
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -57,19 +58,24 @@ struct Tile {
   float4 ks[2], vs[2];
 };
 
-template <int WORDS>
+// Where loads that pass the caches by are faster: no byte is loaded twice, and a value's bytes in a lane are one load.  16 x 16384 tokens of 128 dims 187 -> 170 us,
+// 16 x 32768 of 64 189 -> 172, in 8 bits of 128 200 -> 187; but of 256 dims in bf16 (two loads a lane, from the same lines) 8 x 1024 19 -> 22, of 96 (lanes that repeat
+// others') 2 x 50000 37 -> 42, of 64 in 8 bits no gain.
+template <int DIM, bool INT8>
+constexpr bool kPasses = DIM == 128 || DIM == (INT8 ? 256 : 64);
+
+template <int WORDS, bool PASSES>
 __device__ __forceinline__ void load_words(uint32_t* to, const char* from) {
-  if constexpr (WORDS % 4 == 0) {
+  constexpr int kWords = WORDS % 4 ? WORDS : 4;
+  typedef uint32_t words __attribute__((ext_vector_type(kWords)));
 #pragma unroll
-    for (int w = 0; w < WORDS; w += 4) {
-      const uint4 d = *(const uint4*)(from + 4 * w);
-      to[w] = d.x, to[w + 1] = d.y, to[w + 2] = d.z, to[w + 3] = d.w;
-    }
-  } else if constexpr (WORDS == 2) {
-    const uint2 d = *(const uint2*)from;
-    to[0] = d.x, to[1] = d.y;
-  } else {
-    to[0] = *(const uint32_t*)from;
+  for (int w = 0; w < WORDS; w += kWords) {
+    const words* at = (const words*)(from + 4 * w);
+    words d;
+    if constexpr (PASSES) d = __builtin_nontemporal_load(at);
+    else d = *at;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) to[w + i] = kWords == 1 ? *(const uint32_t*)&d : d[i];
   }
 }
 
@@ -111,7 +117,7 @@ __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
 // them are requested without a condition, keys ahead of values, and nothing else that is loaded is left unused: only then do the
 // compiler's waits count the loads behind those they are for.  (In place of a tile that is not there all lanes read one word of
 // the last one, and a page that is not there is read as page 0 and masked.)
-template <int DIM, bool INT8, bool TRACK>
+template <int DIM, bool INT8, bool TRACK, bool PASSES>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, AttendView a) {
   using T = Tile<DIM, INT8>;
   __shared__ __attribute__((aligned(16))) float lds_sum[kAttendWaves * kHeads * (DIM + 4)];   // [wave][head][DIM + 4]: heads in other banks
@@ -239,20 +245,22 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     return v;
   };
   T x;
-  auto fetch_keys = [&](const Blocks& w, uint32_t lanes) {   // lanes 0: all of them the same words
+  auto fetch_keys = [&](const Blocks& w) {   // (of a block without tokens all lanes read the same words)
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const char* from = c.k + w.at[b];
+      const uint32_t lanes = w.limit[b] ? ~0u : 0u;
 #pragma unroll
-      for (int s = 0; s < T::kLoads; ++s) load_words<4>(&x.k[b][4 * s], from + (kTight ? kSize * first_dim(s) : 0) + offset_of(key_at[kTight ? 0 : s] & lanes));
+      for (int s = 0; s < T::kLoads; ++s) load_words<4, PASSES>(&x.k[b][4 * s], from + (kTight ? kSize * first_dim(s) : 0) + offset_of(key_at[kTight ? 0 : s] & lanes));
       if constexpr (INT8) x.ks[b] = *(const float4*)(c.k_scale + w.mark[b] + 4 * g);
     }
   };
-  auto fetch_values = [&](const Blocks& w, uint32_t lanes) {
+  auto fetch_values = [&](const Blocks& w) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      const uint32_t lanes = w.limit[b] ? ~0u : 0u;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_words<T::kValWords>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + offset_of(val_at & lanes));
+      for (int j = 0; j < 4; ++j) load_words<T::kValWords, PASSES>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + offset_of(val_at & lanes));
       if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
     }
   };
@@ -271,9 +279,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   fetch_q(s);
   Blocks now = blocks_of(s, 0);
   __builtin_amdgcn_sched_barrier(0);   // keys ahead of values, here too: the waits in the loop go by the worst order there is
-  fetch_keys(now, ~0u);
+  fetch_keys(now);
   __builtin_amdgcn_sched_barrier(0);
-  fetch_values(now, ~0u);
+  fetch_values(now);
   __builtin_amdgcn_sched_barrier(0);
   for (;;) {
     static_assert(T::kSteps <= kAttendWaves, "a wavefront per step of q");
@@ -304,9 +312,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         next_s = next_segment();
         fetch_q(next_s);
       }
-      const uint32_t lanes = last && !more ? 0u : ~0u;
       Blocks next = now;
-      if (lanes) next = blocks_of(next_s, last ? 0 : round + 1);
+      next.limit[0] = next.limit[1] = 0;
+      if (!last || more) next = blocks_of(next_s, last ? 0 : round + 1);
       asm volatile("" ::: "memory");   // q is read from LDS for every tile: registers are for what is on its way
       f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -328,7 +336,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         if constexpr (INT8) p[i] *= (&x.ks[i / 4].x)[i % 4];
       }
       __builtin_amdgcn_sched_barrier(0);
-      fetch_keys(next, lanes);
+      fetch_keys(next);
       __builtin_amdgcn_sched_barrier(0);
       // Tokens that take no part: their weight is 0, and the bits of their values are masked out, whatever lies there.  (The masks, and not the
       // loaded words, are what the branch changes: a word that it changed would be waited for there.)
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      fetch_values(next, lanes);
+      fetch_values(next);
       __builtin_amdgcn_sched_barrier(0);
       now = next;
       if (last) break;
@@ -595,11 +603,18 @@ int check_attend(const std::string& who, const tq_cache* cache, const tq_attend_
   return TQ_OK;
 }
 
+// passes: keys and values are not kept in the caches.
 template <int DIM>
-void launch_attend(const CacheView& c, const AttendView& a, uint32_t groups, bool int8, bool track, hipStream_t stream) {
+void launch_attend(const CacheView& c, const AttendView& a, uint32_t groups, bool int8, bool track, bool passes, hipStream_t stream) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(kAttendThreads), 0, stream, c, a); };
-  if (int8) track ? go(k_attend<DIM, true, true>) : go(k_attend<DIM, true, false>);
-  else track ? go(k_attend<DIM, false, true>) : go(k_attend<DIM, false, false>);
+  auto of = [&](auto eight) {
+    constexpr bool I = decltype(eight)::value;
+    if constexpr (kPasses<DIM, I>) {
+      if (passes) return track ? go(k_attend<DIM, I, true, true>) : go(k_attend<DIM, I, false, true>);
+    }
+    track ? go(k_attend<DIM, I, true, false>) : go(k_attend<DIM, I, false, false>);
+  };
+  int8 ? of(std::true_type()) : of(std::false_type());
 }
 
 int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
@@ -623,9 +638,13 @@ int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
                      (a->out_stride ? a->out_stride : row) % 4 == 0 && aligned_to(a->out, 8)};
   const bool int8 = cache->type == TQ_INT8;
   hipStream_t s = (hipStream_t)stream;
-  if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, s);
-  else if (c.head_dim <= 128) launch_attend<128>(c, v, l.groups, int8, a->accumulate, s);
-  else launch_attend<256>(c, v, l.groups, int8, a->accumulate, s);
+  // Little may still be in the L2s (200 tokens of 128 dims 7.2 us, passing them by 7.9; 8 x 1000 of 64 10.7 and 10.1), and what several rows of a sequence or several
+  // chunks of query heads read shall stay there (32 heads on 2, 16 x 8000 tokens 44 and 51).
+  const uint64_t bytes = (uint64_t)a->rows * c.kv_heads * c.capacity * c.head_dim * (int8 ? 2 : 4);
+  const bool passes = !a->seqs && l.chunks == c.kv_heads && bytes >= kPassing && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
+  if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, passes, s);
+  else if (c.head_dim <= 128) launch_attend<128>(c, v, l.groups, int8, a->accumulate, passes, s);
+  else launch_attend<256>(c, v, l.groups, int8, a->accumulate, passes, s);
   if (a->accumulate) hipLaunchKernelGGL(k_attend_scores, dim3((c.capacity + 1023) / 1024, c.kv_heads, c.n_seqs), dim3(256), 0, s, c, v);
   return launched("tq_attend");
 }
