@@ -58,11 +58,10 @@ struct Tile {
   float4 ks[2], vs[2];
 };
 
-// Where loads that pass the caches by are faster: no byte is loaded twice, and a value's bytes in a lane are one load.  16 x 16384 tokens of 128 dims 187 -> 170 us,
-// 16 x 32768 of 64 189 -> 172, in 8 bits of 128 200 -> 187; but of 256 dims in bf16 (two loads a lane, from the same lines) 8 x 1024 19 -> 22, of 96 (lanes that repeat
-// others') 2 x 50000 37 -> 42, of 64 in 8 bits no gain.
+// Where loads that pass the caches by are faster: no byte is loaded twice.  16 x 16384 tokens of 128 dims 187 -> 170 us, 16 x 32768 of 64 189 -> 172, in 8 bits of 128
+// 200 -> 187, 4 x 32768 of 256 99 -> 93; but of 96 (lanes that repeat others') 2 x 50000 37 -> 42, and of 64 in 8 bits no gain.
 template <int DIM, bool INT8>
-constexpr bool kPasses = DIM == 128 || DIM == (INT8 ? 256 : 64);
+constexpr bool kPasses = DIM >= 128 || !INT8;
 
 template <int WORDS, bool PASSES>
 __device__ __forceinline__ void load_words(uint32_t* to, const char* from) {
@@ -192,7 +191,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   uint32_t key_at[kOffsets];
 #pragma unroll
   for (uint32_t s = 0; s < kOffsets; ++s) key_at[s] = n * slot_bytes + (kSpan * kSize * s + 16 * g < kSize * D ? kSpan * kSize * s + 16 * g : 0);
-  const uint32_t val_at = 4 * g * slot_bytes + kSize * (n * T::kVals < D ? n * T::kVals : 0);
+  // A lane's dims of a value are neighbours.  Where they are two loads that pass the caches, each has eight neighbours and the second those of the head's
+  // last 128: two from the same lines would read these twice.
+  constexpr bool kApart = PASSES && T::kValWords > 4;
+  constexpr uint32_t kNear = kApart ? T::kVals / 2 : T::kVals;
+  const uint32_t val_at = 4 * g * slot_bytes + kSize * (n * kNear < D ? n * kNear : 0), second_at = kSize * (D - 128);
 
   struct Segment {   // the part of a (row, chunk) that lies in this share
     uint32_t r, seq, kv, first_head, n_heads, pair, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
@@ -260,7 +263,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     for (int b = 0; b < 2; ++b) {
       const uint32_t lanes = w.limit[b] ? ~0u : 0u;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_words<T::kValWords, PASSES>(x.v[4 * b + j], c.v + w.at[b] + j * slot_bytes + offset_of(val_at & lanes));
+      for (int j = 0; j < 4; ++j) {
+        const char* from = c.v + w.at[b] + j * slot_bytes;
+        load_words<kApart ? 4 : T::kValWords, PASSES>(x.v[4 * b + j], from + offset_of(val_at & lanes));
+        if constexpr (kApart) load_words<4, PASSES>(x.v[4 * b + j] + 4, from + second_at + offset_of(val_at & lanes));
+      }
       if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
     }
   };
@@ -401,7 +408,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       if (last) break;
     }
 
-    // join the wavefronts: lane (g, head) holds dims (4 g + j) * kVals + b of the head, halves of p beside each other
+    // join the wavefronts: lane (g, head) holds dims (4 g + j) * kNear + b of the head, halves of p beside each other
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
     if (lane < kHeads) lds_max[wave * kHeads + lane] = top, lds_total[wave * kHeads + lane] = total;
@@ -410,7 +417,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float4 v = make_float4(ror8_sum(o[b][j]), ror8_sum(o[b + 1][j]), ror8_sum(o[b + 2][j]), ror8_sum(o[b + 3][j]));
-        if (part == 0) *(float4*)&lds_sum[(wave * kHeads + head) * (DIM + 4) + (4 * g + j) * T::kVals + b] = v;
+        if (part == 0) *(float4*)&lds_sum[(wave * kHeads + head) * (DIM + 4) + (b < (int)kNear ? 0 : D - 128) + (4 * g + j) * kNear + b % kNear] = v;
       }
     __syncthreads();
     // the workgroups among which this (row, chunk) is cut
@@ -641,7 +648,8 @@ int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
   // Little may still be in the L2s (200 tokens of 128 dims 7.2 us, passing them by 7.9; 8 x 1000 of 64 10.7 and 10.1), and what several rows of a sequence or several
   // chunks of query heads read shall stay there (32 heads on 2, 16 x 8000 tokens 44 and 51).
   const uint64_t bytes = (uint64_t)a->rows * c.kv_heads * c.capacity * c.head_dim * (int8 ? 2 : 4);
-  const bool passes = !a->seqs && l.chunks == c.kv_heads && bytes >= kPassing && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
+  // (256 dims of bf16: 33 MB 19 us and 21, 67 MB 32 and 30.5.)
+  const bool passes = !a->seqs && l.chunks == c.kv_heads && bytes >= (c.head_dim == 256 && !int8 ? 8 * kPassing : kPassing) && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
   if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, passes, s);
   else if (c.head_dim <= 128) launch_attend<128>(c, v, l.groups, int8, a->accumulate, passes, s);
   else launch_attend<256>(c, v, l.groups, int8, a->accumulate, passes, s);
