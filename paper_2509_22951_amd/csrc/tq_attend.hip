@@ -59,7 +59,8 @@ struct Tile {
 };
 
 // Where loads that pass the caches by are faster: no byte is loaded twice.  16 x 16384 tokens of 128 dims 187 -> 170 us, 16 x 32768 of 64 189 -> 172, in 8 bits of 128
-// 200 -> 187, 4 x 32768 of 256 99 -> 93; but of 96 (lanes that repeat others') 2 x 50000 37 -> 42, and of 64 in 8 bits no gain.
+// 200 -> 187, 4 x 32768 of 256 99 -> 93; 1 x 16000 of 96 16.1 -> 15.4; but of 80 and 48, whose rows
+// begin anywhere in a line, 16 x 8000 37 -> 41 and 93 -> 101, and of 64 in 8 bits no gain.
 template <int DIM, bool INT8>
 constexpr bool kPasses = DIM >= 128 || !INT8;
 
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   }
   if (r >= a.rows) return;   // (lengths that change under the call)
 
-  // a lane's places in a block of 16 tokens: dims that a head does not have are read as its first ones, against zeros of q, and dropped.
+  // a lane's places in a block of 16 tokens: for dims that a head does not have all lanes read the block's first ones, against zeros of q, and drop them.
   // With 256 dims of bf16 the tiles alone take 192 registers of the 256, and what spills waits for all that is on its way: there one
   // offset serves all loads of keys (where a head ends before a load's dims, it has the head's last ones once more), and the
   // two halves of the columns fetch half of q each: 4 x 32768 tokens 110 -> 99 us.  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
@@ -190,12 +191,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   auto first_dim = [&](uint32_t s) { return !kTight ? kSpan * s : D >= kSpan ? min(kSpan * s, D - kSpan) : 0u; };
   uint32_t key_at[kOffsets];
 #pragma unroll
-  for (uint32_t s = 0; s < kOffsets; ++s) key_at[s] = n * slot_bytes + (kSpan * kSize * s + 16 * g < kSize * D ? kSpan * kSize * s + 16 * g : 0);
+  for (uint32_t s = 0; s < kOffsets; ++s) key_at[s] = kSpan * kSize * s + 16 * g < kSize * D ? n * slot_bytes + kSpan * kSize * s + 16 * g : 0;
   // A lane's dims of a value are neighbours.  Where they are two loads that pass the caches, each has eight neighbours and the second those of the head's
   // last 128: two from the same lines would read these twice.
   constexpr bool kApart = PASSES && T::kValWords > 4;
   constexpr uint32_t kNear = kApart ? T::kVals / 2 : T::kVals;
-  const uint32_t val_at = 4 * g * slot_bytes + kSize * (n * kNear < D ? n * kNear : 0), second_at = kSize * (D - 128);
+  const uint32_t val_at = n * kNear < D ? 4 * g * slot_bytes + kSize * n * kNear : 0, second_at = kSize * (D - 128);
 
   struct Segment {   // the part of a (row, chunk) that lies in this share
     uint32_t r, seq, kv, first_head, n_heads, pair, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
@@ -649,7 +650,8 @@ int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
   // chunks of query heads read shall stay there (32 heads on 2, 16 x 8000 tokens 44 and 51).
   const uint64_t bytes = (uint64_t)a->rows * c.kv_heads * c.capacity * c.head_dim * (int8 ? 2 : 4);
   // (256 dims of bf16: 33 MB 19 us and 21, 67 MB 32 and 30.5.)
-  const bool passes = !a->seqs && l.chunks == c.kv_heads && bytes >= (c.head_dim == 256 && !int8 ? 8 * kPassing : kPassing) && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
+  const bool passes = !a->seqs && l.chunks == c.kv_heads && bytes >= (c.head_dim == 256 && !int8 ? 8 * kPassing : kPassing) &&
+                      c.head_dim % 32 == 0 && c.head_dim >= (c.head_dim <= 128 ? 64 : int8 ? 192 : 256);
   if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, passes, s);
   else if (c.head_dim <= 128) launch_attend<128>(c, v, l.groups, int8, a->accumulate, passes, s);
   else launch_attend<256>(c, v, l.groups, int8, a->accumulate, passes, s);

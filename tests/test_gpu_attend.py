@@ -239,10 +239,11 @@ def test_many_rows_and_another_stream():
     close(out, want, p)
 
 
-@pytest.mark.parametrize("kind,track", [("bf16", False), ("int8", True)])
+@pytest.mark.parametrize("kind,track", [("bf16", False), ("int8", True), ("bf16", True)])
 @pytest.mark.parametrize("rows,longest,heads,kv_heads,dim", [
     (16, 500, 8, 8, 64), (16, 700, 16, 8, 64), (17, 1000, 8, 8, 64), (40, 1000, 20, 10, 64), (16, 700, 8, 8, 128), (64, 760, 8, 8, 96), (33, 400, 12, 6, 256),
-    (16, 1270, 8, 8, 64), (4, 5100, 34, 2, 64), (11, 2900, 8, 8, 128), (2, 20000, 3, 3, 64), (65, 1100, 4, 4, 64)])
+    (16, 1270, 8, 8, 64), (4, 5100, 34, 2, 64), (11, 2900, 8, 8, 128), (2, 20000, 3, 3, 64), (65, 1100, 4, 4, 64),
+    (12, 2000, 4, 4, 192), (12, 2000, 2, 2, 80)])
 def test_how_rows_are_cut(rows, longest, heads, kv_heads, dim, kind, track):
     """Rows that are as long as each other, spread, and with one of them far longer: not cut, cut at whole shares, cut anywhere; twice with one workspace."""
     p = Paged(rows, -(-longest // 16), kv_heads=kv_heads, dim=dim, kind=kind, marks=track, seed=rows)
