@@ -103,8 +103,8 @@ __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
   return v;
 }
 
-// Bound: reading the cache.  16 x 32768 tokens, 8 heads of 64 in bf16: 190 us, 5.65 TB/s; 1 x 131072 of 128: 96, 5.6; in 8 bits 16 x 32768 of 128: 192, 5.7, with the
-// vector units at about 90 % (conversion to bf16); 4 x 32768, 4 heads of 256: 99, 5.4.  Few tokens: launch, lengths, page table, keys and values, join, 5.7 us for 200 tokens.
+// Bound: reading the cache.  16 x 32768 tokens, 8 heads of 64 in bf16: 172 us, 6.2 TB/s; 1 x 131072 of 128: 88, 6.1; in 8 bits 16 x 32768 of 128: 175..185, 6.1, with the
+// vector units at about 90 % (conversion to bf16); 4 x 32768, 4 heads of 256: 93, 5.8.  Few tokens: launch, lengths, page table, keys and values, join, 5.7 us for 200 tokens.
 //
 // All (row, chunk, unit of kUnit tokens) in this order are one line, cut into equal shares, one per workgroup: whatever the
 // lengths, every workgroup has as much to do.  Eight wavefronts (one workgroup per compute unit) hold as much on its way as the memory needs: twelve and sixteen,
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   // a lane's places in a block of 16 tokens: for dims that a head does not have all lanes read the block's first ones, against zeros of q, and drop them.
   // With 256 dims of bf16 the tiles alone take 192 registers of the 256, and what spills waits for all that is on its way: there one
   // offset serves all loads of keys (where a head ends before a load's dims, it has the head's last ones once more), and the
-  // two halves of the columns fetch half of q each: 4 x 32768 tokens 110 -> 99 us.  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
+  // two halves of the columns fetch half of q each: 4 x 32768 tokens 110 -> 99 us (through the L2s).  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
   constexpr bool kTight = DIM == 256 && !INT8;
   constexpr uint32_t kSize = INT8 ? 1 : 2, kSpan = INT8 ? 64 : 32, kOffsets = kTight ? 1 : T::kLoads, kFetched = kTight ? 4 : 8;
   const uint32_t slot_bytes = kSize * (uint32_t)c.slot_stride;

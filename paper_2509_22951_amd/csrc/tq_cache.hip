@@ -27,7 +27,7 @@ struct AppendView {
 // rotation lies rotary_dim / 2 values apart: its other half comes from another lane of the same group, so a wavefront has read all
 // of a head before it writes any (q_out may be q), and 8 bits' absmax is a maximum over the group.
 //
-// Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits: 62 us); for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
+// Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits, bf16 q: 56 us); for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
 template <int LANES, bool INT8, bool Q16>
 __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
   typedef __attribute__((address_space(4))) const int32_t constant_i32;
@@ -154,8 +154,8 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   const uint32_t lanes = c.head_dim <= 16 ? 4 : c.head_dim <= 32 ? 8 : c.head_dim <= 64 ? 16 : c.head_dim <= 128 ? 32 : 64;
   const uint32_t n_heads = a->heads + 2 * c.kv_heads, groups = kAppendThreads / lanes, rounds = (n_heads + groups - 1) / groups;
   // A head per group of lanes, until there are many more workgroups than the GPU holds; then several per group, so that their loads are on their way
-  // together, and as evenly as they divide, since a group without a head waits with the others (40 heads of 128 in 8 bits: 8192 rows 75 us with one, 68 with
-  // four and one in turn, 62 with five; 1024 rows 12.6 with one, 13.7 with five).
+  // together, and as evenly as they divide, since a group without a head waits with the others (40 heads of 128 in 8 bits, through the caches: 8192 rows 75 us with one,
+  // 68 with four and one in turn, 62 with five; 1024 rows 12.6 with one, 13.7 with five).
   const uint32_t most = (uint64_t)a->rows * rounds > 16384 ? kMostItems : 1, parts = (rounds + most - 1) / most;
   v.items = (rounds + parts - 1) / parts;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, parts), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v); };
@@ -274,7 +274,7 @@ __device__ __forceinline__ Bin find_bin(const uint32_t* sums, uint32_t left) {  
 
 // Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., AHEAD of them
 // together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.  Bound: memory, for many tokens (16 x 8 lists, 4096
-// rows of 256 bytes of keys and of values each: 120 us, 4.5 TB/s read and written).
+// rows of 256 bytes of keys and of values each: 117 us, 4.6 TB/s read and written).
 template <bool INT8, uint32_t AHEAD>
 __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, const uint32_t* slots_to, const uint32_t* slots_from, uint32_t n,
                                             uint32_t first, uint32_t step) {
