@@ -445,7 +445,8 @@ int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *str
  *   2^25 tokens).
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_workspace gives for the same arguments, zero before the first
  *   call with it; calls whose execution overlaps need one each.
- * Logits, softmax statistics and sums are fp32; sums are made in an order that only the arguments and lengths decide, so results repeat.
+ * Queries, logits, weights, softmax statistics and sums are fp32, none of them rounded to fewer bits; sums are made in an order that only the
+ * arguments and lengths decide, so results repeat.
  * What lies in a cache beyond a row's length is not used, whatever it holds.  heads is a multiple of kv_heads.
  */
 typedef struct tq_attend_args {

@@ -7,8 +7,10 @@
 //   out^T [dim][head] = V^T [dim][token] P^T: the lane that got the logits of tokens 4g..4g+3 of both 16-token blocks (g = l / 16)
 //   supplies the same tokens as its 8 values of the contraction, so P is already where it is needed; it loads DIM / 16
 //   neighbouring dims of those 8 tokens' values and transposes that square in its registers (one v_perm per pair).
-// The 16 columns are 8 heads twice: column c holds the upper 8 bits of head c's mantissas, column c + 8 the next 8, so that
-// q (three parts, two products) enters with all of fp32's 24 bits and p with 16, at a few per cent of the matrix unit's rate.
+// The 16 columns are 8 heads twice: column c holds the upper 8 bits of head c's mantissas, column c + 8 the next 8, and a second
+// product has the last 8 beside zeros, so that q and p enter with all of fp32's 24 bits.  (p with 16 of them, one product: no faster with
+// bf16 caches of up to 128 dims, 1 % with 256, in 8 bits 2 % of 128 dims and 5 % of 64, where the vector units are busy; but up to 2^-17 of
+// each weight off, more than all else together: a result next to the middle of two bf16 values went to the other one in one of a thousand.)
 #include <algorithm>
 
 #include "tq_cache_view.h"
@@ -379,14 +381,15 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       total *= shrink;
 #pragma unroll
       for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
-      bf16x8 pb;
+      bf16x8 p0, p1;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float w = __builtin_amdgcn_exp2f(p[i] - base);
         total += w;
         if constexpr (INT8) w = w > 0.f ? w * (&x.vs[i / 4].x)[i % 4] : 0.f;   // (a masked token's scale may be anything; a NaN weight is in the total)
-        const __bf16 hi = (__bf16)w;
-        pb[i] = part ? (__bf16)(w - (float)hi) : hi;
+        const __bf16 hi = (__bf16)w, mid = (__bf16)(w - (float)hi), lo = (__bf16)(w - (float)hi - (float)mid);
+        p0[i] = part ? mid : hi;
+        p1[i] = part ? (__bf16)0.f : lo;
       }
 #pragma unroll
       for (int b = 0; b < T::kVals; ++b) {
@@ -395,12 +398,14 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         for (int i = 0; i < 4; ++i) {
           if constexpr (INT8) {
             const float lo = (float)(int8_t)(x.v[2 * i][b / 4] >> (8 * (b % 4))), hi = (float)(int8_t)(x.v[2 * i + 1][b / 4] >> (8 * (b % 4)));
-            vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u) & value_bits[i];
+            vt[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);   // (finite, so that a weight of 0 is enough)
           } else {
             vt[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][b / 2], x.v[2 * i][b / 2], b % 2 ? 0x07060302u : 0x05040100u) & value_bits[i];
           }
         }
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3])), pb, o[b], 0, 0, 0);
+        const bf16x8 value = __builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3]));
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, p0, o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, p1, o[b], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
       fetch_values(next);

@@ -272,3 +272,49 @@ def test_rows_that_many_workgroups_share(heads, kv_heads, dim, rows):
             call.launch(stream())
             torch.cuda.synchronize()
             close(out, want, p)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_weights_enter_the_sum_with_all_their_bits(kind, dim):
+    """Large terms that cancel, so that the result's own rounding to bf16 hides nothing.
+
+    Keys are unit vectors, so a logit is one product: q * (scale * log2 e) with two roundings of 2^-24 of a factor of 2^-24 itself, 2^-22.4 of
+    the logit, which is at most 0.5; a weight is off by ln 2 * (2 * 0.5 * 2^-22.4 + 2^-25) and exp2's last place, 2^-23: 2^-21.8 of it, twice that
+    beside the total.  Products of 24 and 8 bits are exact; some ten additions at 2^-24: 2^-19.8 of sum p |v| in all, taken as 2^-19."""
+    rows, heads, scale = 40, 4, 0.125
+    p = Paged(rows, 1, kv_heads=heads, dim=dim, kind=kind)
+    g = torch.Generator().manual_seed(dim)
+    q = torch.zeros((rows, heads, dim))
+    q[..., 0], q[..., 1:4] = 2.7, 1 + 1.6 * torch.rand((rows, heads, 3), generator=g)
+    w = torch.exp(q[..., :4].double() * scale)
+    w /= w.sum(dim=-1, keepdim=True)
+    one = (1 + torch.rand((rows, heads, dim), generator=g)) * torch.where(torch.rand((rows, heads, dim), generator=g) < 0.5, -1, 1)
+    v = torch.zeros((rows, heads, 4, dim), dtype=torch.float64)
+    k, k_scale, v_scale = torch.zeros((rows, heads, 4, dim)), torch.full((rows, heads, 4), 2.0 ** -6), torch.ones((rows, heads, 4))
+    if kind == "bf16":
+        v[:, :, 1] = one.to(torch.bfloat16).double()
+        for t in (2, 3):      # what is left, divided by this token's weight
+            v[:, :, t] = (-(w[..., None] * v).sum(dim=2) / w[..., t, None]).float().to(torch.bfloat16).double()
+        k[..., range(4), range(4)] = 1
+        levels = v
+    else:
+        levels = torch.zeros_like(v)
+        levels[:, :, 1] = levels[:, :, 2] = torch.round(one * 60).double()
+        levels[:, :, 3] = -levels[:, :, 1]
+        v_scale[..., 1:3] = 0.5 + torch.rand((rows, heads, 2), generator=g)
+        v_scale[..., 3] = ((w[..., 1:3] * v_scale[..., 1:3].double()).sum(dim=-1) / w[..., 3]).float()
+        v = levels * v_scale.double()[..., None]
+        k[..., range(4), range(4)] = 64
+    pages = p.tables[:, 0].cpu().long()
+    for name, t, s in (("k", k, k_scale), ("v", levels, v_scale)):
+        getattr(p, name)[pages.cuda(), :, :4] = t.to(getattr(p, name).dtype).cuda()
+        if kind == "int8":
+            getattr(p, name + "_scale")[pages.cuda(), :, :4] = s.cuda()
+    lengths = ints([4] * rows)
+    out = run(p, q.cuda(), lengths, scale=scale)
+    want, size = (w[..., None] * v).sum(dim=2), (w[..., None] * v.abs()).sum(dim=2)
+    assert (attend_reference(p, q, lengths, scale=scale)[0] - want).abs().max() < 2.0 ** -40
+    assert (want.abs() < size * 2.0 ** -12).all()
+    off = (out.cpu().double() - want).abs()
+    assert (off <= want.abs() * 2.0 ** -8 + size * 2.0 ** -19).all(), float((off / size).max() * 2 ** 19)
