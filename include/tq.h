@@ -348,8 +348,8 @@ int tq_listing_destroy(tq_listing h);
  * What stands between the products of a decode step: the norm in front of them, the cache of keys and values, attention over
  * it, and a cache that is kept at a budget.  The products give fp32 y and take bf16 x, and so do these calls.
  *
- * All of them run on the caller's stream and return: no synchronisation, no allocation, nothing kept between calls, so they may
- * be captured in a HIP graph.  Argument structures are read during the call; zero-initialise them and set what you need.
+ * All of them run on the caller's stream and return: no synchronisation, no allocation, nothing kept between calls (but zeros in
+ * the workspace of tq_attend), so they may be captured in a HIP graph.  Argument structures are read during the call; zero-initialise them and set what you need.
  * Strides count elements; 0 stands for rows without gaps.
  */
 #define TQ_BF16 0u
@@ -444,7 +444,9 @@ int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *str
  *   accumulate: 1 adds every token's weight, summed over the query heads of a key/value head, to cache->scores (capacity: at most
  *   2^25 tokens).
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_workspace gives for the same arguments, zero before the first
- *   call with it; calls whose execution overlaps need one each.
+ *   call with it.  It begins with counters (1152 bytes) that every call leaves zero for the next one, whatever that one's arguments: calls of
+ *   any rows, heads and caches may use it one after another.  Nobody else may write to it in between, and calls whose execution
+ *   overlaps need one each.
  * Queries, logits, weights, softmax statistics and sums are fp32, none of them rounded to fewer bits; sums are made in an order that only the
  * arguments and lengths decide, so results repeat.
  * What lies in a cache beyond a row's length is not used, whatever it holds.  heads is a multiple of kv_heads.
@@ -473,7 +475,7 @@ int tq_attend_workspace(const tq_cache *cache, const tq_attend_args *args, uint6
  *   lengths: device, int32 [n_seqs]; lengths_out: min(length, keep), NULL: written to lengths.
  *   scores_out, positions_out: as cache->scores and cache->positions, which they replace as output (slots up to the new length are
  *   written); NULL: in place.
- *   workspace: as for tq_attend, but with any contents.
+ *   workspace: device, 16-byte aligned, of at least the size tq_cache_evict_workspace gives, with any contents.  Not a part of a tq_attend workspace.
  */
 typedef struct tq_evict_args {
   int32_t *lengths;

@@ -551,7 +551,7 @@ class CacheAppend(_CacheCall):
 
 
 class Attend(_CacheCall):
-    """tq_attend with arguments marshalled once.  The workspace is zero before the first launch."""
+    """tq_attend with arguments marshalled once.  The workspace is zero before the first launch, and for tq_attend alone."""
     _entry, _type = "tq_attend", TqAttendArgs
 
     @classmethod

@@ -24,13 +24,17 @@ constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tok
 constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;   // workgroups of a launch (one per compute unit); units of one; parts that are joined at a time
 constexpr uint64_t kPassing = 8 << 20;   // bytes of keys and values
 constexpr uint32_t kMostAligned = 16;   // units of a share
+constexpr uint32_t kCounters = 2 * (kMaxGroups / kCluster) + kMaxGroups;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttendView {
   const void* q;
   uint16_t* out;
   const int32_t *seqs, *lengths;
-  uint32_t* arrived;   // [cluster][2], then [row][chunk]: workgroups whose part is in the partials; zero between calls
+  // [cluster][2], then [workgroup]: the workgroups, or clusters, whose part of a (row, chunk) is in the partials; zero between calls.  Of a
+  // (row, chunk) that is cut the workgroup in which it begins, which begins no other one that reaches beyond it: the same places for
+  // all rows, heads and lengths, so that calls of any of them may follow each other on one workspace.
+  uint32_t* arrived;
   float* partials;     // [workgroup][2]: kHeads x head_dim sums, then maximum and total of every head
   float* logits;       // [row][head][capacity], in units of log 2 (accumulate)
   float2* stats;       // [row][head]: maximum and 1 / total of the whole row (accumulate)
@@ -201,7 +205,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   const uint32_t val_at = n * kNear < D ? 4 * g * slot_bytes + kSize * n * kNear : 0, second_at = kSize * (D - 128);
 
   struct Segment {   // the part of a (row, chunk) that lies in this share
-    uint32_t r, seq, kv, first_head, n_heads, pair, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
+    uint32_t r, seq, kv, first_head, n_heads, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
   };
   auto next_segment = [&] {
     Segment s;
@@ -210,10 +214,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     s.seq = (uint32_t)__builtin_amdgcn_readlane((int)lane_seq, r & 63);
     const uint32_t units = units_of(length);
     s.units = quantum == 1 ? units : (uint32_t)(((float)(units + quantum - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)quantum)) * quantum;
-    s.pair = (pos - row_first) / s.units;
-    s.pair_first = row_first + s.pair * s.units;
-    s.kv = s.pair / per_kv;
-    const uint32_t chunk = s.pair % per_kv, unit = pos - s.pair_first, unit_end = min(s.units, unit + (stop - pos));
+    const uint32_t pair = (pos - row_first) / s.units;
+    s.pair_first = row_first + pair * s.units;
+    s.kv = pair / per_kv;
+    const uint32_t chunk = pair % per_kv, unit = pos - s.pair_first, unit_end = min(s.units, unit + (stop - pos));
     s.first_head = s.kv * a.group + chunk * kHeads;
     s.n_heads = min((uint32_t)kHeads, a.group - chunk * kHeads);
     s.begin = unit * kUnit;
@@ -494,7 +498,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the stores have reached the level that the device shares
         __syncthreads();
         // (a cluster has parts of at most two rows that reach beyond it: one that begins before it, one that begins in it)
-        global_u32* arrived = (global_u32*)(whole ? a.arrived + 2 * (kMaxGroups / kCluster) + (uint64_t)s.r * a.chunks + s.pair
+        global_u32* arrived = (global_u32*)(whole ? a.arrived + 2 * (kMaxGroups / kCluster) + group0
                                                   : a.arrived + 2 * cluster + (group0 >= cluster * kCluster ? 1 : 0));
         if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
@@ -609,7 +613,7 @@ int check_attend(const std::string& who, const tq_cache* cache, const tq_attend_
     return at;
   };
   l->bytes = 0;
-  l->arrived = place(((uint64_t)a->rows * l->chunks + 2 * (kMaxGroups / kCluster)) * 4);
+  l->arrived = place(kCounters * 4);   // first, and as many for every call
   l->partials = place((uint64_t)l->groups * 2 * kHeads * (c->head_dim + 2) * 4);
   l->logits = a->accumulate ? place((uint64_t)a->rows * a->heads * c->capacity * 4) : 0;
   l->stats = a->accumulate ? place((uint64_t)a->rows * a->heads * 8) : 0;

@@ -318,3 +318,21 @@ def test_weights_enter_the_sum_with_all_their_bits(kind, dim):
     assert (want.abs() < size * 2.0 ** -12).all()
     off = (out.cpu().double() - want).abs()
     assert (off <= want.abs() * 2.0 ** -8 + size * 2.0 ** -19).all(), float((off / size).max() * 2 ** 19)
+
+
+def test_one_workspace_serves_calls_of_any_rows_and_heads():
+    """Every row is cut between workgroups in every call, and what one call leaves in the workspace is not what the next one expects there."""
+    p = Paged(16, 256, kv_heads=8, dim=64, marks=True)
+    calls = []
+    for rows, heads, track in [(4, 8, False), (16, 8, False), (1, 8, True), (16, 72, False), (7, 24, True), (16, 8, True)]:
+        q = queries(rows, heads, 64, rows + heads)
+        lengths = ints([4096 - 300 * (r % 3) for r in range(rows)])
+        n = tq.Attend.workspace_bytes(p.describe(), q=ptr(q), lengths=ptr(lengths), rows=rows, heads=heads, scale=0.125, q_type=tq.TQ_FP32, accumulate=int(track))
+        calls.append((rows, q, lengths, track, n, attend_reference(p, q, lengths)))
+    ws = torch.zeros(max(c[4] for c in calls), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        for rows, q, lengths, track, _, (want, added) in calls:
+            p.scores.zero_()
+            close(run(p, q, lengths, accumulate=track, workspace=ws), want, p)
+            if track:
+                assert ((p.scores.cpu().double() - added).abs() <= added * 2.0 ** -14 + added * 2.0 ** -23).all()
