@@ -414,7 +414,7 @@ typedef struct tq_cache {
  *   cos, sin: device, fp32 [n_positions][rotary_dim / 2].  The first rotary_dim values of a head (a multiple of 8, 0: none) are
  *   rotated in pairs (a, b) -> (a cos - b sin, a sin + b cos): value i with value i + rotary_dim / 2 (TQ_ROTARY_HALVES), or 2i with 2i + 1
  *   (TQ_ROTARY_ADJACENT).
- * Values go into a TQ_BF16 cache rounded to nearest even, into a TQ_INT8 cache by the rule of the weights (scale = absmax / 127;
+ * Values go into a TQ_BF16 cache rounded to nearest even (to an infinity from 3.396e38 on), into a TQ_INT8 cache by the rule of the weights (scale = absmax / 127;
  * NaN, if a value is not finite).
  * Where the cache has scores and positions, the slot's get 0 and positions[r].
  * A row whose sequence, slot or position is outside the cache or the table of angles is padding: it writes nothing to the
@@ -449,6 +449,8 @@ int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *str
  *   overlaps need one each.
  * Queries, logits, weights, softmax statistics and sums are fp32, none of them rounded to fewer bits; sums are made in an order that only the
  * arguments and lengths decide, so results repeat.
+ * What is not finite within a row's length does what it does in the formula, slowly: a key that gives a logit of -infinity takes its token's weight
+ * (all of them: zeros), one that gives +infinity or NaN makes that head's result NaN, an infinite or NaN value reaches its own dim, whatever its weight.
  * What lies in a cache beyond a row's length is not used, whatever it holds.  heads is a multiple of kv_heads.
  */
 typedef struct tq_attend_args {

@@ -109,6 +109,80 @@ __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
   return v;
 }
 
+struct Segment {   // the part of a (row, chunk) that lies in a workgroup's share
+  uint32_t r, seq, kv, first_head, n_heads, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
+};
+
+// A wavefront's tokens of a segment once more, a product per value as the formula has them, so that infinities give what they give there.  The
+// results replace those in LDS (and the logits).  32 tokens at a time, two lanes per key, then a lane per dim of the values: slow, and only for what is
+// not finite.  What it needs is read again from the kernel's arguments, and nothing of it computed ahead: the tile loop has no registers for it.
+template <int DIM, bool INT8, bool TRACK>
+__device__ __forceinline__ void take_again(const Segment& s, uint32_t lane, uint32_t wave, float* lds_sum, float* lds_max, float* lds_total) {
+  typedef __attribute__((address_space(4))) const char constant_char;
+  typedef __attribute__((address_space(4))) const CacheView constant_cache;
+  typedef __attribute__((address_space(4))) const AttendView constant_attend;
+  constexpr uint32_t kOwn = (DIM + 63) / 64;
+  constant_char* args = (constant_char*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(args), "+v"(lane));
+  constant_cache& c = *(constant_cache*)args;
+  constant_attend& a = *(constant_attend*)(args + sizeof(CacheView));
+  const uint32_t D = c.head_dim, slot_bytes = (INT8 ? 1 : 2) * (uint32_t)c.slot_stride, n_pages = c.n_pages, mask = (1u << c.page_shift) - 1, t = lane % 32;
+  const bool q16 = a.q16;
+  const float scale = a.scale;
+  const char *keys = c.k, *values = c.v;
+  const float *k_scale = c.k_scale, *v_scale = c.v_scale;
+  const int32_t* table = c.tables + (uint64_t)s.seq * c.table_stride;
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): the logits stored before
+#pragma unroll 1
+  for (uint32_t h = 0; h < s.n_heads; ++h) {
+    const uint64_t q_at = s.r * a.q_stride + (s.first_head + h) * D;
+    float m = -INFINITY, sum_p = 0.f, sum[kOwn] = {};
+#pragma unroll 1
+    for (uint32_t round = 0; round < s.rounds; ++round) {
+      const uint32_t tile = s.begin + round * kUnit + wave * kTile, slot = tile + t;
+      uint32_t page = n_pages;
+      if (slot < s.end) page = (uint32_t)table[slot >> c.page_shift];
+      const bool there = page < n_pages;
+      const uint64_t at = (INT8 ? 1 : 2) * ((there ? page : 0) * c.page_stride + s.kv * c.head_stride) + (uint64_t)(slot & mask) * slot_bytes;
+      const uint64_t mark = (((uint64_t)(there ? page : 0) * c.kv_heads + s.kv) << c.page_shift) + (slot & mask);
+      const char* key = keys + at;
+      float l = 0.f;
+#pragma unroll 1
+      for (uint32_t i = 0, d = lane < 32 ? 0 : D / 2; i < D / 2; ++i, ++d) {
+        const float of_q = (q16 ? bf16_value(((const uint16_t*)a.q)[q_at + d]) : ((const float*)a.q)[q_at + d]) * scale;
+        l = fmaf(of_q, INT8 ? (float)((const int8_t*)key)[d] : bf16_value(((const uint16_t*)key)[d]), l);
+      }
+      l += __shfl_xor(l, 32);
+      if constexpr (INT8) l *= k_scale[mark];
+      if (!there) l = -INFINITY;
+      if (TRACK && lane < 32 && slot < s.end) a.logits[((uint64_t)s.r * a.heads + s.first_head + h) * c.capacity + slot] = l;
+      const float top = fmaxf(m, group_max<32>(l)), base = top == -INFINITY ? 0.f : top, shrink = __builtin_amdgcn_exp2f(m - base);
+      float p = __builtin_amdgcn_exp2f(l - base);
+      m = top;
+      sum_p = fmaf(sum_p, shrink, group_sum<32>(p));
+      if constexpr (INT8) p = there ? p * v_scale[mark] : 0.f;
+#pragma unroll
+      for (uint32_t i = 0; i < kOwn; ++i) sum[i] *= shrink;
+      const uint32_t taking_part = (uint32_t)__ballot(there);   // of lanes 0..31, a bit per token
+#pragma unroll 1
+      for (uint32_t n = 0; n < kTile; ++n) {
+        if (!(taking_part >> n & 1)) continue;
+        const char* value = values + __shfl(at, n);
+        const float weight = __shfl(p, n);
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) {
+          const uint32_t d = lane + 64 * i < D ? lane + 64 * i : 0;
+          sum[i] = fmaf(weight, INT8 ? (float)((const int8_t*)value)[d] : bf16_value(((const uint16_t*)value)[d]), sum[i]);
+        }
+      }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i)
+      if (lane + 64 * i < D) lds_sum[(wave * kHeads + h) * (DIM + 4) + lane + 64 * i] = sum[i];
+    if (lane == 0) lds_max[wave * kHeads + h] = m, lds_total[wave * kHeads + h] = sum_p;
+  }
+}
+
 // Bound: reading the cache.  16 x 32768 tokens, 8 heads of 64 in bf16: 172 us, 6.2 TB/s; 1 x 131072 of 128: 88, 6.1; in 8 bits 16 x 32768 of 128: 175..185, 6.1, with the
 // vector units at about 90 % (conversion to bf16); 4 x 32768, 4 heads of 256: 93, 5.8.  Few tokens: launch, lengths, page table, keys and values, join, 5.7 us for 200 tokens.
 //
@@ -204,9 +278,6 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   constexpr uint32_t kNear = kApart ? T::kVals / 2 : T::kVals;
   const uint32_t val_at = n * kNear < D ? 4 * g * slot_bytes + kSize * n * kNear : 0, second_at = kSize * (D - 128);
 
-  struct Segment {   // the part of a (row, chunk) that lies in this share
-    uint32_t r, seq, kv, first_head, n_heads, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
-  };
   auto next_segment = [&] {
     Segment s;
     s.r = r;
@@ -390,7 +461,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       for (int i = 0; i < 8; ++i) {
         float w = __builtin_amdgcn_exp2f(p[i] - base);
         total += w;
-        if constexpr (INT8) w = w > 0.f ? w * (&x.vs[i / 4].x)[i % 4] : 0.f;   // (a masked token's scale may be anything; a NaN weight is in the total)
+        if constexpr (INT8) w = p[i] != -INFINITY ? w * (&x.vs[i / 4].x)[i % 4] : 0.f;   // (a masked token's scale may be anything)
         const __bf16 hi = (__bf16)w, mid = (__bf16)(w - (float)hi), lo = (__bf16)(w - (float)hi - (float)mid);
         p0[i] = part ? mid : hi;
         p1[i] = part ? (__bf16)0.f : lo;
@@ -429,6 +500,13 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         const float4 v = make_float4(ror8_sum(o[b][j]), ror8_sum(o[b + 1][j]), ror8_sum(o[b + 2][j]), ror8_sum(o[b + 3][j]));
         if (part == 0) *(float4*)&lds_sum[(wave * kHeads + head) * (DIM + 4) + (b < (int)kNear ? 0 : D - 128) + (4 * g + j) * kNear + b % kNear] = v;
       }
+    // A query, key or value that is not finite has met zeros and parts of opposite sign: no total or sum that it went into is finite.
+    float odd = total * 0.f;
+#pragma unroll
+    for (int b = 0; b < T::kVals; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) odd = fmaf(o[b][j], 0.f, odd);
+    if (__builtin_expect(__any(!(odd == 0.f)), 0)) take_again<DIM, INT8, TRACK>(s, lane, wave, lds_sum, lds_max, lds_total);
     __syncthreads();
     // the workgroups among which this (row, chunk) is cut
     const uint32_t n_heads = s.n_heads, group0 = s.pair_first / share, parts = min((s.pair_first + s.units - 1) / share, gridDim.x - 1) - group0 + 1;

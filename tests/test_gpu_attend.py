@@ -336,3 +336,88 @@ def test_one_workspace_serves_calls_of_any_rows_and_heads():
             close(run(p, q, lengths, accumulate=track, workspace=ws), want, p)
             if track:
                 assert ((p.scores.cpu().double() - added).abs() <= added * 2.0 ** -14 + added * 2.0 ** -23).all()
+
+
+def agrees(out, want, vmax):
+    """As close(), with infinities and NaN where the formula has them."""
+    out = out.cpu().double()
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(torch.isinf(out), torch.isinf(want))
+    assert torch.equal(out[torch.isinf(want)], want[torch.isinf(want)])
+    off = (out - want).abs()[fine]
+    assert (off <= want[fine].abs() * 2.0 ** -8 + vmax * 2.0 ** -14).all()
+
+
+INF = float("inf")
+
+
+@pytest.mark.parametrize("dim,length,rows,track", [(64, 40, 2, False), (80, 300, 3, True), (128, 2100, 2, False), (128, 9000, 1, True), (208, 700, 2, False),
+                                                   (256, 20000, 1, False), (64, 41600, 1, True), (16, 77, 2, True)])
+def test_infinities_within_a_length_do_what_the_formula_says(dim, length, rows, track):
+    """A key of -inf (towards this query) takes its token's weight, one of +inf makes the row NaN; an infinite value reaches its own dim alone."""
+    p = Paged(rows, -(-length // 16), kv_heads=4, dim=dim, marks=track, seed=dim)
+    q = queries(rows, 8, dim, length)
+    vmax = p.values("v").abs().max()
+    some = sorted({0, 16, 17, length // 2, length - 1})
+    for s in range(rows):
+        for t in some:
+            page, at = int(p.tables[s, t // 16]), t % 16
+            for h in range(4):      # heads 2 h and 2 h + 1 may see the same key on two sides: one of them is NaN
+                p.k[page, h, at, 3] = -INF if q[s, 2 * h, 3] > 0 else INF
+        page = int(p.tables[s, some[2] // 16])
+        p.v[page, 1, some[2] % 16, 5], p.v[page, 2, some[2] % 16, 6] = INF, -INF      # of a token without weight
+        page = int(p.tables[s, (length - 2) // 16])
+        p.v[page, 3, (length - 2) % 16, 7], p.v[page, 3, (length - 2) % 16, 8] = INF, -INF
+    lengths = ints([length] * rows)
+    before = p.scores.cpu().double() if track else None
+    out = run(p, q, lengths, accumulate=track)
+    want, added = attend_reference(p, q, lengths)
+    assert torch.isfinite(want[:, 0]).all() and torch.isnan(want).any() and torch.isinf(want[:, 6]).any()
+    agrees(out, want, vmax)
+    if track:
+        got, fine = p.scores.cpu().double(), torch.isfinite(added)
+        assert torch.equal(torch.isnan(got), ~fine)
+        assert ((got - before - added).abs()[fine] <= (added * 2.0 ** -14 + (before + added) * 2.0 ** -23)[fine]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_queries_that_are_not_finite_stay_in_their_heads(kind):
+    p = Paged(2, 20, kind=kind)
+    q = queries(2, 8, 64)
+    lengths = ints([310, 33])
+    want = attend_reference(p, q, lengths)[0]
+    q[0, 1, 5], q[0, 6, 0], q[1, 3, 63] = INF, float("nan"), -INF
+    out = run(p, q, lengths)
+    odd = torch.zeros((2, 8), dtype=torch.bool)
+    odd[0, 1] = odd[0, 6] = odd[1, 3] = True
+    assert torch.isnan(out.cpu()[odd]).all()
+    off = (out.cpu().double() - want).abs()[~odd]
+    assert (off <= want[~odd].abs() * 2.0 ** -8 + p.values("v").abs().max() * 2.0 ** -14).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_a_nan_value_reaches_the_result_whatever_its_weight(kind):
+    """0 * NaN is NaN: a token whose weight is too small for a number is still there."""
+    p = Paged(1, 5, kv_heads=1, dim=32, kind=kind)
+    q = queries(1, 2, 32)
+    q[0, 1] = q[0, 0]
+    page, at = int(p.tables[0, 2]), 4
+    if kind == "int8":
+        p.k[page, 0, at], p.k_scale[page, 0, at] = torch.where(q[0, 0] > 0, -127, 127).to(torch.int8), 50.0
+        p.v_scale[page, 0, at] = float("nan")
+    else:
+        p.k[page, 0, at], p.v[page, 0, at] = torch.where(q[0, 0] > 0, -6000.0, 6000.0).to(torch.bfloat16), float("nan")
+    lengths = ints([70])
+    assert torch.isnan(attend_reference(p, q, lengths)[0]).all()
+    assert torch.isnan(run(p, q, lengths)).all()
+
+
+def test_a_row_whose_logits_are_all_minus_infinity_gives_zeros():
+    p = Paged(2, 40, marks=True)
+    q = queries(2, 2, 64).abs()
+    p.k[p.tables[0].long(), :, :, 9] = -INF
+    lengths = ints([600, 600])
+    before = p.scores[0].clone()
+    out = run(p, q, lengths, accumulate=True)
+    assert (out[0] == 0).all() and torch.equal(p.scores[0], before)
+    close(out[1:], attend_reference(p, q, lengths)[0][1:], p)
