@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   // a lane's places in a block of 16 tokens: for dims that a head does not have all lanes read the block's first ones, against zeros of q, and drop them.
   // With 256 dims of bf16 the tiles alone take 192 registers of the 256, and what spills waits for all that is on its way: there one
   // offset serves all loads of keys (where a head ends before a load's dims, it has the head's last ones once more), and the
-  // two halves of the columns fetch half of q each: 4 x 32768 tokens 110 -> 99 us (through the L2s).  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
+  // two halves of the columns fetch half of q each (4 x 32768 tokens through the L2s: 110 -> 99 us).  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
   constexpr bool kTight = DIM == 256 && !INT8;
   constexpr uint32_t kSize = INT8 ? 1 : 2, kSpan = INT8 ? 64 : 32, kOffsets = kTight ? 1 : T::kLoads, kFetched = kTight ? 4 : 8;
   const uint32_t slot_bytes = kSize * (uint32_t)c.slot_stride;
@@ -489,7 +489,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       if (last) break;
     }
 
-    // join the wavefronts: lane (g, head) holds dims (4 g + j) * kNear + b of the head, halves of p beside each other
+    // join the wavefronts: lane (g, head) holds dims (4 g + j) * kNear + b of the head, halves of p beside each other.  (Places in LDS and memory are
+    // made here from the thread's number, which looks new each time: made ahead of all loops they take registers from the tiles, and with 256 dims of
+    // bf16 come back from memory behind the next row's tile, 4 x 32768 tokens 106 us in place of 93.)
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const uint32_t lane = thread & 63, g = lane / 16, head = lane % 8, part = lane / 8 % 2;
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
     if (lane < kHeads) lds_max[wave * kHeads + lane] = top, lds_total[wave * kHeads + lane] = total;
@@ -515,7 +520,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     // a group of DIM / 4 lanes per head, four dims a lane
     constexpr uint32_t kLanes = DIM / 4, kGroups = kAttendThreads / kLanes;
     static_assert(kGroups >= kHeads && kGroups <= kAttendWaves * kHeads, "a group per head; lds_max");
-    const uint32_t of_group = threadIdx.x / kLanes, d0 = threadIdx.x % kLanes * 4;
+    const uint32_t of_group = thread / kLanes, d0 = thread % kLanes * 4;
     const bool joins = of_group < n_heads && d0 < D;
     struct Joined {
       float4 sum;
@@ -578,10 +583,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
         // (a cluster has parts of at most two rows that reach beyond it: one that begins before it, one that begins in it)
         global_u32* arrived = (global_u32*)(whole ? a.arrived + 2 * (kMaxGroups / kCluster) + group0
                                                   : a.arrived + 2 * cluster + (group0 >= cluster * kCluster ? 1 : 0));
-        if (threadIdx.x == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (thread == 0) lds_before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (lds_before != n - 1) break;   // the last one joins: the others' parts are in
-        if (threadIdx.x == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (thread == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         // every group takes a head and every per_head-th part, kAhead parts at a time
         constexpr uint32_t kAhead = 4;
         const uint32_t heads_n = n_heads > 4 ? 8 : n_heads > 2 ? 4 : n_heads, per_head = kGroups / heads_n, h = of_group % heads_n, part0 = of_group / heads_n;
