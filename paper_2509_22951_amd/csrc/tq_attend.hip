@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t row_length(const CacheView& c, const AttendV
 }
 
 typedef __attribute__((address_space(4))) const int32_t constant_i32;
-typedef __attribute__((address_space(1))) const uint32_t global_cu32;
+typedef __attribute__((address_space(1), aligned(2))) const uint32_t global_cu32_any;   // (the memory unit takes 4 bytes from any 2-byte boundary)
 
 template <int DIM, bool INT8>
 struct Tile {
@@ -349,16 +349,17 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       if constexpr (INT8) x.vs[b] = *(const float4*)(c.v_scale + w.mark[b] + 4 * g);
     }
   };
-  // 8 values of a segment's q: lane threadIdx.x % 64 of contraction step threadIdx.x / 64.  They are requested as the words they lie
-  // in, without a condition, so that nothing waits for them here (a lane without values reads the first ones).
+  // 8 values of a segment's q: lane threadIdx.x % 64 of contraction step threadIdx.x / 64.  They are requested as words, two bf16 values in each,
+  // from any address of their type and without a condition, so that nothing waits for them here (a lane without values reads the first ones).
   const uint32_t q_load = INT8 ? wave / 2 : wave, q_dim = first_dim(q_load) + (INT8 ? 16 * g + 8 * (wave % 2) : 8 * g), q_size = a.q16 ? 2 : 4;
   const bool has_q = q_dim >= kSpan * q_load && q_dim < D;
+  constexpr uint32_t kHalf = kFetched / 2;   // words of bf16 values, which come twice
   uint32_t q_words[kFetched];
   auto fetch_q = [&](const Segment& s) {
     const uint64_t row = (uint64_t)a.q + q_size * (s.r * a.q_stride + s.first_head * D);
     const uint32_t lane_at = head < s.n_heads && has_q ? q_size * (head * D + q_dim + (kTight ? 4 * part : 0)) : 0;
 #pragma unroll
-    for (uint32_t j = 0; j < kFetched; ++j) q_words[j] = *(global_cu32*)(((row + q_size * j) & ~(uint64_t)3) + lane_at);   // (lane_at: a multiple of 8)
+    for (uint32_t j = 0; j < kFetched; ++j) q_words[j] = *(global_cu32_any*)(row + (a.q16 ? 0 : j / kHalf * 4 * kHalf) + 4 * (j % kHalf) + lane_at);
   };
   Segment s = next_segment();
   fetch_q(s);
@@ -373,9 +374,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     bf16x8 q0, q1;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {   // (by all wavefronts: a load that some of them never use would be waited for in the loop, and with it those behind it)
-      const uint32_t upper = ((uint32_t)(uint64_t)a.q + 2 * (uint32_t)(s.r * a.q_stride + j)) & 2;   // (of a bf16 value: the half of its word)
-      const uint32_t own = q_words[j % kFetched], other = kTight ? ror8(own) : own, word = (j < 4) == (part == 0) ? own : other;
-      const float one = __uint_as_float((word << (a.q16 && !upper ? 16 : 0)) & (a.q16 ? 0xFFFF0000u : ~0u));
+      const uint32_t own = a.q16 ? q_words[j % kFetched / 2] : q_words[j % kFetched], other = kTight ? ror8(own) : own, word = (j < 4) == (part == 0) ? own : other;
+      const float one = __uint_as_float((word << (a.q16 && j % 2 == 0 ? 16 : 0)) & (a.q16 ? 0xFFFF0000u : ~0u));
       const float v = head < s.n_heads && has_q ? one * a.scale : 0.f;
       const __bf16 hi = (__bf16)v, mid = (__bf16)(v - (float)hi), lo = (__bf16)(v - (float)hi - (float)mid);
       q0[j] = part ? mid : hi;

@@ -421,3 +421,15 @@ def test_a_row_whose_logits_are_all_minus_infinity_gives_zeros():
     out = run(p, q, lengths, accumulate=True)
     assert (out[0] == 0).all() and torch.equal(p.scores[0], before)
     close(out[1:], attend_reference(p, q, lengths)[0][1:], p)
+
+
+@pytest.mark.parametrize("dim", [16, 80, 128, 208, 256])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_queries_at_any_address_of_their_type(dim, dtype):
+    """Rows with odd strides, from addresses one after another; the last row ends where the buffer does."""
+    p = Paged(3, 3, kv_heads=2, dim=dim, kind="int8" if dim == 80 else "bf16")
+    lengths, stride = ints([40, 7, 48]), 4 * dim + 1
+    for first in range(3):
+        buf = queries(1, 1, first + 2 * stride + 4 * dim, first, dtype).view(-1)
+        q = buf.as_strided((3, 4, dim), (stride, dim, 1), first)
+        close(run(p, q, lengths, q_stride=stride), attend_reference(p, q, lengths)[0], p)
