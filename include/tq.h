@@ -474,6 +474,8 @@ int tq_attend_workspace(const tq_cache *cache, const tq_attend_args *args, uint6
  * A token that stays and lies in a slot below `keep` is not moved; those above go, in order, to the slots below that have become
  * free, keys, values, scales, score and position with them.  (The order of tokens in a cache does not matter to attention: keys
  * are rotated before they are stored.)  Sequences that have no more than `keep` tokens are left as they are.
+ * The pages of all slots below lengths[s] have to be there.  A token whose page is not, which attention masks, counts and ranks like any other
+ * here, and keys and values are not moved out of such a page or into one: a token that goes there is lost, with its score and position left.
  *   lengths: device, int32 [n_seqs]; lengths_out: min(length, keep), NULL: written to lengths.
  *   scores_out, positions_out: as cache->scores and cache->positions, which they replace as output (slots up to the new length are
  *   written); NULL: in place.

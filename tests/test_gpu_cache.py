@@ -377,3 +377,27 @@ def test_a_budget_kept_token_after_token():
     assert eager["lengths"].tolist() == [41, 41, 41] and torch.isfinite(eager["out"]).all()
     newest = eager["p"].positions[:, :, :40].amax(dim=2)
     assert (newest == torch.tensor([[129], [129], [76]], device="cuda")).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_attention_after_an_eviction_is_attention_over_the_tokens_that_stay(kind):
+    """The kept tokens of each head, read from the cache as it was, against the cache as it is.  Tolerance as for attention itself: 2^-14 of
+    the largest value, and 2^-8 of the result for its rounding."""
+    keep, n = 90, [320, 90, 200]
+    p = Paged(3, 20, kv_heads=2, dim=64, kind=kind, marks=True, seed=11)
+    lengths, since = ints(n), ints([300, 0, 195])
+    was = {name: p.values(name) for name in ("k", "v")}
+    moves, stays = evict_reference(p, lengths, keep, since)
+    q = torch.randn((3, 4, 64), generator=torch.Generator().manual_seed(5))
+    want = torch.zeros((3, 4, 64), dtype=torch.float64)
+    for s in range(3):
+        for h in range(2):
+            kept = sorted(stays[s, h] + list(moves[s, h].values()))
+            assert len(kept) == min(n[s], keep)
+            k, v = (p.of_sequence(was[name], s, h, n[s])[0][kept] for name in ("k", "v"))
+            want[s, 2 * h:2 * h + 2] = torch.softmax(q[s, 2 * h:2 * h + 2].double() @ k.T / 8, dim=-1) @ v
+    evict(p, lengths, keep, since)
+    call, out = attend_call(p.describe(), p, q.cuda(), lengths)
+    call.launch(stream())
+    torch.cuda.synchronize()
+    assert ((out.cpu().double() - want).abs() <= want.abs() * 2.0 ** -8 + was["v"].abs().max() * 2.0 ** -14).all()
