@@ -390,7 +390,7 @@ int tq_add_rms_norm(const tq_norm_args *args, void *stream);
  *   type: TQ_BF16, or TQ_INT8 with fp32 scales k_scale, v_scale [n_pages][kv_heads][page_size] (one per token and head, symmetric).
  *   page_size: a power of two, 16..1024.  head_dim: a multiple of 16 up to 256.
  *   page_stride, head_stride, slot_stride: all 0 for pages [kv_heads][page_size][head_dim] without gaps, else multiples of 16
- *   bytes, slot_stride at most 2^26 bytes; k, v and the scales 16-byte aligned.
+ *   bytes, of at least head_dim elements and such that no two keys overlap, slot_stride at most 2^26 bytes; k, v and the scales 16-byte aligned.
  *   tables: device, int32 [n_seqs][table_stride] (0: seq_pages), seq_pages of which are a sequence's: it holds up to seq_pages * page_size
  *   tokens, its capacity (at most 2^30).
  *   scores, positions: device, fp32 and int32 [n_seqs][kv_heads][capacity], or NULL: for every token slot the attention weight that

@@ -51,6 +51,8 @@ inline int view_cache(const std::string& who, const tq_cache* c, CacheView* view
   if ((slot * size) % 16 || (head * size) % 16 || (page * size) % 16 || !aligned_to(c->k, 16) || !aligned_to(c->v, 16) ||
       !aligned_to(c->k_scale, 16) || !aligned_to(c->v_scale, 16))
     return refuse(TQ_E_INVALID_ARG, who + ": k, v, their scales and strides must be multiples of 16 bytes");
+  if (slot < c->head_dim || (c->kv_heads > 1 && head < c->head_dim) || (c->n_pages > 1 && page < c->head_dim))
+    return refuse(TQ_E_INVALID_ARG, who + ": a stride of the cache is smaller than head_dim");
   if (slot * size > (1u << 26)) return refuse(TQ_E_UNSUPPORTED, who + ": slot_stride is more than 2^26 bytes");   // (16 slots are within 32 bits)
   if (!aligned_to(c->tables, 4) || !aligned_to(c->scores, 4) || !aligned_to(c->positions, 4))
     return refuse(TQ_E_INVALID_ARG, who + ": tables, scores and positions must be 4-byte aligned");

@@ -94,3 +94,19 @@ def test_no_rows_are_no_work():
     tq.AddNorm(**{**NORM, "rows": 0}).launch()
     tq.CacheAppend(tq.Cache(**CACHE), **{**APPEND, "rows": 0}).launch()
     tq.Attend(tq.Cache(**CACHE), **{**ATTEND, "rows": 0}).launch()
+
+
+@pytest.mark.parametrize("change", [
+    dict(page_stride=16, head_stride=16, slot_stride=16), dict(page_stride=4096, head_stride=1024, slot_stride=56), dict(page_stride=4096, head_stride=48, slot_stride=128),
+    dict(page_stride=32, head_stride=1024, slot_stride=64), dict(type=tq.TQ_INT8, k_scale=A, v_scale=A, page_stride=4096, head_stride=1024, slot_stride=48),
+])
+def test_every_call_refuses_keys_that_overlap(change):
+    cache = tq.Cache(**{**CACHE, "scores": A, **change})
+    for call in (lambda: tq.CacheAppend(cache, **APPEND).launch(), lambda: tq.Attend(cache, **ATTEND).launch(), lambda: tq.CacheEvict(cache, **EVICT).launch(),
+                 lambda: tq.Attend.workspace_bytes(cache, **ATTEND), lambda: tq.CacheEvict.workspace_bytes(cache, **EVICT)):
+        assert "smaller than" in refused(INVALID, call)
+
+
+@pytest.mark.parametrize("change", [dict(page_stride=2048, head_stride=16, slot_stride=64, kv_heads=1), dict(page_stride=16, head_stride=1024, slot_stride=64, n_pages=1)])
+def test_the_stride_between_heads_or_pages_of_which_there_is_one_is_free(change):
+    assert tq.Attend.workspace_bytes(tq.Cache(**{**CACHE, **change}), **ATTEND) > 0
