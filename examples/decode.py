@@ -2,7 +2,7 @@
 attention -> output projection -> norm -> gated feed-forward, layer after layer, the whole step captured in one HIP graph.
 
 Weights are random (0.02 * N(0, 1)); --budget keeps every sequence's cache at that many tokens per head, by accumulated attention
-weight, the newest quarter of them protected.
+weight, the newest quarter of them (one token at least) protected.
 
   python examples/decode.py --layers 4 --hidden 2048 --heads 32 --kv-heads 8 --inter 8192 --batch 4 --tokens 64 --budget 48
 """
@@ -130,7 +130,8 @@ class Decoder:
         # the next token's place
         self.slots.copy_(self.left if self.budget else self.lengths)
         self.positions.add_(1)
-        torch.sub(self.positions, max(1, self.budget // 4), out=self.since)
+        # of the tokens that there are with the next one, the newest quarter is protected
+        torch.sub(self.positions, max(1, self.budget // 4) - 1, out=self.since)
 
     def step(self, tokens, graph=False):
         """One token per sequence in, logits [batch][vocab] out (the decoder's own buffer)."""

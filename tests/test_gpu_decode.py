@@ -100,3 +100,17 @@ def test_a_budget_holds_and_replays_equal_eager_steps():
         assert (kept[..., 1:] > kept[..., :-1]).all()                       # every token once
         assert (kept[..., -budget // 4:] == torch.arange(50 - budget // 4, 50, device="cuda")).all()      # the newest quarter is there
         assert (kept[..., 0] < 50 - budget).any()                           # and something old
+
+
+@pytest.mark.parametrize("budget", [1, 2, 7, 8])
+def test_the_newest_quarter_and_nothing_else_is_protected(budget):
+    """One token where a quarter is less; of a budget of one it is the token of the step itself."""
+    dec = Decoder(**{**SHAPE, "layers": 1}, budget=budget)
+    quarter = max(1, budget // 4)
+    for i in range(3 * budget + 4):
+        dec.step(torch.arange(3, device="cuda"), graph=i >= 2)
+        kept = dec.layers[0]["token"][:, :, :min(i + 1, budget)].sort(dim=-1).values
+        newest = torch.arange(max(0, i + 1 - quarter), i + 1, device="cuda", dtype=kept.dtype)
+        assert (kept[..., -len(newest):] == newest).all()
+        # the next eviction protects the quarter that the next token completes
+        assert dec.since.tolist() == [i + 2 - quarter] * 3
