@@ -26,10 +26,12 @@ def _ptr(t):
 class Decoder:
     """Fixed buffers and prepared calls of a decoder; step(tokens) -> logits.
 
-    budget 0: the cache grows up to `context` tokens; else it is cut back to `budget` tokens after every step."""
+    budget 0: the cache grows up to `context` tokens; else it is cut back to `budget` tokens after every step.  Either way there are
+    angles for `context` positions: one more step is refused."""
 
     def __init__(self, layers, hidden, heads, kv_heads, inter, vocab, batch, context, budget=0, cache="bf16", page=16, seed=0, base=500000.0):
         self.batch, self.heads, self.kv_heads, self.dim, self.budget = batch, heads, kv_heads, hidden // heads, budget
+        self.context, self.steps = context, 0
         rng, dev = np.random.default_rng(seed), "cuda"
         seq_pages = -(-((budget + 1) if budget else context) // page)
         n_pages, kv = batch * seq_pages, kv_heads * self.dim
@@ -135,6 +137,9 @@ class Decoder:
 
     def step(self, tokens, graph=False):
         """One token per sequence in, logits [batch][vocab] out (the decoder's own buffer)."""
+        if self.steps == self.context:
+            raise ValueError(f"this decoder has room for {self.context} tokens per sequence, and has had them")
+        self.steps += 1
         self.tokens.copy_(tokens)
         if not graph:
             self._run()

@@ -114,3 +114,14 @@ def test_the_newest_quarter_and_nothing_else_is_protected(budget):
         assert (kept[..., -len(newest):] == newest).all()
         # the next eviction protects the quarter that the next token completes
         assert dec.since.tolist() == [i + 2 - quarter] * 3
+
+
+@pytest.mark.parametrize("budget", [0, 5])
+@pytest.mark.parametrize("graph", [False, True])
+def test_a_context_that_is_full_is_refused(budget, graph):
+    dec = Decoder(**{**SHAPE, "layers": 1, "context": 9}, budget=budget)
+    for _ in range(9):
+        was = dec.step(torch.arange(3, device="cuda"), graph=graph).clone()
+    with pytest.raises(ValueError, match="9 tokens"):
+        dec.step(torch.arange(3, device="cuda"), graph=graph)
+    assert torch.equal(dec.logits, was) and dec.positions.tolist() == [9] * 3
