@@ -433,3 +433,38 @@ def test_queries_at_any_address_of_their_type(dim, dtype):
         buf = queries(1, 1, first + 2 * stride + 4 * dim, first, dtype).view(-1)
         q = buf.as_strided((3, 4, dim), (stride, dim, 1), first)
         close(run(p, q, lengths, q_stride=stride), attend_reference(p, q, lengths)[0], p)
+
+
+@pytest.mark.parametrize("rows,n,heads,kv_heads,dim", [(1, [41600], 3, 1, 64), (2, [20000, 9001], 2, 1, 128), (3, [41500, 300, 30001], 4, 2, 64), (1, [30000], 2, 1, 256),
+                                                       (16, [1270 - 3 * r for r in range(16)], 4, 4, 64), (5, [5000, 2000, 257, 4097, 3333], 8, 8, 128), (40, [1000] * 40, 10, 10, 64)])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_every_token_at_a_cut_counts_once(rows, n, heads, kv_heads, dim, kind):
+    """The first and last tokens of all stretches of 256, where shares, units and clusters are cut, have nearly all of the weight: the result without
+    one of them, or with one twice, is beyond the tolerance, as the reference itself shows."""
+    p = Paged(rows, -(-max(n) // 16), kv_heads=kv_heads, dim=dim, kind=kind, seed=rows)
+    q = queries(rows, heads, dim, max(n))
+    q[..., 0] = 8
+    edges = [sorted({t for t in range(length) if t % 256 in (0, 255)} | {length - 1}) for length in n]
+    for s in range(rows):
+        t = torch.tensor(edges[s])
+        pages = p.tables[s].cpu().long()[t // 16].cuda()
+        if kind == "bf16":
+            p.k[pages, :, (t % 16).cuda(), 0] = dim ** 0.5
+        else:      # the other dims keep their levels: this one is the largest
+            p.k[pages, :, (t % 16).cuda()] = 0
+            p.k[pages, :, (t % 16).cuda(), 0] = 127
+            p.k_scale[pages, :, (t % 16).cuda()] = dim ** 0.5 / 127
+    lengths = ints(n)
+    want = attend_reference(p, q, lengths)[0]
+    close(run(p, q, lengths), want, p)
+    keys, vals, group = p.values("k"), p.values("v"), heads // kv_heads
+    bound = p.values("v").abs().max() * 2.0 ** -14
+    for s in {0, rows - 1}:
+        k, _ = p.of_sequence(keys, s, 0, n[s])
+        v, _ = p.of_sequence(vals, s, 0, n[s])
+        w = torch.softmax(q[s, :group].cpu().double() @ k.T / dim ** 0.5, dim=-1)
+        assert w[:, edges[s]].sum(dim=1).min() > 0.5
+        for t in edges[s][:: max(1, len(edges[s]) // 8)]:
+            for wrong in (1 - w[:, t], 1 + w[:, t]):      # the total without this token, and with it twice
+                other = (w @ v + (wrong - 1)[:, None] * v[t]) / wrong[:, None]
+                assert ((other - want[s, :group]).abs() > want[s, :group].abs() * 2.0 ** -8 + bound).any()
