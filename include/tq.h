@@ -366,7 +366,8 @@ int tq_listing_destroy(tq_listing h);
  *   weight: device, [cols], TQ_FP32 or TQ_BF16 (weight_type).
  *   out: device, [rows][cols], TQ_BF16 or TQ_INT8 (out_type); out_scale: device, fp32 [rows], with TQ_INT8.
  * Pointers are aligned to their type.  Apart from
- * residual_out == residual (with equal strides) the buffers do not overlap.  rows may be 0 (nothing is done), cols is 1..2^20.
+ * residual_out == residual (with equal strides) the buffers do not overlap.  rows may be 0 (nothing is done); up to 2^22 - 1 rows are
+ * taken, of fewer than 4096 values more of them (a launch has less than 2^32 threads).  cols is 1..2^20.
  */
 typedef struct tq_norm_args {
   const void *residual;
@@ -418,7 +419,7 @@ typedef struct tq_cache {
  * NaN, if a value is not finite).
  * Where the cache has scores and positions, the slot's get 0 and positions[r].
  * A row whose sequence, slot or position is outside the cache or the table of angles is padding: it writes nothing to the
- * cache, and its q_out is zero.  No two rows may have the same slot of one sequence.
+ * cache, and its q_out is zero.  No two rows may have the same slot of one sequence.  Fewer than 2^24 rows.
  */
 #define TQ_ROTARY_HALVES 0u
 #define TQ_ROTARY_ADJACENT 1u

@@ -135,7 +135,7 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   if (a->rotary_dim % 8 || a->rotary_dim > c.head_dim) return refuse(TQ_E_UNSUPPORTED, who + ": rotary_dim must be a multiple of 8 up to head_dim");
   if (a->heads == 0 || a->heads > 65535) return refuse(TQ_E_INVALID_ARG, who + ": heads must be in 1..65535");
   if (a->rows == 0) return TQ_OK;
-  if (a->rows > 0x7FFFFFFFu) return refuse(TQ_E_UNSUPPORTED, who + ": too many rows");
+  if ((uint64_t)a->rows * kAppendThreads > 0xFFFFFFFFu) return refuse(TQ_E_UNSUPPORTED, who + ": too many rows for one launch");
   if (!a->q || !a->k || !a->v || !a->q_out || !a->slots || (a->rotary_dim && (!a->cos || !a->sin))) return refuse(TQ_E_INVALID_ARG, who + ": null pointer");
   if (!a->seqs && a->rows > c.n_seqs) return refuse(TQ_E_INVALID_ARG, who + ": more rows than sequences, and no seqs");
   const uint64_t q_row = (uint64_t)a->heads * c.head_dim, kv_row = (uint64_t)c.kv_heads * c.head_dim;

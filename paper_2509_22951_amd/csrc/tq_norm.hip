@@ -242,6 +242,7 @@ int add_rms_norm(const tq_norm_args* a, void* stream) {
   const uint32_t pieces = (a->cols + 3) / 4;
   const uint32_t chunks = pieces > 8192 ? 0 : pieces > 4096 ? 8 : pieces > 2048 ? 4 : pieces > 1024 ? 2 : 1;
   const uint32_t threads = chunks && chunks < 8 ? ((pieces + chunks - 1) / chunks + 63) / 64 * 64 : 1024;
+  if ((uint64_t)a->rows * threads > 0xFFFFFFFFu) return refuse(TQ_E_UNSUPPORTED, who + ": too many rows for one launch");
   hipStream_t s = (hipStream_t)stream;
   auto go = [&](auto whole) {
     constexpr bool W = decltype(whole)::value;

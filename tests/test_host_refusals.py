@@ -110,3 +110,12 @@ def test_every_call_refuses_keys_that_overlap(change):
 @pytest.mark.parametrize("change", [dict(page_stride=2048, head_stride=16, slot_stride=64, kv_heads=1), dict(page_stride=16, head_stride=1024, slot_stride=64, n_pages=1)])
 def test_the_stride_between_heads_or_pages_of_which_there_is_one_is_free(change):
     assert tq.Attend.workspace_bytes(tq.Cache(**{**CACHE, **change}), **ATTEND) > 0
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 22, 4096), (1 << 22, 1 << 20), (1 << 23, 2048), (1 << 26, 64)])
+def test_norm_refuses_more_rows_than_a_launch_has_threads_for(rows, cols):
+    assert "too many rows" in refused(UNSUPPORTED, lambda: tq.AddNorm(**{**NORM, "rows": rows, "cols": cols}).launch())
+
+
+def test_append_refuses_more_rows_than_a_launch_has_threads_for():
+    assert "too many rows" in refused(UNSUPPORTED, lambda: tq.CacheAppend(tq.Cache(**CACHE), **{**APPEND, "seqs": A, "rows": 1 << 24}).launch())
