@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, kHeads = 8;   // kHeads: query heads of a workgroup
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
-constexpr uint32_t kMaxGroups = 256, kMinShare = 1, kCluster = 16;   // workgroups of a launch (one per compute unit); units of one; parts that are joined at a time
+constexpr uint32_t kMaxGroups = 256, kCluster = 16;   // workgroups of a launch (one per compute unit); parts that are joined at a time
 constexpr uint64_t kPassing = 8 << 20;   // bytes of keys and values
 constexpr uint32_t kMostAligned = 16;   // units of a share
 constexpr uint32_t kCounters = 2 * (kMaxGroups / kCluster) + kMaxGroups;
@@ -52,8 +52,7 @@ __device__ __forceinline__ uint32_t row_length(const CacheView& c, const AttendV
   return (uint32_t)s < c.n_seqs ? (uint32_t)min(max(a.lengths[r], 0), (int32_t)c.capacity) : 0;
 }
 
-typedef __attribute__((address_space(4))) const int32_t constant_i32;
-typedef __attribute__((address_space(1), aligned(2))) const uint32_t global_cu32_any;   // (the memory unit takes 4 bytes from any 2-byte boundary)
+typedef __attribute__((address_space(1), aligned(2))) const uint32_t global_cu32_any;
 
 template <int DIM, bool INT8>
 struct Tile {
@@ -86,17 +85,6 @@ __device__ __forceinline__ void load_words(uint32_t* to, const char* from) {
 }
 
 __device__ __forceinline__ uint32_t units_of(uint32_t length) { return max((length + kUnit - 1) / kUnit, 1u); }   // (an empty row is written too)
-
-// Adds a wavefront-uniform running sum up over 64 lanes: inclusive prefix sums.
-__device__ __forceinline__ uint32_t prefix_sum(uint32_t v) {
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next one
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
-  return v;
-}
 
 // The largest of 64 lanes, in the last one.
 __device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
@@ -212,7 +200,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   uint32_t lane_length = 0, lane_seq = 0;   // of row (r & ~63) + lane
   auto look_at = [&](uint32_t first) {
     if (first + lane < a.rows) lane_length = row_length(c, a, first + lane, &lane_seq);
-    return prefix_sum(first + lane < a.rows ? units_of(lane_length) : 0u);
+    return wave_prefix_sum(first + lane < a.rows ? units_of(lane_length) : 0u);
   };
   uint32_t upto = 0, all = 0, longest = 0;   // longest: units of a row
   for (uint32_t first = (a.rows - 1) & ~63u;; first -= 64) {   // (the first rows last: they stay in the lanes)
@@ -222,7 +210,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     if (first == 0) break;
   }
   all *= a.chunks;
-  const uint32_t even = max(kMinShare, (all + gridDim.x - 1) / gridDim.x);
+  const uint32_t even = (all + gridDim.x - 1) / gridDim.x;
   uint32_t share = even, quantum = 1;
   // Where the shares are small, a share that has the end of one row and the start of another is joined twice, one after the other, and a row is in
   // more parts than it need be.  So every (row, chunk) is rounded up to whole quanta, and a share is whole quanta: the longest row's units, and no row is
@@ -233,7 +221,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   if (a.rows <= 64 && even <= kMostAligned && longest > 1 && (even > 1 || (DIM <= 64 && longest == 2))) {
     const uint32_t units = lane < a.rows ? units_of(lane_length) : 0;
     auto attempt = [&](uint32_t q, uint32_t most) {
-      const uint32_t quanta = prefix_sum((uint32_t)(((float)(units + q - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)q)));   // (exact: far fewer than 2^20 units)
+      const uint32_t quanta = wave_prefix_sum((uint32_t)(((float)(units + q - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)q)));   // (exact: far fewer than 2^20 units)
       const uint32_t total = scalar(__shfl(quanta, 63)) * a.chunks, mine = total <= gridDim.x ? q : (total + gridDim.x - 1) / gridDim.x * q;
       if (mine > most) return false;
       upto = quanta * q, all = total * q, share = mine, quantum = q;
@@ -640,7 +628,6 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
 __global__ __launch_bounds__(256) void k_attend_scores(CacheView c, AttendView a) {
   const uint32_t slot = (blockIdx.x * 256 + threadIdx.x) * 4, kv = blockIdx.y, s = blockIdx.z;
   if (slot >= c.capacity) return;   // (a multiple of 16)
-  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
   float* to = c.scores + ((uint64_t)s * c.kv_heads + kv) * c.capacity + slot;
   const f32x4_any were = *(const f32x4_any*)to;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -689,7 +676,7 @@ int check_attend(const std::string& who, const tq_cache* cache, const tq_attend_
   l->chunks = c->kv_heads * ((group + kHeads - 1) / kHeads);
   const uint64_t most = (uint64_t)a->rows * l->chunks * ((c->capacity + kUnit - 1) / kUnit);   // units, if all rows are full
   if (most >= (1u << 31) - kMaxGroups) return refuse(TQ_E_UNSUPPORTED, who + ": rows * heads * capacity is beyond what one call takes");
-  l->groups = (uint32_t)std::min<uint64_t>(kMaxGroups, std::max<uint64_t>(1, (most + kMinShare - 1) / kMinShare));
+  l->groups = (uint32_t)std::min<uint64_t>(kMaxGroups, std::max<uint64_t>(1, most));
   auto place = [&](uint64_t n) {
     const uint64_t at = l->bytes;
     l->bytes += (n + 255) / 256 * 256;

@@ -8,11 +8,6 @@ namespace {
 
 constexpr int kAppendThreads = 256, kMostItems = 6;
 
-// (the memory unit takes 16 bytes from any 4-byte boundary, 8 from any 2-byte one)
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-
 struct AppendView {
   const float *q, *k, *v;
   void* q_out;
@@ -30,7 +25,6 @@ struct AppendView {
 // Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits, bf16 q: 56 us); for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
 template <int LANES, bool INT8, bool Q16>
 __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
-  typedef __attribute__((address_space(4))) const int32_t constant_i32;
   constexpr uint32_t kGroups = kAppendThreads / LANES;
   const uint32_t r = blockIdx.x, D = c.head_dim;
   const uint32_t t = threadIdx.x % LANES, i = 4 * t, first_head = blockIdx.y * (a.items * kGroups) + threadIdx.x / LANES;
@@ -203,16 +197,6 @@ __device__ __forceinline__ uint32_t rank_of(float score, bool is_protected) {
   if (score != score) return 0;
   const uint32_t b = __float_as_uint(score + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-
-__device__ __forceinline__ uint32_t wave_prefix_sum(uint32_t v) {   // inclusive
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next one
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
-  return v;
 }
 
 // The ranks of slots first + k * stride .. + 3 of a list, whose slots begin at `row`; those from `length` on are read as the list's first ones.  All

@@ -22,6 +22,14 @@ struct CacheView {
   uint32_t n_pages, page_shift, kv_heads, head_dim, n_seqs, seq_pages, capacity;
 };
 
+// Values at any address that their type allows: the memory unit takes 16 bytes from any 4-byte boundary as it does from a 16-byte one, 4 and 8 from any 2-byte one.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef __attribute__((address_space(4))) const int32_t constant_i32;   // not written while a kernel runs: read through the scalar cache
+
 inline int refuse(int code, const std::string& what) {
   set_error(what);
   return code;
@@ -101,6 +109,17 @@ template <int N>
 __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
   for (int d = 1; d < N; d *= 2) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Sums over a wavefront's lanes up to and with each.
+__device__ __forceinline__ uint32_t wave_prefix_sum(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next one
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // lane 31 to the upper half
   return v;
 }
 

@@ -19,13 +19,7 @@ struct NormView {
   float eps;
 };
 
-// Four values at a time, at any address that their type allows: the memory unit takes 16 bytes from a 4-byte boundary as it
-// does from a 16-byte one.
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32_any __attribute__((aligned(1)));
-
-// Values i..i+3 of a row of n, fp32 or bf16; those beyond it are zero.  WHOLE: n is a multiple of 4.
+// Four values at a time, at any address that their type allows: values i..i+3 of a row of n, fp32 or bf16; those beyond it are zero.  WHOLE: n is a multiple of 4.
 template <bool WHOLE, bool BF16>
 __device__ __forceinline__ void load_values(const void* row, uint32_t i, uint32_t n, float (&v)[4]) {
   if (WHOLE || i + 4 <= n) {
