@@ -145,13 +145,11 @@ class Decoder:
             self._run()
             return self.logits
         if self.graph is None:
-            state = [t.clone() for t in (self.slots, self.lengths, self.positions, self.since, self.left)]
-            side, self.graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+            graph = torch.cuda.CUDAGraph()
             torch.cuda.synchronize()
-            with torch.cuda.graph(self.graph, stream=side):
+            with torch.cuda.graph(graph, stream=torch.cuda.Stream()):   # (recorded, not run)
                 self._run()
-            for t, was in zip((self.slots, self.lengths, self.positions, self.since, self.left), state):
-                t.copy_(was)
+            self.graph = graph
         self.graph.replay()
         return self.logits
 
