@@ -8,9 +8,9 @@
 //   supplies the same tokens as its 8 values of the contraction, so P is already where it is needed; it loads DIM / 16
 //   neighbouring dims of those 8 tokens' values and transposes that square in its registers (one v_perm per pair).
 // The 16 columns are 8 heads twice: column c holds the upper 8 bits of head c's mantissas, column c + 8 the next 8, and a second
-// product has the last 8 beside zeros, so that q and p enter with all of fp32's 24 bits.  (p with 16 of them, one product: no faster with
-// bf16 caches of up to 128 dims, 1 % with 256, in 8 bits 2 % of 128 dims and 5 % of 64, where the vector units are busy; but up to 2^-17 of
-// each weight off, more than all else together: a result next to the middle of two bf16 values went to the other one in one of a thousand.)
+// product has the last 8 beside zeros, so that q and p enter with all of fp32's 24 bits.  (p with 16 of them, one product: the same time within
+// 1 % but for 200 tokens, 5.8 us in place of 6.0; but up to 2^-17 of each weight off, more than all else together: a result next to the
+// middle of two bf16 values went to the other one in one of a thousand.)
 #include <algorithm>
 
 #include "tq_cache_view.h"
@@ -444,16 +444,23 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       total *= shrink;
 #pragma unroll
       for (int b = 0; b < T::kVals; ++b) o[b] *= shrink;
-      bf16x8 p0, p1;
+      uint32_t p0[4], p1[4];   // pairs of tokens
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float w = __builtin_amdgcn_exp2f(p[i] - base);
-        total += w;
-        if constexpr (INT8) w = p[i] != -INFINITY ? w * (&x.vs[i / 4].x)[i % 4] : 0.f;   // (a masked token's scale may be anything)
-        const __bf16 hi = (__bf16)w, mid = (__bf16)(w - (float)hi), lo = (__bf16)(w - (float)hi - (float)mid);
-        p0[i] = part ? mid : hi;
-        p1[i] = part ? (__bf16)0.f : lo;
+      for (int i = 0; i < 8; i += 2) {
+        float w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          w[j] = __builtin_amdgcn_exp2f(p[i + j] - base);
+          total += w[j];
+          if constexpr (INT8) w[j] = p[i + j] != -INFINITY ? w[j] * (&x.vs[i / 4].x)[i % 4 + j] : 0.f;   // (a masked token's scale may be anything)
+        }
+        const uint32_t hi = pack_bf16(w[0], w[1]);
+        w[0] -= bf16_value(hi), w[1] -= __uint_as_float(hi & 0xFFFF0000u);
+        const uint32_t mid = pack_bf16(w[0], w[1]);
+        w[0] -= bf16_value(mid), w[1] -= __uint_as_float(mid & 0xFFFF0000u);
+        p0[i / 2] = part ? mid : hi, p1[i / 2] = part ? 0 : pack_bf16(w[0], w[1]);
       }
+      const bf16x8 upper = __builtin_bit_cast(bf16x8, make_uint4(p0[0], p0[1], p0[2], p0[3])), lower = __builtin_bit_cast(bf16x8, make_uint4(p1[0], p1[1], p1[2], p1[3]));
 #pragma unroll
       for (int b = 0; b < T::kVals; ++b) {
         uint32_t vt[4];
@@ -467,8 +474,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
           }
         }
         const bf16x8 value = __builtin_bit_cast(bf16x8, make_uint4(vt[0], vt[1], vt[2], vt[3]));
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, p0, o[b], 0, 0, 0);
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, p1, o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, upper, o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, lower, o[b], 0, 0, 0);
+        if constexpr (INT8) asm volatile("" : "+v"(o[b]));   // (values are widened as they are needed: all of them ahead, 256 dims spill 47 registers, 54 -> 70 us)
       }
       __builtin_amdgcn_sched_barrier(0);
       fetch_values(next);
