@@ -23,7 +23,7 @@ constexpr int kAttendWaves = 8, kAttendThreads = kAttendWaves * 64, kTile = 32, 
 constexpr uint32_t kUnit = kAttendWaves * kTile;                          // tokens that a workgroup takes at a time
 constexpr uint32_t kMaxGroups = 256, kCluster = 16;   // workgroups of a launch (one per compute unit); parts that are joined at a time
 constexpr uint64_t kPassing = 8 << 20;   // bytes of keys and values
-constexpr uint32_t kMostAligned = 16;   // units of a share
+constexpr uint32_t kMostAligned = 16;   // units of a share (8 and 32: no difference seen)
 constexpr uint32_t kCounters = 2 * (kMaxGroups / kCluster) + kMaxGroups;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -212,13 +212,18 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   all *= a.chunks;
   const uint32_t even = (all + gridDim.x - 1) / gridDim.x;
   uint32_t share = even, quantum = 1;
-  // Where the shares are small, a share that has the end of one row and the start of another is joined twice, one after the other, and a row is in
-  // more parts than it need be.  So every (row, chunk) is rounded up to whole quanta, and a share is whole quanta: the longest row's units, and no row is
-  // cut, or the fewest from an even share on with which every part has a workgroup.  A compute unit alone draws 41 bytes per ns, among all of them 24, so that
-  // shares that differ by a half do not take longer by as much; a join takes about 4 us.  Of 64 dims, 16 x 700 tokens: 15.3 -> 11.1 us, 16 ragged ones up to 1000
-  // 14.6 -> 12.2; of 128, 16 x 1250 24.9 -> 22.8, 2 x 20000 37.8 -> 36.0; where rows were cut evenly before, 0.1 to 0.4 us more.  Longer shares take their next row's
-  // loads while they join, and are cut anywhere.
-  if (a.rows <= 64 && even <= kMostAligned && longest > 1 && (even > 1 || (DIM <= 64 && longest == 2))) {
+  // Where the shares are small, a share that has the end of one row and the start of another is joined twice, one after the other, and a row
+  // is in more parts than it need be.  So every (row, chunk) is rounded up to whole quanta, and a share is whole quanta: the longest row's
+  // units, and no row is cut, or the fewest from an even share on with which every part has a workgroup.  Shares may be half as
+  // long again for that: a compute unit alone draws 41 bytes per ns, among all of them 24, and a join takes about 4 us.  Cut anywhere
+  // and so, us: 16 x 700 tokens of 64 dims 14.5 and 11.2, of 128 20.1 and 18.0; 16 x 1250 17.5 and 14.7, 25.9 and 22.4; 2 x 20000 23.0 and
+  // 20.9, 35.7 and 33.4; 16 ragged rows up to 2000 17.3 and 15.2, 24.2 and 22.1; but 12 x 2200 of 128 28.6 and 30.0.
+  // A row of a few units is better not cut at all, the fewer bytes its tokens have: up to four units of keys of 64 bytes (16 x 1000 of 32 dims 10.8,
+  // cut 12.3; of 64 in 8 bits 12.0, 12.4; but of 64 in 16 bits 13.4, 12.5, of 128 22.8, 18.2), three of all others (16 x 700 of 64 dims 11.2, 12.2; of
+  // 96 15.1, 15.6; of 128 18.0, 17.5).  Where there is a workgroup for every unit, two units of up to 128 bytes (4 x 500 of 64 dims 8.0, cut 8.6, in 8 bits
+  // 8.2, 8.8; of 128 12.8, 11.5).  Shares of more than kMostAligned units take their next row's loads while they join, and are cut anywhere.
+  constexpr uint32_t kMostBytes = (INT8 ? 1 : 2) * DIM;   // (of a key of this variant: a rule on D would cost the others 0.3 us)
+  if (a.rows <= 64 && even <= kMostAligned && longest > 1 && (even > 1 || (longest == 2 && kMostBytes <= 128))) {
     const uint32_t units = lane < a.rows ? units_of(lane_length) : 0;
     auto attempt = [&](uint32_t q, uint32_t most) {
       const uint32_t quanta = wave_prefix_sum((uint32_t)(((float)(units + q - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)q)));   // (exact: far fewer than 2^20 units)
@@ -227,8 +232,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       upto = quanta * q, all = total * q, share = mine, quantum = q;
       return true;
     };
-    bool done = longest <= (DIM <= 64 ? 4 : 3) && attempt(longest, even + (even > 1 ? 2 : 1));
-    const uint32_t most = even + (even > 4 ? even / 4 : even / 2);
+    bool done = longest <= (DIM <= 64 && (INT8 ? 1 : 2) * D <= 64 ? 4 : 3) && attempt(longest, even + (even > 1 ? 2 : 1));
+    const uint32_t most = even + even / 2;
     for (uint32_t q = even; q <= most && !done; ++q) done = attempt(q, most);
   }
   uint32_t pos = blockIdx.x * share;
