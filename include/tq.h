@@ -349,7 +349,8 @@ int tq_listing_destroy(tq_listing h);
  * it, and a cache that is kept at a budget.  The products give fp32 y and take bf16 x, and so do these calls.
  *
  * All of them run on the caller's stream and return: no synchronisation, no allocation, nothing kept between calls (but zeros in
- * the workspace of tq_attend), so they may be captured in a HIP graph.  Argument structures are read during the call; zero-initialise them and set what you need.
+ * the workspace of tq_attend), so they may be captured in a HIP graph.  Argument structures are read during the call; zero-initialise
+ * them and set what you need.
  * Strides count elements; 0 stands for rows without gaps.
  */
 #define TQ_BF16 0u
@@ -359,8 +360,8 @@ int tq_listing_destroy(tq_listing h);
 /*
  * h = residual + delta, in fp32;  residual_out = h in the residual's type;  y = h / sqrt(mean(h^2) + eps) * weight, from the
  * unrounded h;  out = y as bf16 (the x of the next product), or as int8 with one scale per row by the rule of the weights
- * (tq_encode): scale = max|y| / 127, round half to even.  Sums in fp32.  A row with a NaN is NaN throughout, one with an infinity NaN there and zero elsewhere; as int8 its
- * scale is NaN.
+ * (tq_encode): scale = max|y| / 127, round half to even.  Sums in fp32.  A row with a NaN is NaN throughout, one with an infinity NaN
+ * there and zero elsewhere; as int8 its scale is NaN.
  *   residual, residual_out: device, [rows][cols], TQ_FP32 or TQ_BF16 (residual_type); residual_out may be residual, or NULL.
  *   delta: device, fp32 [rows][cols], a product's y, or NULL (nothing is added).
  *   weight: device, [cols], TQ_FP32 or TQ_BF16 (weight_type).
@@ -415,8 +416,8 @@ typedef struct tq_cache {
  *   cos, sin: device, fp32 [n_positions][rotary_dim / 2].  The first rotary_dim values of a head (a multiple of 8, 0: none) are
  *   rotated in pairs (a, b) -> (a cos - b sin, a sin + b cos): value i with value i + rotary_dim / 2 (TQ_ROTARY_HALVES), or 2i with 2i + 1
  *   (TQ_ROTARY_ADJACENT).
- * Values go into a TQ_BF16 cache rounded to nearest even (to an infinity from 3.396e38 on), into a TQ_INT8 cache by the rule of the weights (scale = absmax / 127;
- * NaN, if a value is not finite).
+ * Values go into a TQ_BF16 cache rounded to nearest even (to an infinity from 3.396e38 on), into a TQ_INT8 cache by the rule of the
+ * weights (scale = absmax / 127; NaN, if a value is not finite).
  * Where the cache has scores and positions, the slot's get 0 and positions[r].
  * A row whose sequence, slot or position is outside the cache or the table of angles is padding: it writes nothing to the
  * cache, and its q_out is zero.  No two rows may have the same slot of one sequence.  Fewer than 2^24 rows.
@@ -440,8 +441,8 @@ int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *str
  * Row r belongs to sequence seqs[r] (NULL: sequence r).  Rows of one sequence with rising lengths are a prompt or a draft, causally masked.
  *   q: device, TQ_FP32 or TQ_BF16 (q_type) [rows][heads * head_dim]; an fp32 q is used unrounded.
  *   out: device, bf16 [rows][heads * head_dim]: the x of the output projection.
- *   lengths: device, int32 [rows], not written while the call runs; lengths beyond the capacity count as the capacity.  A row without tokens (length <= 0, a
- *   sequence that is not there, only pages that are not there) gives zeros.
+ *   lengths: device, int32 [rows], not written while the call runs; lengths beyond the capacity count as the capacity.  A row without
+ *   tokens (length <= 0, a sequence that is not there, only pages that are not there) gives zeros.
  *   accumulate: 1 adds every token's weight, summed over the query heads of a key/value head, to cache->scores (capacity: at most
  *   2^25 tokens).
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_workspace gives for the same arguments, zero before the first
@@ -450,8 +451,9 @@ int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *str
  *   overlaps need one each.
  * Queries, logits, weights, softmax statistics and sums are fp32, none of them rounded to fewer bits; sums are made in an order that only the
  * arguments and lengths decide, so results repeat.
- * What is not finite within a row's length does what it does in the formula, slowly: a key that gives a logit of -infinity takes its token's weight
- * (all of them: zeros), one that gives +infinity or NaN makes that head's result NaN, an infinite or NaN value reaches its own dim, whatever its weight.
+ * What is not finite within a row's length does what it does in the formula, slowly: a key that gives a logit of -infinity takes its
+ * token's weight (all of them: zeros), one that gives +infinity or NaN makes that head's result NaN, an infinite or NaN value reaches its
+ * own dim, whatever its weight.
  * What lies in a cache beyond a row's length is not used, whatever it holds.  heads is a multiple of kv_heads.
  */
 typedef struct tq_attend_args {

@@ -9,7 +9,7 @@
 //   neighbouring dims of those 8 tokens' values and transposes that square in its registers (one v_perm per pair).
 // The 16 columns are 8 heads twice: column c holds the upper 8 bits of head c's mantissas, column c + 8 the next 8, and a second
 // product has the last 8 beside zeros, so that q and p enter with all of fp32's 24 bits.  (p with 16 of them, one product: the same time within
-// 1 % but for 200 tokens, 5.8 us in place of 6.0; but up to 2^-17 of each weight off, more than all else together: a result next to the
+// 2 %, 200 tokens 5.8 us in place of 6.0; but up to 2^-17 of each weight off, more than all else together: a result next to the
 // middle of two bf16 values went to the other one in one of a thousand.)
 #include <algorithm>
 
@@ -63,9 +63,9 @@ struct Tile {
   float4 ks[2], vs[2];
 };
 
-// Where loads that pass the caches by are faster: no byte is loaded twice.  16 x 16384 tokens of 128 dims 187 -> 170 us, 16 x 32768 of 64 189 -> 172, in 8 bits of 128
-// 200 -> 187, 4 x 32768 of 256 99 -> 93; 1 x 16000 of 96 16.1 -> 15.4; but of 80 and 48, whose rows
-// begin anywhere in a line, 16 x 8000 37 -> 41 and 93 -> 101, and of 64 in 8 bits no gain.
+// Where loads that pass the caches by are faster: no byte is loaded twice.  Through the caches and past them, us: 16 x 16384 tokens of 128 dims
+// 180 and 166, 16 x 32768 of 64 190 and 176, of 128 in 8 bits 201 and 188, 4 x 32768 of 256 99 and 93; 1 x 16000 of 96 16.2 and 15.5 (2 x 50000
+// 37 and 38); but of 80 and 48, whose rows begin anywhere in a line, 16 x 8000 64 and 72, 42 and 43, and of 64 in 8 bits no gain.
 template <int DIM, bool INT8>
 constexpr bool kPasses = DIM >= 128 || !INT8;
 
@@ -101,9 +101,10 @@ struct Segment {   // the part of a (row, chunk) that lies in a workgroup's shar
   uint32_t r, seq, kv, first_head, n_heads, pair_first, units, begin, end, rounds;   // rounds of kUnit tokens, the same for every wavefront
 };
 
-// A wavefront's tokens of a segment once more, a product per value as the formula has them, so that infinities give what they give there.  The
-// results replace those in LDS (and the logits).  32 tokens at a time, two lanes per key, then a lane per dim of the values: slow, and only for what is
-// not finite.  What it needs is read again from the kernel's arguments, and nothing of it computed ahead: the tile loop has no registers for it.
+// A wavefront's tokens of a segment once more, a product per value as the formula has them, so that infinities give what they give there.
+// The results replace those in LDS (and the logits).  32 tokens at a time, two lanes per key, then a lane per dim of the values: slow, and
+// only for what is not finite (8 x 8192 tokens, 8 heads of 128: 47 us, with one infinite key 352, with infinities in all keys 1017).  What it
+// needs is read again from the kernel's arguments, and nothing of it computed ahead: the tile loop has no registers for it.
 template <int DIM, bool INT8, bool TRACK>
 __device__ __forceinline__ void take_again(const Segment& s, uint32_t lane, uint32_t wave, float* lds_sum, float* lds_max, float* lds_total) {
   typedef __attribute__((address_space(4))) const char constant_char;
@@ -171,14 +172,16 @@ __device__ __forceinline__ void take_again(const Segment& s, uint32_t lane, uint
   }
 }
 
-// Bound: reading the cache.  16 x 32768 tokens, 8 heads of 64 in bf16: 172 us, 6.2 TB/s; 1 x 131072 of 128: 88, 6.1; in 8 bits 16 x 32768 of 128: 175..185, 6.1, with the
-// vector units at about 90 % (conversion to bf16); 4 x 32768, 4 heads of 256: 93, 5.8.  Few tokens: launch, lengths, page table, keys and values, join, 5.7 us for 200 tokens.
+// Bound: reading the cache.  16 x 32768 tokens, 8 heads of 64 in bf16: 170..176 us, 6.1..6.3 TB/s; 1 x 131072 of 128: 87..92, 5.8..6.2; in 8 bits
+// 16 x 32768 of 128: 174..190, 5.8..6.4, with the vector units busy nearly all of the time (conversion to bf16); 4 x 32768, 4 heads of 256: 93, 5.8.
+// Few tokens: launch, lengths, page table, keys and values, join, 6.0 us for 200 tokens.
 //
-// All (row, chunk, unit of kUnit tokens) in this order are one line, cut into equal shares, one per workgroup: whatever the
-// lengths, every workgroup has as much to do.  Eight wavefronts (one workgroup per compute unit) hold as much on its way as the memory needs: twelve and sixteen,
-// or two workgroups per unit, leave too few registers for a tile ahead (16 x 16384 of 128: 188, 198, 281, 191 us).  A (row, chunk) that lies in one share is finished there; of one that is cut every
-// workgroup leaves its maximum, total and weighted sum in memory and counts itself in, and the last one joins them, in the order
-// of the line; more than kCluster parts are joined by clusters first.  Nobody waits for anybody.
+// All (row, chunk, unit of kUnit tokens) in this order are one line, cut into equal shares, one per workgroup: whatever the lengths, every
+// workgroup has as much to do.  Eight wavefronts (one workgroup per compute unit) hold as much on its way as the memory needs: twelve and
+// sixteen, or two workgroups per unit, leave too few registers for a tile ahead (16 x 16384 of 128: 188, 198, 281, 191 us).  A (row, chunk)
+// that lies in one share is finished there; of one that is cut every workgroup leaves its maximum, total and weighted sum in memory and
+// counts itself in, and the last one joins them, in the order of the line; more than kCluster parts are joined by clusters first.  Nobody
+// waits for anybody.
 //
 // A wavefront asks for the next tile's keys as soon as the logits of this one are made, and for its values when they are multiplied
 // in, also where the next tile is another row's: a row's end is worked on while the next one's first tile is on its way.  All of
@@ -214,14 +217,17 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   uint32_t share = even, quantum = 1;
   // Where the shares are small, a share that has the end of one row and the start of another is joined twice, one after the other, and a row
   // is in more parts than it need be.  So every (row, chunk) is rounded up to whole quanta, and a share is whole quanta: the longest row's
-  // units, and no row is cut, or the fewest from an even share on with which every part has a workgroup.  Shares may be half as
-  // long again for that: a compute unit alone draws 41 bytes per ns, among all of them 24, and a join takes about 4 us.  Cut anywhere
-  // and so, us: 16 x 700 tokens of 64 dims 14.5 and 11.2, of 128 20.1 and 18.0; 16 x 1250 17.5 and 14.7, 25.9 and 22.4; 2 x 20000 23.0 and
-  // 20.9, 35.7 and 33.4; 16 ragged rows up to 2000 17.3 and 15.2, 24.2 and 22.1; but 12 x 2200 of 128 28.6 and 30.0.
-  // A row of a few units is better not cut at all, the fewer bytes its tokens have: up to four units of keys of 64 bytes (16 x 1000 of 32 dims 10.8,
-  // cut 12.3; of 64 in 8 bits 12.0, 12.4; but of 64 in 16 bits 13.4, 12.5, of 128 22.8, 18.2), three of all others (16 x 700 of 64 dims 11.2, 12.2; of
-  // 96 15.1, 15.6; of 128 18.0, 17.5).  Where there is a workgroup for every unit, two units of up to 128 bytes (4 x 500 of 64 dims 8.0, cut 8.6, in 8 bits
-  // 8.2, 8.8; of 128 12.8, 11.5).  Shares of more than kMostAligned units take their next row's loads while they join, and are cut anywhere.
+  // units, and no row is cut, or the fewest from an even share on with which every part has a workgroup.  Cut anywhere and so, us: 16 x 700
+  // tokens of 64 dims 14.5 and 11.2, of 128 20.1 and 18.0; 16 x 1250 17.5 and 14.7, 25.9 and 22.4; 2 x 20000 23.0 and 20.9, 35.7 and 33.4; 16
+  // ragged rows up to 2000 17.3 and 15.2, 24.2 and 22.1; but 12 x 2200 of 128 28.6 and 30.0.
+  // Shares may be longer than even ones for that, since a compute unit alone draws 41 bytes per ns, among all of them 24, and a join takes
+  // about 4 us: by a half up to four units (in 8 bits, 128 dims, 16 ragged rows up to 1500 17.1, by a quarter 18.6; up to 2500 20.5, 21.8),
+  // by a quarter beyond (16 ragged rows up to 6000 43.4, by a half 47.4; 12 x 7000 of 64 dims 38, 42, of 128 64.5, 72).
+  // A row of a few units is better not cut at all, the fewer bytes its tokens have: up to four units of keys of 64 bytes (16 x 1000 of 32
+  // dims 10.8, cut 12.3; of 64 in 8 bits 12.0, 12.4; but of 64 in 16 bits 13.4, 12.5, of 128 22.8, 18.2), three of all others (16 x 700 of 64
+  // dims 11.2, 12.2; of 96 15.1, 15.6; of 128 18.0, 17.5).  Where there is a workgroup for every unit, two units of up to 128 bytes (4 x 500
+  // of 64 dims 8.0, cut 8.6, in 8 bits 8.2, 8.8; of 128 12.8, 11.5).
+  // Shares of more than kMostAligned units take their next row's loads while they join, and are cut anywhere.
   constexpr uint32_t kMostBytes = (INT8 ? 1 : 2) * DIM;   // (of a key of this variant: a rule on D would cost the others 0.3 us)
   if (a.rows <= 64 && even <= kMostAligned && longest > 1 && (even > 1 || (longest == 2 && kMostBytes <= 128))) {
     const uint32_t units = lane < a.rows ? units_of(lane_length) : 0;
@@ -233,7 +239,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
       return true;
     };
     bool done = longest <= (DIM <= 64 && (INT8 ? 1 : 2) * D <= 64 ? 4 : 3) && attempt(longest, even + (even > 1 ? 2 : 1));
-    const uint32_t most = even + (even > 4 ? even / 4 : even / 2);   // (of the shares: a half longer all the way, 16 ragged rows up to 6000 43.4 -> 47.4 us)
+    const uint32_t most = even + (even > 4 ? even / 4 : even / 2);
     for (uint32_t q = even; q <= most && !done; ++q) done = attempt(q, most);
   }
   uint32_t pos = blockIdx.x * share;
@@ -254,10 +260,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   }
   if (r >= a.rows) return;   // (lengths that change under the call)
 
-  // a lane's places in a block of 16 tokens: for dims that a head does not have all lanes read the block's first ones, against zeros of q, and drop them.
-  // With 256 dims of bf16 the tiles alone take 192 registers of the 256, and what spills waits for all that is on its way: there one
-  // offset serves all loads of keys (where a head ends before a load's dims, it has the head's last ones once more), and the
-  // two halves of the columns fetch half of q each (4 x 32768 tokens through the L2s: 110 -> 99 us).  Elsewhere that only adds to a call's start, 0.1 to 0.5 us of 6 or 7.
+  // a lane's places in a block of 16 tokens: for dims that a head does not have all lanes read the block's first ones, against zeros of q,
+  // and drop them. With 256 dims of bf16 the tiles alone take 192 registers of the 256, and what spills waits for all that is on its way:
+  // there one offset serves all loads of keys (where a head ends before a load's dims, it has the head's last ones once more), and the two
+  // halves of the columns fetch half of q each (4 x 32768 tokens through the L2s: 110 -> 99 us).  Elsewhere that only adds to a call's start,
+  // 0.1 to 0.5 us of 6 or 7.
   constexpr bool kTight = DIM == 256 && !INT8;
   constexpr uint32_t kSize = INT8 ? 1 : 2, kSpan = INT8 ? 64 : 32, kOffsets = kTight ? 1 : T::kLoads, kFetched = kTight ? 4 : 8;
   const uint32_t slot_bytes = kSize * (uint32_t)c.slot_stride;
@@ -265,8 +272,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
   uint32_t key_at[kOffsets];
 #pragma unroll
   for (uint32_t s = 0; s < kOffsets; ++s) key_at[s] = kSpan * kSize * s + 16 * g < kSize * D ? n * slot_bytes + kSpan * kSize * s + 16 * g : 0;
-  // A lane's dims of a value are neighbours.  Where they are two loads that pass the caches, each has eight neighbours and the second those of the head's
-  // last 128: two from the same lines would read these twice.
+  // A lane's dims of a value are neighbours.  Where they are two loads that pass the caches, each has eight neighbours and the second those
+  // of the head's last 128: two from the same lines would read these twice.
   constexpr bool kApart = PASSES && T::kValWords > 4;
   constexpr uint32_t kNear = kApart ? T::kVals / 2 : T::kVals;
   const uint32_t val_at = n * kNear < D ? 4 * g * slot_bytes + kSize * n * kNear : 0, second_at = kSize * (D - 128);
@@ -366,7 +373,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(CacheView c, Atten
     static_assert(T::kSteps <= kAttendWaves, "a wavefront per step of q");
     bf16x8 q0, q1;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {   // (by all wavefronts: a load that some of them never use would be waited for in the loop, and with it those behind it)
+    for (int j = 0; j < 8; ++j) {   // (by all wavefronts: a load that some of them never use would be waited for in the loop)
       const uint32_t own = a.q16 ? q_words[j % kFetched / 2] : q_words[j % kFetched], other = kTight ? ror8(own) : own, word = (j < 4) == (part == 0) ? own : other;
       const float one = __uint_as_float((word << (a.q16 && j % 2 == 0 ? 16 : 0)) & (a.q16 ? 0xFFFF0000u : ~0u));
       const float v = head < s.n_heads && has_q ? one * a.scale : 0.f;
@@ -738,10 +745,11 @@ int attend(const tq_cache* cache, const tq_attend_args* a, void* stream) {
                      (a->out_stride ? a->out_stride : row) % 4 == 0 && aligned_to(a->out, 8)};
   const bool int8 = cache->type == TQ_INT8;
   hipStream_t s = (hipStream_t)stream;
-  // Little may still be in the L2s (200 tokens of 128 dims 7.2 us, passing them by 7.9; 8 x 1000 of 64 10.7 and 10.1), and what several rows of a sequence or several
-  // chunks of query heads read shall stay there (32 heads on 2, 16 x 8000 tokens 44 and 51).
+  // Little may still be in the L2s (200 tokens of 128 dims 7.5 us, passing them by 8.3; 8 x 1000 of 64 10.8 and 10.3), and what several rows of a
+  // sequence or several chunks of query heads read shall stay there (32 heads on 2, 16 x 8000 tokens 44.5 and 50).  By the capacity, since only
+  // the GPU knows the lengths.
   const uint64_t bytes = (uint64_t)a->rows * c.kv_heads * c.capacity * c.head_dim * (int8 ? 2 : 4);
-  // (256 dims of bf16: 33 MB 19 us and 21, 67 MB 32 and 30.5.)
+  // (256 dims of bf16: 33 MB 19.2 us and 19.6, 66 MB 23.9 and 23.4; of 208, whose last 128 overlap the first, 4 x 8000 28.7 and 34.7.)
   const bool passes = !a->seqs && l.chunks == c.kv_heads && bytes >= (c.head_dim == 256 && !int8 ? 8 * kPassing : kPassing) &&
                       c.head_dim % 32 == 0 && c.head_dim >= (c.head_dim <= 128 ? 64 : int8 ? 192 : 256);
   if (c.head_dim <= 64) launch_attend<64>(c, v, l.groups, int8, a->accumulate, passes, s);

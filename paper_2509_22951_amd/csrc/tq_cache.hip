@@ -22,7 +22,8 @@ struct AppendView {
 // rotation lies rotary_dim / 2 values apart: its other half comes from another lane of the same group, so a wavefront has read all
 // of a head before it writes any (q_out may be q), and 8 bits' absmax is a maximum over the group.
 //
-// Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits, bf16 q: 56 us); for a few rows the chain slot -> page -> store, beside slot -> angles -> rotation.
+// Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits, bf16 q: 56 us); for a few rows the chain slot -> page -> store,
+// beside slot -> angles -> rotation.
 template <int LANES, bool INT8, bool Q16>
 __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
   constexpr uint32_t kGroups = kAppendThreads / LANES;
@@ -31,7 +32,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, Ap
   const uint32_t n_heads = a.heads + 2 * c.kv_heads;
   const int32_t seq = a.seqs ? ((constant_i32*)a.seqs)[r] : (int32_t)r, slot = ((constant_i32*)a.slots)[r], pos = a.positions ? ((constant_i32*)a.positions)[r] : slot;
   const bool there = (uint32_t)seq < c.n_seqs && (uint32_t)slot < c.capacity && (a.rotary_dim == 0 || (uint32_t)pos < a.n_positions);
-  f32x4_any x[kMostItems];   // requested ahead of what decides whether the row is there; read once (512 rows of 40 heads of 128: 8.7 us, past the caches 7.9)
+  f32x4_any x[kMostItems];   // ahead of what decides whether the row is there; read once (512 rows of 40 heads of 128: 8.7 us, past the caches 7.9)
 #pragma unroll
   for (int k = 0; k < kMostItems; ++k) {
     if (k && k >= (int)a.items) break;
@@ -147,9 +148,9 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   const bool int8 = cache->type == TQ_INT8;
   const uint32_t lanes = c.head_dim <= 16 ? 4 : c.head_dim <= 32 ? 8 : c.head_dim <= 64 ? 16 : c.head_dim <= 128 ? 32 : 64;
   const uint32_t n_heads = a->heads + 2 * c.kv_heads, groups = kAppendThreads / lanes, rounds = (n_heads + groups - 1) / groups;
-  // A head per group of lanes, until there are many more workgroups than the GPU holds; then several per group, so that their loads are on their way
-  // together, and as evenly as they divide, since a group without a head waits with the others (40 heads of 128 in 8 bits, through the caches: 8192 rows 75 us with one,
-  // 68 with four and one in turn, 62 with five; 1024 rows 12.6 with one, 13.7 with five).
+  // A head per group of lanes, until there are many more workgroups than the GPU holds; then several per group, so that their loads are on
+  // their way together, and as evenly as they divide, since a group without a head waits with the others (40 heads of 128 in 8 bits, through
+  // the caches: 8192 rows 75 us with one, 68 with four and one in turn, 62 with five; 1024 rows 12.6 with one, 13.7 with five).
   const uint32_t most = (uint64_t)a->rows * rounds > 16384 ? kMostItems : 1, parts = (rounds + most - 1) / most;
   v.items = (rounds + parts - 1) / parts;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, parts), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v); };
@@ -199,10 +200,10 @@ __device__ __forceinline__ uint32_t rank_of(float score, bool is_protected) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The ranks of slots first + k * stride .. + 3 of a list, whose slots begin at `row`; those from `length` on are read as the list's first ones.  All
-// loads are requested before any of them is used, and without a condition: behind one they would come one after another (8 lists
-// of 16384 slots, all of the call: 24.1 us in place of 19.9).  copies: what stays in its place goes to scores_out and positions_out, with what will be written over there
-// by a token that is moved.
+// The ranks of slots first + k * stride .. + 3 of a list, whose slots begin at `row`; those from `length` on are read as the list's first
+// ones.  All loads are requested before any of them is used, and without a condition: behind one they would come one after another (8 lists
+// of 16384 slots, all of the call: 24.1 us in place of 19.9).  copies: what stays in its place goes to scores_out and positions_out, with
+// what will be written over there by a token that is moved.
 template <int STRIDES>
 __device__ __forceinline__ void ranks_at(const CacheView& c, const EvictView& e, uint64_t row, uint32_t first, uint32_t stride, uint32_t length, int32_t since, bool copies,
                                          uint32_t (&rank)[STRIDES][4]) {
@@ -256,9 +257,9 @@ __device__ __forceinline__ Bin find_bin(const uint32_t* sums, uint32_t left) {  
   return {255 - (uint32_t)__builtin_amdgcn_readlane((int)b, one), (uint32_t)__builtin_amdgcn_readlane((int)over, one), (uint32_t)__builtin_amdgcn_readlane((int)in, one)};
 }
 
-// Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., AHEAD of them
-// together (a token is a chain of list, page tables, then its bytes).  No slot is both written and read.  Bound: memory, for many tokens (16 x 8 lists, 4096
-// rows of 256 bytes of keys and of values each: 117 us, 4.6 TB/s read and written).
+// Moves keys, values, scales and marks of a list's tokens: a group of 16 lanes per token, first, first + step, ..., AHEAD of them together (a
+// token is a chain of list, page tables, then its bytes).  No slot is both written and read.  Bound: memory, for many tokens (16 x 8 lists,
+// 4096 rows of 256 bytes of keys and of values each: 117 us, 4.6 TB/s read and written).
 template <bool INT8, uint32_t AHEAD>
 __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView& e, uint32_t s, uint32_t h, const uint32_t* slots_to, const uint32_t* slots_from, uint32_t n,
                                             uint32_t first, uint32_t step) {
@@ -271,7 +272,7 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 #pragma unroll
     for (uint32_t i = 0; i < AHEAD; ++i) {
       const uint32_t at = min(m + i * step, n - 1);
-      to[i] = min(slots_to[at], c.capacity - 1), of[i] = min(slots_from[e.slices ? n - 1 - at : at], c.capacity - 1);   // (lengths that change under the call)
+      to[i] = min(slots_to[at], c.capacity - 1), of[i] = min(slots_from[e.slices ? n - 1 - at : at], c.capacity - 1);   // (lengths that change)
     }
 #pragma unroll
     for (uint32_t i = 0; i < AHEAD; ++i) {
@@ -285,11 +286,11 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
       u32x4 x[AHEAD][2];
       const bool more = p0 - lane + 16 < 2 * pieces;
       auto piece = [&](uint32_t p) { return p < pieces ? c.k + 16 * p : c.v + 16 * (p - pieces); };
-      auto load = [&](int half) {
+      auto load = [&](int half) {   // (in place of a token that is not moved, one of page 0)
         const uint32_t p = p0 + 16 * half;
         const char* from = piece(p < 2 * pieces ? p : 0);
 #pragma unroll
-        for (uint32_t i = 0; i < AHEAD; ++i) x[i][half] = __builtin_nontemporal_load((const u32x4*)(from + place(there[i] ? of_page[i] : 0, of[i])));   // (in place of a token that is not moved, one of page 0)
+        for (uint32_t i = 0; i < AHEAD; ++i) x[i][half] = __builtin_nontemporal_load((const u32x4*)(from + place(there[i] ? of_page[i] : 0, of[i])));
       };
       auto store = [&](int half) {
         const uint32_t p = p0 + 16 * half;
@@ -322,12 +323,13 @@ __device__ __forceinline__ void move_tokens(const CacheView& c, const EvictView&
 // 8 bits over those that agree with the bits found), then one look in the order of the slots that numbers the equal ones at the
 // limit, the free slots below `keep` and the kept ones above.
 //
-// A workgroup per list; a thread has 4 neighbouring slots of every kStride, and their ranks in registers.  Scores share few exponents, so that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there
-// are several copies of it.  Bound: one workgroup's chain of loads, four rounds of histogram and look, numbering: 8 lists of 1152 slots 6.7 us with their
-// 128 moves, of 16384 18.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
+// A workgroup per list; a thread has 4 neighbouring slots of every kStride, and their ranks in registers.  Scores share few exponents, so
+// that a histogram of the top 8 bits would have a wavefront's lanes add to few words one after another: there are several copies of it.
+// Bound: one workgroup's chain of loads, four rounds of histogram and look, numbering: 8 lists of 1152 slots 6.7 us with their 128 moves, of
+// 16384 18.  MOVES: the tokens are moved here too (lengths_out is not lengths, and there are few of them).
 template <int THREADS, int STRIDES, bool INT8, bool MOVES>
 __global__ __launch_bounds__(THREADS) void k_evict_select(CacheView c, EvictView e) {
-  constexpr int kWaves = THREADS / 64, kCopies = kWaves < 8 ? kWaves : 8;   // (a copy per lane costs more to clear and add up than it saves: 16384 slots 19.9 -> 22.8 us)
+  constexpr int kWaves = THREADS / 64, kCopies = kWaves < 8 ? kWaves : 8;   // (a copy per lane: 16384 slots 19.9 -> 22.8 us, to clear and add up)
   __shared__ __attribute__((aligned(16))) uint32_t bins[256 * kCopies], sums[256], totals[2][64];
   constexpr uint32_t kStride = THREADS * 4;
   const uint32_t h = blockIdx.x, s = blockIdx.y, list = s * c.kv_heads + h, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -644,11 +646,12 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
     if (moves) int8 ? go(k_evict_select<T, S, true, true>) : go(k_evict_select<T, S, false, true>);
     else go(k_evict_select<T, S, false, false>);
   };
-  // As many threads as a list has fours of slots, as far as there are: a barrier among fewer wavefronts is shorter (8 lists of 1152 slots: 512 threads 7.7 us, 1024 9.4).
+  // As many threads as a list has fours of slots, as far as there are: a barrier among fewer wavefronts is shorter (8 lists of 1152 slots:
+  // 512 threads 7.7 us, 1024 9.4), and as few strides (8 lists of 8000 slots with four, two of them empty: 16.4 us in place of 12.5).
   if (c.capacity <= 1024) select(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 2048) select(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
   else if (c.capacity <= 4096) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
-  else if (c.capacity <= 8192) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());   // (with four strides, two of them empty: 8000 slots 16.4 us in place of 12.5)
+  else if (c.capacity <= 8192) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
   else if (!e.slices) select(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
   else
     for (uint32_t round = 0; round <= 4; ++round) {

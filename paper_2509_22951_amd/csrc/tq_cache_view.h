@@ -22,7 +22,8 @@ struct CacheView {
   uint32_t n_pages, page_shift, kv_heads, head_dim, n_seqs, seq_pages, capacity;
 };
 
-// Values at any address that their type allows: the memory unit takes 16 bytes from any 4-byte boundary as it does from a 16-byte one, 4 and 8 from any 2-byte one.
+// Values at any address that their type allows: the memory unit takes 16 bytes from any 4-byte boundary as it does from a 16-byte one, 4 and
+// 8 from any 2-byte one.
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));

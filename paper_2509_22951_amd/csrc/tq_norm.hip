@@ -19,7 +19,8 @@ struct NormView {
   float eps;
 };
 
-// Four values at a time, at any address that their type allows: values i..i+3 of a row of n, fp32 or bf16; those beyond it are zero.  WHOLE: n is a multiple of 4.
+// Four values at a time, at any address that their type allows: values i..i+3 of a row of n, fp32 or bf16; those beyond it are zero.  WHOLE:
+// n is a multiple of 4.
 template <bool WHOLE, bool BF16>
 __device__ __forceinline__ void load_values(const void* row, uint32_t i, uint32_t n, float (&v)[4]) {
   if (WHOLE || i + 4 <= n) {
