@@ -110,6 +110,7 @@ __device__ __forceinline__ void take_again(const Segment& s, uint32_t lane, uint
   typedef __attribute__((address_space(4))) const char constant_char;
   typedef __attribute__((address_space(4))) const CacheView constant_cache;
   typedef __attribute__((address_space(4))) const AttendView constant_attend;
+  static_assert(sizeof(CacheView) % alignof(AttendView) == 0, "the kernel's arguments lie side by side");
   constexpr uint32_t kOwn = (DIM + 63) / 64;
   constant_char* args = (constant_char*)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(args), "+v"(lane));

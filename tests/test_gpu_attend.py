@@ -468,3 +468,36 @@ def test_every_token_at_a_cut_counts_once(rows, n, heads, kv_heads, dim, kind):
             for wrong in (1 - w[:, t], 1 + w[:, t]):      # the total without this token, and with it twice
                 other = (w @ v + (wrong - 1)[:, None] * v[t]) / wrong[:, None]
                 assert ((other - want[s, :group]).abs() > want[s, :group].abs() * 2.0 ** -8 + bound).any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("order", ["pthd", "tphd"])
+def test_what_is_not_finite_in_pools_of_any_order_with_pages_that_are_not_there(kind, order):
+    """bf16 queries, keys and values (or their scales) that are not finite in some tokens, two chunks of query heads, weights added up."""
+    p = Paged(3, 60, kv_heads=2, dim=80, kind=kind, order=order, marks=True, table_stride=70, seed=3)
+    p.tables[0, 5], p.tables[1, 0], p.tables[2, 59] = -1, p.n_pages, -1
+    q = queries(3, 18, 80, dtype=torch.bfloat16).abs()
+    vmax = p.values("v").abs().max()
+    lengths = ints([950, 333, 960])
+    for s, t in ((0, 17), (0, 400), (1, 300), (2, 940)):
+        page, at = int(p.tables[s, t // 16]), t % 16
+        if kind == "bf16":
+            p.k[page, 0, at, 11] = -INF
+            p.v[page, 1, at, 3] = INF
+        elif s == 0:
+            p.v_scale[page, 1, at] = float("nan")
+        else:
+            p.k_scale[page, 1, at] = float("nan")
+    before = p.scores.cpu().double()
+    out = run(p, q, lengths, accumulate=True)
+    want, added = attend_reference(p, q, lengths)
+    assert torch.isfinite(want[:, :9]).all() and not torch.isfinite(want[:, 9:]).all()
+    agrees(out, want, vmax)
+    got, fine = p.scores.cpu().double(), torch.isfinite(added)
+    there = torch.zeros_like(fine)
+    for s in range(3):
+        for h in range(2):
+            there[s, h, :int(lengths[s])] = p.of_sequence(p.values("k"), s, h, int(lengths[s]))[1]
+    assert torch.equal(torch.isnan(got)[there], ~fine[there])
+    fine &= there
+    assert ((got - before - added).abs()[fine] <= (added * 2.0 ** -14 + (before + added) * 2.0 ** -23)[fine]).all()
