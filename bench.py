@@ -39,7 +39,7 @@ PROFILED_TRAFFIC = {
 
 
 # sources of kernels that no workload here runs; no other source includes them
-BETWEEN_PRODUCTS = ("tq_norm.hip", "tq_cache.hip", "tq_attend.hip", "tq_cache_view.h")
+BETWEEN_PRODUCTS = ("tq_norm.hip", "tq_cache.hip", "tq_attend.hip", "tq_tree.hip", "tq_accept.hip", "tq_sample.hip", "tq_cache_view.h")
 
 
 def csrc_digest() -> str:

@@ -436,6 +436,21 @@ typedef struct tq_append_args {
 int tq_cache_append(const tq_cache *cache, const tq_append_args *args, void *stream);
 
 /*
+ * tq_cache_append for models that norm every query and key head before its rotation:
+ *   x <- x / sqrt(mean(x^2) + eps) * weight, over the head_dim values of a head, in fp32; values (v) are not normed.
+ * A head with a NaN is NaN throughout, one with an infinity NaN there and zero elsewhere.  Rows that are padding stay zero.
+ *   q_weight, k_weight: device, TQ_FP32 or TQ_BF16 (weight_type), aligned to it: head_dim weights for all heads (stride 0), or a row of
+ *   them for every query or key head (stride: at least head_dim elements from one head's to the next's).  NULL: ones.
+ */
+typedef struct tq_head_norm {
+  const void *q_weight, *k_weight;
+  uint64_t q_weight_stride, k_weight_stride;
+  float eps;
+  uint32_t weight_type;
+} tq_head_norm;
+int tq_cache_append_normed(const tq_cache *cache, const tq_append_args *args, const tq_head_norm *norm, void *stream);
+
+/*
  * Attention of one new token per row over the pages of its sequence:
  *   out[r][h] = sum_t p[t] v[t],  p = softmax over t < lengths[r] of scale * q[r][h] . k[t],  keys and values of head h / (heads / kv_heads).
  * Row r belongs to sequence seqs[r] (NULL: sequence r).  Rows of one sequence with rising lengths are a prompt or a draft, causally masked.
@@ -496,6 +511,95 @@ typedef struct tq_evict_args {
 } tq_evict_args;
 int tq_cache_evict(const tq_cache *cache, const tq_evict_args *args, void *stream);
 int tq_cache_evict_workspace(const tq_cache *cache, const tq_evict_args *args, uint64_t *bytes);
+
+/*
+ * A tree of drafted tokens behind every sequence, whose nodes are rows of one step: their products are batched (TQ_MAX_BATCH), their keys
+ * and values appended to the cache behind the sequence's tokens, node i of tree t in slot lengths[t] + i, and every node attends to its sequence's
+ * tokens and to its ancestors.  Of what is then drawn at the nodes, the longest branch that agrees with the draft is accepted.
+ *   masks: device, uint64 [trees][nodes]: bit j of masks[t][i]: node i attends to node j.  A tree's own masks have a node's ancestors and itself.
+ *   sizes: device, int32 [trees]: a tree has its first sizes[t] nodes (0..nodes); NULL: all of them.  The rows of the others are padding.
+ *   lengths: device, int32 [trees]: tokens of the sequence ahead of the tree (a negative one counts as 0).
+ *   seqs: device, int32 [trees]: the sequence of each tree, no two alike; NULL: sequence t.
+ */
+#define TQ_MAX_NODES 64
+
+/*
+ * Attention of the nodes: row t * nodes + i is node i of tree t,
+ *   out[r][h] = sum_s p[s] v[s],  p = softmax of scale * q[r][h] . k[s]  over the slots s < lengths[t] and the slots lengths[t] + j, j < sizes[t], with bit j of
+ *   masks[t][i]; keys and values of head h / (heads / kv_heads).
+ * Slots beyond the capacity and pages that are not there are masked.  A row with nothing to attend to, of a sequence that is not there, and one that is padding, are zero.
+ *   q: device, TQ_FP32 or TQ_BF16 (q_type) [trees * nodes][heads * head_dim]; an fp32 q is used unrounded.  out: device, bf16 [trees * nodes][heads * head_dim].
+ *   Neither lengths, sizes, seqs, masks nor q are written while the call runs.
+ *   workspace: device, 16-byte aligned, of at least the size tq_attend_tree_workspace gives for the same arguments, with any contents; calls whose execution
+ *   overlaps need one each.
+ * Precision, what is not finite, and what lies in a cache where a row does not attend to it: as in tq_attend.  trees is at most 65535.
+ */
+typedef struct tq_tree_args {
+  const void *q;
+  void *out;
+  const int32_t *seqs, *lengths, *sizes;
+  const uint64_t *masks;
+  void *workspace;
+  uint64_t workspace_bytes;
+  uint32_t trees, nodes, heads, q_type;
+  uint64_t q_stride, out_stride;
+  float scale;
+  uint32_t reserved;
+} tq_tree_args;
+int tq_attend_tree(const tq_cache *cache, const tq_tree_args *args, void *stream);
+int tq_attend_tree_workspace(const tq_cache *cache, const tq_tree_args *args, uint64_t *bytes);
+
+/*
+ * The accepted branch of each tree.  It begins with node 0 (the token drawn last, whose keys were not in the cache yet) and goes on from a node p to its child - a
+ * node c > p with masks[c] = masks[p] and its own bit - whose drafted token is the one drawn at p, the lowest such c, until there is none.
+ *   drafted, sampled: device, int32 [trees][nodes]: the nodes' tokens, and what was drawn (tq_sample) from the logits at each.
+ *   path: device, int32 [trees][nodes]: the accepted nodes, rising, -1 behind them.  accepted: device, int32 [trees]: how many.
+ *   next: device, int32 [trees]: the token drawn at the last of them (-1 for a tree without nodes), the next tree's node 0.
+ *   lengths_out: device, int32 [trees]: lengths[t] + accepted[t].  Not lengths itself; the outputs do not overlap each other or the inputs.
+ * caches: host array of n (0..4096) caches that hold these sequences, the layers of a model.  In each of them the accepted nodes' keys, values, scales, scores and positions
+ * move to the slots lengths[t] + 0, 1, ..., in order; what lay in the slots behind them is not used any more and may be anything.  Nothing is moved
+ * into or out of a slot beyond a cache's capacity, a page that is not there or a sequence that is not there.  n = 0: only the branches.
+ */
+typedef struct tq_accept_args {
+  const uint64_t *masks;
+  const int32_t *sizes, *seqs, *lengths, *drafted, *sampled;
+  int32_t *path, *accepted, *next, *lengths_out;
+  uint32_t trees, nodes;
+} tq_accept_args;
+int tq_tree_accept(uint32_t n, const tq_cache *const *caches, const tq_accept_args *args, void *stream);
+
+/*
+ * One token per row, drawn from its logits (a product's y) with a random number of the caller's.  With the tokens of a row in order of falling logit (equal ones:
+ * the lowest token first) and weights w = exp((logit - largest) / temperature), those are kept that all of these keep, and the first one always:
+ *   top_k: the first top_k tokens (0 or less: all);
+ *   top_p: the tokens ahead of which less than top_p of the weight of all tokens lies (1 or more: all);
+ *   min_p: the tokens with w >= min_p (0 or less: all).
+ * tokens[r] is the first token, by number, at which the weight of the kept ones up to and with it exceeds uniform[r] times that of all kept ones (the last kept
+ * one, if none does); probs[r] its share of that weight.  A temperature that is not above 0 takes the first token in order, with probability 1.
+ * Weights and sums are held in 64 bits, so that what is drawn is what the formula draws; results repeat.
+ * A logit of -infinity or NaN is a masked token and never drawn; a row of nothing else gives token -1 with probability 0.  If there are logits of +infinity, only they have
+ * weight, equal shares of it.
+ *   logits: device, fp32 [rows][vocab], logits_stride elements apart (0: vocab).
+ *   temperature, top_p, min_p: device, fp32 [rows], top_k: device, int32 [rows]; NULL: 1, 1, 0, 0 for every row.  A NaN in top_p or min_p counts as 1 and 0.
+ *   uniform: device, fp32 [rows], in [0, 1).
+ *   tokens: device, int32 [rows]; probs: device, fp32 [rows], or NULL.
+ *   workspace: device, 16-byte aligned, of at least the size tq_sample_workspace gives for the same arguments, with any contents; calls whose execution
+ *   overlaps need one each.
+ * vocab is 1..2^20, rows at most 65535.
+ */
+typedef struct tq_sample_args {
+  const float *logits;
+  const float *temperature, *top_p, *min_p, *uniform;
+  const int32_t *top_k;
+  int32_t *tokens;
+  float *probs;
+  void *workspace;
+  uint64_t workspace_bytes;
+  uint64_t logits_stride;
+  uint32_t rows, vocab;
+} tq_sample_args;
+int tq_sample(const tq_sample_args *args, void *stream);
+int tq_sample_workspace(const tq_sample_args *args, uint64_t *bytes);
 
 #ifdef __cplusplus
 }

@@ -26,6 +26,7 @@ EXPORTS = [
     "tq_listing_build_table", "tq_listing_compress", "tq_listing_create", "tq_listing_decompress", "tq_listing_get_info",
     "tq_listing_destroy",
     "tq_add_rms_norm", "tq_cache_append", "tq_attend", "tq_attend_workspace", "tq_cache_evict", "tq_cache_evict_workspace",
+    "tq_cache_append_normed", "tq_attend_tree", "tq_attend_tree_workspace", "tq_tree_accept", "tq_sample", "tq_sample_workspace",
 ]
 
 
@@ -99,6 +100,10 @@ class TqAppendArgs(_Args):
                 ("k_stride", _U64), ("v_stride", _U64), ("q_out_stride", _U64), ("q_out_type", _U32), ("pairing", _U32)]
 
 
+class TqHeadNorm(_Args):
+    _fields_ = [("q_weight", _VP), ("k_weight", _VP), ("q_weight_stride", _U64), ("k_weight_stride", _U64), ("eps", _F32), ("weight_type", _U32)]
+
+
 class TqAttendArgs(_Args):
     _fields_ = [("q", _VP), ("out", _VP), ("seqs", _VP), ("lengths", _VP), ("workspace", _VP), ("workspace_bytes", _U64), ("rows", _U32),
                 ("heads", _U32), ("q_stride", _U64), ("out_stride", _U64), ("scale", _F32), ("q_type", _U32), ("accumulate", _U32),
@@ -108,6 +113,21 @@ class TqAttendArgs(_Args):
 class TqEvictArgs(_Args):
     _fields_ = [("lengths", _VP), ("lengths_out", _VP), ("since", _VP), ("scores_out", _VP), ("positions_out", _VP), ("workspace", _VP),
                 ("workspace_bytes", _U64), ("keep", _U32), ("reserved", _U32)]
+
+
+class TqTreeArgs(_Args):
+    _fields_ = [("q", _VP), ("out", _VP), ("seqs", _VP), ("lengths", _VP), ("sizes", _VP), ("masks", _VP), ("workspace", _VP), ("workspace_bytes", _U64),
+                ("trees", _U32), ("nodes", _U32), ("heads", _U32), ("q_type", _U32), ("q_stride", _U64), ("out_stride", _U64), ("scale", _F32), ("reserved", _U32)]
+
+
+class TqAcceptArgs(_Args):
+    _fields_ = [("masks", _VP), ("sizes", _VP), ("seqs", _VP), ("lengths", _VP), ("drafted", _VP), ("sampled", _VP), ("path", _VP), ("accepted", _VP),
+                ("next", _VP), ("lengths_out", _VP), ("trees", _U32), ("nodes", _U32)]
+
+
+class TqSampleArgs(_Args):
+    _fields_ = [("logits", _VP), ("temperature", _VP), ("top_p", _VP), ("min_p", _VP), ("uniform", _VP), ("top_k", _VP), ("tokens", _VP), ("probs", _VP),
+                ("workspace", _VP), ("workspace_bytes", _U64), ("logits_stride", _U64), ("rows", _U32), ("vocab", _U32)]
 
 
 def lib_path() -> str:
@@ -187,7 +207,11 @@ def load() -> ctypes.CDLL:
     lib.tq_listing_destroy.argtypes = [vp]
     lib.tq_add_rms_norm.restype = ci
     lib.tq_add_rms_norm.argtypes = [vp, vp]
-    for name in ("tq_cache_append", "tq_attend", "tq_attend_workspace", "tq_cache_evict", "tq_cache_evict_workspace"):
+    lib.tq_sample.restype = lib.tq_sample_workspace.restype = lib.tq_cache_append_normed.restype = lib.tq_tree_accept.restype = ci
+    lib.tq_sample.argtypes = lib.tq_sample_workspace.argtypes = [vp, vp]
+    lib.tq_cache_append_normed.argtypes = [vp, vp, vp, vp]
+    lib.tq_tree_accept.argtypes = [u32, vp, vp, vp]
+    for name in ("tq_cache_append", "tq_attend", "tq_attend_workspace", "tq_cache_evict", "tq_cache_evict_workspace", "tq_attend_tree", "tq_attend_tree_workspace"):
         getattr(lib, name).restype = ci
         getattr(lib, name).argtypes = [vp, vp, vp]
     _LIB = lib
@@ -502,6 +526,7 @@ class Listing:
 
 TQ_BF16, TQ_FP32, TQ_INT8 = 0, 1, 2
 TQ_ROTARY_HALVES, TQ_ROTARY_ADJACENT = 0, 1
+TQ_MAX_NODES = 64
 
 
 class Cache:
@@ -550,6 +575,23 @@ class CacheAppend(_CacheCall):
     _entry, _type = "tq_cache_append", TqAppendArgs
 
 
+class HeadNorm:
+    """The norm of tq_cache_append_normed, as tq_head_norm; the calls with it keep it."""
+
+    def __init__(self, **fields):
+        self.args = TqHeadNorm(**fields)
+        self.address = ctypes.addressof(self.args)
+
+
+class CacheAppendNormed(_CacheCall):
+    """tq_cache_append_normed with arguments marshalled once."""
+    _entry, _type = "tq_cache_append_normed", TqAppendArgs
+
+    def __init__(self, cache: Cache, norm: HeadNorm, **fields):
+        super().__init__(cache, **fields)
+        self.norm, self._at = norm, (*self._at, norm.address)
+
+
 class Attend(_CacheCall):
     """tq_attend with arguments marshalled once.  The workspace is zero before the first launch, and for tq_attend alone."""
     _entry, _type = "tq_attend", TqAttendArgs
@@ -566,3 +608,46 @@ class CacheEvict(_CacheCall):
     @classmethod
     def workspace_bytes(cls, cache: Cache, **fields) -> int:
         return cls._workspace(cache, fields)
+
+
+class AttendTree(_CacheCall):
+    """tq_attend_tree with arguments marshalled once."""
+    _entry, _type = "tq_attend_tree", TqTreeArgs
+
+    @classmethod
+    def workspace_bytes(cls, cache: Cache, **fields) -> int:
+        return cls._workspace(cache, fields)
+
+
+class TreeAccept:
+    """tq_tree_accept with arguments marshalled once; caches: the layers whose keys and values move."""
+
+    def __init__(self, caches, **fields):
+        self.caches, self.args = list(caches), TqAcceptArgs(**fields)
+        n = len(self.caches)
+        self._list = (_VP * max(n, 1))(*[c.address for c in self.caches])
+        self._call, self._at = load().tq_tree_accept, (n, ctypes.addressof(self._list), ctypes.addressof(self.args))
+
+    def launch(self, stream: int = 0) -> None:
+        rc = self._call(*self._at, stream)
+        if rc:
+            _check(rc)
+
+
+class Sample:
+    """tq_sample with arguments marshalled once."""
+
+    def __init__(self, **fields):
+        self.args = TqSampleArgs(**fields)
+        self._call, self._at = load().tq_sample, ctypes.addressof(self.args)
+
+    def launch(self, stream: int = 0) -> None:
+        rc = self._call(self._at, stream)
+        if rc:
+            _check(rc)
+
+    @classmethod
+    def workspace_bytes(cls, **fields) -> int:
+        args, n = TqSampleArgs(**fields), _U64()
+        _check(load().tq_sample_workspace(ctypes.addressof(args), ctypes.addressof(n)))
+        return n.value

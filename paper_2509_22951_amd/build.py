@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtq.so")
-SOURCES = ["tq_encode.cpp", "tq_blob.cpp", "tq_device.hip", "tq_listing.hip", "tq_norm.hip", "tq_cache.hip", "tq_attend.hip"]
+SOURCES = ["tq_encode.cpp", "tq_blob.cpp", "tq_device.hip", "tq_listing.hip", "tq_norm.hip", "tq_cache.hip", "tq_attend.hip", "tq_tree.hip", "tq_accept.hip", "tq_sample.hip"]
 HEADERS = ["tq_format.h", "tq_plan.h", "tq_choice.h", "tq_level.h", "tq_kernels_common.h", "tq_kernel_dot.h", "tq_strip_decode.h", "tq_kernel_ring.h", "tq_kernel_runs.h",
            "tq_kernel_strip.h", "tq_cache_view.h",
            os.path.join("..", "..", "include", "tq.h")]

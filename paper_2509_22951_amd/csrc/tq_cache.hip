@@ -1,4 +1,4 @@
-// The paged cache: new tokens go in (tq_cache_append), tokens with little attention weight go out (tq_cache_evict).
+// The paged cache: new tokens go in (tq_cache_append, tq_cache_append_normed), tokens with little attention weight go out (tq_cache_evict).
 #include <algorithm>
 
 #include "tq_cache_view.h"
@@ -17,6 +17,15 @@ struct AppendView {
   uint32_t heads, rotary_dim, n_positions, adjacent, items;
 };
 
+struct NoNorm {};
+
+struct HeadNormView {
+  const void *q_weight, *k_weight;
+  uint64_t q_stride, k_stride;
+  float eps;
+  uint32_t weight16;
+};
+
 // One workgroup takes a.items * kAppendThreads / LANES of the heads (query, key and value heads in this order) of one row; LANES lanes of a
 // wavefront take a head, 4 values each, and a.items heads one after another, all of them requested ahead.  A pair of the halves
 // rotation lies rotary_dim / 2 values apart: its other half comes from another lane of the same group, so a wavefront has read all
@@ -24,8 +33,12 @@ struct AppendView {
 //
 // Bound: device memory for prompts (8192 rows of 40 heads of 128 to 8 bits, bf16 q: 56 us); for a few rows the chain slot -> page -> store,
 // beside slot -> angles -> rotation.
-template <int LANES, bool INT8, bool Q16>
-__global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a) {
+//
+// With a norm (NORM is HeadNormView) the mean of a query's or key's squares is a sum over the same group of lanes, taken before the rotation;
+// its weights are requested with the values.
+template <int LANES, bool INT8, bool Q16, typename NORM>
+__global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a, NORM norm) {
+  constexpr bool kNormed = std::is_same_v<NORM, HeadNormView>;
   constexpr uint32_t kGroups = kAppendThreads / LANES;
   const uint32_t r = blockIdx.x, D = c.head_dim;
   const uint32_t t = threadIdx.x % LANES, i = 4 * t, first_head = blockIdx.y * (a.items * kGroups) + threadIdx.x / LANES;
@@ -40,6 +53,29 @@ __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, Ap
     const bool is_q = head < a.heads, is_v = head >= a.heads + c.kv_heads;
     const uint32_t h = is_q ? head : is_v ? head - a.heads - c.kv_heads : head - a.heads;
     x[k] = __builtin_nontemporal_load((const f32x4_any*)((is_q ? a.q + r * a.q_stride : is_v ? a.v + r * a.v_stride : a.k + r * a.k_stride) + h * D + (i < D ? i : 0)));
+  }
+  float w[kNormed ? kMostItems : 1][4];
+  if constexpr (kNormed) {
+#pragma unroll
+    for (int k = 0; k < kMostItems; ++k) {
+      if (k && k >= (int)a.items) break;
+      const uint32_t head = first_head + k * kGroups;
+      const bool is_q = head < a.heads;
+      const uint32_t h = is_q ? head : head < a.heads + c.kv_heads ? head - a.heads : 0;
+      const char* of = (const char*)(is_q ? norm.q_weight : norm.k_weight);
+      const uint64_t at = h * (is_q ? norm.q_stride : norm.k_stride) + (i < D ? i : 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[k][j] = 1.f;
+      if (of && norm.weight16) {
+        const u16x4_any d = *(const u16x4_any*)(of + 2 * at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[k][j] = bf16_value(d[j]);
+      } else if (of) {
+        const f32x4_any d = *(const f32x4_any*)(of + 4 * at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[k][j] = d[j];
+      }
+    }
   }
   uint32_t page = c.n_pages;
   if (there) page = (uint32_t)((constant_i32*)c.tables)[(uint64_t)(uint32_t)seq * c.table_stride + ((uint32_t)slot >> c.page_shift)];
@@ -66,6 +102,17 @@ __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, Ap
     float y[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = mine && there ? x[k][j] : 0.f;
+    if constexpr (kNormed) {
+      const float share = 1.f / (float)D;   // of a value in the mean, taken before it is squared: a sum of squares overflows sooner
+      float square = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) square = fmaf(y[j] * share, y[j], square);
+      const float inv = 1.f / sqrtf(group_sum<LANES>(square) + norm.eps);
+      if (!is_v && there) {   // (a row that is padding stays zero, whatever eps)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = y[j] * inv * w[k][j];
+      }
+    }
     if (a.adjacent) {
       if (turned && !is_v) {
         const float z[4] = {y[0] * cs[0] - y[1] * sn[0], y[0] * sn[0] + y[1] * cs[0], y[2] * cs[1] - y[3] * sn[1], y[2] * sn[1] + y[3] * cs[1]};
@@ -120,8 +167,9 @@ __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, Ap
   }
 }
 
-int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
-  const std::string who = "tq_cache_append";
+template <typename NORM>
+int cache_append(const char* name, const tq_cache* cache, const tq_append_args* a, const NORM& norm, void* stream) {
+  const std::string who = name;
   CacheView c;
   if (int rc = view_cache(who, cache, &c)) return rc;
   if (!a) return refuse(TQ_E_INVALID_ARG, who + ": null argument");
@@ -153,18 +201,30 @@ int cache_append(const tq_cache* cache, const tq_append_args* a, void* stream) {
   // the caches: 8192 rows 75 us with one, 68 with four and one in turn, 62 with five; 1024 rows 12.6 with one, 13.7 with five).
   const uint32_t most = (uint64_t)a->rows * rounds > 16384 ? kMostItems : 1, parts = (rounds + most - 1) / most;
   v.items = (rounds + parts - 1) / parts;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, parts), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a->rows, parts), dim3(kAppendThreads), 0, (hipStream_t)stream, c, v, norm); };
   auto of = [&](auto n) {
     constexpr int L = decltype(n)::value;
-    if (int8) q16 ? go(k_cache_append<L, true, true>) : go(k_cache_append<L, true, false>);
-    else q16 ? go(k_cache_append<L, false, true>) : go(k_cache_append<L, false, false>);
+    if (int8) q16 ? go(k_cache_append<L, true, true, NORM>) : go(k_cache_append<L, true, false, NORM>);
+    else q16 ? go(k_cache_append<L, false, true, NORM>) : go(k_cache_append<L, false, false, NORM>);
   };
   if (lanes == 4) of(std::integral_constant<int, 4>());
   else if (lanes == 8) of(std::integral_constant<int, 8>());
   else if (lanes == 16) of(std::integral_constant<int, 16>());
   else if (lanes == 32) of(std::integral_constant<int, 32>());
   else of(std::integral_constant<int, 64>());
-  return launched("tq_cache_append");
+  return launched(name);
+}
+
+int cache_append_normed(const tq_cache* cache, const tq_append_args* a, const tq_head_norm* n, void* stream) {
+  const std::string who = "tq_cache_append_normed";
+  if (!n || !cache) return refuse(TQ_E_INVALID_ARG, who + ": null argument");
+  if (n->weight_type != TQ_FP32 && n->weight_type != TQ_BF16) return refuse(TQ_E_UNSUPPORTED, who + ": weights are TQ_FP32 or TQ_BF16");
+  if (!(n->eps >= 0.f) || !(n->eps < INFINITY)) return refuse(TQ_E_INVALID_ARG, who + ": eps must be a number of at least zero");
+  const size_t size = n->weight_type == TQ_BF16 ? 2 : 4;
+  if (!aligned_to(n->q_weight, size) || !aligned_to(n->k_weight, size)) return refuse(TQ_E_INVALID_ARG, who + ": a weight is not aligned to its type");
+  if ((n->q_weight_stride && n->q_weight_stride < cache->head_dim) || (n->k_weight_stride && n->k_weight_stride < cache->head_dim))
+    return refuse(TQ_E_INVALID_ARG, who + ": a stride of the weights is smaller than head_dim");
+  return cache_append(who.c_str(), cache, a, HeadNormView{n->q_weight, n->k_weight, n->q_weight_stride, n->k_weight_stride, n->eps, n->weight_type == TQ_BF16}, stream);
 }
 
 // ---- eviction --------------------------------------------------------------------------------------------------------
@@ -673,7 +733,11 @@ int cache_evict(const tq_cache* cache, const tq_evict_args* a, void* stream) {
 }  // namespace tq
 
 extern "C" int tq_cache_append(const tq_cache* cache, const tq_append_args* args, void* stream) {
-  return tq::contained("tq_cache_append", [&] { return tq::cache_append(cache, args, stream); });
+  return tq::contained("tq_cache_append", [&] { return tq::cache_append("tq_cache_append", cache, args, tq::NoNorm{}, stream); });
+}
+
+extern "C" int tq_cache_append_normed(const tq_cache* cache, const tq_append_args* args, const tq_head_norm* norm, void* stream) {
+  return tq::contained("tq_cache_append_normed", [&] { return tq::cache_append_normed(cache, args, norm, stream); });
 }
 
 extern "C" int tq_cache_evict(const tq_cache* cache, const tq_evict_args* args, void* stream) {
