@@ -1,8 +1,8 @@
 // Attention of a tree of drafted tokens over a paged cache (tq_attend_tree).
 //
 // All nodes of a tree and all query heads that share a key/value head are columns of one product, so that a token's key and value are read once for all of them.  A
-// workgroup takes up to 8 tiles of 16 columns and a stage of tokens at a time: keys and values go from memory through registers (8 bits become bf16 there) to LDS, and a
-// wavefront per column tile, or several that share out the tokens, reads them in the shape of v_mfma_f32_16x16x32_bf16:
+// workgroup takes up to 12 tiles of 16 columns and a stage of tokens at a time: keys and values go to LDS (8 bits become bf16 there), and a
+// wavefront per column tile, or several that share out its tokens, reads them in the shape of v_mfma_f32_16x16x32_bf16:
 //   logits [token][column] = K [token][dim] Q^T: lane l supplies token l % 16 and 8 neighbouring dims.
 //   out^T [dim][column] = V^T [dim][token] P^T: the lane that got the logits of tokens 4g..4g+3 of both 16-token blocks (g = l / 16) supplies the same tokens as its 8
 //   values of the contraction, so P is already where it is needed; V is transposed on its way out of LDS.
@@ -15,7 +15,9 @@
 namespace tq {
 namespace {
 
-constexpr int kTreeWaves = 8, kTreeThreads = kTreeWaves * 64, kMostTiles = 8, kTile = 32;
+constexpr int kLoaders = 8, kTile = 32;   // wavefronts that load; tokens that a wavefront multiplies at a time
+template <int DIM>
+constexpr int kTreeWaves = DIM == 256 ? 8 : 12;   // two or three per SIMD: q and the sums take 160 or 80 registers
 constexpr uint32_t kMaxGroups = 256;      // workgroups of a launch: one per compute unit
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -24,7 +26,7 @@ struct TreeView {
   uint16_t* out;
   const int32_t *seqs, *lengths, *sizes;
   const uint64_t* masks;
-  float* partials;     // [workgroup][2]: [column][DIM] sums, then maximum and total of every column
+  float* partials;     // [workgroup][2]: [column tile][block of 16 dims][lane] four sums, then [column] maximum and total
   uint64_t q_stride, out_stride;
   float scale;         // times log2(e)
   uint32_t trees, nodes, heads, group, columns, tiles, chunks;   // columns of a key/value head; column tiles of a chunk; chunks per key/value head
@@ -35,7 +37,8 @@ struct TreeView {
 struct Seen {
   uint32_t seq, length, end, size;
 };
-__device__ __forceinline__ Seen seen_by(const CacheView& c, const TreeView& a, uint32_t t) {
+template <typename C, typename A>
+__device__ __forceinline__ Seen seen_by(C& c, A& a, uint32_t t) {
   const int32_t s = a.seqs ? a.seqs[t] : (int32_t)t;
   const uint32_t size = a.sizes ? (uint32_t)min(max(a.sizes[t], 0), (int32_t)a.nodes) : a.nodes, length = (uint32_t)max(a.lengths[t], 0);
   if ((uint32_t)s >= c.n_seqs || size == 0) return Seen{0, 0, 0, size};
@@ -49,7 +52,8 @@ __device__ __forceinline__ float value_at(const char* from, uint32_t d) {
 }
 
 // Four dims of a row's head, divided by the weights' total.
-__device__ __forceinline__ void write_out(const TreeView& a, uint32_t size, uint32_t t, uint32_t node, uint32_t head, uint32_t D, uint32_t d0, float4 sum, float total) {
+template <typename A>
+__device__ __forceinline__ void write_out(A& a, uint32_t size, uint32_t t, uint32_t node, uint32_t head, uint32_t D, uint32_t d0, float4 sum, float total) {
   if (d0 >= D) return;
   const float inv = total == 0.f || node >= size ? 0.f : 1.f / total;
   if (node >= size) sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -60,37 +64,67 @@ __device__ __forceinline__ void write_out(const TreeView& a, uint32_t size, uint
 
 template <int DIM, bool INT8>
 struct Shape {
+  static constexpr int kWaves = kTreeWaves<DIM>, kThreads = kWaves * 64;
   static constexpr int kTokens = 16384 / DIM, kTiles = kTokens / kTile;      // of a stage: 32 KB of keys and as much of values in LDS
   static constexpr int kSteps = DIM / 32, kBlocks = DIM / 16, kRow = DIM * 2; // contraction steps of the logits, blocks of 16 dims, bytes of a row in LDS
   static constexpr int kSize = INT8 ? 1 : 2, kPieces = DIM * kSize / 16;      // 16-byte pieces of a row in memory
-  static constexpr int kLoads = kTokens * kPieces / kTreeThreads, kRows = 64 / kPieces;   // loads of a lane for a stage; rows that a wavefront loads at a time
+  static constexpr int kOwnRows = kTokens / kLoaders, kRows = 64 / kPieces, kLoads = kOwnRows / kRows;   // rows that a wavefront loads of a stage, and at a time
+  static constexpr int kOwnBlocks = kOwnRows > 16 ? kOwnRows / 16 : 1, kPerBlock = kLoads / kOwnBlocks;
+  static constexpr uint32_t kKeyMask = 7, kValueMask = 3;   // see below
+  static_assert(kOwnRows % 8 == 0, "a loader begins where the places of pieces do");
+  static constexpr uint32_t kPartial = kBlocks * 256 + 32;                    // floats of a column tile's partial
 };
 
-// All (tree, key/value head, chunk, unit of a stage) in this order are one line, cut into equal shares, one per workgroup.
-struct Line {
-  uint32_t all, share;
-};
 template <int TOKENS>
 __device__ __forceinline__ uint32_t units_of(uint32_t end) { return max((end + TOKENS - 1) / TOKENS, 1u); }   // (a tree without tokens is written too)
 
+// All (tree, key/value head, chunk, unit of a stage) in this order are one line, cut into equal shares, one per workgroup.  What lies in several shares leaves its parts
+// in memory, and k_join_tree joins them.
 template <int DIM, bool INT8, bool Q16>
-__global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, TreeView a) {
+__global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
   constexpr int kParts = Q16 ? 1 : 3;
-  constexpr uint32_t kT = S::kTokens, kBytes = kT * S::kRow, kJoin = kTreeWaves * 16 * (DIM + 4) * 4;
-  __shared__ __attribute__((aligned(16))) char lds[(4 * kBytes > kJoin ? 4 * kBytes : kJoin)];   // keys, values, keys, values; at a segment's end [wave][column][DIM + 4] sums
-  __shared__ __attribute__((aligned(16))) uint32_t lds_kind[2][kT];     // 0: of the context, 1 + j: node j, kNobody
-  __shared__ __attribute__((aligned(16))) float lds_scale[2][2][INT8 ? kT : 4];
-  __shared__ float lds_max[kTreeWaves * 16], lds_total[kTreeWaves * 16], lds_weight[kTreeThreads];
-  __shared__ uint64_t lds_at[kTreeThreads];
-  __shared__ uint32_t lds_odd, lds_odd_column[kMostTiles * 16];
-  constexpr uint32_t kNobody = 255;
+  constexpr uint32_t kT = S::kTokens, kBytes = kT * S::kRow, kAll = 64, kNobody = 65;
+  // Keys, then values of a stage; those of the next one are on their way into lds_1, or lds_0.  Of 8 bits, one stage as bf16 in lds_0, and two as they are in memory.
+  // (Arrays of their own, so that the compiler sees that a read of one does not wait for loads into the other.)
+  __shared__ __attribute__((aligned(16))) char lds_0[2 * kBytes], lds_1[INT8 ? kBytes : 2 * kBytes], lds_2[INT8 ? kBytes : 16];
+  __shared__ __attribute__((aligned(16))) uint32_t lds_kind[2][kT];     // j: of node j; kAll: of the context, kNobody
+  __shared__ __attribute__((aligned(16))) float lds_scale[2][INT8 ? kT : 4], lds_own_scale[2][2][INT8 ? kT : 4];   // of keys (times `scale`), of values; as they are in memory
+  __shared__ float lds_max[S::kWaves * 16], lds_total[S::kWaves * 16], lds_weight[256];
+  __shared__ uint64_t lds_at[256];
+  __shared__ __attribute__((aligned(16))) uint32_t lds_some[2][kLoaders];   // a loader's rows of a stage: some of them are not of the context
+  __shared__ uint32_t lds_odd, lds_odd_column[S::kWaves * 16];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane / 16, n = lane % 16, D = c.head_dim;
   auto scalar = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+  // A thread's number that looks new each time: what is made of it is made where it is used, and takes no registers from the products.
+  auto anew = [](uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+  };
+  auto stage = [&](auto b) -> char* {
+    if constexpr (INT8) return decltype(b)::value ? lds_2 : lds_1;
+    else return decltype(b)::value ? lds_1 : lds_0;
+  };
+
+  // The arguments, read again where they are used once in a while: the loop over the stages has no registers for all of them.
+  typedef __attribute__((address_space(4))) const char constant_char;
+  typedef __attribute__((address_space(4))) const CacheView constant_cache;
+  typedef __attribute__((address_space(4))) const TreeView constant_tree;
+  static_assert(sizeof(CacheView) % alignof(TreeView) == 0, "the kernel's arguments lie side by side");
+  auto arguments = [] {
+    constant_char* at = (constant_char*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return at;
+  };
+#define ARGUMENTS_ANEW                            \
+  constant_char* arguments_at = arguments();      \
+  constant_cache& c = *(constant_cache*)arguments_at; \
+  constant_tree& a = *(constant_tree*)(arguments_at + sizeof(CacheView))
 
   // this workgroup's share, and the tree it begins in
   uint32_t lane_units = 0;   // of tree (t & ~63) + lane
-  auto look_at = [&](uint32_t first) {
+  auto look_at = [&](uint32_t first) __attribute__((always_inline)) {
+    ARGUMENTS_ANEW;
     lane_units = first + lane < a.trees ? units_of<kT>(seen_by(c, a, first + lane).end) : 0u;
     return wave_prefix_sum(lane_units);
   };
@@ -125,7 +159,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, Tr
     Seen of;
     uint32_t t, kv, first_column, unit, n_units, first, units;   // first: where the whole of it begins on the line, units long
   };
-  auto next_segment = [&] {
+  auto next_segment = [&]() __attribute__((always_inline)) {
+    ARGUMENTS_ANEW;
     Segment s;
     s.t = t, s.of = seen_by(c, a, t);
     s.of.seq = scalar(s.of.seq), s.of.length = scalar(s.of.length), s.of.end = scalar(s.of.end), s.of.size = scalar(s.of.size);
@@ -135,74 +170,137 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, Tr
     s.kv = pair / a.chunks, s.first_column = pair % a.chunks * a.tiles * 16;
     s.unit = pos - s.first, s.n_units = min(s.units - s.unit, stop - pos);
     pos += s.n_units;
-    if (pos == tree_first + s.units * pairs) {
+    if (pos == tree_first + s.units * (c.kv_heads * a.chunks)) {
       tree_first = pos, ++t;
       if ((t & 63) == 0 && pos < stop) look_at(t);
     }
     return s;
   };
 
-  // ---- from memory to registers ----
-  const uint32_t piece = lane % S::kPieces, row_of_lane = lane / S::kPieces;
-  const uint32_t slot_bytes = S::kSize * (uint32_t)c.slot_stride;
-  const uint32_t lane_at = row_of_lane * slot_bytes + (16 * piece < S::kSize * D ? 16 * piece : 0);   // (dims that a head does not have: its first ones, against zeros of q)
-  uint4 in_k[S::kLoads], in_v[S::kLoads];
-  float in_ks[S::kLoads], in_vs[S::kLoads];
-  uint32_t in_limit[S::kLoads], in_first[S::kLoads], in_length = 0;   // rows of a load that are there; their first slot
-  auto fetch_one = [&](const Segment& s, uint32_t unit, int i) {
-    constant_i32* table = (constant_i32*)(c.tables + (uint64_t)s.of.seq * c.table_stride);
-    const uint32_t newest = max(s.of.end, 1u) - 1, slot = unit * kT + (i * kTreeWaves + wave) * S::kRows, from = min(slot, newest & ~(uint32_t)(S::kRows - 1));
-    const uint32_t id = scalar((uint32_t)table[from >> c.page_shift]), page = id < c.n_pages ? id : 0, in_page = from & ((1u << c.page_shift) - 1);
-    in_first[i] = slot;
-    in_limit[i] = id < c.n_pages && slot < s.of.end ? min(s.of.end - slot, (uint32_t)S::kRows) : 0u;
-    const uint64_t at = S::kSize * ((uint64_t)page * c.page_stride + s.kv * c.head_stride + in_page * c.slot_stride);
-    in_k[i] = *(const uint4*)(c.k + at + lane_at);
-    in_v[i] = *(const uint4*)(c.v + at + lane_at);
-    if constexpr (INT8) {
-      const uint64_t mark = (((uint64_t)page * c.kv_heads + s.kv) << c.page_shift) + in_page + row_of_lane;
-      in_ks[i] = c.k_scale[mark], in_vs[i] = c.v_scale[mark];
-    }
+  // ---- from memory to LDS ----
+  // A loader takes kOwnRows rows of a stage; 16 tokens lie in one page.  The pages are looked up ahead of the barrier in front of the loads.  Rows are pieces of 8 dims, in places that
+  // spread the lanes of a read over the banks: piece p of row r of the keys in place p ^ (r & kKeyMask), of the values in p ^ (2 * (r & kValueMask)).
+  struct Place {   // a stage: of a segment, or none
+    Segment s;
+    uint32_t unit;
+    bool there;
   };
-  // ---- from registers to LDS: rows of pieces of 8 dims, in places that spread the lanes of a read over the banks ----
-  auto store_one = [&](uint32_t buffer, int i) {
-    const uint32_t row = (i * kTreeWaves + wave) * S::kRows + row_of_lane;
-    const bool there = row_of_lane < in_limit[i];
-    char* keys = lds + buffer * 2 * kBytes + row * S::kRow;
-    char* values = keys + kBytes;
-    constexpr uint32_t kKeyMask = DIM == 64 ? 7 : 15, kValueMask = DIM == 64 ? 3 : 7;
-    auto put = [&](uint32_t p, uint4 k, uint4 v) {
-      *(uint4*)(keys + ((p ^ (row & kKeyMask)) * 16)) = k;
-      *(uint4*)(values + ((p ^ ((row & kValueMask) << 1)) * 16)) = v;
-    };
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    const uint4 k = there ? in_k[i] : none, v = there ? in_v[i] : none;
-    if constexpr (INT8) {
-      auto wide = [](uint32_t x, uint32_t y) { return __builtin_bit_cast(uint4, i8x8_to_bf16x8(make_uint2(x, y))); };
-      put(2 * piece, wide(k.x, k.y), wide(v.x, v.y));
-      put(2 * piece + 1, wide(k.z, k.w), wide(v.z, v.w));
-    } else {
-      put(piece, k, v);
+  auto after = [&](const Place& p) __attribute__((always_inline)) {
+    Place n = p;
+    ++n.unit;
+    if (p.there && n.unit == p.s.n_units) {
+      n.unit = 0, n.there = pos < stop;
+      if (n.there) n.s = next_segment();
     }
-    if (piece == 0) {
-      const uint32_t slot = in_first[i] + row_of_lane;
-      lds_kind[buffer][row] = !there ? kNobody : slot < in_length ? 0u : 1 + slot - in_length;
-      // (an infinite scale of a key makes NaN of a level of zero, and is NaN here, so that the tokens are taken again)
-      if constexpr (INT8) lds_scale[buffer][0][row] = there ? fmaf(in_ks[i], a.scale, in_ks[i] * 0.f) : 0.f, lds_scale[buffer][1][row] = there ? in_vs[i] : 0.f;
+    return n;
+  };
+  const bool loads = wave < kLoaders;
+  const uint32_t slot_bytes = S::kSize * (uint32_t)c.slot_stride;
+  uint32_t ids[S::kOwnBlocks];
+  auto look_up = [&](const Place& p) __attribute__((always_inline)) {
+    constant_i32* table = (constant_i32*)(c.tables + (uint64_t)p.s.of.seq * c.table_stride);
+    const uint32_t newest = max(p.s.of.end, 1u) - 1, slot = (p.s.unit + p.unit) * kT + wave * S::kOwnRows;
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) ids[b] = (uint32_t)table[min(slot + 16 * b, newest) >> c.page_shift];
+  };
+  auto fetch = [&](const Place& p, auto buffer) __attribute__((always_inline)) {
+    constexpr int kBuffer = decltype(buffer)::value;
+    if (!loads) return;
+    const uint32_t lane = anew(tid) & 63, piece = lane % S::kPieces, row_of_lane = lane / S::kPieces;
+    const uint32_t newest = max(p.s.of.end, 1u) - 1;
+    const uint32_t first = (p.s.unit + p.unit) * kT + wave * S::kOwnRows;
+    uint32_t limit[S::kOwnBlocks];   // tokens of a block, from its first row here, that are there
+    uint64_t at[S::kOwnBlocks], mark[S::kOwnBlocks];
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) {
+      const uint32_t slot = first + 16 * b, from = min(slot, newest & ~(uint32_t)(S::kOwnRows < 16 ? S::kOwnRows - 1 : 15)), id = scalar(ids[b]);
+      const uint32_t page = id < c.n_pages ? id : 0, in_page = from & ((1u << c.page_shift) - 1);
+      limit[b] = id < c.n_pages && slot < p.s.of.end ? min(p.s.of.end - slot, 16u) : 0u;
+      at[b] = S::kSize * ((uint64_t)page * c.page_stride + p.s.kv * c.head_stride + in_page * c.slot_stride);
+      mark[b] = (((uint64_t)page * c.kv_heads + p.s.kv) << c.page_shift) + in_page;
+    }
+    typedef __attribute__((address_space(1))) const uint32_t global_cu32;
+    typedef __attribute__((address_space(3))) uint32_t lds_mu32;
+    bool some = first + S::kOwnRows > p.s.of.length;
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) some |= limit[b] < 16;
+    if (lane == 0) lds_some[kBuffer][wave] = some;
+    if (lane < S::kOwnRows) {
+      const uint32_t slot = first + lane, here = S::kOwnBlocks > 1 && lane >= 16 ? limit[S::kOwnBlocks - 1] : limit[0];
+      lds_kind[kBuffer][wave * S::kOwnRows + lane] = lane % 16 >= here ? kNobody : slot < p.s.of.length ? kAll : slot - p.s.of.length;
+    }
+    if constexpr (INT8) {
+      if (lane < S::kOwnRows) {
+        const uint64_t of = (S::kOwnBlocks > 1 && lane >= 16 ? mark[S::kOwnBlocks - 1] : mark[0]) + lane % 16;
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.k_scale + of), (lds_mu32*)&lds_own_scale[kBuffer][0][wave * S::kOwnRows], 4, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.v_scale + of), (lds_mu32*)&lds_own_scale[kBuffer][1][wave * S::kOwnRows], 4, 0, 0);
+      }
+    }
+    // `all`: every row is there, and all of its dims.  Else, in place of rows that are not there the block's first one comes again, so that what is beside a weight of zero is a
+    // number, and of dims that a head does not have its first ones, against zeros of q.
+    auto request = [&](auto all) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i) {
+        const int b = i / S::kPerBlock;
+        const uint32_t before = (i % S::kPerBlock) * S::kRows, r = i * S::kRows + row_of_lane;   // rows of the block ahead of this load's; row of this loader, as its swizzle goes
+        uint32_t of_k = (INT8 ? piece : piece ^ (r & S::kKeyMask)) * 16, of_v = (INT8 ? piece : piece ^ ((r & S::kValueMask) << 1)) * 16;
+        uint64_t from = at[b] + before * slot_bytes;
+        uint32_t row_at = row_of_lane * slot_bytes;
+        if constexpr (!decltype(all)::value) {
+          if (of_k >= S::kSize * D) of_k = 0;
+          if (of_v >= S::kSize * D) of_v = 0;
+          from = at[b], row_at = before + row_of_lane < limit[b] ? (before + row_of_lane) * slot_bytes : 0;
+        }
+        char* to = stage(buffer) + (wave * S::kOwnRows + i * S::kRows) * S::kPieces * 16;
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.k + from + (row_at + of_k)), (lds_mu32*)to, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.v + from + (row_at + of_v)), (lds_mu32*)(to + kT * S::kPieces * 16), 16, 0, 0);
+      }
+    };
+    if (S::kSize * D == S::kPieces * 16 && !some) request(std::true_type());
+    else request(std::false_type());
+  };
+  auto convert = [&](auto buffer) __attribute__((always_inline)) {   // 8 bits -> bf16
+    constexpr int kBuffer = decltype(buffer)::value;
+    if constexpr (INT8) {
+      const uint32_t tid = anew(threadIdx.x);
+      constexpr uint32_t kAll = 2 * kT * S::kPieces;
+#pragma unroll
+      for (uint32_t first = 0; first < kAll; first += S::kThreads) {
+        const uint32_t i = first + tid, values = i / (kT * S::kPieces), r = i / S::kPieces % kT, piece = i % S::kPieces;
+        if (first + S::kThreads > kAll && i >= kAll) break;
+        const uint4 x = *(const uint4*)(stage(buffer) + 16 * i);
+        char* row = lds_0 + values * kBytes + r * S::kRow;
+        const uint32_t swizzle = values ? (r & S::kValueMask) << 1 : r & S::kKeyMask;
+        *(uint4*)(row + ((2 * piece) ^ swizzle) * 16) = __builtin_bit_cast(uint4, i8x8_to_bf16x8(make_uint2(x.x, x.y)));
+        *(uint4*)(row + ((2 * piece + 1) ^ swizzle) * 16) = __builtin_bit_cast(uint4, i8x8_to_bf16x8(make_uint2(x.z, x.w)));
+      }
+      if (tid < kT) {
+        // (an infinite scale of a key makes NaN of a level of zero, and is NaN here, so that the tokens are taken again)
+        const bool there = lds_kind[kBuffer][tid] != kNobody;
+        const float k = lds_own_scale[kBuffer][0][tid], v = lds_own_scale[kBuffer][1][tid];
+        lds_scale[0][tid] = there ? fmaf(k, a.scale, k * 0.f) : 0.f, lds_scale[1][tid] = there ? v : 0.f;
+      }
     }
   };
 
-  const uint32_t over = min((uint32_t)(kTreeWaves / a.tiles), (uint32_t)S::kTiles);   // wavefronts that share out the tokens of a column tile
+  // ---- a column tile per wavefront, or for several, that share out the tiles of tokens ----
+  uint32_t over = 1;
+  while (over < (uint32_t)S::kTiles && 2 * over * a.tiles <= (uint32_t)S::kWaves) over *= 2;
   const uint32_t of_tile = wave % a.tiles, of_tokens = wave / a.tiles;
   const bool works = of_tokens < over;
-  const uint32_t key_at = n * S::kRow, key_swizzle = g ^ (n & (DIM == 64 ? 7 : 15));
-  const uint32_t value_row = 4 * g + n / 4, value_at0 = value_row * S::kRow + ((value_row & (DIM == 64 ? 3 : 7)) * 32) + n % 4 * 8;
+  const uint32_t key_at = n * S::kRow, key_swizzle = g ^ (n & S::kKeyMask);
+  const uint32_t value_row = 4 * g + n / 4, value_at0 = value_row * S::kRow + (value_row & S::kValueMask) * 32 + n % 4 * 8;
   bf16x8 q[kParts][S::kSteps];
   uint64_t mask = 0;
   auto column_of = [&](const Segment& s, uint32_t column, uint32_t* node) {   // -> query head
+    ARGUMENTS_ANEW;
     *node = column / a.group;
     return s.kv * a.group + column % a.group;
   };
-  auto load_q = [&](const Segment& s) {
+  auto load_q = [&](const Segment& s) __attribute__((always_inline)) {
+    ARGUMENTS_ANEW;
+    const uint32_t D = c.head_dim;
+    const uint32_t lane = anew(threadIdx.x) & 63, g = lane / 16, n = lane % 16;
     const uint32_t column = s.first_column + of_tile * 16 + n;
     const bool has = works && column < a.columns;
     uint32_t node, head = column_of(s, has ? column : 0, &node);
@@ -231,8 +329,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, Tr
 
   f32x4 o[S::kBlocks];
   float top = -INFINITY, total = 0.f;
-  auto take_tile = [&](uint32_t buffer, uint32_t tile) {
-    const char* keys = lds + buffer * 2 * kBytes + tile * kTile * S::kRow;
+  auto take_tile = [&](auto buffer, uint32_t tile, bool some) __attribute__((always_inline)) {
+    constexpr int kBuffer = decltype(buffer)::value;
+    const char* keys = (INT8 ? lds_0 : stage(buffer)) + tile * kTile * S::kRow;
     const char* values = keys + kBytes;
     f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -245,30 +344,49 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, Tr
 #pragma unroll
         for (int b = 0; b < 2; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[b], q[part][i], l[b], 0, 0, 0);
     }
-    float p[8];
-    uint4 kind[2];
+    // The values are asked for ahead of what the weights take.
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    bf16x8 value[S::kBlocks];
+    auto ask = [&](int b) __attribute__((always_inline)) {
+      const char* from = values + (value_at0 ^ (b * 32));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 16 * S::kRow));
+      value[b] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    constexpr int kEarly = 2;
+#pragma unroll
+    for (int b = 0; b < kEarly; ++b) ask(b);
+    float p[8];   // logits, without `scale` where they have no other one
     float4 vs[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      kind[b] = *(const uint4*)&lds_kind[buffer][tile * kTile + 16 * b + 4 * g];
-      float4 ks = make_float4(a.scale, a.scale, a.scale, a.scale);
       if constexpr (INT8) {
-        ks = *(const float4*)&lds_scale[buffer][0][tile * kTile + 16 * b + 4 * g];
-        vs[b] = *(const float4*)&lds_scale[buffer][1][tile * kTile + 16 * b + 4 * g];
+        const float4 ks = *(const float4*)&lds_scale[0][tile * kTile + 16 * b + 4 * g];
+        vs[b] = *(const float4*)&lds_scale[1][tile * kTile + 16 * b + 4 * g];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[4 * b + j] = l[b][j] * (&ks.x)[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[4 * b + j] = l[b][j];
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[4 * b + j] = l[b][j] * (&ks.x)[j];
     }
-    if (__any((kind[0].x | kind[0].y | kind[0].z | kind[0].w | kind[1].x | kind[1].y | kind[1].z | kind[1].w) != 0)) {
+    if (some) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t k = (&kind[i / 4].x)[i % 4];
-        if (!(k == 0 || (k != kNobody && mask >> (k - 1) & 1))) p[i] = -INFINITY;
+      for (int b = 0; b < 2; ++b) {
+        const uint4 kind = *(const uint4*)&lds_kind[kBuffer][tile * kTile + 16 * b + 4 * g];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t k = (&kind.x)[j], word = k & 32 ? (uint32_t)(mask >> 32) : (uint32_t)mask;
+          const uint32_t sees = (k == kAll ? 1u : 0u) | (k < kAll ? word >> (k & 31) & 1u : 0u);
+          p[4 * b + j] = sees ? p[4 * b + j] : -INFINITY;
+        }
       }
     }
     float m = p[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) m = fmaxf(m, p[i]);
+    const float scale = INT8 ? 1.f : a.scale;
+    m *= scale;
     // The weights' reference follows the maximum when that has grown by more than 8 (2^8 is far from any bound of fp32).
     if (__any(m > top + 8.f)) {
       m = fmaxf(m, top);
@@ -286,7 +404,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, Tr
       float w[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        w[j] = __builtin_amdgcn_exp2f(p[i + j] - base);
+        w[j] = __builtin_amdgcn_exp2f(fmaf(p[i + j], scale, -base));
         total += w[j];
         if constexpr (INT8) w[j] *= (&vs[i / 4].x)[i % 4 + j];
       }
@@ -297,195 +415,231 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attend_tree(CacheView c, Tr
         w[0] -= __uint_as_float(lo & 0xFFFF0000u), w[1] -= __uint_as_float(hi & 0xFFFF0000u);
       }
     }
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 #pragma unroll
-    for (int b = 0; b < S::kBlocks; ++b) {
-      const char* from = values + (value_at0 ^ (b * 32));
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 16 * S::kRow));
-      const bf16x8 value = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    for (int first = 0; first < S::kBlocks; first += kEarly) {
+      if (first)
+#pragma unroll
+        for (int b = 0; b < kEarly; ++b) ask(first + b);
 #pragma unroll
       for (int k = 0; k < 3; ++k)
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, __builtin_bit_cast(bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), o[b], 0, 0, 0);
+#pragma unroll
+        for (int b = first; b < first + kEarly; ++b)
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[b], __builtin_bit_cast(bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), o[b], 0, 0, 0);
     }
   };
 
-  // A segment's tokens once more, a product per value as the formula has them, so that infinities give what they give there: only for what is not finite, and
-  // slow.  Its results replace those in LDS.
-  auto take_again = [&](const Segment& s, float* sums) {
-    const uint32_t begin = s.unit * kT, end = min(s.of.end, (s.unit + s.n_units) * kT), mine = min(a.columns - s.first_column, a.tiles * 16);
-    for (uint32_t col = 0; col < mine; ++col) {
-      if (!lds_odd_column[col]) continue;
-      uint32_t node, head = column_of(s, s.first_column + col, &node);
-      const uint64_t row = (uint64_t)s.t * a.nodes + node, sees = a.masks[row];
-      const uint64_t q_at = row * a.q_stride + head * D;
-      float m = -INFINITY, sum_p = 0.f, sum = 0.f;
-      for (uint32_t first = begin; first < end && node < s.of.size; first += kTreeThreads) {
-        const uint32_t slot = first + tid;
-        uint32_t page = c.n_pages;
-        if (slot < end && (slot < s.of.length || sees >> (slot - s.of.length) & 1)) page = (uint32_t)c.tables[(uint64_t)s.of.seq * c.table_stride + (slot >> c.page_shift)];
-        const bool there = page < c.n_pages;
-        const uint32_t in_page = slot & ((1u << c.page_shift) - 1);
-        const uint64_t at = S::kSize * ((uint64_t)(there ? page : 0) * c.page_stride + s.kv * c.head_stride + in_page * c.slot_stride);
-        const uint64_t mark = (((uint64_t)(there ? page : 0) * c.kv_heads + s.kv) << c.page_shift) + in_page;
-        float l = -INFINITY;
-        if (there) {
-          const float scale = INT8 ? c.k_scale[mark] : 1.f;
-          const bool after = fabsf(scale) < INFINITY;   // (an infinite scale makes NaN of a level of zero)
-          l = 0.f;
-          for (uint32_t x = 0; x < D; ++x) {
-            const float of_q = (Q16 ? bf16_value(((const uint16_t*)a.q)[q_at + x]) : ((const float*)a.q)[q_at + x]) * a.scale;
-            l = fmaf(of_q, after ? value_at<INT8>(c.k + at, x) : value_at<INT8>(c.k + at, x) * scale, l);
-          }
-          if (after) l *= scale;
+  // A column's tokens of a segment once more, a product per value as the formula has them, so that infinities give what they give there: only for what is not finite, and
+  // slow.  256 threads take a token each, then a dim each; the sums go to `sums`.
+  auto take_again = [&](const Segment& s, uint32_t col, float* sums) __attribute__((always_inline)) {
+    constexpr uint32_t kN = 256;
+    ARGUMENTS_ANEW;
+    const uint32_t D = c.head_dim;
+    const uint32_t tid = anew(threadIdx.x);
+    const uint32_t begin = s.unit * kT, end = min(s.of.end, (s.unit + s.n_units) * kT);
+    uint32_t node, head = column_of(s, s.first_column + col, &node);
+    const uint64_t row = (uint64_t)s.t * a.nodes + node, sees = node < s.of.size ? a.masks[row] : 0;
+    const uint64_t q_at = row * a.q_stride + head * D;
+    float m = -INFINITY, sum_p = 0.f, sum = 0.f;
+    for (uint32_t first = begin; first < end && node < s.of.size; first += kN) {
+      const uint32_t slot = first + tid;
+      uint32_t page = c.n_pages;
+      if (tid < kN && slot < end && (slot < s.of.length || sees >> (slot - s.of.length) & 1)) page = (uint32_t)c.tables[(uint64_t)s.of.seq * c.table_stride + (slot >> c.page_shift)];
+      const bool there = page < c.n_pages;
+      const uint32_t in_page = slot & ((1u << c.page_shift) - 1);
+      const uint64_t at = S::kSize * ((uint64_t)(there ? page : 0) * c.page_stride + s.kv * c.head_stride + in_page * c.slot_stride);
+      const uint64_t mark = (((uint64_t)(there ? page : 0) * c.kv_heads + s.kv) << c.page_shift) + in_page;
+      float l = -INFINITY;
+      if (there) {
+        const float scale = INT8 ? c.k_scale[mark] : 1.f;
+        const bool after = fabsf(scale) < INFINITY;   // (an infinite scale makes NaN of a level of zero)
+        l = 0.f;
+#pragma unroll 1
+        for (uint32_t x = 0; x < D; ++x) {
+          const float of_q = (Q16 ? bf16_value(((const uint16_t*)a.q)[q_at + x]) : ((const float*)a.q)[q_at + x]) * a.scale;
+          l = fmaf(of_q, after ? value_at<INT8>(c.k + at, x) : value_at<INT8>(c.k + at, x) * scale, l);
         }
-        __syncthreads();
-        lds_weight[tid] = l, lds_at[tid] = there ? at : ~0ull;
-        __syncthreads();
-        float most = m;
-        for (uint32_t i = 0; i < kTreeThreads; ++i) most = fmaxf(most, lds_weight[i]);
-        const float base = most == -INFINITY ? 0.f : most, shrink = exp2f(m - base);
-        m = most, sum_p *= shrink, sum *= shrink;
-        const float p = there ? exp2f(l - base) : 0.f, with_scale = there && INT8 ? p * c.v_scale[mark] : p;
-        __syncthreads();
-        lds_weight[tid] = p;
-        __syncthreads();
-        for (uint32_t i = 0; i < kTreeThreads; ++i) sum_p += lds_weight[i];
-        __syncthreads();
-        lds_weight[tid] = with_scale;
-        __syncthreads();
-        if (tid < D)
-          for (uint32_t i = 0; i < kTreeThreads; ++i)
-            if (lds_at[i] != ~0ull) sum = fmaf(lds_weight[i], value_at<INT8>(c.v + lds_at[i], tid), sum);
+        if (after) l *= scale;
       }
-      // the first of the wavefronts that share this tile has it all, the others nothing
-      for (uint32_t w = 0; w < over; ++w) {
-        const uint32_t at = (col / 16 + w * a.tiles) * 16 + col % 16;
-        if (tid < DIM) sums[at * (DIM + 4) + tid] = w ? 0.f : sum;
-        if (tid == 0) lds_max[at] = w ? -INFINITY : m, lds_total[at] = w ? 0.f : sum_p;
+      __syncthreads();
+      if (tid < kN) lds_weight[tid] = l, lds_at[tid] = there ? at : ~0ull;
+      __syncthreads();
+      float most = m;
+#pragma unroll 1
+      for (uint32_t i = 0; i < kN; ++i) most = fmaxf(most, lds_weight[i]);
+      const float base = most == -INFINITY ? 0.f : most, shrink = __builtin_amdgcn_exp2f(m - base);
+      m = most, sum_p *= shrink, sum *= shrink;
+      const float p = there ? __builtin_amdgcn_exp2f(l - base) : 0.f, with_scale = there && INT8 ? p * c.v_scale[mark] : p;
+      __syncthreads();
+      if (tid < kN) lds_weight[tid] = p;
+      __syncthreads();
+#pragma unroll 1
+      for (uint32_t i = 0; i < kN; ++i) sum_p += lds_weight[i];
+      __syncthreads();
+      if (tid < kN) lds_weight[tid] = with_scale;
+      __syncthreads();
+      if (tid < D) {
+#pragma unroll 1
+        for (uint32_t i = 0; i < kN; ++i)
+          if (lds_at[i] != ~0ull) sum = fmaf(lds_weight[i], value_at<INT8>(c.v + lds_at[i], tid), sum);
       }
     }
+    if (tid < DIM) sums[tid] = sum;
+    if (tid == 0) lds_max[col] = m, lds_total[col] = sum_p;
+    __syncthreads();
   };
 
-  auto finish = [&](const Segment& s) {
-    float* sums = (float*)lds;
+  // The end of a segment: the wavefronts of a column tile join, in LDS that its last stage took, and the first of them writes.
+  auto finish = [&](const Segment& s, float* sums) __attribute__((always_inline)) {
+    ARGUMENTS_ANEW;
+    const uint32_t D = c.head_dim;
+    const uint32_t tid = anew(threadIdx.x), lane = tid & 63, g = lane / 16, n = lane % 16;
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
+    if (tid == 0) lds_odd = 0;
+    if (tid < S::kWaves * 16) lds_odd_column[tid] = 0;
+    __syncthreads();   // everyone is done with the stage
+    for (uint32_t half = over / 2; half; half /= 2) {
+      if (works && of_tokens >= half && of_tokens < 2 * half) {
+        const uint32_t at = (of_tokens - half) * a.tiles + of_tile;
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b) *(f32x4*)&sums[((at * S::kBlocks + b) * 64 + lane) * 4] = o[b];
+        if (g == 0) lds_max[at * 16 + n] = top, lds_total[at * 16 + n] = total;
+      }
+      __syncthreads();
+      if (of_tokens < half) {
+        const uint32_t at = of_tokens * a.tiles + of_tile;
+        const float other = lds_max[at * 16 + n], m = fmaxf(top, other), base = m == -INFINITY ? 0.f : m;
+        const float e = __builtin_amdgcn_exp2f(top - base), f = __builtin_amdgcn_exp2f(other - base);
+        total = fmaf(f, lds_total[at * 16 + n], total * e), top = m;
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b) {
+          const f32x4 v = *(const f32x4*)&sums[((at * S::kBlocks + b) * 64 + lane) * 4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[b][j] = fmaf(f, v[j], o[b][j] * e);
+        }
+      }
+      __syncthreads();
+    }
+    const uint32_t column = s.first_column + of_tile * 16 + n;
+    const bool mine = of_tokens == 0 && column < a.columns;
     float odd = total * 0.f;   // a query, key or value that is not finite leaves no total or sum finite that it went into
 #pragma unroll
     for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
       for (int j = 0; j < 4; ++j) odd = fmaf(o[b][j], 0.f, odd);
-    if (tid == 0) lds_odd = 0;
-    if (tid < kMostTiles * 16) lds_odd_column[tid] = 0;
-    __syncthreads();   // everyone is done with the stages
-    if (works) {
-#pragma unroll
-      for (int b = 0; b < S::kBlocks; ++b) *(f32x4*)&sums[(wave * 16 + n) * (DIM + 4) + b * 16 + 4 * g] = o[b];
-      if (g == 0) lds_max[wave * 16 + n] = top, lds_total[wave * 16 + n] = total;
-      if (!(odd == 0.f)) lds_odd = lds_odd_column[of_tile * 16 + n] = 1;
-    }
+    if (mine && !(odd == 0.f)) lds_odd = lds_odd_column[of_tile * 16 + n] = 1;
     __syncthreads();
     if (__builtin_expect(lds_odd, 0)) {
-      take_again(s, sums);
-      __syncthreads();
-    }
-    constexpr uint32_t kLanes = DIM / 4, kAtATime = kTreeThreads / kLanes;   // lanes of a column, four dims each
-    const uint32_t d0 = tid % kLanes * 4, mine = min(a.columns - s.first_column, a.tiles * 16);
-    const bool whole = s.n_units == s.units;
-    float* to_part = a.partials + (uint64_t)(2 * blockIdx.x + (blockIdx.x * share >= s.first ? 0 : 1)) * (a.tiles * 16 * (DIM + 2));
-    for (uint32_t col = tid / kLanes; col < mine; col += kAtATime) {
-      float m = -INFINITY, sum_p = 0.f;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t w = 0; w < over; ++w) m = fmaxf(m, lds_max[(col / 16 + w * a.tiles) * 16 + col % 16]);
-      const float base = m == -INFINITY ? 0.f : m;
-      for (uint32_t w = 0; w < over; ++w) {
-        const uint32_t at = (col / 16 + w * a.tiles) * 16 + col % 16;
-        const float f = __builtin_amdgcn_exp2f(lds_max[at] - base);
-        const float4 v = *(const float4*)&sums[at * (DIM + 4) + d0];
-        sum_p = fmaf(f, lds_total[at], sum_p);
-        sum.x = fmaf(f, v.x, sum.x), sum.y = fmaf(f, v.y, sum.y), sum.z = fmaf(f, v.z, sum.z), sum.w = fmaf(f, v.w, sum.w);
-      }
-      if (whole) {
-        uint32_t node, head = column_of(s, s.first_column + col, &node);
-        write_out(a, s.of.size, s.t, node, head, D, d0, sum, sum_p);
-      } else {
-        *(float4*)&to_part[col * DIM + d0] = sum;
-        if (d0 == 0) *(float2*)&to_part[a.tiles * 16 * DIM + 2 * col] = make_float2(m, sum_p);
+#pragma unroll 1
+      for (uint32_t col = 0; col < a.tiles * 16; ++col) {
+        if (!lds_odd_column[col]) continue;
+        take_again(s, col, sums);
+        if (of_tokens == 0 && of_tile * 16 + n == col) {
+          top = lds_max[col], total = lds_total[col];
+#pragma unroll
+          for (int b = 0; b < S::kBlocks; ++b) o[b] = *(const f32x4*)&sums[16 * b + 4 * g];
+        }
+        __syncthreads();
       }
     }
-    __syncthreads();   // LDS is free again
+    if (of_tokens != 0) return;
+    if (s.n_units == s.units) {
+      if (!mine) return;
+      uint32_t node, head = column_of(s, column, &node);
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) write_out(a, s.of.size, s.t, node, head, D, 16 * b + 4 * g, make_float4(o[b][0], o[b][1], o[b][2], o[b][3]), total);
+    } else {
+      float* to = a.partials + (uint64_t)(2 * blockIdx.x + (blockIdx.x * share >= s.first ? 0 : 1)) * (a.tiles * S::kPartial) + of_tile * S::kPartial;
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) *(f32x4*)&to[(b * 64 + lane) * 4] = o[b];
+      if (g == 0) *(float2*)&to[S::kBlocks * 256 + 2 * n] = make_float2(top, total);
+    }
   };
 
-  Segment s = next_segment(), next = s;
-  uint32_t unit = 0, buffer = 0;
-  in_length = s.of.length;
-#pragma unroll
-  for (int i = 0; i < S::kLoads; ++i) fetch_one(s, s.unit, i);
-  load_q(s);
-  for (;;) {
-    if (unit == 0) {
+  typedef std::integral_constant<int, 0> First;
+  typedef std::integral_constant<int, 1> Second;
+  Place now{next_segment(), 0, true};
+  look_up(now);
+  fetch(now, First());
+  Place next = after(now);
+  look_up(next);
+  load_q(now.s);
+  auto take = [&](auto buffer, auto other) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this stage's loads
+    __syncthreads();
+    if constexpr (INT8) {
+      convert(buffer);
+      __syncthreads();
+    }
+    if (next.there) fetch(next, other);
+    if (works) {
+      constexpr int kBuffer = decltype(buffer)::value;
+      const uint4 x = *(const uint4*)&lds_some[kBuffer][0], y = *(const uint4*)&lds_some[kBuffer][4];
+      const bool some = scalar(x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w) != 0;
+      for (uint32_t tile = of_tokens; tile < (uint32_t)S::kTiles; tile += over) take_tile(buffer, tile, some);
+    }
+  };
+  for (bool odd = false;; odd = !odd) {
+    if (now.unit == 0) {
       top = -INFINITY, total = 0.f;
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const bool last = unit + 1 == s.n_units, more = pos < stop;
-#pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) store_one(buffer, i);
-    if (last && more) next = next_segment();
-    if (!last || more) {
-      in_length = next.of.length;
-      const uint32_t at = last ? next.unit : s.unit + unit + 1;
-#pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) fetch_one(last ? next : s, at, i);
+    odd ? take(Second(), First()) : take(First(), Second());
+    if (now.unit + 1 == now.s.n_units) {
+      finish(now.s, (float*)(odd && !INT8 ? lds_1 : lds_0));
+      if (!next.there) break;
+      load_q(next.s);
     }
-    __syncthreads();
-    if (works)
-      for (uint32_t tile = of_tokens; tile < (uint32_t)S::kTiles; tile += over) take_tile(buffer, tile);
-    buffer ^= 1, ++unit;
-    if (!last) continue;
-    finish(s);
-    if (!more) break;
-    s = next, unit = 0;
-    load_q(s);
+    now = next, next = after(next);
+    look_up(next);
   }
 }
 
-// The parts of what lies in more than one share, joined in the order of the line.  A wavefront takes a column, all lanes four dims at a time.
-template <int DIM, int TOKENS>
+#undef ARGUMENTS_ANEW
+
+// The parts of what lies in more than one share, joined in the order of the line: a wavefront per 16 columns and 16 dims.
+template <int DIM>
 __global__ __launch_bounds__(256) void k_join_tree(CacheView c, TreeView a) {
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = c.kv_heads * a.chunks, D = c.head_dim;
-  const uint32_t per_tree = c.kv_heads * a.columns;
-  for (uint64_t of = (uint64_t)blockIdx.x * 4 + wave; of < (uint64_t)a.trees * per_tree; of += (uint64_t)gridDim.x * 4) {
-    const uint32_t t = (uint32_t)(of / per_tree), kv = (uint32_t)(of % per_tree) / a.columns, column = (uint32_t)of % per_tree % a.columns;
+  using S = Shape<DIM, false>;
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane / 16, n = lane % 16, pairs = c.kv_heads * a.chunks, D = c.head_dim, blocks = (D + 15) / 16;
+  const uint64_t per_tree = (uint64_t)pairs * a.tiles * blocks;
+  for (uint64_t of = (uint64_t)blockIdx.x * 4 + wave; of < a.trees * per_tree; of += (uint64_t)gridDim.x * 4) {
+    const uint32_t t = (uint32_t)(of / per_tree), rest = (uint32_t)(of % per_tree), b = rest % blocks, tile = rest / blocks % a.tiles, pair = rest / blocks / a.tiles;
     uint32_t all = 0, before = 0;
     for (uint32_t first = 0; first < a.trees; first += 64) {
-      const uint32_t units = first + lane < a.trees ? units_of<TOKENS>(seen_by(c, a, first + lane).end) : 0u;
+      const uint32_t units = first + lane < a.trees ? units_of<S::kTokens>(seen_by(c, a, first + lane).end) : 0u;
       all += units;
       if (first + lane < t) before += units;
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d), before += __shfl_xor(before, d);
     const Seen seen = seen_by(c, a, t);
-    const uint32_t units = units_of<TOKENS>(seen.end), share = (all * pairs + a.groups - 1) / a.groups;
-    const uint32_t chunk = column / (a.tiles * 16), col = column % (a.tiles * 16), first = before * pairs + (kv * a.chunks + chunk) * units;
+    const uint32_t units = units_of<S::kTokens>(seen.end), share = (all * pairs + a.groups - 1) / a.groups, first = before * pairs + pair * units;
     const uint32_t group0 = first / share, group1 = (first + units - 1) / share;
     if (group0 == group1) continue;
-    auto part_of = [&](uint32_t group) { return a.partials + (uint64_t)(2 * group + (group * share >= first ? 0 : 1)) * (a.tiles * 16 * (DIM + 2)); };
+    auto part_of = [&](uint32_t group) { return a.partials + ((uint64_t)(2 * group + (group * share >= first ? 0 : 1)) * a.tiles + tile) * S::kPartial; };
     float m = -INFINITY, sum_p = 0.f;
-    for (uint32_t group = group0; group <= group1; ++group) m = fmaxf(m, part_of(group)[a.tiles * 16 * DIM + 2 * col]);
-    const float base = m == -INFINITY ? 0.f : m;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    const uint32_t d0 = 4 * lane < DIM ? 4 * lane : 0;
-    for (uint32_t group = group0; group <= group1; ++group) {
-      const float* from = part_of(group);
-      const float2 st = *(const float2*)&from[a.tiles * 16 * DIM + 2 * col];
-      const float f = __builtin_amdgcn_exp2f(st.x - base);
-      const float4 v = *(const float4*)&from[col * DIM + d0];
-      sum_p = fmaf(f, st.y, sum_p);
-      sum.x = fmaf(f, v.x, sum.x), sum.y = fmaf(f, v.y, sum.y), sum.z = fmaf(f, v.z, sum.z), sum.w = fmaf(f, v.w, sum.w);
+    constexpr uint32_t kAhead = 8;
+    for (uint32_t group = group0; group <= group1; group += kAhead) {
+      float4 v[kAhead];
+      float2 st[kAhead];
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) {
+        const float* from = part_of(min(group + i, group1));
+        v[i] = *(const float4*)&from[(b * 64 + lane) * 4], st[i] = *(const float2*)&from[S::kBlocks * 256 + 2 * n];
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) {
+        if (group + i > group1) continue;
+        const float to = fmaxf(m, st[i].x), base = to == -INFINITY ? 0.f : to, e = __builtin_amdgcn_exp2f(m - base), f = __builtin_amdgcn_exp2f(st[i].x - base);
+        m = to, sum_p = fmaf(f, st[i].y, sum_p * e);
+        sum.x = fmaf(f, v[i].x, sum.x * e), sum.y = fmaf(f, v[i].y, sum.y * e), sum.z = fmaf(f, v[i].z, sum.z * e), sum.w = fmaf(f, v[i].w, sum.w * e);
+      }
     }
-    if (4 * lane < DIM) write_out(a, seen.size, t, column / a.group, kv * a.group + column % a.group, D, d0, sum, sum_p);
+    const uint32_t column = (pair % a.chunks * a.tiles + tile) * 16 + n;
+    if (column < a.columns) write_out(a, seen.size, t, column / a.group, pair / a.chunks * a.group + column % a.group, D, 16 * b + 4 * g, sum, sum_p);
   }
 }
 
@@ -505,13 +659,13 @@ int check_tree(const std::string& who, const tq_cache* cache, const tq_tree_args
   if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return refuse(TQ_E_INVALID_ARG, who + ": scale must be positive");
   const uint32_t group = a->heads / c->kv_heads, dim = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256, tokens = 16384 / dim;
   l->columns = a->nodes * group;
-  const uint32_t all_tiles = (l->columns + 15) / 16;
-  l->chunks = (all_tiles + kMostTiles - 1) / kMostTiles;
+  const uint32_t all_tiles = (l->columns + 15) / 16, most = dim == 256 ? kTreeWaves<256> : kTreeWaves<64>;
+  l->chunks = (all_tiles + most - 1) / most;
   l->tiles = (all_tiles + l->chunks - 1) / l->chunks;
   l->units = (c->capacity + tokens - 1) / tokens;
-  const uint64_t most = (uint64_t)a->trees * c->kv_heads * l->chunks * l->units;   // if all sequences are full
-  if (most >= (1u << 31) - kMaxGroups) return refuse(TQ_E_UNSUPPORTED, who + ": trees * heads * capacity is beyond what one call takes");
-  l->groups = (uint32_t)std::min<uint64_t>(kMaxGroups, std::max<uint64_t>(1, most));
+  const uint64_t line = (uint64_t)a->trees * c->kv_heads * l->chunks * l->units;   // if all sequences are full
+  if (line >= (1u << 31) - kMaxGroups) return refuse(TQ_E_UNSUPPORTED, who + ": trees * heads * capacity is beyond what one call takes");
+  l->groups = (uint32_t)std::min<uint64_t>(kMaxGroups, std::max<uint64_t>(1, line));
   l->bytes = l->units > 1 ? (uint64_t)l->groups * 2 * l->tiles * 16 * (dim + 2) * 4 : 16;
   return TQ_OK;
 }
@@ -534,17 +688,14 @@ int attend_tree(const tq_cache* cache, const tq_tree_args* a, void* stream) {
   const TreeView v{a->q, (uint16_t*)a->out, a->seqs, a->lengths, a->sizes, a->masks, (float*)a->workspace, a->q_stride ? a->q_stride : row, a->out_stride ? a->out_stride : row,
                    a->scale * kLog2e, a->trees, a->nodes, a->heads, a->heads / c.kv_heads, l.columns, l.tiles, l.chunks, l.groups};
   hipStream_t st = (hipStream_t)stream;
-  auto go = [&](auto dim, auto kernel) {
-    constexpr int kDim = decltype(dim)::value;
-    hipLaunchKernelGGL(kernel, dim3(l.groups), dim3(kTreeThreads), 0, st, c, v);
-    if (l.units == 1) return;   // nothing is cut
-    const uint64_t columns = (uint64_t)a->trees * c.kv_heads * l.columns;
-    hipLaunchKernelGGL((k_join_tree<kDim, 16384 / kDim>), dim3((uint32_t)std::min<uint64_t>((columns + 3) / 4, 16384)), dim3(256), 0, st, c, v);
-  };
   auto of = [&](auto dim) {
     constexpr int kDim = decltype(dim)::value;
-    if (cache->type == TQ_INT8) q16 ? go(dim, k_attend_tree<kDim, true, true>) : go(dim, k_attend_tree<kDim, true, false>);
-    else q16 ? go(dim, k_attend_tree<kDim, false, true>) : go(dim, k_attend_tree<kDim, false, false>);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(l.groups), dim3(kTreeWaves<kDim> * 64), 0, st, c, v); };
+    if (cache->type == TQ_INT8) q16 ? go(k_attend_tree<kDim, true, true>) : go(k_attend_tree<kDim, true, false>);
+    else q16 ? go(k_attend_tree<kDim, false, true>) : go(k_attend_tree<kDim, false, false>);
+    if (l.units == 1) return;   // nothing is cut
+    const uint64_t waves = (uint64_t)a->trees * c.kv_heads * l.chunks * l.tiles * ((c.head_dim + 15) / 16);
+    hipLaunchKernelGGL(k_join_tree<kDim>, dim3((uint32_t)std::min<uint64_t>((waves + 3) / 4, 16384)), dim3(256), 0, st, c, v);
   };
   if (c.head_dim <= 64) of(std::integral_constant<int, 64>());
   else if (c.head_dim <= 128) of(std::integral_constant<int, 128>());
