@@ -92,9 +92,9 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   __shared__ __attribute__((aligned(16))) float lds_scale[2][INT8 ? kT : 4], lds_own_scale[2][2][INT8 ? kT : 4];   // of keys (times `scale`), of values; as they are in memory
   __shared__ float lds_max[S::kWaves * 16], lds_total[S::kWaves * 16], lds_weight[256];
   __shared__ uint64_t lds_at[256];
-  __shared__ __attribute__((aligned(16))) uint32_t lds_some[2][kLoaders];   // a loader's rows of a stage: some of them are not of the context
+  __shared__ __attribute__((aligned(16))) uint32_t lds_some[2][kLoaders];   // a loader's rows of a stage: some of them are not of the context, and their kinds are told
   __shared__ uint32_t lds_odd, lds_odd_column[S::kWaves * 16];
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane / 16, n = lane % 16, D = c.head_dim;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), D = c.head_dim;
   auto scalar = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
   // A thread's number that looks new each time: what is made of it is made where it is used, and takes no registers from the products.
   auto anew = [](uint32_t v) {
@@ -196,6 +196,10 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   };
   const bool loads = wave < kLoaders;
   const uint32_t slot_bytes = S::kSize * (uint32_t)c.slot_stride;
+  const uint64_t page_bytes = S::kSize * c.page_stride;
+  typedef __attribute__((address_space(1))) const uint32_t global_cu32;
+  typedef __attribute__((address_space(3))) uint32_t lds_mu32;
+  constexpr int kKeyPlaces = S::kRows >= 8 || INT8 ? 1 : 8 / S::kRows, kValuePlaces = S::kRows >= 4 || INT8 ? 1 : 4 / S::kRows;
   uint32_t ids[S::kOwnBlocks];
   auto look_up = [&](const Place& p) __attribute__((always_inline)) {
     constant_i32* table = (constant_i32*)(c.tables + (uint64_t)p.s.of.seq * c.table_stride);
@@ -206,58 +210,72 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   auto fetch = [&](const Place& p, auto buffer) __attribute__((always_inline)) {
     constexpr int kBuffer = decltype(buffer)::value;
     if (!loads) return;
-    const uint32_t lane = anew(tid) & 63, piece = lane % S::kPieces, row_of_lane = lane / S::kPieces;
-    const uint32_t newest = max(p.s.of.end, 1u) - 1;
+    const uint32_t lane = anew(tid) & 63;
+    // Where a lane's piece of the i-th row group lies beside the group's first byte (of dims that a head does not have: its first ones, against zeros of q).
+    uint32_t key_from[kKeyPlaces], value_from[kValuePlaces];
+#pragma unroll
+    for (int i = 0; i < kKeyPlaces; ++i) {
+      const uint32_t piece = lane % S::kPieces, row = lane / S::kPieces, r = i * S::kRows + row;
+      const uint32_t of_k = (INT8 ? piece : piece ^ (r & S::kKeyMask)) * 16, of_v = (INT8 ? piece : piece ^ ((r & S::kValueMask) << 1)) * 16;
+      key_from[i] = row * slot_bytes + (of_k < S::kSize * D ? of_k : 0);
+      if (i < kValuePlaces) value_from[i] = row * slot_bytes + (of_v < S::kSize * D ? of_v : 0);
+    }
     const uint32_t first = (p.s.unit + p.unit) * kT + wave * S::kOwnRows;
-    uint32_t limit[S::kOwnBlocks];   // tokens of a block, from its first row here, that are there
-    uint64_t at[S::kOwnBlocks], mark[S::kOwnBlocks];
+    bool plain = first + S::kOwnRows <= p.s.of.length;
 #pragma unroll
-    for (int b = 0; b < S::kOwnBlocks; ++b) {
-      const uint32_t slot = first + 16 * b, from = min(slot, newest & ~(uint32_t)(S::kOwnRows < 16 ? S::kOwnRows - 1 : 15)), id = scalar(ids[b]);
-      const uint32_t page = id < c.n_pages ? id : 0, in_page = from & ((1u << c.page_shift) - 1);
-      limit[b] = id < c.n_pages && slot < p.s.of.end ? min(p.s.of.end - slot, 16u) : 0u;
-      at[b] = S::kSize * ((uint64_t)page * c.page_stride + p.s.kv * c.head_stride + in_page * c.slot_stride);
-      mark[b] = (((uint64_t)page * c.kv_heads + p.s.kv) << c.page_shift) + in_page;
-    }
-    typedef __attribute__((address_space(1))) const uint32_t global_cu32;
-    typedef __attribute__((address_space(3))) uint32_t lds_mu32;
-    bool some = first + S::kOwnRows > p.s.of.length;
-#pragma unroll
-    for (int b = 0; b < S::kOwnBlocks; ++b) some |= limit[b] < 16;
-    if (lane == 0) lds_some[kBuffer][wave] = some;
-    if (lane < S::kOwnRows) {
-      const uint32_t slot = first + lane, here = S::kOwnBlocks > 1 && lane >= 16 ? limit[S::kOwnBlocks - 1] : limit[0];
-      lds_kind[kBuffer][wave * S::kOwnRows + lane] = lane % 16 >= here ? kNobody : slot < p.s.of.length ? kAll : slot - p.s.of.length;
-    }
-    if constexpr (INT8) {
-      if (lane < S::kOwnRows) {
-        const uint64_t of = (S::kOwnBlocks > 1 && lane >= 16 ? mark[S::kOwnBlocks - 1] : mark[0]) + lane % 16;
-        __builtin_amdgcn_global_load_lds((global_cu32*)(c.k_scale + of), (lds_mu32*)&lds_own_scale[kBuffer][0][wave * S::kOwnRows], 4, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_cu32*)(c.v_scale + of), (lds_mu32*)&lds_own_scale[kBuffer][1][wave * S::kOwnRows], 4, 0, 0);
-      }
-    }
-    // `all`: every row is there, and all of its dims.  Else, in place of rows that are not there the block's first one comes again, so that what is beside a weight of zero is a
-    // number, and of dims that a head does not have its first ones, against zeros of q.
-    auto request = [&](auto all) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) {
-        const int b = i / S::kPerBlock;
-        const uint32_t before = (i % S::kPerBlock) * S::kRows, r = i * S::kRows + row_of_lane;   // rows of the block ahead of this load's; row of this loader, as its swizzle goes
-        uint32_t of_k = (INT8 ? piece : piece ^ (r & S::kKeyMask)) * 16, of_v = (INT8 ? piece : piece ^ ((r & S::kValueMask) << 1)) * 16;
-        uint64_t from = at[b] + before * slot_bytes;
-        uint32_t row_at = row_of_lane * slot_bytes;
-        if constexpr (!decltype(all)::value) {
-          if (of_k >= S::kSize * D) of_k = 0;
-          if (of_v >= S::kSize * D) of_v = 0;
-          from = at[b], row_at = before + row_of_lane < limit[b] ? (before + row_of_lane) * slot_bytes : 0;
-        }
-        char* to = stage(buffer) + (wave * S::kOwnRows + i * S::kRows) * S::kPieces * 16;
-        __builtin_amdgcn_global_load_lds((global_cu32*)(c.k + from + (row_at + of_k)), (lds_mu32*)to, 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_cu32*)(c.v + from + (row_at + of_v)), (lds_mu32*)(to + kT * S::kPieces * 16), 16, 0, 0);
-      }
+    for (int b = 0; b < S::kOwnBlocks; ++b) plain &= ids[b] < c.n_pages;
+    char* to = stage(buffer) + wave * S::kOwnRows * S::kPieces * 16;
+    auto request = [&](uint64_t at, uint32_t of_k, uint32_t of_v, int i) __attribute__((always_inline)) {
+      __builtin_amdgcn_global_load_lds((global_cu32*)(c.k + at + of_k), (lds_mu32*)(to + i * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_cu32*)(c.v + at + of_v), (lds_mu32*)(to + i * 1024 + kT * S::kPieces * 16), 16, 0, 0);
     };
-    if (S::kSize * D == S::kPieces * 16 && !some) request(std::true_type());
-    else request(std::false_type());
+    auto request_scales = [&](uint64_t mark) __attribute__((always_inline)) {   // (by the lanes of the wavefront's rows)
+      __builtin_amdgcn_global_load_lds((global_cu32*)(c.k_scale + mark), (lds_mu32*)&lds_own_scale[kBuffer][0][wave * S::kOwnRows], 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_cu32*)(c.v_scale + mark), (lds_mu32*)&lds_own_scale[kBuffer][1][wave * S::kOwnRows], 4, 0, 0);
+    };
+    const uint32_t page_mask = (1u << c.page_shift) - 1;
+    if (__builtin_expect(plain, 1)) {
+      if (lane == 0) lds_some[kBuffer][wave] = 0;
+#pragma unroll
+      for (int b = 0; b < S::kOwnBlocks; ++b) {
+        const uint64_t at = ids[b] * page_bytes + (uint64_t)(p.s.kv * c.head_stride) * S::kSize + (uint64_t)((first + 16 * b) & page_mask) * slot_bytes;
+#pragma unroll
+        for (int j = 0; j < S::kPerBlock; ++j) {
+          const int i = b * S::kPerBlock + j;
+          request(at + j * S::kRows * slot_bytes, key_from[i % kKeyPlaces], value_from[i % kValuePlaces], i);
+        }
+      }
+      if constexpr (INT8) {
+        if (lane < S::kOwnRows) {
+          const uint32_t id = S::kOwnBlocks > 1 && lane >= 16 ? ids[S::kOwnBlocks - 1] : ids[0];
+          request_scales((((uint64_t)id * c.kv_heads + p.s.kv) << c.page_shift) + ((first + lane) & page_mask));
+        }
+      }
+    } else {
+      // In place of rows that are not there the block's first one comes again, so that what is beside a weight of zero is a number.
+      const uint32_t newest = max(p.s.of.end, 1u) - 1, row_of_lane = lane / S::kPieces;
+      uint32_t here_of_lane = 0;
+      uint64_t mark_of_lane = 0;
+#pragma unroll
+      for (int b = 0; b < S::kOwnBlocks; ++b) {
+        const uint32_t slot = first + 16 * b, from = min(slot, newest & ~(uint32_t)(S::kOwnRows < 16 ? S::kOwnRows - 1 : 15)), id = scalar(ids[b]);
+        const uint32_t page = id < c.n_pages ? id : 0, in_page = from & page_mask, limit = id < c.n_pages && slot < p.s.of.end ? min(p.s.of.end - slot, 16u) : 0u;
+        const uint64_t at = page * page_bytes + (uint64_t)(p.s.kv * c.head_stride) * S::kSize + (uint64_t)in_page * slot_bytes;
+#pragma unroll
+        for (int j = 0; j < S::kPerBlock; ++j) {
+          const int i = b * S::kPerBlock + j;
+          const uint32_t row = j * S::kRows + row_of_lane, row_at = row < limit ? row * slot_bytes : 0;
+          request(at, key_from[i % kKeyPlaces] - row_of_lane * slot_bytes + row_at, value_from[i % kValuePlaces] - row_of_lane * slot_bytes + row_at, i);
+        }
+        if (S::kOwnBlocks == 1 || (int)(lane / 16) == b) here_of_lane = limit, mark_of_lane = (((uint64_t)page * c.kv_heads + p.s.kv) << c.page_shift) + in_page + lane % 16;
+      }
+      if (lane == 0) lds_some[kBuffer][wave] = 1;
+      if (lane < S::kOwnRows) {
+        const uint32_t slot = first + lane;
+        lds_kind[kBuffer][wave * S::kOwnRows + lane] = lane % 16 >= here_of_lane ? kNobody : slot < p.s.of.length ? kAll : slot - p.s.of.length;
+        if constexpr (INT8) request_scales(mark_of_lane);
+      }
+    }
   };
   auto convert = [&](auto buffer) __attribute__((always_inline)) {   // 8 bits -> bf16
     constexpr int kBuffer = decltype(buffer)::value;
@@ -276,7 +294,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       }
       if (tid < kT) {
         // (an infinite scale of a key makes NaN of a level of zero, and is NaN here, so that the tokens are taken again)
-        const bool there = lds_kind[kBuffer][tid] != kNobody;
+        const bool there = !lds_some[kBuffer][tid / S::kOwnRows] || lds_kind[kBuffer][tid] != kNobody;
         const float k = lds_own_scale[kBuffer][0][tid], v = lds_own_scale[kBuffer][1][tid];
         lds_scale[0][tid] = there ? fmaf(k, a.scale, k * 0.f) : 0.f, lds_scale[1][tid] = there ? v : 0.f;
       }
@@ -288,12 +306,10 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   while (over < (uint32_t)S::kTiles && 2 * over * a.tiles <= (uint32_t)S::kWaves) over *= 2;
   const uint32_t of_tile = wave % a.tiles, of_tokens = wave / a.tiles;
   const bool works = of_tokens < over;
-  const uint32_t key_at = n * S::kRow, key_swizzle = g ^ (n & S::kKeyMask);
-  const uint32_t value_row = 4 * g + n / 4, value_at0 = value_row * S::kRow + (value_row & S::kValueMask) * 32 + n % 4 * 8;
   bf16x8 q[kParts][S::kSteps];
-  uint64_t mask = 0;
+  __shared__ uint64_t lds_mask[S::kWaves * 16];
   auto column_of = [&](const Segment& s, uint32_t column, uint32_t* node) {   // -> query head
-    ARGUMENTS_ANEW;
+    constant_tree& a = *(constant_tree*)(arguments() + sizeof(CacheView));
     *node = column / a.group;
     return s.kv * a.group + column % a.group;
   };
@@ -305,7 +321,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     const bool has = works && column < a.columns;
     uint32_t node, head = column_of(s, has ? column : 0, &node);
     const uint64_t row = (uint64_t)s.t * a.nodes + node;
-    mask = has && node < s.of.size ? a.masks[row] : 0;
+    if (of_tokens == 0 && g == 0) lds_mask[of_tile * 16 + n] = has && node < s.of.size ? a.masks[row] : 0;   // (a barrier ahead of the next stage's weights)
 #pragma unroll
     for (int i = 0; i < S::kSteps; ++i) {
       const uint32_t d = i * 32 + 8 * g;
@@ -333,16 +349,25 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     constexpr int kBuffer = decltype(buffer)::value;
     const char* keys = (INT8 ? lds_0 : stage(buffer)) + tile * kTile * S::kRow;
     const char* values = keys + kBytes;
+    const uint32_t lane = anew(tid) & 63, g = lane / 16, n = lane % 16;
+    const uint32_t key_at = n * S::kRow, key_swizzle = g ^ (n & S::kKeyMask);
+    const uint32_t value_row = 4 * g + n / 4, value_at0 = value_row * S::kRow + (value_row & S::kValueMask) * 32 + n % 4 * 8;
     f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    constexpr int kKeySteps = S::kSteps < 2 ? S::kSteps : 2;   // of which all keys are asked for at once
 #pragma unroll
-    for (int i = 0; i < S::kSteps; ++i) {
-      bf16x8 key[2];
+    for (int first = 0; first < S::kSteps; first += kKeySteps) {
+      bf16x8 key[kKeySteps][2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) key[b] = *(const bf16x8*)(keys + b * 16 * S::kRow + key_at + ((key_swizzle ^ (4 * i)) * 16));
+      for (int i = 0; i < kKeySteps; ++i)
 #pragma unroll
-      for (int part = 0; part < kParts; ++part)
+        for (int b = 0; b < 2; ++b) key[i][b] = *(const bf16x8*)(keys + b * 16 * S::kRow + key_at + ((key_swizzle ^ (4 * (first + i))) * 16));
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[b], q[part][i], l[b], 0, 0, 0);
+      for (int i = 0; i < kKeySteps; ++i)
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[i][b], q[part][first + i], l[b], 0, 0, 0);
     }
     // The values are asked for ahead of what the weights take.
     typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -371,9 +396,12 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       }
     }
     if (some) {
+      const uint64_t mask = lds_mask[of_tile * 16 + n];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const uint4 kind = *(const uint4*)&lds_kind[kBuffer][tile * kTile + 16 * b + 4 * g];
+        const uint32_t row = tile * kTile + 16 * b + 4 * g;
+        uint4 kind = *(const uint4*)&lds_kind[kBuffer][row];
+        if (!lds_some[kBuffer][row / S::kOwnRows]) kind = make_uint4(kAll, kAll, kAll, kAll);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t k = (&kind.x)[j], word = k & 32 ? (uint32_t)(mask >> 32) : (uint32_t)mask;
