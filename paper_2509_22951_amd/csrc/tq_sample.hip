@@ -6,7 +6,8 @@
 namespace tq {
 namespace {
 
-constexpr uint32_t kMostVocab = 1u << 20, kThreads = 256, kPart = 8 * kThreads;   // kPart: logits of a workgroup
+constexpr uint32_t kMostVocab = 1u << 20, kThreads = 256, kFew = 2, kMany = 8;   // kFew, kMany: four logits each, of a thread
+constexpr uint32_t kMostParts = kMostVocab / (4 * kFew * kThreads);
 constexpr uint32_t kBinThreads = 1024, kBinPart = 8 * kBinThreads, kBins = 2048, kBinsPerUnit = 32, kListed = 2048;   // bins of (largest - logit) / temperature; keys held in LDS
 
 // What the launches leave each other, for every row.
@@ -15,8 +16,9 @@ struct Notes {
   uint64_t* mass;      // [row][kBins]: weights of a bin
   uint32_t* count;     // [row][kBins]: tokens of a bin
   double* kept;        // [row][part]: weight of what is kept beyond doubt
-  uint32_t* listed;    // [row][2]: tokens in the list, workgroups that are done
-  uint32_t* list;      // [row][vocab]: tokens of the bin that the cut lies in
+  uint32_t* listed;    // [row][part]: tokens in the part's list
+  uint64_t* list;      // [row][vocab]: of every part, where its tokens begin, the keys of those in the bin that the cut lies in
+  uint32_t* done;      // [row]: workgroups that are
 };
 
 struct SampleView {
@@ -38,18 +40,36 @@ __device__ __forceinline__ uint32_t rank_of(float l) {
 }
 __device__ __forceinline__ uint64_t key_of(float l, uint32_t i) { return (uint64_t)rank_of(l) << 32 | (uint32_t)~i; }
 
+__device__ __forceinline__ float logit_of_rank(uint32_t rank) { return __uint_as_float(rank >> 31 ? rank & 0x7FFFFFFFu : ~rank); }
+
+// exp((l - top) / temperature) as 2^y, y = (l - top) * (log2(e) / temperature): 2^n times the series of 2^f, ln(2)^k / k! f^k, for |f| <= 1/2, whose 13 terms leave 2^-52 of it.  Few
+// instructions and no branches: a workgroup runs through them once, and what does not fit the instruction cache is waited for.  (Its coefficients are in scalar registers; as literals
+// each costs two moves, and 64 rows of 128256 without filters took 131 us.)
 struct Weigher {
-  double top, temperature;
+  double top, per_unit, c[13];
+  float top32;
+  __device__ __forceinline__ Weigher(float t, float temperature)
+      : top(t), per_unit(1.4426950408889634074 / (double)temperature),
+        c{1., 6.9314718055994531e-01, 2.4022650695910071e-01, 5.5504108664821580e-02, 9.6181291076284772e-03, 1.3333558146428443e-03, 1.5403530393381609e-04, 1.5252733804059840e-05,
+          1.3215486790144309e-06, 1.0178086009239699e-07, 7.0549116208011233e-09, 4.4455382718708115e-10, 2.5678435993488205e-11},
+        top32(t) {
+#pragma unroll
+    for (int k = 0; k < 13; ++k) asm("" : "+s"(c[k]));
+  }
   __device__ __forceinline__ double operator()(float l) const {
-    if (!(l > -INFINITY)) return 0.;
-    if (top == INFINITY) return l == INFINITY ? 1. : 0.;
-    return exp(((double)l - top) / temperature);
+    const double y = fmax(((double)l - top) * per_unit, -1100.), n = rint(y), f = y - n;
+    double s = c[12];
+#pragma unroll
+    for (int k = 11; k >= 0; --k) s = fma(s, f, c[k]);
+    s = ldexp(s, (int)n);
+    s = l == top32 ? 1. : s;
+    return l > -INFINITY ? s : 0.;
   }
 };
 
 // How a row is to be drawn from.
 struct Filter {
-  float top, temperature, p, least;
+  float top, temperature, per_bin, p, least;   // per_bin: bins of a unit of the logit
   uint32_t first, k;
   bool drawn, by_rank, by_mass;   // drawn: not merely the first token; by_rank, by_mass: top_k or top_p leaves something out
 };
@@ -65,6 +85,13 @@ __device__ __forceinline__ T wave_sum(T v) {
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
   return v;
 }
+__device__ __forceinline__ uint32_t wave_least(uint32_t v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = min(v, (uint32_t)__shfl_xor((int)v, d));
+  return v;
+}
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) { return ~wave_least(~v); }
+
 // Sums over a wavefront's lanes up to and with each, in the same order every time.
 template <typename T>
 __device__ __forceinline__ T wave_upto(T v) {
@@ -78,6 +105,11 @@ __device__ __forceinline__ T wave_upto(T v) {
 
 // The first token's key of the row, from the parts' (by all threads; slots: one per wavefront).
 __device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, uint64_t* slots) {
+  Filter f;
+  f.temperature = a.temperature ? a.temperature[r] : 1.f;
+  f.per_bin = (float)kBinsPerUnit / f.temperature;
+  f.p = a.top_p ? a.top_p[r] : 1.f, f.least = a.min_p ? a.min_p[r] : 0.f;
+  const int32_t k = a.top_k ? a.top_k[r] : 0;
   uint64_t best = 0;
   for (uint32_t i = threadIdx.x; i < a.parts; i += blockDim.x) best = max(best, a.notes.keys[(uint64_t)r * a.parts + i]);
   best = wave_max(best);
@@ -85,12 +117,8 @@ __device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, uin
   __syncthreads();
   best = slots[0];
   for (uint32_t w = 1; w < blockDim.x / 64; ++w) best = max(best, slots[w]);
-  Filter f;
   f.first = ~(uint32_t)best;
-  f.top = a.logits[r * a.stride + f.first];
-  f.temperature = a.temperature ? a.temperature[r] : 1.f;
-  f.p = a.top_p ? a.top_p[r] : 1.f, f.least = a.min_p ? a.min_p[r] : 0.f;
-  const int32_t k = a.top_k ? a.top_k[r] : 0;
+  f.top = best >> 32 ? logit_of_rank((uint32_t)(best >> 32)) : -INFINITY;
   f.k = k > 0 ? min((uint32_t)k, a.vocab) : a.vocab;
   f.drawn = f.top > -INFINITY && f.temperature > 0.f;
   f.by_rank = f.k < a.vocab, f.by_mass = f.p < 1.f;
@@ -111,27 +139,32 @@ __device__ __forceinline__ void four_of(const float* row, uint32_t i, uint32_t n
 
 // The bin of a logit: never lower for a smaller one, since each step rounds in order.
 __device__ __forceinline__ float distance_of(const Filter& f, float l) {
-  if (l == f.top) return 0.f;
-  return l > -INFINITY ? (f.top - l) / f.temperature * (float)kBinsPerUnit : INFINITY;
+  const float d = (f.top - l) * f.per_bin;
+  return l == f.top ? 0.f : l > -INFINITY ? d : INFINITY;
 }
 __device__ __forceinline__ uint32_t bin_of(float distance) { return distance < (float)(kBins - 1) ? (uint32_t)distance : kBins - 1; }
 
+// Every part is 1024 * CHUNKS tokens: of few rows small ones, so that there is a workgroup for every compute unit; of many rows larger ones.
+template <int CHUNKS>
+constexpr uint32_t kPart = 4 * CHUNKS * kThreads;
+
 // First launch: the first token of every part; bins and counters are cleared for the next ones.
+template <int CHUNKS>
 __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
   __shared__ uint64_t slots[kThreads / 64];
   const uint32_t part = blockIdx.x, r = blockIdx.y, tid = threadIdx.x;
   const float* row = a.logits + r * a.stride;
-  float v[2][4];
+  float v[CHUNKS][4];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) four_of(row, part * kPart + c * (kPart / 2) + 4 * tid, a.vocab, v[c]);
+  for (int c = 0; c < CHUNKS; ++c) four_of(row, part * kPart<CHUNKS> + 4 * (c * kThreads + tid), a.vocab, v[c]);
   for (uint32_t i = part * kThreads + tid; i < kBins; i += a.parts * kThreads) a.notes.mass[(uint64_t)r * kBins + i] = 0, a.notes.count[(uint64_t)r * kBins + i] = 0;
-  if (part == 0 && tid < 2) a.notes.listed[2 * r + tid] = 0;
+  if (part == 0 && tid == 0) a.notes.done[r] = 0;
   uint64_t best = 0;
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
+  for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t i = part * kPart + c * (kPart / 2) + 4 * tid + j;
+      const uint32_t i = part * kPart<CHUNKS> + 4 * (c * kThreads + tid) + j;
       if (i < a.vocab) best = max(best, key_of(v[c][j], i));
     }
   best = wave_max(best);
@@ -155,17 +188,18 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleView a) {
   for (uint32_t b = tid; b < kBins; b += kBinThreads) lds_mass[b] = 0, lds_count[b] = 0;
   const Filter f = filter_of(a, r, slots);
   if (!f.drawn || (!f.by_rank && !f.by_mass)) return;
-  const Weigher weight{(double)f.top, (double)f.temperature};
+  const Weigher weight(f.top, f.temperature);
   const double unit = (double)(1ull << a.mass_bits);
 #pragma unroll
   for (int c = 0; c < 2; ++c)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t i = blockIdx.x * kBinPart + c * (kBinPart / 2) + 4 * tid + j;
-      if (i >= a.vocab) continue;
       const uint32_t b = bin_of(distance_of(f, v[c][j]));
+      const uint64_t mass = (uint64_t)(weight(v[c][j]) * unit + 0.5);
+      if (i >= a.vocab) continue;
       atomicAdd(&lds_count[b], 1u);
-      if (f.by_mass) atomicAdd((unsigned long long*)&lds_mass[b], (unsigned long long)(weight(v[c][j]) * unit + 0.5));
+      if (f.by_mass) atomicAdd((unsigned long long*)&lds_mass[b], (unsigned long long)mass);
     }
   __syncthreads();
   for (uint32_t b = tid; b < kBins; b += kBinThreads)
@@ -214,16 +248,17 @@ __device__ __forceinline__ Cut find_cut(const uint32_t (&count)[PER], const uint
 // Third launch: the weight of what is kept in every part, and the tokens of the bin that the cut lies in; the last workgroup of a row finds the cut and draws.
 //
 // Bound: the three launches; 64 rows of 128256 logits are read three times, twice of it from the caches.
+template <int CHUNKS>
 __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
-  __shared__ uint64_t slots[kThreads / 64], lds_m[kThreads / 64], lds_keys[kListed], lds_mass[256], lds_more[kMostVocab / kPart];
-  __shared__ uint32_t lds_n[kThreads / 64], lds_count[256], lds_base, lds_done, lds_token, lds_last;
+  __shared__ uint64_t slots[kThreads / 64], lds_m[kThreads / 64], lds_keys[kListed], lds_mass[256], lds_more[kMostParts];
+  __shared__ uint32_t lds_n[kThreads / 64], lds_count[256], lds_upto[kMostParts], lds_base, lds_done, lds_token, lds_last;
   __shared__ double lds_sum[kThreads / 64], lds_share;
   __shared__ Cut lds_cut;
   const uint32_t part = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float* row = a.logits + r * a.stride;
-  float v[2][4];
+  float v[CHUNKS][4];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) four_of(row, part * kPart + c * (kPart / 2) + 4 * tid, a.vocab, v[c]);
+  for (int c = 0; c < CHUNKS; ++c) four_of(row, part * kPart<CHUNKS> + 4 * (c * kThreads + tid), a.vocab, v[c]);
   const Filter f = filter_of(a, r, slots);
   if (!f.drawn) {
     if (part == 0 && tid == 0) {
@@ -232,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     }
     return;
   }
-  const Weigher weight{(double)f.top, (double)f.temperature};
+  const Weigher weight(f.top, f.temperature);
   const double unit = (double)(1ull << a.mass_bits), least = (double)f.least;
   auto mass_of = [&](float l) { return (uint64_t)(weight(l) * unit + 0.5); };
   const bool cuts = f.by_rank || f.by_mass;
@@ -257,20 +292,21 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   }
   auto kept_weight = [&](float l, uint32_t i) {   // of a token that no cut leaves out
     const double w = weight(l);
-    return i == f.first || !(w < least) ? w : 0.;
+    return ((i == f.first) | !(w < least)) ? w : 0.;
   };
 
   // this part
+  const uint32_t part_first = part * kPart<CHUNKS>;
   double sum = 0.;
   uint32_t n = 0;
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
+  for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t i = part * kPart + c * (kPart / 2) + 4 * tid + j;
-      if (i >= a.vocab) continue;
-      const uint32_t b = cuts ? bin_of(distance_of(f, v[c][j])) : 0;
-      if (b < cut.bin) sum += kept_weight(v[c][j], i);
+      const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
+      const uint32_t b = i >= a.vocab ? kBins + 1 : cuts ? bin_of(distance_of(f, v[c][j])) : 0;
+      const double w = kept_weight(v[c][j], i);   // (beyond the row: none)
+      sum += b < cut.bin ? w : 0.;
       n += b == cut.bin;
     }
   sum = wave_sum(sum);
@@ -287,40 +323,74 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     double all = 0.;
     for (uint32_t w = 0; w < kThreads / 64; ++w) all += lds_sum[w];
     __hip_atomic_store((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + part], __builtin_bit_cast(uint64_t, all), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    lds_base = all_n ? __hip_atomic_fetch_add(&a.notes.listed[2 * r], all_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+    __hip_atomic_store(&a.notes.listed[(uint64_t)r * a.parts + part], all_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  __syncthreads();
   if (all_n) {
-    at += lds_base;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t i = part * kPart + c * (kPart / 2) + 4 * tid + j;
-        if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin) __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + at++], i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
+        if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin)
+          __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + part_first + at++], key_of(v[c][j], i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
   }
   // the stores have reached the level that the device shares; the last workgroup goes on with all of the row
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (tid == 0) lds_done = __hip_atomic_fetch_add(&a.notes.listed[2 * r + 1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 0) lds_done = __hip_atomic_fetch_add(&a.notes.done[r], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (lds_done != a.parts - 1) return;
 
   // The cut within the bin: narrowed by a 256th of the bin, then by 8 bits of the key at a time, until few enough are left to compare all with each other.
   uint64_t last = 0;   // tokens of at least this key are kept
-  for (uint32_t i = tid; i < a.parts; i += kThreads) lds_more[i] = 0;
-  const uint32_t all_listed = cuts ? __hip_atomic_load(&a.notes.listed[2 * r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+  constexpr int kPer = kMostParts / kThreads;
+  double weights[kPer];
+  uint32_t listed[kPer], all_listed = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const uint32_t of = tid * kPer + i;
+    weights[i] = 0., listed[i] = 0;
+    if (of < a.parts) {
+      weights[i] = __builtin_bit_cast(double, __hip_atomic_load((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+      if (cuts) listed[i] = __hip_atomic_load(&a.notes.listed[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      lds_more[of] = 0;
+    }
+  }
+  // (keys in the order of the parts: lds_upto[part] of them up to and with a part)
   auto read_key = [&](uint32_t at) {
-    const uint32_t i = __hip_atomic_load(&a.notes.list[(uint64_t)r * a.vocab + at], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return key_of(row[i], i);
+    uint32_t low = 0, high = a.parts - 1;
+    while (low < high) {
+      const uint32_t middle = (low + high) / 2;
+      if (lds_upto[middle] > at) high = middle;
+      else low = middle + 1;
+    }
+    const uint32_t in_part = at - (low ? lds_upto[low - 1] : 0);
+    return __hip_atomic_load(&a.notes.list[(uint64_t)r * a.vocab + low * kPart<CHUNKS> + in_part], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   };
   if (cuts) {
-    for (uint32_t i = tid; i < min(all_listed, kListed); i += kThreads) lds_keys[i] = read_key(i);
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) mine += listed[i];
+    uint32_t in_wave = wave_upto(mine);
+    if (lane == 63) lds_n[wave] = in_wave;
     __syncthreads();
+    uint32_t before = in_wave - mine;
+    for (uint32_t w = 0; w < kThreads / 64; ++w) {
+      if (w < wave) before += lds_n[w];
+      all_listed += lds_n[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      before += listed[i];
+      if (tid * kPer + i < a.parts) lds_upto[tid * kPer + i] = before;
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < min(all_listed, kListed); i += kThreads) lds_keys[i] = read_key(i);
   }
+  __syncthreads();
   auto listed_key = [&](uint32_t at) { return at < kListed ? lds_keys[at] : read_key(at); };
-  auto logit_of = [&](uint64_t key) { return row[~(uint32_t)key]; };
+  auto logit_of = [&](uint64_t key) { return logit_of_rank((uint32_t)(key >> 32)); };
   if (cuts) {
     uint32_t left = all_listed, sub = 256;
     int shift = 64;   // bits of the key from here up are known
@@ -390,20 +460,16 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
       const uint64_t key = listed_key(i);
       if (key < last) continue;
       const uint32_t token = ~(uint32_t)key;
-      atomicAdd((unsigned long long*)&lds_more[token / kPart], (unsigned long long)(kept_weight(row[token], token) * unit + 0.5));
+      atomicAdd((unsigned long long*)&lds_more[token / kPart<CHUNKS>], (unsigned long long)(kept_weight(logit_of(key), token) * unit + 0.5));
     }
   }
   __syncthreads();
 
   // The part that the number falls into, then the token.
-  constexpr int kPer = kMostVocab / kPart / kThreads;
-  double weights[kPer], mine = 0.;
+  double mine = 0.;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const uint32_t of = tid * kPer + i;
-    weights[i] = 0.;
-    if (of < a.parts)
-      weights[i] = __builtin_bit_cast(double, __hip_atomic_load((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) + (double)lds_more[of] / unit;
+    if (tid * kPer + i < a.parts) weights[i] += (double)lds_more[tid * kPer + i] / unit;
     mine += weights[i];
   }
   // Sums up to a thread's, and of all: the wavefronts' in LDS.
@@ -427,15 +493,17 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   __syncthreads();
   {
     double reached = upto - mine;
+    uint32_t first_of = ~0u, last_of = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const uint32_t of = tid * kPer + i;
       reached += weights[i];
-      if (of < a.parts && weights[i] > 0.) {
-        atomicMax(&lds_last, of);
-        if (reached > place) atomicMin(&lds_base, of);
-      }
+      const bool has = of < a.parts && weights[i] > 0.;
+      last_of = has ? of : last_of;
+      first_of = has && reached > place ? min(first_of, of) : first_of;
     }
+    first_of = wave_least(first_of), last_of = wave_most(last_of);
+    if (lane == 0) atomicMin(&lds_base, first_of), atomicMax(&lds_last, last_of);
   }
   __syncthreads();
   const uint32_t of = lds_base != ~0u ? lds_base : lds_last;
@@ -448,43 +516,45 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   }
   __syncthreads();
   double reached = lds_share;
-  const uint32_t first = of * kPart;
-  uint32_t last_kept = 0;   // (a token's number and one)
+  // (a thread takes neighbouring tokens here, so that one sum over the threads is enough; from the caches)
+  const uint32_t at0 = of * kPart<CHUNKS> + 4 * CHUNKS * tid;
+  double w[CHUNKS][4], own = 0.;
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    float x[4];
-    double w[4], four = 0.;
-    const uint32_t at0 = first + c * (kPart / 2) + 4 * tid;
-    four_of(row, at0, a.vocab, x);
+  for (int c = 0; c < CHUNKS; ++c) {
+    four_of(row, at0 + 4 * c, a.vocab, v[c]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      w[j] = at0 + j < a.vocab && key_of(x[j], at0 + j) >= last ? kept_weight(x[j], at0 + j) : 0.;
-      four += w[j];
+      const uint32_t i = at0 + 4 * c + j;
+      const double one = kept_weight(v[c][j], i);
+      w[c][j] = ((i < a.vocab) & (key_of(v[c][j], i) >= last)) ? one : 0.;
+      own += w[c][j];
     }
-    double all;
-    double here = reached + upto_of(four, &all) - four;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      here += w[j];
-      if (w[j] > 0.) {
-        last_kept = at0 + j + 1;
-        if (!beyond && here > place) atomicMin(&lds_token, at0 + j);
-      }
-    }
-    reached += all;
   }
-  if (last_kept) atomicMax(&lds_last, last_kept + kMostVocab);   // (above every part's number)
+  double all_here;
+  double here = reached + upto_of(own, &all_here) - own;
+  uint32_t last_kept = 0, mine_first = ~0u;   // (a token's number and one; a token)
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      here += w[c][j];
+      last_kept = w[c][j] > 0. ? at0 + 4 * c + j + 1 : last_kept;
+      mine_first = w[c][j] > 0. && here > place ? min(mine_first, at0 + 4 * c + j) : mine_first;
+    }
+  mine_first = wave_least(beyond ? ~0u : mine_first), last_kept = wave_most(last_kept);
+  if (lane == 0) atomicMin(&lds_token, mine_first), atomicMax(&lds_last, last_kept + kMostVocab);   // (above every part's number)
   __syncthreads();
   if (tid == 0) {
     const uint32_t token = lds_token != ~0u ? lds_token : lds_last - kMostVocab - 1;
     a.tokens[r] = (int32_t)token;
-    if (a.probs) a.probs[r] = (float)(weight(row[token]) / total);
+    if (a.probs) a.probs[r] = (float)(weight(logit_of_rank(rank_of(row[token]))) / total);
   }
 }
 
 struct Layout {
-  uint64_t keys, kept, mass, count, listed, list, bytes;   // offsets
+  uint64_t keys, kept, mass, count, listed, list, done, bytes;   // offsets
   uint32_t parts;
+  bool many;
 };
 
 int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
@@ -497,14 +567,17 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
     l->bytes += (n + 255) / 256 * 256;
     return at;
   };
-  l->parts = (a->vocab + kPart - 1) / kPart;
+  l->many = (uint64_t)a->rows * ((a->vocab + kPart<kFew> - 1) / kPart<kFew>) > 1024;
+  const uint32_t part = l->many ? kPart<kMany> : kPart<kFew>;
+  l->parts = (a->vocab + part - 1) / part;
   l->bytes = 0;
   l->keys = place((uint64_t)a->rows * l->parts * 8);
   l->kept = place((uint64_t)a->rows * l->parts * 8);
   l->mass = place((uint64_t)a->rows * kBins * 8);
   l->count = place((uint64_t)a->rows * kBins * 4);
-  l->listed = place((uint64_t)a->rows * 8);
-  l->list = place((uint64_t)a->rows * a->vocab * 4);
+  l->listed = place((uint64_t)a->rows * l->parts * 4);
+  l->done = place((uint64_t)a->rows * 4);
+  l->list = place((uint64_t)a->rows * a->vocab * 8);
   return TQ_OK;
 }
 
@@ -523,13 +596,19 @@ int sample(const tq_sample_args* a, void* stream) {
   uint32_t bits = 62;
   while ((a->vocab >> (62 - bits)) > 0) --bits;   // a sum of vocab weights of at most 1 stays below 2^63
   char* ws = (char*)a->workspace;
-  const Notes notes{(uint64_t*)(ws + l.keys), (uint64_t*)(ws + l.mass), (uint32_t*)(ws + l.count), (double*)(ws + l.kept), (uint32_t*)(ws + l.listed), (uint32_t*)(ws + l.list)};
+  const Notes notes{(uint64_t*)(ws + l.keys), (uint64_t*)(ws + l.mass), (uint32_t*)(ws + l.count), (double*)(ws + l.kept), (uint32_t*)(ws + l.listed), (uint64_t*)(ws + l.list),
+                    (uint32_t*)(ws + l.done)};
   const SampleView v{a->logits, a->temperature, a->top_p, a->min_p, a->uniform, a->top_k, a->tokens, a->probs, notes, a->logits_stride ? a->logits_stride : a->vocab, a->rows, a->vocab,
                      l.parts, bits};
   hipStream_t st = (hipStream_t)stream;
-  hipLaunchKernelGGL(k_sample_first, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
-  if (a->top_k || a->top_p) hipLaunchKernelGGL(k_sample_bins, dim3((a->vocab + kBinPart - 1) / kBinPart, a->rows), dim3(kBinThreads), 0, st, v);
-  hipLaunchKernelGGL(k_sample_draw, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
+  auto go = [&](auto chunks) {
+    constexpr int kChunks = decltype(chunks)::value;
+    hipLaunchKernelGGL(k_sample_first<kChunks>, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
+    if (a->top_k || a->top_p) hipLaunchKernelGGL(k_sample_bins, dim3((a->vocab + kBinPart - 1) / kBinPart, a->rows), dim3(kBinThreads), 0, st, v);
+    hipLaunchKernelGGL(k_sample_draw<kChunks>, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
+  };
+  if (l.many) go(std::integral_constant<int, kMany>());
+  else go(std::integral_constant<int, kFew>());
   return launched("tq_sample");
 }
 
