@@ -6,7 +6,7 @@
 namespace tq {
 namespace {
 
-constexpr uint32_t kMostVocab = 1u << 20, kThreads = 256, kFew = 2, kMany = 8;   // kFew, kMany: four logits each, of a thread
+constexpr uint32_t kMostVocab = 1u << 20, kThreads = 256, kFew = 2, kMany = 4;   // kFew, kMany: four logits each, of a thread
 constexpr uint32_t kMostParts = kMostVocab / (4 * kFew * kThreads);
 constexpr uint32_t kBinThreads = 1024, kBinPart = 8 * kBinThreads, kBins = 2048, kBinsPerUnit = 32, kListed = 2048;   // bins of (largest - logit) / temperature; keys held in LDS
 
@@ -182,6 +182,8 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleView a) {
   __shared__ uint32_t lds_count[kBins];
   const uint32_t r = blockIdx.y, tid = threadIdx.x;
   const float* row = a.logits + r * a.stride;
+  // (before anything is asked for: of a row without these filters, and of a greedy one, nothing is read)
+  if (!((a.top_k && a.top_k[r] > 0) || (a.top_p && a.top_p[r] < 1.f)) || (a.temperature && !(a.temperature[r] > 0.f))) return;
   float v[2][4];
 #pragma unroll
   for (int c = 0; c < 2; ++c) four_of(row, blockIdx.x * kBinPart + c * (kBinPart / 2) + 4 * tid, a.vocab, v[c]);
@@ -259,6 +261,15 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   float v[CHUNKS][4];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) four_of(row, part * kPart<CHUNKS> + 4 * (c * kThreads + tid), a.vocab, v[c]);
+  // (the bins are asked for before it is known whether the row has any: two waits for memory in place of three)
+  constexpr int kBinsPer = kBins / kThreads;
+  uint32_t count[kBinsPer];
+  uint64_t mass[kBinsPer];
+#pragma unroll
+  for (int i = 0; i < kBinsPer; ++i) {
+    count[i] = a.notes.count[(uint64_t)r * kBins + tid * kBinsPer + i];
+    mass[i] = a.notes.mass[(uint64_t)r * kBins + tid * kBinsPer + i];
+  }
   const Filter f = filter_of(a, r, slots);
   if (!f.drawn) {
     if (part == 0 && tid == 0) {
@@ -274,21 +285,16 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   Cut cut{kBins, 0, 0};
   double target = 0.;
   if (cuts) {
-    constexpr int kPer = kBins / kThreads;
-    uint32_t count[kPer];
-    uint64_t mass[kPer], all = 0;
+    uint64_t all = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      count[i] = a.notes.count[(uint64_t)r * kBins + tid * kPer + i], mass[i] = f.by_mass ? a.notes.mass[(uint64_t)r * kBins + tid * kPer + i] : 0;
-      all += mass[i];
-    }
+    for (int i = 0; i < kBinsPer; ++i) all += mass[i];
     all = wave_sum((unsigned long long)all);
     if (lane == 0) lds_m[wave] = all;
     __syncthreads();
     all = 0;
     for (uint32_t w = 0; w < kThreads / 64; ++w) all += lds_m[w];
     target = (double)f.p * (double)all;
-    cut = find_cut<kPer>(count, mass, 0, 0, f.k, f.by_mass, target, lds_n, lds_m, &lds_cut);
+    cut = find_cut<kBinsPer>(count, mass, 0, 0, f.k, f.by_mass, target, lds_n, lds_m, &lds_cut);
   }
   auto kept_weight = [&](float l, uint32_t i) {   // of a token that no cut leaves out
     const double w = weight(l);
