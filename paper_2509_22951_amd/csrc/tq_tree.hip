@@ -80,6 +80,26 @@ __device__ __forceinline__ uint32_t units_of(uint32_t end) { return max((end + T
 
 // All (tree, key/value head, chunk, unit of a stage) in this order are one line, cut into equal shares, one per workgroup.  What lies in several shares leaves its parts
 // in memory, and k_join_tree joins them.
+//
+// A workgroup that has the end of one (tree, head, chunk) and the start of another finishes one and takes up the other's queries in between, which costs about two stages.
+// Where there are no more of them than workgroups, and shares need not be longer than by two units for it, every one of them is rounded up to whole shares, so that
+// no workgroup has two (8 trees of 15 nodes, ragged up to 6001 tokens, 24 heads on 8: 67 us cut anywhere, 46 so).
+struct Cutting {
+  uint32_t share;
+  bool whole;   // rounded up
+};
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(v), 63); }
+// all: units of all trees; units: of tree threadIdx.x % 64, if there are no more than 64 trees.
+__device__ __forceinline__ Cutting cutting_of(uint32_t all, uint32_t units, uint32_t trees, uint32_t pairs, uint32_t groups) {
+  const uint32_t even = (all * pairs + groups - 1) / groups;
+  if (trees <= 64 && trees * pairs <= groups) {   // (few units in all then: below 2^31, as is their number times two)
+    for (uint32_t share = even; share <= even + 2; ++share)
+      if (wave_total((units + share - 1) / share) * pairs <= groups) return Cutting{share, true};
+  }
+  return Cutting{even, false};
+}
+__device__ __forceinline__ uint32_t rounded(uint32_t units, const Cutting& cut) { return cut.whole ? (units + cut.share - 1) / cut.share * cut.share : units; }
+
 template <int DIM, bool INT8, bool Q16>
 __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
@@ -135,8 +155,10 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     all += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
     if (first == 0) break;
   }
+  const Cutting cutting = cutting_of(all, lane_units, a.trees, pairs, gridDim.x);
+  const uint32_t share = cutting.share;
+  if (cutting.whole) upto = wave_prefix_sum(rounded(lane_units, cutting)), all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   all *= pairs;
-  const uint32_t share = (all + gridDim.x - 1) / gridDim.x;
   uint32_t pos = blockIdx.x * share;
   const uint32_t stop = min(pos + share, all);
   if (pos >= stop) return;
@@ -165,12 +187,12 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     s.t = t, s.of = seen_by(c, a, t);
     s.of.seq = scalar(s.of.seq), s.of.length = scalar(s.of.length), s.of.end = scalar(s.of.end), s.of.size = scalar(s.of.size);
     s.units = (uint32_t)__builtin_amdgcn_readlane((int)lane_units, t & 63);
-    const uint32_t pair = (pos - tree_first) / s.units;
-    s.first = tree_first + pair * s.units;
+    const uint32_t on_line = rounded(s.units, cutting), pair = (pos - tree_first) / on_line;
+    s.first = tree_first + pair * on_line;
     s.kv = pair / a.chunks, s.first_column = pair % a.chunks * a.tiles * 16;
     s.unit = pos - s.first, s.n_units = min(s.units - s.unit, stop - pos);
-    pos += s.n_units;
-    if (pos == tree_first + s.units * (c.kv_heads * a.chunks)) {
+    pos += min(on_line - s.unit, stop - pos);
+    if (pos == tree_first + on_line * (c.kv_heads * a.chunks)) {
       tree_first = pos, ++t;
       if ((t & 63) == 0 && pos < stop) look_at(t);
     }
@@ -631,19 +653,19 @@ template <int DIM>
 __global__ __launch_bounds__(256) void k_join_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, false>;
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane / 16, n = lane % 16, pairs = c.kv_heads * a.chunks, D = c.head_dim, blocks = (D + 15) / 16;
-  const uint64_t per_tree = (uint64_t)pairs * a.tiles * blocks;
-  for (uint64_t of = (uint64_t)blockIdx.x * 4 + wave; of < a.trees * per_tree; of += (uint64_t)gridDim.x * 4) {
-    const uint32_t t = (uint32_t)(of / per_tree), rest = (uint32_t)(of % per_tree), b = rest % blocks, tile = rest / blocks % a.tiles, pair = rest / blocks / a.tiles;
-    uint32_t all = 0, before = 0;
+  const uint32_t per_tree = pairs * a.tiles * blocks, pieces = a.trees * per_tree;   // (below 2^31)
+  for (uint32_t of = blockIdx.x * 4 + wave; of < pieces; of += gridDim.x * 4) {
+    const uint32_t t = of / per_tree, rest = of % per_tree, b = rest % blocks, tile = rest / blocks % a.tiles, pair = rest / blocks / a.tiles;
+    uint32_t all = 0, before = 0, units = 0;
     for (uint32_t first = 0; first < a.trees; first += 64) {
-      const uint32_t units = first + lane < a.trees ? units_of<S::kTokens>(seen_by(c, a, first + lane).end) : 0u;
-      all += units;
-      if (first + lane < t) before += units;
+      units = first + lane < a.trees ? units_of<S::kTokens>(seen_by(c, a, first + lane).end) : 0u;
+      all += wave_total(units), before += wave_total(first + lane < t ? units : 0u);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d), before += __shfl_xor(before, d);
+    const Cutting cutting = cutting_of(all, units, a.trees, pairs, a.groups);
+    if (cutting.whole) before = wave_total(lane < t ? rounded(units, cutting) : 0u);
     const Seen seen = seen_by(c, a, t);
-    const uint32_t units = units_of<S::kTokens>(seen.end), share = (all * pairs + a.groups - 1) / a.groups, first = before * pairs + pair * units;
+    units = units_of<S::kTokens>(seen.end);
+    const uint32_t share = cutting.share, first = before * pairs + pair * rounded(units, cutting);
     const uint32_t group0 = first / share, group1 = (first + units - 1) / share;
     if (group0 == group1) continue;
     auto part_of = [&](uint32_t group) { return a.partials + ((uint64_t)(2 * group + (group * share >= first ? 0 : 1)) * a.tiles + tile) * S::kPartial; };
@@ -692,7 +714,7 @@ int check_tree(const std::string& who, const tq_cache* cache, const tq_tree_args
   l->tiles = (all_tiles + l->chunks - 1) / l->chunks;
   l->units = (c->capacity + tokens - 1) / tokens;
   const uint64_t line = (uint64_t)a->trees * c->kv_heads * l->chunks * l->units;   // if all sequences are full
-  if (line >= (1u << 31) - kMaxGroups) return refuse(TQ_E_UNSUPPORTED, who + ": trees * heads * capacity is beyond what one call takes");
+  if (line >= (1u << 31) - kMaxGroups || (uint64_t)a->trees * c->kv_heads * l->chunks * l->tiles * 16 >= (1u << 31) - 65536) return refuse(TQ_E_UNSUPPORTED, who + ": trees * heads * capacity is beyond what one call takes");
   l->groups = (uint32_t)std::min<uint64_t>(kMaxGroups, std::max<uint64_t>(1, line));
   l->bytes = l->units > 1 ? (uint64_t)l->groups * 2 * l->tiles * 16 * (dim + 2) * 4 : 16;
   return TQ_OK;
