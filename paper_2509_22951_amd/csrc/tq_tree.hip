@@ -62,16 +62,34 @@ __device__ __forceinline__ void write_out(A& a, uint32_t size, uint32_t t, uint3
   *(u32x2_any*)to = u32x2_any{lo, hi};
 }
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Four int8 levels as f16: the bits of 1024 + (level + 128), less 1152.
+__device__ __forceinline__ uint2 levels_to_f16(uint32_t four) {
+  const uint32_t u = four ^ 0x80808080u;
+  const f16x2 less = {(_Float16)-1152.f, (_Float16)-1152.f};
+  const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + less, hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + less;
+  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+
 template <int DIM, bool INT8>
 struct Shape {
   static constexpr int kWaves = kTreeWaves<DIM>, kThreads = kWaves * 64;
-  static constexpr int kTokens = 16384 / DIM, kTiles = kTokens / kTile;      // of a stage: 32 KB of keys and as much of values in LDS
-  static constexpr int kSteps = DIM / 32, kBlocks = DIM / 16, kRow = DIM * 2; // contraction steps of the logits, blocks of 16 dims, bytes of a row in LDS
-  static constexpr int kSize = INT8 ? 1 : 2, kPieces = DIM * kSize / 16;      // 16-byte pieces of a row in memory
+  static constexpr int kSize = INT8 ? 1 : 2, kRow = DIM * kSize, kPieces = kRow / 16;   // bytes of a row, in memory and in LDS; its 16-byte pieces
+  static constexpr int kTokens = 32768 / kRow, kTiles = kTokens / kTile;   // of a stage: 32 KB of keys and as much of values in LDS
+  static constexpr int kSteps = DIM / (INT8 ? 64 : 32), kBlocks = DIM / 16; // contraction steps of the logits, blocks of 16 dims
   static constexpr int kOwnRows = kTokens / kLoaders, kRows = 64 / kPieces, kLoads = kOwnRows / kRows;   // rows that a wavefront loads of a stage, and at a time
   static constexpr int kOwnBlocks = kOwnRows > 16 ? kOwnRows / 16 : 1, kPerBlock = kLoads / kOwnBlocks;
-  static constexpr uint32_t kKeyMask = 7, kValueMask = 3;   // see below
-  static_assert(kOwnRows % 8 == 0, "a loader begins where the places of pieces do");
+  // Piece p of row r lies in place p ^ key_swizzle(r), or p ^ value_swizzle(r), so that the lanes of a read are spread over the banks.  Keys are read as 16 rows' same
+  // piece.  Values are transposed as they are read: bf16 by 16 lanes from 4 rows' two neighbouring pieces, 8 bits by 32 lanes from rows 0..7 and 16..23, or 8..15 and 24..31, of one.
+  static constexpr int kShift = DIM == 64 ? 2 : DIM == 128 ? 1 : 0;   // (8 bits: as many rows' bits of a number lie side by side in the 64 banks)
+  static __device__ constexpr uint32_t key_swizzle(uint32_t r) { return INT8 ? (r >> kShift) & (kPieces - 1) : r & 7; }
+  static __device__ constexpr uint32_t value_swizzle(uint32_t r) { return INT8 ? ((r >> kShift) & ((8 >> kShift) - 1)) | (r >> 4 & 1) << (3 - kShift) : (r & 3) << 1; }
+  static constexpr int places(int period) { return kRows >= period ? 1 : period / kRows < kLoads ? period / kRows : kLoads; }
+  static constexpr int kKeyPlaces = places(INT8 ? 16 : 8), kValuePlaces = places(INT8 ? 32 : 4);   // loads after which a lane's piece is the same again
+  static_assert(kOwnRows % 8 == 0, "a loader begins where the places of bf16 pieces do");
   static constexpr uint32_t kPartial = kBlocks * 256 + 32;                    // floats of a column tile's partial
 };
 
@@ -103,13 +121,24 @@ __device__ __forceinline__ uint32_t rounded(uint32_t units, const Cutting& cut) 
 template <int DIM, bool INT8, bool Q16>
 __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
-  constexpr int kParts = Q16 ? 1 : 3;
+  constexpr int kParts = Q16 && !INT8 ? 1 : 3, kWeightParts = INT8 ? 2 : 3;
+  typedef std::conditional_t<INT8, i32x4, bf16x8> key8;      // what a lane supplies of a row of keys or q
+  typedef std::conditional_t<INT8, i32x4, f32x4> logits4;
+  typedef std::conditional_t<INT8, f16x8, bf16x8> value8;
+  auto multiply_keys = [](key8 of_rows, key8 of_columns, logits4 sum) __attribute__((always_inline)) {
+    if constexpr (INT8) return __builtin_amdgcn_mfma_i32_16x16x64_i8(of_rows, of_columns, sum, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(of_rows, of_columns, sum, 0, 0, 0);
+  };
+  auto multiply_values = [](value8 of_rows, value8 of_columns, f32x4 sum) __attribute__((always_inline)) {
+    if constexpr (INT8) return __builtin_amdgcn_mfma_f32_16x16x32_f16(of_rows, of_columns, sum, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(of_rows, of_columns, sum, 0, 0, 0);
+  };
   constexpr uint32_t kT = S::kTokens, kBytes = kT * S::kRow, kAll = 64, kNobody = 65;
-  // Keys, then values of a stage; those of the next one are on their way into lds_1, or lds_0.  Of 8 bits, one stage as bf16 in lds_0, and two as they are in memory.
+  // Keys, then values of a stage; those of the next one are on their way into lds_1, or lds_0.
   // (Arrays of their own, so that the compiler sees that a read of one does not wait for loads into the other.)
-  __shared__ __attribute__((aligned(16))) char lds_0[2 * kBytes], lds_1[INT8 ? kBytes : 2 * kBytes], lds_2[INT8 ? kBytes : 16];
+  __shared__ __attribute__((aligned(16))) char lds_0[2 * kBytes], lds_1[2 * kBytes];
   __shared__ __attribute__((aligned(16))) uint32_t lds_kind[2][kT];     // j: of node j; kAll: of the context, kNobody
-  __shared__ __attribute__((aligned(16))) float lds_scale[2][INT8 ? kT : 4], lds_own_scale[2][2][INT8 ? kT : 4];   // of keys (times `scale`), of values; as they are in memory
+  __shared__ __attribute__((aligned(16))) float lds_scale_0[2][INT8 ? kT : 4], lds_scale_1[2][INT8 ? kT : 4];   // of keys, of values
   __shared__ float lds_max[S::kWaves * 16], lds_total[S::kWaves * 16], lds_weight[256];
   __shared__ uint64_t lds_at[256];
   __shared__ __attribute__((aligned(16))) uint32_t lds_some[2][kLoaders];   // a loader's rows of a stage: some of them are not of the context, and their kinds are told
@@ -121,10 +150,8 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     asm volatile("" : "+v"(v));
     return v;
   };
-  auto stage = [&](auto b) -> char* {
-    if constexpr (INT8) return decltype(b)::value ? lds_2 : lds_1;
-    else return decltype(b)::value ? lds_1 : lds_0;
-  };
+  auto stage = [&](auto b) -> char* { return decltype(b)::value ? lds_1 : lds_0; };
+  auto scales = [&](auto b, int of_values) -> float* { return decltype(b)::value ? lds_scale_1[of_values] : lds_scale_0[of_values]; };
 
   // The arguments, read again where they are used once in a while: the loop over the stages has no registers for all of them.
   typedef __attribute__((address_space(4))) const char constant_char;
@@ -200,8 +227,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   };
 
   // ---- from memory to LDS ----
-  // A loader takes kOwnRows rows of a stage; 16 tokens lie in one page.  The pages are looked up ahead of the barrier in front of the loads.  Rows are pieces of 8 dims, in places that
-  // spread the lanes of a read over the banks: piece p of row r of the keys in place p ^ (r & kKeyMask), of the values in p ^ (2 * (r & kValueMask)).
+  // A loader takes kOwnRows rows of a stage; 16 tokens lie in one page.  The pages are looked up ahead of the barrier in front of the loads.
   struct Place {   // a stage: of a segment, or none
     Segment s;
     uint32_t unit;
@@ -221,7 +247,6 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   const uint64_t page_bytes = S::kSize * c.page_stride;
   typedef __attribute__((address_space(1))) const uint32_t global_cu32;
   typedef __attribute__((address_space(3))) uint32_t lds_mu32;
-  constexpr int kKeyPlaces = S::kRows >= 8 || INT8 ? 1 : 8 / S::kRows, kValuePlaces = S::kRows >= 4 || INT8 ? 1 : 4 / S::kRows;
   uint32_t ids[S::kOwnBlocks];
   auto look_up = [&](const Place& p) __attribute__((always_inline)) {
     constant_i32* table = (constant_i32*)(c.tables + (uint64_t)p.s.of.seq * c.table_stride);
@@ -233,93 +258,51 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     constexpr int kBuffer = decltype(buffer)::value;
     if (!loads) return;
     const uint32_t lane = anew(tid) & 63;
-    // Where a lane's piece of the i-th row group lies beside the group's first byte (of dims that a head does not have: its first ones, against zeros of q).
-    uint32_t key_from[kKeyPlaces], value_from[kValuePlaces];
+    // The piece of a row that a lane loads with the i-th group of rows (of dims that a head does not have: its first one, against zeros of q).
+    const uint32_t place = lane % S::kPieces, row_of_lane = lane / S::kPieces;
+    auto piece_at = [&](uint32_t swizzle) __attribute__((always_inline)) {
+      const uint32_t of = (place ^ swizzle) * 16;
+      return of < S::kSize * D ? of : 0;
+    };
+    uint32_t key_from[S::kKeyPlaces], value_from[S::kValuePlaces];
 #pragma unroll
-    for (int i = 0; i < kKeyPlaces; ++i) {
-      const uint32_t piece = lane % S::kPieces, row = lane / S::kPieces, r = i * S::kRows + row;
-      const uint32_t of_k = (INT8 ? piece : piece ^ (r & S::kKeyMask)) * 16, of_v = (INT8 ? piece : piece ^ ((r & S::kValueMask) << 1)) * 16;
-      key_from[i] = row * slot_bytes + (of_k < S::kSize * D ? of_k : 0);
-      if (i < kValuePlaces) value_from[i] = row * slot_bytes + (of_v < S::kSize * D ? of_v : 0);
-    }
-    const uint32_t first = (p.s.unit + p.unit) * kT + wave * S::kOwnRows;
-    bool plain = first + S::kOwnRows <= p.s.of.length;
+    for (int i = 0; i < S::kKeyPlaces; ++i) key_from[i] = piece_at(S::key_swizzle(wave * S::kOwnRows + i * S::kRows + row_of_lane));
 #pragma unroll
-    for (int b = 0; b < S::kOwnBlocks; ++b) plain &= ids[b] < c.n_pages;
+    for (int i = 0; i < S::kValuePlaces; ++i) value_from[i] = piece_at(S::value_swizzle(wave * S::kOwnRows + i * S::kRows + row_of_lane));
+    const uint32_t first = (p.s.unit + p.unit) * kT + wave * S::kOwnRows, page_mask = (1u << c.page_shift) - 1;
     char* to = stage(buffer) + wave * S::kOwnRows * S::kPieces * 16;
-    auto request = [&](uint64_t at, uint32_t of_k, uint32_t of_v, int i) __attribute__((always_inline)) {
-      __builtin_amdgcn_global_load_lds((global_cu32*)(c.k + at + of_k), (lds_mu32*)(to + i * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_cu32*)(c.v + at + of_v), (lds_mu32*)(to + i * 1024 + kT * S::kPieces * 16), 16, 0, 0);
-    };
-    auto request_scales = [&](uint64_t mark) __attribute__((always_inline)) {   // (by the lanes of the wavefront's rows)
-      __builtin_amdgcn_global_load_lds((global_cu32*)(c.k_scale + mark), (lds_mu32*)&lds_own_scale[kBuffer][0][wave * S::kOwnRows], 4, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_cu32*)(c.v_scale + mark), (lds_mu32*)&lds_own_scale[kBuffer][1][wave * S::kOwnRows], 4, 0, 0);
-    };
-    const uint32_t page_mask = (1u << c.page_shift) - 1;
-    if (__builtin_expect(plain, 1)) {
-      if (lane == 0) lds_some[kBuffer][wave] = 0;
+    bool some = first + S::kOwnRows > p.s.of.length;
+    uint32_t limit_of_lane = 0;   // of the 16 tokens that token first + lane is one of: how many are there
+    uint64_t mark_of_lane = 0;
 #pragma unroll
-      for (int b = 0; b < S::kOwnBlocks; ++b) {
-        const uint64_t at = ids[b] * page_bytes + (uint64_t)(p.s.kv * c.head_stride) * S::kSize + (uint64_t)((first + 16 * b) & page_mask) * slot_bytes;
-#pragma unroll
-        for (int j = 0; j < S::kPerBlock; ++j) {
-          const int i = b * S::kPerBlock + j;
-          request(at + j * S::kRows * slot_bytes, key_from[i % kKeyPlaces], value_from[i % kValuePlaces], i);
-        }
-      }
-      if constexpr (INT8) {
-        if (lane < S::kOwnRows) {
-          const uint32_t id = S::kOwnBlocks > 1 && lane >= 16 ? ids[S::kOwnBlocks - 1] : ids[0];
-          request_scales((((uint64_t)id * c.kv_heads + p.s.kv) << c.page_shift) + ((first + lane) & page_mask));
-        }
-      }
-    } else {
+    for (int b = 0; b < S::kOwnBlocks; ++b) {
       // In place of rows that are not there the block's first one comes again, so that what is beside a weight of zero is a number.
-      const uint32_t newest = max(p.s.of.end, 1u) - 1, row_of_lane = lane / S::kPieces;
-      uint32_t here_of_lane = 0;
-      uint64_t mark_of_lane = 0;
+      const uint32_t newest = max(p.s.of.end, 1u) - 1, slot = first + 16 * b, from = min(slot, newest & ~(uint32_t)(S::kOwnRows < 16 ? S::kOwnRows - 1 : 15)), id = scalar(ids[b]);
+      const uint32_t page = id < c.n_pages ? id : 0, in_page = from & page_mask, limit = id < c.n_pages && slot < p.s.of.end ? min(p.s.of.end - slot, 16u) : 0u;
+      some |= id >= c.n_pages;
+      const uint64_t at = page * page_bytes + (uint64_t)(p.s.kv * c.head_stride) * S::kSize + (uint64_t)in_page * slot_bytes;
 #pragma unroll
-      for (int b = 0; b < S::kOwnBlocks; ++b) {
-        const uint32_t slot = first + 16 * b, from = min(slot, newest & ~(uint32_t)(S::kOwnRows < 16 ? S::kOwnRows - 1 : 15)), id = scalar(ids[b]);
-        const uint32_t page = id < c.n_pages ? id : 0, in_page = from & page_mask, limit = id < c.n_pages && slot < p.s.of.end ? min(p.s.of.end - slot, 16u) : 0u;
-        const uint64_t at = page * page_bytes + (uint64_t)(p.s.kv * c.head_stride) * S::kSize + (uint64_t)in_page * slot_bytes;
-#pragma unroll
-        for (int j = 0; j < S::kPerBlock; ++j) {
-          const int i = b * S::kPerBlock + j;
-          const uint32_t row = j * S::kRows + row_of_lane, row_at = row < limit ? row * slot_bytes : 0;
-          request(at, key_from[i % kKeyPlaces] - row_of_lane * slot_bytes + row_at, value_from[i % kValuePlaces] - row_of_lane * slot_bytes + row_at, i);
-        }
-        if (S::kOwnBlocks == 1 || (int)(lane / 16) == b) here_of_lane = limit, mark_of_lane = (((uint64_t)page * c.kv_heads + p.s.kv) << c.page_shift) + in_page + lane % 16;
+      for (int j = 0; j < S::kPerBlock; ++j) {
+        const int i = b * S::kPerBlock + j;
+        const uint32_t row = j * S::kRows + row_of_lane, row_at = row < limit ? row * slot_bytes : 0;
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.k + at + (row_at + key_from[i % S::kKeyPlaces])), (lds_mu32*)(to + i * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.v + at + (row_at + value_from[i % S::kValuePlaces])), (lds_mu32*)(to + i * 1024 + kT * S::kPieces * 16), 16, 0, 0);
       }
-      if (lane == 0) lds_some[kBuffer][wave] = 1;
-      if (lane < S::kOwnRows) {
-        const uint32_t slot = first + lane;
-        lds_kind[kBuffer][wave * S::kOwnRows + lane] = lane % 16 >= here_of_lane ? kNobody : slot < p.s.of.length ? kAll : slot - p.s.of.length;
-        if constexpr (INT8) request_scales(mark_of_lane);
+      if (S::kOwnBlocks == 1 || (int)(lane / 16) == b) {
+        limit_of_lane = limit;
+        mark_of_lane = (((uint64_t)page * c.kv_heads + p.s.kv) << c.page_shift) + in_page + (lane % 16 < limit ? lane % 16 : 0);
       }
     }
-  };
-  auto convert = [&](auto buffer) __attribute__((always_inline)) {   // 8 bits -> bf16
-    constexpr int kBuffer = decltype(buffer)::value;
     if constexpr (INT8) {
-      const uint32_t tid = anew(threadIdx.x);
-      constexpr uint32_t kAll = 2 * kT * S::kPieces;
-#pragma unroll
-      for (uint32_t first = 0; first < kAll; first += S::kThreads) {
-        const uint32_t i = first + tid, values = i / (kT * S::kPieces), r = i / S::kPieces % kT, piece = i % S::kPieces;
-        if (first + S::kThreads > kAll && i >= kAll) break;
-        const uint4 x = *(const uint4*)(stage(buffer) + 16 * i);
-        char* row = lds_0 + values * kBytes + r * S::kRow;
-        const uint32_t swizzle = values ? (r & S::kValueMask) << 1 : r & S::kKeyMask;
-        *(uint4*)(row + ((2 * piece) ^ swizzle) * 16) = __builtin_bit_cast(uint4, i8x8_to_bf16x8(make_uint2(x.x, x.y)));
-        *(uint4*)(row + ((2 * piece + 1) ^ swizzle) * 16) = __builtin_bit_cast(uint4, i8x8_to_bf16x8(make_uint2(x.z, x.w)));
+      if (lane < S::kOwnRows) {   // (the wavefront's rows' scales, a lane each)
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.k_scale + mark_of_lane), (lds_mu32*)&scales(buffer, 0)[wave * S::kOwnRows], 4, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_cu32*)(c.v_scale + mark_of_lane), (lds_mu32*)&scales(buffer, 1)[wave * S::kOwnRows], 4, 0, 0);
       }
-      if (tid < kT) {
-        // (an infinite scale of a key makes NaN of a level of zero, and is NaN here, so that the tokens are taken again)
-        const bool there = !lds_some[kBuffer][tid / S::kOwnRows] || lds_kind[kBuffer][tid] != kNobody;
-        const float k = lds_own_scale[kBuffer][0][tid], v = lds_own_scale[kBuffer][1][tid];
-        lds_scale[0][tid] = there ? fmaf(k, a.scale, k * 0.f) : 0.f, lds_scale[1][tid] = there ? v : 0.f;
-      }
+    }
+    if (lane == 0) lds_some[kBuffer][wave] = some;
+    if (__builtin_expect(some, 0)) {
+      const uint32_t slot = first + lane;
+      if (lane < S::kOwnRows) lds_kind[kBuffer][wave * S::kOwnRows + lane] = lane % 16 >= limit_of_lane ? kNobody : slot < p.s.of.length ? kAll : slot - p.s.of.length;
     }
   };
 
@@ -328,7 +311,8 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   while (over < (uint32_t)S::kTiles && 2 * over * a.tiles <= (uint32_t)S::kWaves) over *= 2;
   const uint32_t of_tile = wave % a.tiles, of_tokens = wave / a.tiles;
   const bool works = of_tokens < over;
-  bf16x8 q[kParts][S::kSteps];
+  key8 q[kParts][S::kSteps];   // 8 bits: three digits of a whole number, in units of the largest value / 127.0, that logits are multiplied by
+  float logit_scale = a.scale;
   __shared__ uint64_t lds_mask[S::kWaves * 16];
   auto column_of = [&](const Segment& s, uint32_t column, uint32_t* node) {   // -> query head
     constant_tree& a = *(constant_tree*)(arguments() + sizeof(CacheView));
@@ -344,22 +328,58 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     uint32_t node, head = column_of(s, has ? column : 0, &node);
     const uint64_t row = (uint64_t)s.t * a.nodes + node;
     if (of_tokens == 0 && g == 0) lds_mask[of_tile * 16 + n] = has && node < s.of.size ? a.masks[row] : 0;   // (a barrier ahead of the next stage's weights)
-#pragma unroll
-    for (int i = 0; i < S::kSteps; ++i) {
-      const uint32_t d = i * 32 + 8 * g;
+    auto read = [&](uint32_t d, float* v) __attribute__((always_inline)) {   // eight
       const bool own = has && d < D;
       const uint64_t at = row * a.q_stride + head * D + (own ? d : 0);
       if constexpr (Q16) {
         const u16x4_any lo = *(const u16x4_any*)((const uint16_t*)a.q + at), hi = *(const u16x4_any*)((const uint16_t*)a.q + at + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[0][i][j] = own ? __builtin_bit_cast(__bf16, (uint16_t)(j < 4 ? lo[j % 4] : hi[j % 4])) : (__bf16)0.f;
+        for (int j = 0; j < 8; ++j) v[j] = own ? bf16_value(j < 4 ? lo[j % 4] : hi[j % 4]) : 0.f;
       } else {
         const f32x4_any lo = *(const f32x4_any*)((const float*)a.q + at), hi = *(const f32x4_any*)((const float*)a.q + at + 4);
 #pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = own ? (j < 4 ? lo[j % 4] : hi[j % 4]) : 0.f;
+      }
+    };
+    if constexpr (INT8) {
+      float v[S::kSteps][16], most = 0.f, odd = 0.f;
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) {
+        read(i * 64 + 16 * g, &v[i][0]), read(i * 64 + 16 * g + 8, &v[i][8]);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) most = fmaxf(most, fabsf(v[i][j])), odd = fmaf(v[i][j], 0.f, odd);
+      }
+      most = fmaxf(most, __shfl_xor(most, 16)), most = fmaxf(most, __shfl_xor(most, 32));
+      odd += __shfl_xor(odd, 16), odd += __shfl_xor(odd, 32);
+      const float up = fminf(8323072.f / most, 0x1p126f);   // 127 * 2^16; (of nothing but zeros: zeros)
+      logit_scale = a.scale / up + odd;                    // (a query that is not finite: NaN, so that the tokens are taken again)
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t digits[3] = {0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int32_t whole = odd == 0.f ? (int32_t)rintf(v[i][4 * w + j] * up) : 0;
+            const uint32_t u = (uint32_t)(whole + 0x8080);   // digits of -128..127: those of 0..255, less 128, and the upper one as it is
+            digits[0] |= (u >> 16 & 255) << (8 * j), digits[1] |= ((u >> 8 & 255) ^ 128) << (8 * j), digits[2] |= ((u & 255) ^ 128) << (8 * j);
+          }
+#pragma unroll
+          for (int k = 0; k < 3; ++k) q[k][i][w] = (int)digits[k];
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) {
+        float v[8];
+        read(i * 32 + 8 * g, v);
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float v = own ? (j < 4 ? lo[j % 4] : hi[j % 4]) : 0.f;
-          const __bf16 upper = (__bf16)v, middle = (__bf16)(v - (float)upper);
-          q[0][i][j] = upper, q[kParts > 1][i][j] = middle, q[kParts - 1][i][j] = (__bf16)(v - (float)upper - (float)middle);
+          float left = v[j];
+#pragma unroll
+          for (int k = 0; k < kParts; ++k) {
+            q[k][i][j] = (__bf16)left;
+            left -= (float)q[k][i][j];
+          }
         }
       }
     }
@@ -367,51 +387,90 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
 
   f32x4 o[S::kBlocks];
   float top = -INFINITY, total = 0.f;
+  // 8 bits: weights times their values' scales are two f16 parts each, 22 bits, and are multiplied by 2^raised for that: by as much as keeps a column's below 2^15.  So are the sums.
+  constexpr int kRaised = 126;
+  constexpr float kMostWeight = 32768.f;
+  int raised = kRaised;
   auto take_tile = [&](auto buffer, uint32_t tile, bool some) __attribute__((always_inline)) {
     constexpr int kBuffer = decltype(buffer)::value;
-    const char* keys = (INT8 ? lds_0 : stage(buffer)) + tile * kTile * S::kRow;
+    const char* keys = stage(buffer) + tile * kTile * S::kRow;
     const char* values = keys + kBytes;
     const uint32_t lane = anew(tid) & 63, g = lane / 16, n = lane % 16;
-    const uint32_t key_at = n * S::kRow, key_swizzle = g ^ (n & S::kKeyMask);
-    const uint32_t value_row = 4 * g + n / 4, value_at0 = value_row * S::kRow + (value_row & S::kValueMask) * 32 + n % 4 * 8;
-    f32x4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    const uint32_t key_at = n * S::kRow, key_place = g ^ S::key_swizzle(n);
+    logits4 l[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, less[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
     constexpr int kKeySteps = S::kSteps < 2 ? S::kSteps : 2;   // of which all keys are asked for at once
+    auto key_of = [&](int i, int b) __attribute__((always_inline)) { return *(const key8*)(keys + b * 16 * S::kRow + key_at + ((key_place ^ (4 * i)) * 16)); };
+    if constexpr (INT8) {   // the sums of the lowest digits, and 256 times the upper ones' and the middle ones'
+      key8 key[S::kSteps][2];
 #pragma unroll
-    for (int first = 0; first < S::kSteps; first += kKeySteps) {
-      bf16x8 key[kKeySteps][2];
+      for (int i = 0; i < S::kSteps; ++i)
 #pragma unroll
-      for (int i = 0; i < kKeySteps; ++i)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) key[i][b] = *(const bf16x8*)(keys + b * 16 * S::kRow + key_at + ((key_swizzle ^ (4 * (first + i))) * 16));
+        for (int b = 0; b < 2; ++b) key[i][b] = key_of(i, b);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < kKeySteps; ++i)
+      for (int part = 0; part < 3; ++part) {
 #pragma unroll
-        for (int part = 0; part < kParts; ++part)
+        for (int i = 0; i < S::kSteps; ++i)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[i][b], q[part][first + i], l[b], 0, 0, 0);
+          for (int b = 0; b < 2; ++b) (part == 1 ? less : l)[b] = multiply_keys(key[i][b], q[part == 0 ? 0 : 3 - part][i], (part == 1 ? less : l)[b]);
+        if (part == 1)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) l[b] <<= 8;   // (below 2^22 of 256 dims)
+      }
+    } else {
+#pragma unroll
+      for (int first = 0; first < S::kSteps; first += kKeySteps) {
+        key8 key[kKeySteps][2];
+#pragma unroll
+        for (int i = 0; i < kKeySteps; ++i)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) key[i][b] = key_of(first + i, b);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kKeySteps; ++i)
+#pragma unroll
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) l[b] = multiply_keys(key[i][b], q[part][first + i], l[b]);
+      }
     }
     // The values are asked for ahead of what the weights take.
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    bf16x8 value[S::kBlocks];
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+    const uint32_t value_row = INT8 ? 4 * g + n / 2 % 4 + n / 8 * 16 : 4 * g + n / 4;
+    const uint32_t value_at0 = value_row * S::kRow + S::value_swizzle(value_row) * 16 + (INT8 ? n % 2 : n % 4) * 8;
+    std::conditional_t<INT8, i32x2, value8> asked[S::kBlocks];
     auto ask = [&](int b) __attribute__((always_inline)) {
-      const char* from = values + (value_at0 ^ (b * 32));
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 16 * S::kRow));
-      value[b] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      const char* from = values + (value_at0 ^ (b * 16 * S::kSize));
+      if constexpr (INT8) {
+        asked[b] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)from);
+      } else {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 16 * S::kRow));
+        asked[b] = __builtin_bit_cast(value8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
     };
-    constexpr int kEarly = 2;
+    auto value_of = [&](int b) __attribute__((always_inline)) {
+      if constexpr (INT8) {
+        const uint2 lo = levels_to_f16((uint32_t)asked[b][0]), hi = levels_to_f16((uint32_t)asked[b][1]);
+        return __builtin_bit_cast(value8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+      } else {
+        return asked[b];
+      }
+    };
+    constexpr int kEarly = INT8 ? 4 : 2;
 #pragma unroll
     for (int b = 0; b < kEarly; ++b) ask(b);
-    float p[8];   // logits, without `scale` where they have no other one
+    float p[8], most_scale = 0.f;   // logits, without `logit_scale`
     float4 vs[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       if constexpr (INT8) {
-        const float4 ks = *(const float4*)&lds_scale[0][tile * kTile + 16 * b + 4 * g];
-        vs[b] = *(const float4*)&lds_scale[1][tile * kTile + 16 * b + 4 * g];
+        const float4 ks = *(const float4*)&scales(buffer, 0)[tile * kTile + 16 * b + 4 * g];
+        vs[b] = *(const float4*)&scales(buffer, 1)[tile * kTile + 16 * b + 4 * g];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) p[4 * b + j] = l[b][j] * (&ks.x)[j];
+        for (int j = 0; j < 4; ++j) p[4 * b + j] = fmaf((float)l[b][j], 256.f, (float)less[b][j]) * (&ks.x)[j], most_scale = fmaxf(most_scale, fabsf((&ks.x)[j]));
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) p[4 * b + j] = l[b][j];
@@ -429,40 +488,69 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
           const uint32_t k = (&kind.x)[j], word = k & 32 ? (uint32_t)(mask >> 32) : (uint32_t)mask;
           const uint32_t sees = (k == kAll ? 1u : 0u) | (k < kAll ? word >> (k & 31) & 1u : 0u);
           p[4 * b + j] = sees ? p[4 * b + j] : -INFINITY;
+          if constexpr (INT8) (&vs[b].x)[j] = sees ? (&vs[b].x)[j] : 0.f;
         }
       }
     }
     float m = p[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) m = fmaxf(m, p[i]);
-    const float scale = INT8 ? 1.f : a.scale;
+    const float scale = INT8 ? logit_scale : a.scale;
     m *= scale;
     // The weights' reference follows the maximum when that has grown by more than 8 (2^8 is far from any bound of fp32).
-    if (__any(m > top + 8.f)) {
+    if (__any(m > top + 8.f || (INT8 && !(most_scale < INFINITY)))) {
+      // (an infinite scale of a key makes NaN of a level of zero: the tokens are taken again, unless none of them is this column's)
+      if (INT8 && !(most_scale < INFINITY)) total = __builtin_nanf("");
       m = fmaxf(m, top);
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
-      const float shrink = __builtin_amdgcn_exp2f(top - (m == -INFINITY ? 0.f : m));
+      const float lower = top - (m == -INFINITY ? 0.f : m);
+      float shrink = __builtin_amdgcn_exp2f(lower);
       top = m, total *= shrink;
+      if constexpr (INT8) {   // the sums are left about as they are, as far as that goes
+        const float more = fminf(floorf(-lower), (float)(kRaised - raised));
+        raised += (int)more, shrink = __builtin_amdgcn_exp2f(lower + more);
+      }
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) o[b] *= shrink;
     }
     const float base = top == -INFINITY ? 0.f : top;
-    uint32_t part[3][4];
+    float w[8], most_weight = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], scale, -base));
+      total += w[i];
+      if constexpr (INT8) w[i] *= (&vs[i / 4].x)[i % 4], most_weight = fmaxf(most_weight, fabsf(w[i]));
+    }
+    if constexpr (INT8) {
+      if (__any(most_weight * ldexpf(1.f, raised) > kMostWeight)) {
+        most_weight = fmaxf(most_weight, __shfl_xor(most_weight, 16));
+        most_weight = fmaxf(most_weight, __shfl_xor(most_weight, 32));
+        // to 2^12 .. 2^13 (what is infinite stays so)
+        const int to = most_weight * ldexpf(1.f, raised) > kMostWeight ? max(12 - (most_weight < INFINITY ? ilogbf(most_weight) : 128), -kRaised) : raised;
+        const float shrink = ldexpf(1.f, to - raised);
+        raised = to;
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b) o[b] *= shrink;
+      }
+      const float up = ldexpf(1.f, raised);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] *= up;
+    }
+    uint32_t part[kWeightParts][4];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      float w[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        w[j] = __builtin_amdgcn_exp2f(fmaf(p[i + j], scale, -base));
-        total += w[j];
-        if constexpr (INT8) w[j] *= (&vs[i / 4].x)[i % 4 + j];
-      }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {   // the upper 8 bits of the mantissas, the next 8, the last 8
-        const uint32_t lo = __float_as_uint(w[0]), hi = __float_as_uint(w[1]);
-        part[k][i / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-        w[0] -= __uint_as_float(lo & 0xFFFF0000u), w[1] -= __uint_as_float(hi & 0xFFFF0000u);
+      for (int k = 0; k < kWeightParts; ++k) {
+        if constexpr (INT8) {   // 11 bits, the next 11
+          const f16x2 two = {(_Float16)w[i], (_Float16)w[i + 1]};
+          part[k][i / 2] = __builtin_bit_cast(uint32_t, two);
+          w[i] -= (float)two[0], w[i + 1] -= (float)two[1];
+        } else {   // the upper 8 bits of the mantissas, the next 8, the last 8
+          const uint32_t lo = __float_as_uint(w[i]), hi = __float_as_uint(w[i + 1]);
+          part[k][i / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+          w[i] -= __uint_as_float(lo & 0xFFFF0000u), w[i + 1] -= __uint_as_float(hi & 0xFFFF0000u);
+        }
       }
     }
 #pragma unroll
@@ -470,11 +558,14 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       if (first)
 #pragma unroll
         for (int b = 0; b < kEarly; ++b) ask(first + b);
+      value8 value[kEarly];
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
+      for (int b = 0; b < kEarly; ++b) value[b] = value_of(first + b);
 #pragma unroll
-        for (int b = first; b < first + kEarly; ++b)
-          o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[b], __builtin_bit_cast(bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), o[b], 0, 0, 0);
+      for (int k = 0; k < kWeightParts; ++k)
+#pragma unroll
+        for (int b = 0; b < kEarly; ++b)
+          o[first + b] = multiply_values(value[b], __builtin_bit_cast(value8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), o[first + b]);
     }
   };
 
@@ -545,6 +636,11 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     const uint32_t tid = anew(threadIdx.x), lane = tid & 63, g = lane / 16, n = lane % 16;
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
+    if constexpr (INT8) {
+      const float down = ldexpf(1.f, -raised);
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) o[b] *= down;
+    }
     if (tid == 0) lds_odd = 0;
     if (tid < S::kWaves * 16) lds_odd_column[tid] = 0;
     __syncthreads();   // everyone is done with the stage
@@ -617,10 +713,6 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   auto take = [&](auto buffer, auto other) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this stage's loads
     __syncthreads();
-    if constexpr (INT8) {
-      convert(buffer);
-      __syncthreads();
-    }
     if (next.there) fetch(next, other);
     if (works) {
       constexpr int kBuffer = decltype(buffer)::value;
@@ -629,29 +721,32 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       for (uint32_t tile = of_tokens; tile < (uint32_t)S::kTiles; tile += over) take_tile(buffer, tile, some);
     }
   };
-  for (bool odd = false;; odd = !odd) {
+  auto step = [&](auto buffer, auto other) __attribute__((always_inline)) {
     if (now.unit == 0) {
-      top = -INFINITY, total = 0.f;
+      top = -INFINITY, total = 0.f, raised = kRaised;
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    odd ? take(Second(), First()) : take(First(), Second());
+    take(buffer, other);
     if (now.unit + 1 == now.s.n_units) {
-      finish(now.s, (float*)(odd && !INT8 ? lds_1 : lds_0));
-      if (!next.there) break;
+      finish(now.s, (float*)stage(buffer));
+      if (!next.there) return true;
       load_q(next.s);
     }
     now = next, next = after(next);
     look_up(next);
-  }
+    return false;
+  };
+  // (Two steps a turn, so that the compiler knows of each read which of the stages on their way it could meet, and waits for none.)
+  while (!step(First(), Second()) && !step(Second(), First())) {}
 }
 
 #undef ARGUMENTS_ANEW
 
 // The parts of what lies in more than one share, joined in the order of the line: a wavefront per 16 columns and 16 dims.
-template <int DIM>
+template <int DIM, bool INT8>
 __global__ __launch_bounds__(256) void k_join_tree(CacheView c, TreeView a) {
-  using S = Shape<DIM, false>;
+  using S = Shape<DIM, INT8>;
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane / 16, n = lane % 16, pairs = c.kv_heads * a.chunks, D = c.head_dim, blocks = (D + 15) / 16;
   const uint32_t per_tree = pairs * a.tiles * blocks, pieces = a.trees * per_tree;   // (below 2^31)
   for (uint32_t of = blockIdx.x * 4 + wave; of < pieces; of += gridDim.x * 4) {
@@ -707,7 +802,7 @@ int check_tree(const std::string& who, const tq_cache* cache, const tq_tree_args
   if (a->trees > 65535) return refuse(TQ_E_UNSUPPORTED, who + ": more than 65535 trees");
   if (!a->seqs && a->trees > c->n_seqs) return refuse(TQ_E_INVALID_ARG, who + ": more trees than sequences, and no seqs");
   if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return refuse(TQ_E_INVALID_ARG, who + ": scale must be positive");
-  const uint32_t group = a->heads / c->kv_heads, dim = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256, tokens = 16384 / dim;
+  const uint32_t group = a->heads / c->kv_heads, dim = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256, tokens = (cache->type == TQ_INT8 ? 32768 : 16384) / dim;   // of a stage
   l->columns = a->nodes * group;
   const uint32_t all_tiles = (l->columns + 15) / 16, most = dim == 256 ? kTreeWaves<256> : kTreeWaves<64>;
   l->chunks = (all_tiles + most - 1) / most;
@@ -745,7 +840,7 @@ int attend_tree(const tq_cache* cache, const tq_tree_args* a, void* stream) {
     else q16 ? go(k_attend_tree<kDim, false, true>) : go(k_attend_tree<kDim, false, false>);
     if (l.units == 1) return;   // nothing is cut
     const uint64_t waves = (uint64_t)a->trees * c.kv_heads * l.chunks * l.tiles * ((c.head_dim + 15) / 16);
-    hipLaunchKernelGGL(k_join_tree<kDim>, dim3((uint32_t)std::min<uint64_t>((waves + 3) / 4, 16384)), dim3(256), 0, st, c, v);
+    hipLaunchKernelGGL((cache->type == TQ_INT8 ? k_join_tree<kDim, true> : k_join_tree<kDim, false>), dim3((uint32_t)std::min<uint64_t>((waves + 3) / 4, 16384)), dim3(256), 0, st, c, v);
   };
   if (c.head_dim <= 64) of(std::integral_constant<int, 64>());
   else if (c.head_dim <= 128) of(std::integral_constant<int, 128>());
