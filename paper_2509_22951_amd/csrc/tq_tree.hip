@@ -395,7 +395,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     constexpr int kBuffer = decltype(buffer)::value;
     const char* keys = stage(buffer) + tile * kTile * S::kRow;
     const char* values = keys + kBytes;
-    const uint32_t lane = anew(tid) & 63, g = lane / 16, n = lane % 16;
+    const uint32_t g = lane / 16, n = lane % 16;
     const uint32_t key_at = n * S::kRow, key_place = g ^ S::key_swizzle(n);
     logits4 l[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, less[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
     constexpr int kKeySteps = S::kSteps < 2 ? S::kSteps : 2;   // of which all keys are asked for at once
