@@ -570,16 +570,29 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   };
 
   // A column's tokens of a segment once more, a product per value as the formula has them, so that infinities give what they give there: only for what is not finite, and
-  // slow.  256 threads take a token each, then a dim each; the sums go to `sums`.
+  // slow.  256 threads take a token each, then all of them a dim of every so-manieth token; the sums go to `sums`, LDS of 32 KB at least.
   auto take_again = [&](const Segment& s, uint32_t col, float* sums) __attribute__((always_inline)) {
-    constexpr uint32_t kN = 256;
+    constexpr uint32_t kN = 256, kTeams = S::kThreads / DIM;
+    constexpr uint64_t kNothing = 1ull << 63;
     ARGUMENTS_ANEW;
     const uint32_t D = c.head_dim;
-    const uint32_t tid = anew(threadIdx.x);
+    const uint32_t tid = anew(threadIdx.x), team = tid / DIM, dim = tid % DIM;
     const uint32_t begin = s.unit * kT, end = min(s.of.end, (s.unit + s.n_units) * kT);
     uint32_t node, head = column_of(s, s.first_column + col, &node);
     const uint64_t row = (uint64_t)s.t * a.nodes + node, sees = node < s.of.size ? a.masks[row] : 0;
     const uint64_t q_at = row * a.q_stride + head * D;
+    float *lds_q = sums, *slots = sums + DIM, *of_teams = sums + 2 * DIM;
+    if (tid < D) lds_q[tid] = (Q16 ? bf16_value(((const uint16_t*)a.q)[q_at + tid]) : ((const float*)a.q)[q_at + tid]) * a.scale;
+    __syncthreads();
+    // over the 256 tokens, in the same order every time
+    auto over_all = [&](float v, auto join) __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) v = join(v, __shfl_xor(v, d));
+      __syncthreads();
+      if (tid < kN && tid % 64 == 0) slots[tid / 64] = v;
+      __syncthreads();
+      return join(join(slots[0], slots[1]), join(slots[2], slots[3]));
+    };
     float m = -INFINITY, sum_p = 0.f, sum = 0.f;
     for (uint32_t first = begin; first < end && node < s.of.size; first += kN) {
       const uint32_t slot = first + tid;
@@ -594,37 +607,39 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
         const float scale = INT8 ? c.k_scale[mark] : 1.f;
         const bool after = fabsf(scale) < INFINITY;   // (an infinite scale makes NaN of a level of zero)
         l = 0.f;
-#pragma unroll 1
-        for (uint32_t x = 0; x < D; ++x) {
-          const float of_q = (Q16 ? bf16_value(((const uint16_t*)a.q)[q_at + x]) : ((const float*)a.q)[q_at + x]) * a.scale;
-          l = fmaf(of_q, after ? value_at<INT8>(c.k + at, x) : value_at<INT8>(c.k + at, x) * scale, l);
+        for (uint32_t x = 0; x < D; x += 16 / S::kSize) {
+          const uint4 piece = *(const uint4*)(c.k + at + x * S::kSize);
+#pragma unroll
+          for (int j = 0; j < 16 / S::kSize; ++j) {
+            const float value = value_at<INT8>((const char*)&piece, j);
+            l = fmaf(lds_q[x + j], after ? value : value * scale, l);
+          }
         }
         if (after) l *= scale;
       }
+      const float most = fmaxf(m, over_all(l, [](float x, float y) { return fmaxf(x, y); })), base = most == -INFINITY ? 0.f : most, shrink = __builtin_amdgcn_exp2f(m - base);
+      const float p = there ? __builtin_amdgcn_exp2f(l - base) : 0.f;
+      m = most, sum *= shrink;
+      sum_p = fmaf(sum_p, shrink, over_all(p, [](float x, float y) { return x + y; }));
+      if (tid < kN) lds_weight[tid] = there && INT8 ? p * c.v_scale[mark] : p, lds_at[tid] = there ? at : at | kNothing;
       __syncthreads();
-      if (tid < kN) lds_weight[tid] = l, lds_at[tid] = there ? at : ~0ull;
-      __syncthreads();
-      float most = m;
-#pragma unroll 1
-      for (uint32_t i = 0; i < kN; ++i) most = fmaxf(most, lds_weight[i]);
-      const float base = most == -INFINITY ? 0.f : most, shrink = __builtin_amdgcn_exp2f(m - base);
-      m = most, sum_p *= shrink, sum *= shrink;
-      const float p = there ? __builtin_amdgcn_exp2f(l - base) : 0.f, with_scale = there && INT8 ? p * c.v_scale[mark] : p;
-      __syncthreads();
-      if (tid < kN) lds_weight[tid] = p;
-      __syncthreads();
-#pragma unroll 1
-      for (uint32_t i = 0; i < kN; ++i) sum_p += lds_weight[i];
-      __syncthreads();
-      if (tid < kN) lds_weight[tid] = with_scale;
-      __syncthreads();
-      if (tid < D) {
-#pragma unroll 1
-        for (uint32_t i = 0; i < kN; ++i)
-          if (lds_at[i] != ~0ull) sum = fmaf(lds_weight[i], value_at<INT8>(c.v + lds_at[i], tid), sum);
+      if (dim < D) {
+#pragma unroll 8
+        for (uint32_t i = team; i < kN; i += kTeams) {
+          const uint64_t from = lds_at[i];
+          const float value = value_at<INT8>(c.v + (from & ~kNothing), dim);
+          sum = from & kNothing ? sum : fmaf(lds_weight[i], value, sum);
+        }
       }
     }
-    if (tid < DIM) sums[tid] = sum;
+    of_teams[tid] = sum;   // (kTeams * DIM are all threads)
+    __syncthreads();
+    if (tid < DIM) {
+      sum = of_teams[tid];
+#pragma unroll
+      for (uint32_t i = 1; i < kTeams; ++i) sum += of_teams[i * DIM + tid];
+      sums[tid] = sum;   // (everyone is done with q)
+    }
     if (tid == 0) lds_max[col] = m, lds_total[col] = sum_p;
     __syncthreads();
   };
