@@ -1,12 +1,14 @@
 // Attention of a tree of drafted tokens over a paged cache (tq_attend_tree).
 //
 // All nodes of a tree and all query heads that share a key/value head are columns of one product, so that a token's key and value are read once for all of them.  A
-// workgroup takes up to 12 tiles of 16 columns and a stage of tokens at a time: keys and values go to LDS (8 bits become bf16 there), and a
-// wavefront per column tile, or several that share out its tokens, reads them in the shape of v_mfma_f32_16x16x32_bf16:
-//   logits [token][column] = K [token][dim] Q^T: lane l supplies token l % 16 and 8 neighbouring dims.
+// workgroup takes up to 12 tiles of 16 columns and a stage of tokens at a time: keys and values go from memory to LDS as they are, and a
+// wavefront per column tile, or several that share out its tokens, reads them in the shape of the 16 x 16 matrix instructions:
+//   logits [token][column] = K [token][dim] Q^T: lane l supplies 16 bytes of token l % 16.
 //   out^T [dim][column] = V^T [dim][token] P^T: the lane that got the logits of tokens 4g..4g+3 of both 16-token blocks (g = l / 16) supplies the same tokens as its 8
 //   values of the contraction, so P is already where it is needed; V is transposed on its way out of LDS.
-// q and p enter as three bf16 parts each, all of fp32's 24 bits.
+// bf16: q (if fp32) and the weights enter as three bf16 parts each, all of fp32's 24 bits.  8 bits: q as a whole number of 24 bits, in units of a row's largest value / (127 * 2^16),
+// whose three digits of 8 bits meet the keys in integer products, which are exact; values become f16 in registers, which is exact too, and meet weights (times the
+// values' scales) of two f16 parts, 22 bits.
 #include <algorithm>
 
 #include "tq_cache_view.h"
@@ -101,7 +103,7 @@ __device__ __forceinline__ uint32_t units_of(uint32_t end) { return max((end + T
 //
 // A workgroup that has the end of one (tree, head, chunk) and the start of another finishes one and takes up the other's queries in between, which costs about two stages.
 // Where there are no more of them than workgroups, and shares need not be longer than by two units for it, every one of them is rounded up to whole shares, so that
-// no workgroup has two (8 trees of 15 nodes, ragged up to 6001 tokens, 24 heads on 8: 67 us cut anywhere, 46 so).
+// no workgroup has two (8 trees of 15 nodes, ragged up to 6001 tokens, 24 heads on 8: 66 us cut anywhere, 37 so).
 struct Cutting {
   uint32_t share;
   bool whole;   // rounded up
@@ -118,6 +120,15 @@ __device__ __forceinline__ Cutting cutting_of(uint32_t all, uint32_t units, uint
 }
 __device__ __forceinline__ uint32_t rounded(uint32_t units, const Cutting& cut) { return cut.whole ? (units + cut.share - 1) / cut.share * cut.share : units; }
 
+// Bound: reading the cache while there are few columns, the matrix and vector units from two or three column tiles on.  24 heads on 8, 128 dims, bf16, 16 x 16384 tokens (171 us at the
+// 6.3 TB/s of a read stream): 5 nodes, one tile, 201 us, 5.3 TB/s; 16 nodes, three, 255; 20 nodes, four, 287.  1 x 131000 tokens, 64 nodes, 12 tiles: 291 us, with q in bf16 229: three parts
+// of q and three of the weights are 6 products where 2 would be the least; the matrix units are busy 59 % of the time.  16 x 32700 tokens in 8 bits (176 us): 5 nodes 238, 16 nodes 364:
+// vector instructions are issued 82 % of the time, of which values' widening is a quarter.
+//
+// Why so: 12 wavefronts, because of the 168 registers that leaves each (8 of them with everything in registers and no LDS: 80 us for the ragged batch, 368, 462; 4 with three column tiles each and
+// 512 registers: 131, 420, 813; the sums' copies between the two halves of the register file cost more than the reads that were saved).  Two stages of 64 KB: what is on its way
+// meanwhile, 16 MB on the card, is more than memory's latency times its rate; cut in halves with two barriers a stage it was no faster (77, 298, 470).  Loads go to LDS directly, since a
+// stage in registers on its way spills.
 template <int DIM, bool INT8, bool Q16>
 __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
@@ -758,7 +769,9 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
 
 #undef ARGUMENTS_ANEW
 
-// The parts of what lies in more than one share, joined in the order of the line: a wavefront per 16 columns and 16 dims.
+// The parts of what lies in more than one share, joined in the order of the line: a wavefront per 16 columns and 16 dims.  A launch of its own, which a sequence that can not be longer than a stage
+// does without: the last workgroup to arrive would join alone what all of them share here.  Bound: its launch and three waits behind each other, 5.5 us for the ragged batch of 8 x 15 nodes; the parts, 25 MB written and
+// read, 11.6 us for 64 nodes over 131000 tokens.
 template <int DIM, bool INT8>
 __global__ __launch_bounds__(256) void k_join_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
