@@ -528,7 +528,8 @@ int tq_cache_evict_workspace(const tq_cache *cache, const tq_evict_args *args, u
  *   out[r][h] = sum_s p[s] v[s],  p = softmax of scale * q[r][h] . k[s]  over the slots s < lengths[t] and the slots lengths[t] + j, j < sizes[t], with bit j of
  *   masks[t][i]; keys and values of head h / (heads / kv_heads).
  * Slots beyond the capacity and pages that are not there are masked.  A row with nothing to attend to, of a sequence that is not there, and one that is padding, are zero.
- *   q: device, TQ_FP32 or TQ_BF16 (q_type) [trees * nodes][heads * head_dim]; an fp32 q is used unrounded.  out: device, bf16 [trees * nodes][heads * head_dim].
+ *   q: device, TQ_FP32 or TQ_BF16 (q_type) [trees * nodes][heads * head_dim]; an fp32 q is used unrounded over a TQ_BF16 cache, over a TQ_INT8 one
+ *   to 2^-24 of its head's largest value.  out: device, bf16 [trees * nodes][heads * head_dim].
  *   Neither lengths, sizes, seqs, masks nor q are written while the call runs.
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_tree_workspace gives for the same arguments, with any contents; calls whose execution
  *   overlaps need one each.
@@ -556,7 +557,7 @@ int tq_attend_tree_workspace(const tq_cache *cache, const tq_tree_args *args, ui
  *   path: device, int32 [trees][nodes]: the accepted nodes, rising, -1 behind them.  accepted: device, int32 [trees]: how many.
  *   next: device, int32 [trees]: the token drawn at the last of them (-1 for a tree without nodes), the next tree's node 0.
  *   lengths_out: device, int32 [trees]: lengths[t] + accepted[t].  Not lengths itself; the outputs do not overlap each other or the inputs.
- * caches: host array of n (0..4096) caches that hold these sequences, the layers of a model.  In each of them the accepted nodes' keys, values, scales, scores and positions
+ * caches: host array of n (0..4096) caches that hold these sequences, the layers of a model, none of them twice.  In each of them the accepted nodes' keys, values, scales, scores and positions
  * move to the slots lengths[t] + 0, 1, ..., in order; what lay in the slots behind them is not used any more and may be anything.  Nothing is moved
  * into or out of a slot beyond a cache's capacity, a page that is not there or a sequence that is not there.  n = 0: only the branches.
  */

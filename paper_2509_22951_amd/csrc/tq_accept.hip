@@ -1,5 +1,6 @@
 // The accepted branch of a tree of drafted tokens, and its keys and values moved together in every layer (tq_tree_accept).
 #include <algorithm>
+#include <vector>
 
 #include "tq_cache_view.h"
 
@@ -114,6 +115,11 @@ int tree_accept(uint32_t n, const tq_cache* const* caches, const tq_accept_args*
     if (int rc = view_cache(who, caches[i], &c)) return rc;
     if (!a->seqs && a->trees > c.n_seqs) return refuse(TQ_E_INVALID_ARG, who + ": more trees than sequences, and no seqs");
   }
+  // (layers that share their keys would have them moved twice, at the same time)
+  std::vector<std::pair<const void*, const void*>> pools(n);
+  for (uint32_t i = 0; i < n; ++i) pools[i] = {caches[i]->k, caches[i]->tables};
+  std::sort(pools.begin(), pools.end());
+  if (std::adjacent_find(pools.begin(), pools.end()) != pools.end()) return refuse(TQ_E_INVALID_ARG, who + ": a cache is there twice");
   if (a->trees == 0) return TQ_OK;
   if (!a->masks || !a->lengths || !a->drafted || !a->sampled || !a->path || !a->accepted || !a->next || !a->lengths_out)
     return refuse(TQ_E_INVALID_ARG, who + ": null pointer");

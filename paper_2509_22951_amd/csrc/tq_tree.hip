@@ -8,7 +8,8 @@
 //   values of the contraction, so P is already where it is needed; V is transposed on its way out of LDS.
 // bf16: q (if fp32) and the weights enter as three bf16 parts each, all of fp32's 24 bits.  8 bits: q as a whole number of 24 bits, in units of a row's largest value / (127 * 2^16),
 // whose three digits of 8 bits meet the keys in integer products, which are exact; values become f16 in registers, which is exact too, and meet weights (times the
-// values' scales) of two f16 parts, 22 bits.
+// values' scales) of two f16 parts, 22 bits.  (q loses up to 2^-24 of its largest value in every dim: over 256 dims that is 2^-8 of what
+// the rounding of a key to 8 bits in the one dim of that value can be.)
 #include <algorithm>
 
 #include "tq_cache_view.h"
@@ -400,7 +401,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   float top = -INFINITY, total = 0.f;
   // 8 bits: weights times their values' scales are two f16 parts each, 22 bits, and are multiplied by 2^raised for that: by as much as keeps a column's below 2^15.  So are the sums.
   constexpr int kRaised = 126;
-  constexpr float kMostWeight = 32768.f;
+  constexpr float kMostWeight = 32768.f, kMostScale = 0x1p80f;   // (sums of levels and digits are below 2^39)
   int raised = kRaised;
   auto take_tile = [&](auto buffer, uint32_t tile, bool some) __attribute__((always_inline)) {
     constexpr int kBuffer = decltype(buffer)::value;
@@ -509,9 +510,9 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     const float scale = INT8 ? logit_scale : a.scale;
     m *= scale;
     // The weights' reference follows the maximum when that has grown by more than 8 (2^8 is far from any bound of fp32).
-    if (__any(m > top + 8.f || (INT8 && !(most_scale < INFINITY)))) {
-      // (an infinite scale of a key makes NaN of a level of zero: the tokens are taken again, unless none of them is this column's)
-      if (INT8 && !(most_scale < INFINITY)) total = __builtin_nanf("");
+    if (__any(m > top + 8.f || (INT8 && !(most_scale < kMostScale)))) {
+      // (an infinite scale of a key makes NaN of a level of zero, and one this large could make an infinity of a logit that is none: the tokens are taken again)
+      if (INT8 && !(most_scale < kMostScale)) total = __builtin_nanf("");
       m = fmaxf(m, top);
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));

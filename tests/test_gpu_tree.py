@@ -294,6 +294,97 @@ def test_weights_enter_the_sum_with_all_their_bits(kind, dim):
     assert ((out - want).abs() <= want.abs() * 2.0 ** -8 + size * 2.0 ** -22).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("order", ["rising", "falling", "shuffled", "signs"])
+def test_values_scales_of_any_size(order, dim):
+    """8 bits, scales from 1e-30 to 1e30, beside weights about as different: off by 2^-14 of sum p |v|, as above, whatever the largest of the scales is."""
+    n, nodes, heads = 700, 5, 6
+    p = Paged(2, -(-(n + nodes) // 16), kv_heads=2, dim=dim, kind="int8", seed=dim)
+    bits = bits_of(random_parents(2, nodes))
+    q = queries(2, nodes, heads, dim, dim)
+    size = 10.0 ** torch.linspace(-30, 30, n + nodes)
+    if order == "falling":
+        size = size.flip(0)
+    if order in ("shuffled", "signs"):
+        size = size[torch.randperm(n + nodes, generator=torch.Generator().manual_seed(dim))]
+    if order == "signs":
+        size[::2] *= -1
+    for s in range(2):
+        for slot in range(n + nodes):
+            p.v_scale[int(p.tables[s, slot // 16]), :, slot % 16] = size[slot]
+    lengths = ints([n, n // 2])
+    out, want = run(p, q, lengths, bits).cpu().double(), tree_reference(p, q, lengths, bits)
+    signed_v, p.v, p.v_scale = (p.v, p.v_scale), p.v.abs(), p.v_scale.abs()
+    terms = tree_reference(p, q, lengths, bits)
+    p.v, p.v_scale = signed_v
+    assert torch.isfinite(out).all() and ((out - want).abs() <= want.abs() * 2.0 ** -8 + terms * 2.0 ** -14).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_logits_that_rise_from_token_to_token(kind, dim):
+    """The largest so far grows over and over, by 1 a token, in 8 bits with values' scales that fall as the weights rise."""
+    n, nodes = 900, 3
+    p = Paged(1, -(-(n + nodes) // 16), kv_heads=1, dim=dim, kind=kind, seed=dim)
+    q = torch.zeros((1, nodes, 2, dim), device="cuda")
+    q[..., 0] = 1.0
+    bits = bits_of(random_parents(1, nodes))
+    for slot in range(n + nodes):
+        page, at = int(p.tables[0, slot // 16]), slot % 16
+        p.k[page, 0, at, 0] = 1 if kind == "int8" else slot % 256
+        if kind == "int8":
+            p.k_scale[page, 0, at] = float(slot)
+            p.v_scale[page, 0, at] = 2.0 ** max(-100, 40 - 1.4 * slot)
+    lengths = ints([n])
+    out, want = run(p, q, lengths, bits, scale=1.0).cpu().double(), tree_reference(p, q, lengths, bits, scale=1.0)
+    signed_v, p.v, p.v_scale = (p.v, p.v_scale), p.v.abs(), p.v_scale
+    terms = tree_reference(p, q, lengths, bits, scale=1.0)
+    p.v, p.v_scale = signed_v
+    # logits up to 2^10 in place of 2^5: 2^-10 of the terms, taken twice
+    assert torch.isfinite(out).all() and ((out - want).abs() <= want.abs() * 2.0 ** -8 + terms * 2.0 ** -9).all()
+
+
+def test_keys_scales_far_from_those_of_queries():
+    """Logits of ordinary size from 8-bit keys of 1e30 and queries of 1e-30, all of them negative."""
+    n, nodes, heads, dim = 200, 4, 3, 64
+    p = Paged(1, -(-(n + nodes) // 16), kv_heads=1, dim=dim, kind="int8")
+    p.k.copy_(-p.k.abs())
+    bits = bits_of(random_parents(1, nodes))
+    q = queries(1, nodes, heads, dim).abs()
+    lengths = ints([n])
+    for size in (2.0 ** 60, 2.0 ** 75, 2.0 ** 90, 2.0 ** 100):
+        scale, p.k_scale = p.k_scale, p.k_scale * size
+        close(run(p, q / size, lengths, bits), tree_reference(p, q / size, lengths, bits), p)
+        p.k_scale = scale
+
+
+def test_graphs_that_share_a_workspace():
+    """Two calls of different trees captured into graphs of their own with one workspace, replayed in turn."""
+    p = Paged(3, 60, dim=128, kind="int8")
+    made, wants, graphs, shared = [], [], [], None
+    for trees, nodes, lengths in ((3, 12, [900, 31, 333]), (1, 40, [700])):
+        bits = bits_of(random_parents(trees, nodes))
+        q = queries(trees, nodes, 8, 128, nodes)
+        if shared is None:
+            shared = torch.zeros(1 << 27, dtype=torch.uint8, device="cuda")
+        made.append(tree_call(p.describe(), q, ints(lengths), masks_of(bits), workspace=shared))
+        wants.append(tree_reference(p, q, ints(lengths), bits))
+    for call, _ in made:
+        call.launch(stream())
+    torch.cuda.synchronize()
+    for call, _ in made:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=torch.cuda.Stream()):
+            call.launch(stream())
+    for _ in range(3):
+        for graph, (_, out), want in zip(graphs, made, wants):
+            out.fill_(float("nan"))
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, out), want in zip(made, wants):
+            close(out, want, p)
+
+
 def test_a_pool_beyond_32_bits_of_offset():
     p = Paged(1, 5, kv_heads=2, dim=64)
     base = 2 ** 31 // (2 * 16 * 64) + 5

@@ -46,6 +46,13 @@ def test_accept_refuses(code, change):
     refused(code, lambda: tq.TreeAccept([tq.Cache(**CACHE)], **{**ACCEPT, **change}).launch())
 
 
+def test_accept_refuses_a_cache_that_is_there_twice():
+    one, other_tables, other_pool = tq.Cache(**CACHE), tq.Cache(**{**CACHE, "tables": CACHE["tables"] + 4096}), tq.Cache(**{**CACHE, "k": CACHE["k"] + 4096})
+    for caches in ([one, one], [other_pool, one, other_tables, tq.Cache(**CACHE)]):
+        assert "twice" in refused(INVALID, lambda: tq.TreeAccept(caches, **ACCEPT).launch())
+    tq.TreeAccept([one, other_tables, other_pool], **{**ACCEPT, "trees": 0}).launch()
+
+
 @pytest.mark.parametrize("code,change", [
     (INVALID, dict(logits=0)), (INVALID, dict(uniform=0)), (INVALID, dict(tokens=0)), (INVALID, dict(workspace=0)), (INVALID, dict(workspace=A + 8)), (INVALID, dict(workspace_bytes=8)),
     (UNSUPPORTED, dict(vocab=0)), (UNSUPPORTED, dict(vocab=(1 << 20) + 1)), (UNSUPPORTED, dict(rows=65536)), (INVALID, dict(logits_stride=99)), (INVALID, dict(logits=A + 2)),
