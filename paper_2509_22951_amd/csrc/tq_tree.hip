@@ -42,8 +42,11 @@ struct Seen {
 };
 template <typename C, typename A>
 __device__ __forceinline__ Seen seen_by(C& c, A& a, uint32_t t) {
-  const int32_t s = a.seqs ? a.seqs[t] : (int32_t)t;
-  const uint32_t size = a.sizes ? (uint32_t)min(max(a.sizes[t], 0), (int32_t)a.nodes) : a.nodes, length = (uint32_t)max(a.lengths[t], 0);
+  // (three loads at once, where a condition would put them behind each other)
+  const int32_t *lengths = a.lengths, *seqs = a.seqs ? a.seqs : lengths, *sizes = a.sizes ? a.sizes : lengths;
+  const int32_t of_lengths = lengths[t], of_seqs = seqs[t], of_sizes = sizes[t];
+  const int32_t s = a.seqs ? of_seqs : (int32_t)t;
+  const uint32_t size = a.sizes ? (uint32_t)min(max(of_sizes, 0), (int32_t)a.nodes) : a.nodes, length = (uint32_t)max(of_lengths, 0);
   if ((uint32_t)s >= c.n_seqs || size == 0) return Seen{0, 0, 0, size};
   return Seen{(uint32_t)s, min(length, c.capacity), (uint32_t)min((uint64_t)length + size, (uint64_t)c.capacity), size};
 }
