@@ -7,6 +7,7 @@ namespace tq {
 namespace {
 
 constexpr uint32_t kMostVocab = 1u << 20, kThreads = 256, kFew = 2, kMany = 4;   // kFew, kMany: four logits each, of a thread
+constexpr uint32_t kApart = 32;   // words from one counter to the next, in a cache line of its own
 constexpr uint32_t kMostParts = kMostVocab / (4 * kFew * kThreads);
 constexpr uint32_t kBinThreads = 1024, kBinPart = 8 * kBinThreads, kBins = 2048, kBinsPerUnit = 32, kListed = 2048;   // bins of (largest - logit) / temperature; keys held in LDS
 
@@ -15,10 +16,10 @@ struct Notes {
   uint64_t* keys;      // [row][part]: the first token's key
   uint64_t* mass;      // [row][kBins]: weights of a bin
   uint32_t* count;     // [row][kBins]: tokens of a bin
-  double* kept;        // [row][part]: weight of what is kept beyond doubt
+  double* kept;        // [row][part]: weight of what is kept beyond doubt; of an open row, of all tokens relative to the part's first one
   uint32_t* listed;    // [row][part]: tokens in the part's list
   uint64_t* list;      // [row][vocab]: of every part, where its tokens begin, the keys of those in the bin that the cut lies in
-  uint32_t* done;      // [row]: workgroups that are
+  uint32_t* done;      // [row * kApart]: workgroups that are
 };
 
 struct SampleView {
@@ -103,13 +104,26 @@ __device__ __forceinline__ T wave_upto(T v) {
   return v;
 }
 
+// What the caller asks of a row.  (Four loads at once, where conditions would put them behind each other.)
+struct Asked {
+  float temperature, p, least;
+  int32_t k;
+};
+__device__ __forceinline__ Asked asked_of(const SampleView& a, uint32_t r) {
+  const float t = (a.temperature ? a.temperature : a.uniform)[r], p = (a.top_p ? a.top_p : a.uniform)[r], least = (a.min_p ? a.min_p : a.uniform)[r];
+  const int32_t k = (a.top_k ? a.top_k : (const int32_t*)a.uniform)[r];
+  return Asked{a.temperature ? t : 1.f, a.top_p ? p : 1.f, a.min_p ? least : 0.f, a.top_k ? k : 0};
+}
+__device__ __forceinline__ bool limited(const Asked& x, uint32_t vocab) { return x.k > 0 && (uint32_t)x.k < vocab; }
+// A row that is drawn from without filters: its parts' weights are summed in the first launch already, relative to their own first tokens'.
+__device__ __forceinline__ bool is_open(const Asked& x, uint32_t vocab) { return x.temperature > 0.f && !limited(x, vocab) && !(x.p < 1.f) && !(x.least > 0.f); }
+
 // The first token's key of the row, from the parts' (by all threads; slots: one per wavefront).
-__device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, uint64_t* slots) {
+__device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, const Asked& x, uint64_t* slots) {
   Filter f;
-  f.temperature = a.temperature ? a.temperature[r] : 1.f;
+  f.temperature = x.temperature;
   f.per_bin = (float)kBinsPerUnit / f.temperature;
-  f.p = a.top_p ? a.top_p[r] : 1.f, f.least = a.min_p ? a.min_p[r] : 0.f;
-  const int32_t k = a.top_k ? a.top_k[r] : 0;
+  f.p = x.p, f.least = x.least;
   uint64_t best = 0;
   for (uint32_t i = threadIdx.x; i < a.parts; i += blockDim.x) best = max(best, a.notes.keys[(uint64_t)r * a.parts + i]);
   best = wave_max(best);
@@ -119,7 +133,7 @@ __device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, uin
   for (uint32_t w = 1; w < blockDim.x / 64; ++w) best = max(best, slots[w]);
   f.first = ~(uint32_t)best;
   f.top = best >> 32 ? logit_of_rank((uint32_t)(best >> 32)) : -INFINITY;
-  f.k = k > 0 ? min((uint32_t)k, a.vocab) : a.vocab;
+  f.k = limited(x, a.vocab) ? (uint32_t)x.k : a.vocab;
   f.drawn = f.top > -INFINITY && f.temperature > 0.f;
   f.by_rank = f.k < a.vocab, f.by_mass = f.p < 1.f;
   return f;
@@ -148,17 +162,19 @@ __device__ __forceinline__ uint32_t bin_of(float distance) { return distance < (
 template <int CHUNKS>
 constexpr uint32_t kPart = 4 * CHUNKS * kThreads;
 
-// First launch: the first token of every part; bins and counters are cleared for the next ones.
+// First launch: the first token of every part, and an open row's weights; bins and counters are cleared for the next ones.
 template <int CHUNKS>
 __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
   __shared__ uint64_t slots[kThreads / 64];
+  __shared__ double sums[kThreads / 64];
   const uint32_t part = blockIdx.x, r = blockIdx.y, tid = threadIdx.x;
   const float* row = a.logits + r * a.stride;
+  const Asked asked = asked_of(a, r);
   float v[CHUNKS][4];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) four_of(row, part * kPart<CHUNKS> + 4 * (c * kThreads + tid), a.vocab, v[c]);
   for (uint32_t i = part * kThreads + tid; i < kBins; i += a.parts * kThreads) a.notes.mass[(uint64_t)r * kBins + i] = 0, a.notes.count[(uint64_t)r * kBins + i] = 0;
-  if (part == 0 && tid == 0) a.notes.done[r] = 0;
+  if (part == 0 && tid == 0) a.notes.done[(uint64_t)r * kApart] = 0;
   uint64_t best = 0;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c)
@@ -170,9 +186,21 @@ __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
   best = wave_max(best);
   if ((tid & 63) == 0) slots[tid >> 6] = best;
   __syncthreads();
+  for (uint32_t w = 0; w < kThreads / 64; ++w) best = max(best, slots[w]);
+  if (tid == 0) a.notes.keys[(uint64_t)r * a.parts + part] = best;
+  if (!is_open(asked, a.vocab)) return;
+  const Weigher weight(logit_of_rank((uint32_t)(best >> 32)), asked.temperature);
+  double sum = 0.;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += weight(v[c][j]);   // (NaN beyond the row)
+  sum = wave_sum(sum);
+  if ((tid & 63) == 0) sums[tid >> 6] = sum;
+  __syncthreads();
   if (tid == 0) {
-    for (uint32_t w = 1; w < kThreads / 64; ++w) best = max(best, slots[w]);
-    a.notes.keys[(uint64_t)r * a.parts + part] = best;
+    for (uint32_t w = 1; w < kThreads / 64; ++w) sum += sums[w];
+    a.notes.kept[(uint64_t)r * a.parts + part] = sum;
   }
 }
 
@@ -183,12 +211,13 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleView a) {
   const uint32_t r = blockIdx.y, tid = threadIdx.x;
   const float* row = a.logits + r * a.stride;
   // (before anything is asked for: of a row without these filters, and of a greedy one, nothing is read)
-  if (!((a.top_k && a.top_k[r] > 0) || (a.top_p && a.top_p[r] < 1.f)) || (a.temperature && !(a.temperature[r] > 0.f))) return;
+  const Asked asked = asked_of(a, r);
+  if (!(limited(asked, a.vocab) || asked.p < 1.f) || !(asked.temperature > 0.f)) return;
   float v[2][4];
 #pragma unroll
   for (int c = 0; c < 2; ++c) four_of(row, blockIdx.x * kBinPart + c * (kBinPart / 2) + 4 * tid, a.vocab, v[c]);
   for (uint32_t b = tid; b < kBins; b += kBinThreads) lds_mass[b] = 0, lds_count[b] = 0;
-  const Filter f = filter_of(a, r, slots);
+  const Filter f = filter_of(a, r, asked, slots);
   if (!f.drawn || (!f.by_rank && !f.by_mass)) return;
   const Weigher weight(f.top, f.temperature);
   const double unit = (double)(1ull << a.mass_bits);
@@ -247,7 +276,8 @@ __device__ __forceinline__ Cut find_cut(const uint32_t (&count)[PER], const uint
   return *lds_cut;
 }
 
-// Third launch: the weight of what is kept in every part, and the tokens of the bin that the cut lies in; the last workgroup of a row finds the cut and draws.
+// Third launch: the weight of what is kept in every part, and the tokens of the bin that the cut lies in; the last workgroup of a row finds the cut and draws.  Of an open row, whose parts
+// are summed, the first one draws.
 //
 // Bound: a chain of waits.  Few rows: logits and the parts' first keys -> weights -> sums over the workgroup -> store, count -> the parts' sums -> the part that has the token ->
 // its logits -> weights once more: 13 us for 32000 tokens, beside 2.2 and 7 of the launches ahead.  16 rows of 128256 with filters: 25 us, beside 3.5 and 7 (read: 8 MB, 1.3 us).  64 rows without: 31 us, beside 8.2
@@ -259,21 +289,30 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   __shared__ uint32_t lds_n[kThreads / 64], lds_count[256], lds_upto[kMostParts], lds_base, lds_done, lds_token, lds_last;
   __shared__ double lds_sum[kThreads / 64], lds_share;
   __shared__ Cut lds_cut;
-  const uint32_t part = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t part = blockIdx.y, r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float* row = a.logits + r * a.stride;
-  float v[CHUNKS][4];
-#pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) four_of(row, part * kPart<CHUNKS> + 4 * (c * kThreads + tid), a.vocab, v[c]);
-  // (the bins are asked for before it is known whether the row has any: two waits for memory in place of three)
+  // (the bins are asked for ahead of the largest logit: two waits for memory in place of three.  Of few rows all of it is asked for before it is known whether the row is open, 14.0 us for one
+  // of 32000 logits in place of 15.3; of many, whose reading takes longer than the wait, after that: 64 open rows of 128256 9.5 us in place of 24.)
   constexpr int kBinsPer = kBins / kThreads;
+  float v[CHUNKS][4];
   uint32_t count[kBinsPer];
   uint64_t mass[kBinsPer];
+  auto ask = [&] {
 #pragma unroll
-  for (int i = 0; i < kBinsPer; ++i) {
-    count[i] = a.notes.count[(uint64_t)r * kBins + tid * kBinsPer + i];
-    mass[i] = a.notes.mass[(uint64_t)r * kBins + tid * kBinsPer + i];
-  }
-  const Filter f = filter_of(a, r, slots);
+    for (int c = 0; c < CHUNKS; ++c) four_of(row, part * kPart<CHUNKS> + 4 * (c * kThreads + tid), a.vocab, v[c]);
+#pragma unroll
+    for (int i = 0; i < kBinsPer; ++i) {
+      count[i] = a.notes.count[(uint64_t)r * kBins + tid * kBinsPer + i];
+      mass[i] = a.notes.mass[(uint64_t)r * kBins + tid * kBinsPer + i];
+    }
+  };
+  if constexpr (CHUNKS == kFew) ask();
+  const Asked asked = asked_of(a, r);
+  const bool open = is_open(asked, a.vocab);
+  if (open && part) return;
+  if constexpr (CHUNKS != kFew)
+    if (!open) ask();
+  const Filter f = filter_of(a, r, asked, slots);
   if (!f.drawn) {
     if (part == 0 && tid == 0) {
       a.tokens[r] = f.top > -INFINITY ? (int32_t)f.first : -1;
@@ -305,51 +344,53 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   };
 
   // this part
-  const uint32_t part_first = part * kPart<CHUNKS>;
-  double sum = 0.;
-  uint32_t n = 0;
-#pragma unroll
-  for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
-      const uint32_t b = i >= a.vocab ? kBins + 1 : cuts ? bin_of(distance_of(f, v[c][j])) : 0;
-      const double w = kept_weight(v[c][j], i);   // (beyond the row: none)
-      sum += b < cut.bin ? w : 0.;
-      n += b == cut.bin;
-    }
-  sum = wave_sum(sum);
-  const uint32_t n_upto = wave_upto(n);
-  __syncthreads();
-  if (lane == 63) lds_n[wave] = n_upto, lds_sum[wave] = sum;
-  __syncthreads();
-  uint32_t at = n_upto - n, all_n = 0;
-  for (uint32_t w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) at += lds_n[w];
-    all_n += lds_n[w];
-  }
-  if (tid == 0) {
-    double all = 0.;
-    for (uint32_t w = 0; w < kThreads / 64; ++w) all += lds_sum[w];
-    __hip_atomic_store((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + part], __builtin_bit_cast(uint64_t, all), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&a.notes.listed[(uint64_t)r * a.parts + part], all_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  if (all_n) {
+  if (!open) {
+    const uint32_t part_first = part * kPart<CHUNKS>;
+    double sum = 0.;
+    uint32_t n = 0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
-        if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin)
-          __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + part_first + at++], key_of(v[c][j], i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t b = i >= a.vocab ? kBins + 1 : cuts ? bin_of(distance_of(f, v[c][j])) : 0;
+        const double w = kept_weight(v[c][j], i);   // (beyond the row: none)
+        sum += b < cut.bin ? w : 0.;
+        n += b == cut.bin;
       }
+    sum = wave_sum(sum);
+    const uint32_t n_upto = wave_upto(n);
+    __syncthreads();
+    if (lane == 63) lds_n[wave] = n_upto, lds_sum[wave] = sum;
+    __syncthreads();
+    uint32_t at = n_upto - n, all_n = 0;
+    for (uint32_t w = 0; w < kThreads / 64; ++w) {
+      if (w < wave) at += lds_n[w];
+      all_n += lds_n[w];
+    }
+    if (tid == 0) {
+      double all = 0.;
+      for (uint32_t w = 0; w < kThreads / 64; ++w) all += lds_sum[w];
+      __hip_atomic_store((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + part], __builtin_bit_cast(uint64_t, all), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&a.notes.listed[(uint64_t)r * a.parts + part], all_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (all_n) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
+          if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin)
+            __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + part_first + at++], key_of(v[c][j], i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    // the stores have reached the level that the device shares; the last workgroup goes on with all of the row
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) lds_done = __hip_atomic_fetch_add(&a.notes.done[(uint64_t)r * kApart], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (lds_done != a.parts - 1) return;
   }
-  // the stores have reached the level that the device shares; the last workgroup goes on with all of the row
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (tid == 0) lds_done = __hip_atomic_fetch_add(&a.notes.done[r], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (lds_done != a.parts - 1) return;
 
   // The cut within the bin: narrowed by a 256th of the bin, then by 8 bits of the key at a time, until few enough are left to compare all with each other.
   uint64_t last = 0;   // tokens of at least this key are kept
@@ -362,6 +403,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     weights[i] = 0., listed[i] = 0;
     if (of < a.parts) {
       weights[i] = __builtin_bit_cast(double, __hip_atomic_load((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+      if (open) weights[i] *= weight(logit_of_rank((uint32_t)(a.notes.keys[(uint64_t)r * a.parts + of] >> 32)));
       if (cuts) listed[i] = __hip_atomic_load(&a.notes.listed[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       lds_more[of] = 0;
     }
@@ -585,7 +627,7 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
   l->mass = place((uint64_t)a->rows * kBins * 8);
   l->count = place((uint64_t)a->rows * kBins * 4);
   l->listed = place((uint64_t)a->rows * l->parts * 4);
-  l->done = place((uint64_t)a->rows * 4);
+  l->done = place((uint64_t)a->rows * kApart * 4);
   l->list = place((uint64_t)a->rows * a->vocab * 8);
   return TQ_OK;
 }
@@ -614,7 +656,7 @@ int sample(const tq_sample_args* a, void* stream) {
     constexpr int kChunks = decltype(chunks)::value;
     hipLaunchKernelGGL(k_sample_first<kChunks>, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
     if (a->top_k || a->top_p) hipLaunchKernelGGL(k_sample_bins, dim3((a->vocab + kBinPart - 1) / kBinPart, a->rows), dim3(kBinThreads), 0, st, v);
-    hipLaunchKernelGGL(k_sample_draw<kChunks>, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
+    hipLaunchKernelGGL(k_sample_draw<kChunks>, dim3(a->rows, l.parts), dim3(kThreads), 0, st, v);
   };
   if (l.many) go(std::integral_constant<int, kMany>());
   else go(std::integral_constant<int, kFew>());
