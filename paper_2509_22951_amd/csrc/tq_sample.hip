@@ -9,7 +9,7 @@ namespace {
 constexpr uint32_t kMostVocab = 1u << 20, kThreads = 256, kFew = 2, kMany = 4;   // kFew, kMany: four logits each, of a thread
 constexpr uint32_t kApart = 32;   // words from one counter to the next, in a cache line of its own
 constexpr uint32_t kMostParts = kMostVocab / (4 * kFew * kThreads);
-constexpr uint32_t kBinThreads = 1024, kBinPart = 8 * kBinThreads, kBins = 2048, kBinsPerUnit = 32, kListed = 2048;   // bins of (largest - logit) / temperature; keys held in LDS
+constexpr uint32_t kBinThreads = 1024, kBins = 2048, kBinsPerUnit = 32, kListed = 2048;   // bins of (largest - logit) / temperature; keys held in LDS
 
 // What the launches leave each other, for every row.
 struct Notes {
@@ -204,7 +204,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
   }
 }
 
-// Second launch, for rows with top_k or top_p: tokens and weights of every bin.
+// Second launch, for rows with top_k or top_p: tokens and weights of every bin.  PER tokens a thread.
+template <int PER>
 __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleView a) {
   __shared__ uint64_t slots[kBinThreads / 64], lds_mass[kBins];
   __shared__ uint32_t lds_count[kBins];
@@ -213,25 +214,28 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleView a) {
   // (before anything is asked for: of a row without these filters, and of a greedy one, nothing is read)
   const Asked asked = asked_of(a, r);
   if (!(limited(asked, a.vocab) || asked.p < 1.f) || !(asked.temperature > 0.f)) return;
-  float v[2][4];
+  const uint32_t first = blockIdx.x * (PER * kBinThreads);
+  float v[PER];
+  auto token = [&](int j) { return PER == 8 ? first + j / 4 * (4 * kBinThreads) + 4 * tid + j % 4 : first + j * kBinThreads + tid; };
+  if constexpr (PER == 8) {
+    four_of(row, token(0), a.vocab, *(float(*)[4])&v[0]), four_of(row, token(4), a.vocab, *(float(*)[4])&v[4]);
+  } else {
 #pragma unroll
-  for (int c = 0; c < 2; ++c) four_of(row, blockIdx.x * kBinPart + c * (kBinPart / 2) + 4 * tid, a.vocab, v[c]);
+    for (int j = 0; j < PER; ++j) v[j] = token(j) < a.vocab ? row[token(j)] : 0.f;
+  }
   for (uint32_t b = tid; b < kBins; b += kBinThreads) lds_mass[b] = 0, lds_count[b] = 0;
   const Filter f = filter_of(a, r, asked, slots);
   if (!f.drawn || (!f.by_rank && !f.by_mass)) return;
   const Weigher weight(f.top, f.temperature);
   const double unit = (double)(1ull << a.mass_bits);
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t i = blockIdx.x * kBinPart + c * (kBinPart / 2) + 4 * tid + j;
-      const uint32_t b = bin_of(distance_of(f, v[c][j]));
-      const uint64_t mass = (uint64_t)(weight(v[c][j]) * unit + 0.5);
-      if (i >= a.vocab) continue;
-      atomicAdd(&lds_count[b], 1u);
-      if (f.by_mass) atomicAdd((unsigned long long*)&lds_mass[b], (unsigned long long)mass);
-    }
+  for (int j = 0; j < PER; ++j) {
+    const uint32_t b = bin_of(distance_of(f, v[j]));
+    const uint64_t mass = (uint64_t)(weight(v[j]) * unit + 0.5);
+    if (token(j) >= a.vocab) continue;
+    atomicAdd(&lds_count[b], 1u);
+    if (f.by_mass) atomicAdd((unsigned long long*)&lds_mass[b], (unsigned long long)mass);
+  }
   __syncthreads();
   for (uint32_t b = tid; b < kBins; b += kBinThreads)
     if (lds_count[b]) {
@@ -655,7 +659,12 @@ int sample(const tq_sample_args* a, void* stream) {
   auto go = [&](auto chunks) {
     constexpr int kChunks = decltype(chunks)::value;
     hipLaunchKernelGGL(k_sample_first<kChunks>, dim3(l.parts, a->rows), dim3(kThreads), 0, st, v);
-    if (a->top_k || a->top_p) hipLaunchKernelGGL(k_sample_bins, dim3((a->vocab + kBinPart - 1) / kBinPart, a->rows), dim3(kBinThreads), 0, st, v);
+    if (a->top_k || a->top_p) {
+      // a workgroup per compute unit before a thread takes more than two tokens
+      const uint32_t small = (a->vocab + 2 * kBinThreads - 1) / (2 * kBinThreads), large = (a->vocab + 8 * kBinThreads - 1) / (8 * kBinThreads);
+      if ((uint64_t)small * a->rows <= 256) hipLaunchKernelGGL(k_sample_bins<2>, dim3(small, a->rows), dim3(kBinThreads), 0, st, v);
+      else hipLaunchKernelGGL(k_sample_bins<8>, dim3(large, a->rows), dim3(kBinThreads), 0, st, v);
+    }
     hipLaunchKernelGGL(k_sample_draw<kChunks>, dim3(a->rows, l.parts), dim3(kThreads), 0, st, v);
   };
   if (l.many) go(std::integral_constant<int, kMany>());
