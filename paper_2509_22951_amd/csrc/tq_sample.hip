@@ -75,34 +75,44 @@ struct Filter {
   bool drawn, by_rank, by_mass;   // drawn: not merely the first token; by_rank, by_mass: top_k or top_p leaves something out
 };
 
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v = max(v, (uint64_t)__shfl_xor((unsigned long long)v, d));
-  return v;
-}
-template <typename T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
-}
-__device__ __forceinline__ uint32_t wave_least(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v = min(v, (uint32_t)__shfl_xor((int)v, d));
-  return v;
-}
-__device__ __forceinline__ uint32_t wave_most(uint32_t v) { return ~wave_least(~v); }
-
-// Sums over a wavefront's lanes up to and with each, in the same order every time.
-template <typename T>
-__device__ __forceinline__ T wave_upto(T v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const T other = __shfl_up(v, d);
-    if ((threadIdx.x & 63) >= (uint32_t)d) v += other;
+// A value of 4 or 8 bytes from another lane of the same wavefront (0 where there is none), within the vector registers.  (Shuffles through LDS: 14.2 us for one row's last launch, 23.7 for 16
+// rows', in place of 11.9 and 20.8.)
+template <int CONTROL, int ROWS, bool ZERO, typename T>
+__device__ __forceinline__ T from_lane(T v) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, ROWS, 0xf, ZERO));
+  } else {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CONTROL, ROWS, 0xf, ZERO), hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CONTROL, ROWS, 0xf, ZERO);
+    return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
   }
-  return v;
 }
+template <typename T>
+__device__ __forceinline__ T of_lane(T v, uint32_t lane) {   // (the same for all lanes)
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(T, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane));
+  }
+}
+// Of a wavefront's lanes up to and with each, joined in the same order every time; 0 joined with a value is that value.  By all lanes.
+template <typename T, typename JOIN>
+__device__ __forceinline__ T wave_joined(T v, JOIN join) {
+  v = join(v, from_lane<0x111, 0xf, true>(v));
+  v = join(v, from_lane<0x112, 0xf, true>(v));
+  v = join(v, from_lane<0x114, 0xf, true>(v));
+  v = join(v, from_lane<0x118, 0xf, true>(v));
+  v = join(v, from_lane<0x142, 0xa, false>(v));   // lane 15 of a row to the next one
+  return join(v, from_lane<0x143, 0xc, false>(v));   // lane 31 to the upper half
+}
+template <typename T>
+__device__ __forceinline__ T wave_upto(T v) { return wave_joined(v, [](T x, T y) { return x + y; }); }
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) { return of_lane(wave_upto(v), 63); }
+template <typename T>
+__device__ __forceinline__ T wave_most(T v) { return of_lane(wave_joined(v, [](T x, T y) { return max(x, y); }), 63); }
+__device__ __forceinline__ uint32_t wave_least(uint32_t v) { return ~wave_most(~v); }
 
 // What the caller asks of a row.  (Four loads at once, where conditions would put them behind each other.)
 struct Asked {
@@ -126,7 +136,7 @@ __device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, con
   f.p = x.p, f.least = x.least;
   uint64_t best = 0;
   for (uint32_t i = threadIdx.x; i < a.parts; i += blockDim.x) best = max(best, a.notes.keys[(uint64_t)r * a.parts + i]);
-  best = wave_max(best);
+  best = wave_most(best);
   if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = best;
   __syncthreads();
   best = slots[0];
@@ -183,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
       const uint32_t i = part * kPart<CHUNKS> + 4 * (c * kThreads + tid) + j;
       if (i < a.vocab) best = max(best, key_of(v[c][j], i));
     }
-  best = wave_max(best);
+  best = wave_most(best);
   if ((tid & 63) == 0) slots[tid >> 6] = best;
   __syncthreads();
   for (uint32_t w = 0; w < kThreads / 64; ++w) best = max(best, slots[w]);
@@ -259,7 +269,7 @@ __device__ __forceinline__ Cut find_cut(const uint32_t (&count)[PER], const uint
 #pragma unroll
   for (int i = 0; i < PER; ++i) n += count[i], m += mass[i];
   const uint32_t n_upto = wave_upto(n);
-  const uint64_t m_upto = wave_upto((unsigned long long)m);
+  const uint64_t m_upto = wave_upto(m);
   __syncthreads();
   if (lane == 63) lds_n[wave] = n_upto, lds_m[wave] = m_upto;
   __syncthreads();
@@ -283,10 +293,10 @@ __device__ __forceinline__ Cut find_cut(const uint32_t (&count)[PER], const uint
 // Third launch: the weight of what is kept in every part, and the tokens of the bin that the cut lies in; the last workgroup of a row finds the cut and draws.  Of an open row, whose parts
 // are summed, the first one draws.
 //
-// Bound: a chain of waits.  Few rows: logits and the parts' first keys -> weights -> sums over the workgroup -> store, count -> the parts' sums -> the part that has the token ->
-// its logits -> weights once more: 13 us for 32000 tokens, beside 2.2 and 7 of the launches ahead.  16 rows of 128256 with filters: 25 us, beside 3.5 and 7 (read: 8 MB, 1.3 us).  64 rows without: 31 us, beside 8.2
-// and 3.9, of it about 10 for the weights, 30 instructions of 64 bits each, and as much for the chain.  Why three launches: a row's largest logit is needed ahead of every weight, and the cut ahead of every
-// sum; one workgroup per row, that needs no launch between, took 284 us for the first and 621 for the second.
+// Bound: a chain of waits.  One row: logits, bins and the parts' first keys 1.8 us -> the bin of the cut 1.3 -> weights, sums over the workgroup, the list's stores 2.3 -> count 0.5 -> the parts' sums and lists 2 ->
+// the cut within the bin 1 -> the part that has the token 0.9 -> its logits, weights once more 1.6: 11.5..11.9 us for 32000 tokens, beside 2.1..3.0 and 4.0..4.9 of the launches ahead.  16 rows of 128256 with filters:
+// 20.2 us, beside 4.1 and 6.2 (read: 8 MB, 1.3 us).  64 open rows: 7.6 us, beside 14.1 of the first launch (33 MB read, 5.2 us; weights, some 30 instructions of 64 bits each, 10) and 2.5.  Why three
+// launches: a row's largest logit is needed ahead of every weight that is compared with others, and the cut ahead of every sum; one workgroup per row, that needs no launch between, took 284 us for the first and 621 for the second.
 template <int CHUNKS>
 __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   __shared__ uint64_t slots[kThreads / 64], lds_m[kThreads / 64], lds_keys[kListed], lds_mass[256], lds_more[kMostParts];
@@ -295,8 +305,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   __shared__ Cut lds_cut;
   const uint32_t part = blockIdx.y, r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float* row = a.logits + r * a.stride;
-  // (the bins are asked for ahead of the largest logit: two waits for memory in place of three.  Of few rows all of it is asked for before it is known whether the row is open, 14.0 us for one
-  // of 32000 logits in place of 15.3; of many, whose reading takes longer than the wait, after that: 64 open rows of 128256 9.5 us in place of 24.)
+  // (the bins are asked for ahead of the largest logit: two waits for memory in place of three.  Of few rows all of it is asked for before it is known whether the row is open, 1.2 us less for one
+  // of 32000 logits; of many, whose reading takes longer than the wait, after that: 64 open rows of 128256 9.5 us in place of 24.)
   constexpr int kBinsPer = kBins / kThreads;
   float v[CHUNKS][4];
   uint32_t count[kBinsPer];
@@ -334,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     uint64_t all = 0;
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) all += mass[i];
-    all = wave_sum((unsigned long long)all);
+    all = wave_sum(all);
     if (lane == 0) lds_m[wave] = all;
     __syncthreads();
     all = 0;
@@ -499,13 +509,12 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
       uint32_t before = cut.above;
       uint64_t mass_before = cut.above_mass;
       for (uint32_t j = 0; j < left; ++j) {
-        const uint64_t other = (uint64_t)__shfl((unsigned long long)mine, j), its = (uint64_t)__shfl((unsigned long long)my_mass, j);
+        const uint64_t other = of_lane(mine, j), its = of_lane(my_mass, j);
         if (other > mine) ++before, mass_before += its;
       }
       const bool stays = lane < left && (before == 0 || (before < f.k && (!f.by_mass || (double)mass_before < target)));
       uint64_t least_key = stays ? mine : ~0ull;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) least_key = min(least_key, (uint64_t)__shfl_xor((unsigned long long)least_key, d));
+      least_key = ~wave_most(~least_key);
       if (lane == 0) slots[0] = least_key;
     }
     __syncthreads();
