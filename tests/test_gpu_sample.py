@@ -164,6 +164,50 @@ def test_results_repeat_on_another_stream_with_a_workspace_of_other_calls():
             assert torch.equal(tokens, first[0]) and torch.equal(probs, first[1])
 
 
+@pytest.mark.parametrize("rows,vocab", [(48, 100000), (3, 70001), (300, 9000)])
+def test_rows_without_filters_beside_others(rows, vocab):
+    """Their weights are summed relative to each part's own largest logit: parts of masked tokens, parts far below the others, parts with infinities."""
+    inf = float("inf")
+    x = peaked(rows, vocab, rows)
+    x[0, : vocab // 2] = -inf
+    x[1, 5000:] = float("nan")
+    x[2, : vocab // 3] -= 60
+    if rows > 3:
+        x[3, [17, vocab - 1]] = inf
+        x[4, 4096:8192] = inf
+        x[5, : vocab - 1] = -inf
+        x[6] = 0.25
+    few = [FILTERS[0] if r % 3 else FILTERS[r % len(FILTERS)] for r in range(rows)]
+    t, k, p, m = zip(*few)
+    u = np.random.default_rng(rows).random(rows, dtype=np.float32).tolist()
+    check(x, t, k, p, m, u)
+    check(x, None, None, None, None, u)
+    check(x, [0.01] * rows, [vocab] * rows, [1.0] * rows, None, u)      # (top_k of all tokens leaves none out)
+
+
+def test_graphs_that_share_a_workspace():
+    made = []
+    shared = torch.full((1 << 26,), 0xEE, dtype=torch.uint8, device="cuda")
+    for rows, vocab, seed in ((5, 30000, 11), (40, 60000, 12), (1, 777, 13)):
+        t, k, p, m = ([FILTERS[(r + seed) % len(FILTERS)][i] for r in range(rows)] for i in range(4))
+        made.append(call(peaked(rows, vocab, seed), t, k, p, m, np.random.default_rng(seed).random(rows, dtype=np.float32).tolist(), workspace=shared))
+    wants, graphs = [], []
+    for one, tokens, probs in made:
+        one.launch(stream())
+        torch.cuda.synchronize()
+        wants.append((tokens.clone(), probs.clone()))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=torch.cuda.Stream()):
+            one.launch(stream())
+    for _ in range(3):
+        for graph, (_, tokens, probs) in zip(graphs, made):
+            tokens.zero_(), probs.zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, tokens, probs), want in zip(made, wants):
+            assert torch.equal(tokens, want[0]) and torch.equal(probs, want[1])
+
+
 def test_how_often_tokens_are_drawn():
     """4096 evenly spaced numbers: every token is drawn as often as its share says, give or take the two ends."""
     x = torch.tensor([2.0, 1.0, 0.0, -1.0, 1.5, -30.0], device="cuda")
