@@ -366,7 +366,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       }
       most = fmaxf(most, __shfl_xor(most, 16)), most = fmaxf(most, __shfl_xor(most, 32));
       odd += __shfl_xor(odd, 16), odd += __shfl_xor(odd, 32);
-      const float up = fminf(8323072.f / most, 0x1p126f);   // 127 * 2^16; (of nothing but zeros: zeros)
+      const float up = fminf(127.f * 65536.f / most, 0x1p126f);   // (of nothing but zeros: zeros)
       logit_scale = a.scale / up + odd;                    // (a query that is not finite: NaN, so that the tokens are taken again)
 #pragma unroll
       for (int i = 0; i < S::kSteps; ++i)

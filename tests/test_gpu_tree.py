@@ -263,12 +263,9 @@ def test_every_token_counts_once():
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_weights_enter_the_sum_with_all_their_bits(kind, dim):
-    """Large terms that cancel, so that the result's own rounding to bf16 hides nothing.
-
-    Two tokens of the same key and opposite values, and a third one far smaller: the first two cancel exactly in fp32 sums of exact products if each
-    weight enters with all of its 24 bits, whatever they are; with 16 of them too, but a third value of 1 beside 2^10 is 2^-10 of the terms: a weight
-    that is off by more than 2^-24 of itself in one term and not in the other would show.  The keys differ by what makes the weights differ:
-    weights w and 2 w (logits log 2 apart, through q = 1 and keys of one dim), values 2 v and -v."""
+    """Large terms that cancel, so that the result's own rounding to bf16 hides nothing: two tokens of equal logits, through keys in two dims with equal queries, and opposite
+    values, and a third one with values of at most 1 beside their 60 to 120.  Equal weights leave nothing of the first two but the rounding of the fp32 sum; a weight that
+    entered one of the terms with fewer bits than the other would leave more."""
     nodes, heads = 3, 2
     p = Paged(4, 2, kv_heads=1, dim=dim, kind=kind)
     g = torch.Generator().manual_seed(dim)
@@ -292,6 +289,34 @@ def test_weights_enter_the_sum_with_all_their_bits(kind, dim):
     size = v.double().abs()[:, None, None, :]
     # equal logits, equal weights: two equal products cancel but for the fp32 sum's rounding, 2^-23 of them
     assert ((out - want).abs() <= want.abs() * 2.0 ** -8 + size * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_nearly_equal_weights_of_opposite_values(kind, dim):
+    """Logits 2^-7 apart at most, of 1 or 2: what is left of values v and -v is 2^-8 of them or less, and each bit of a weight below its eighth shows.
+
+    A logit is off by 2^-22 (two fp32 roundings of it), a weight by that, by 2^-23 from the exponential function, by 2^-22 from its parts and by 2^-23 from the sum, both weights
+    together by less than 2^-19 of v.  Parts of 16 bits in all would be up to 2^-16 off."""
+    nodes, heads = 16, 3
+    p = Paged(2, 2, kv_heads=1, dim=dim, kind=kind)
+    g = torch.Generator().manual_seed(dim)
+    q = torch.zeros((2, nodes, heads, dim))
+    q[..., 0] = 1 + torch.rand((2, nodes, heads), generator=g)
+    q[..., 1] = q[..., 0] + (torch.rand((2, nodes, heads), generator=g) - 0.5) * 2.0 ** -6
+    v = torch.round((1 + torch.rand((2, dim), generator=g)) * 60)
+    for s in range(2):
+        page = int(p.tables[s, 0])
+        for slot, value in enumerate((v[s], -v[s])):
+            row = torch.zeros(dim)
+            row[slot] = 1
+            p.k[page, 0, slot] = row.to(p.k.dtype).cuda()
+            p.v[page, 0, slot] = value.to(p.v.dtype).cuda()
+        if kind == "int8":
+            p.k_scale[page, 0, :2], p.v_scale[page, 0, :2] = 1.0, 1.0
+    lengths, bits = ints([2, 2]), [[0] * nodes] * 2
+    out, want = run(p, q.cuda(), lengths, bits, scale=1.0).cpu().double(), tree_reference(p, q.cuda(), lengths, bits, scale=1.0)
+    assert ((out - want).abs() <= want.abs() * 2.0 ** -8 + v.double()[:, None, None, :] * 2.0 ** -19).all()
 
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
