@@ -128,25 +128,32 @@ __device__ __forceinline__ bool limited(const Asked& x, uint32_t vocab) { return
 // A row that is drawn from without filters: its parts' weights are summed in the first launch already, relative to their own first tokens'.
 __device__ __forceinline__ bool is_open(const Asked& x, uint32_t vocab) { return x.temperature > 0.f && !limited(x, vocab) && !(x.p < 1.f) && !(x.least > 0.f); }
 
-// The first token's key of the row, from the parts' (by all threads; slots: one per wavefront).
-__device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, const Asked& x, uint64_t* slots) {
+// From the first token's key.
+__device__ __forceinline__ Filter filter_from(const Asked& x, uint32_t vocab, uint64_t best) {
   Filter f;
   f.temperature = x.temperature;
   f.per_bin = (float)kBinsPerUnit / f.temperature;
   f.p = x.p, f.least = x.least;
-  uint64_t best = 0;
-  for (uint32_t i = threadIdx.x; i < a.parts; i += blockDim.x) best = max(best, a.notes.keys[(uint64_t)r * a.parts + i]);
+  f.first = ~(uint32_t)best;
+  f.top = best >> 32 ? logit_of_rank((uint32_t)(best >> 32)) : -INFINITY;
+  f.k = limited(x, vocab) ? (uint32_t)x.k : vocab;
+  f.drawn = f.top > -INFINITY && f.temperature > 0.f;
+  f.by_rank = f.k < vocab, f.by_mass = f.p < 1.f;
+  return f;
+}
+// The largest of all threads' keys (by all threads; slots: one per wavefront).
+__device__ __forceinline__ uint64_t largest_of(uint64_t best, uint64_t* slots) {
   best = wave_most(best);
   if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = best;
   __syncthreads();
   best = slots[0];
   for (uint32_t w = 1; w < blockDim.x / 64; ++w) best = max(best, slots[w]);
-  f.first = ~(uint32_t)best;
-  f.top = best >> 32 ? logit_of_rank((uint32_t)(best >> 32)) : -INFINITY;
-  f.k = limited(x, a.vocab) ? (uint32_t)x.k : a.vocab;
-  f.drawn = f.top > -INFINITY && f.temperature > 0.f;
-  f.by_rank = f.k < a.vocab, f.by_mass = f.p < 1.f;
-  return f;
+  return best;
+}
+__device__ __forceinline__ Filter filter_of(const SampleView& a, uint32_t r, const Asked& x, uint64_t* slots) {
+  uint64_t best = 0;
+  for (uint32_t i = threadIdx.x; i < a.parts; i += blockDim.x) best = max(best, a.notes.keys[(uint64_t)r * a.parts + i]);
+  return filter_from(x, a.vocab, largest_of(best, slots));
 }
 
 // Four neighbouring logits; those beyond the row are masked.
@@ -195,10 +202,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
       const uint32_t i = part * kPart<CHUNKS> + 4 * (c * kThreads + tid) + j;
       if (i < a.vocab) best = max(best, key_of(v[c][j], i));
     }
-  best = wave_most(best);
-  if ((tid & 63) == 0) slots[tid >> 6] = best;
-  __syncthreads();
-  for (uint32_t w = 0; w < kThreads / 64; ++w) best = max(best, slots[w]);
+  best = largest_of(best, slots);
   if (tid == 0) a.notes.keys[(uint64_t)r * a.parts + part] = best;
   if (!is_open(asked, a.vocab)) return;
   const Weigher weight(logit_of_rank((uint32_t)(best >> 32)), asked.temperature);
@@ -295,18 +299,20 @@ __device__ __forceinline__ Cut find_cut(const uint32_t (&count)[PER], const uint
 }
 
 // Third launch: the weight of what is kept in every part, and the tokens of the bin that the cut lies in; the last workgroup of a row finds the cut and draws.  Of an open row, whose parts
-// are summed, the first one draws.
+// are summed, the first one draws.  A whole row (WHOLE: no more than a part) needs no launch ahead: its first token, its bins and its list are the workgroup's own.
 //
 // Bound: a chain of waits.  One row: logits, bins and the parts' first keys 1.8 us -> the bin of the cut 1.3 -> weights, sums over the workgroup, the list's stores 2.3 -> count 0.5 -> the parts' sums and lists 2 ->
 // the cut within the bin 1 -> the part that has the token 0.9 -> its logits, weights once more 1.6: 11.5..11.9 us for 32000 tokens, beside 2.1..3.0 and 4.0..4.9 of the launches ahead.  16 rows of 128256 with filters:
 // 20.2 us, beside 4.1 and 6.2 (read: 8 MB, 1.3 us).  64 open rows: 7.6 us, beside 14.1 of the first launch (33 MB read, 5.2 us; weights, some 30 instructions of 64 bits each, 10) and 2.5.  Why three
 // launches: a row's largest logit is needed ahead of every weight that is compared with others, and the cut ahead of every sum; one workgroup per row, that needs no launch between, took 284 us for the first and 621 for the second.
-template <int CHUNKS>
+template <int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   __shared__ uint64_t slots[kThreads / 64], lds_m[kThreads / 64], lds_keys[kListed], lds_mass[256], lds_more[kMostParts];
   __shared__ uint32_t lds_n[kThreads / 64], lds_count[256], lds_upto[kMostParts], lds_base, lds_done, lds_token, lds_last;
   __shared__ double lds_sum[kThreads / 64], lds_share;
   __shared__ Cut lds_cut;
+  __shared__ uint64_t lds_bin_mass[WHOLE ? kBins : 1];
+  __shared__ uint32_t lds_bin_count[WHOLE ? kBins : 1];
   const uint32_t part = blockIdx.y, r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float* row = a.logits + r * a.stride;
   // (the bins are asked for ahead of the largest logit: two waits for memory in place of three.  Of few rows all of it is asked for before it is known whether the row is open, 1.2 us less for one
@@ -324,13 +330,29 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
       mass[i] = a.notes.mass[(uint64_t)r * kBins + tid * kBinsPer + i];
     }
   };
-  if constexpr (CHUNKS == kFew) ask();
+  if constexpr (CHUNKS == kFew && !WHOLE) ask();
   const Asked asked = asked_of(a, r);
-  const bool open = is_open(asked, a.vocab);
+  const bool open = !WHOLE && is_open(asked, a.vocab);
   if (open && part) return;
-  if constexpr (CHUNKS != kFew)
-    if (!open) ask();
-  const Filter f = filter_of(a, r, asked, slots);
+  Filter f;
+  if constexpr (WHOLE) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) four_of(row, 4 * (c * kThreads + tid), a.vocab, v[c]);
+#pragma unroll
+    for (int i = 0; i < kBinsPer; ++i) lds_bin_count[i * kThreads + tid] = 0, lds_bin_mass[i * kThreads + tid] = 0;
+    uint64_t best = 0;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t i = 4 * (c * kThreads + tid) + j;
+        if (i < a.vocab) best = max(best, key_of(v[c][j], i));
+      }
+    f = filter_from(asked, a.vocab, largest_of(best, slots));
+  } else {
+    if (CHUNKS != kFew && !open) ask();
+    f = filter_of(a, r, asked, slots);
+  }
   if (!f.drawn) {
     if (part == 0 && tid == 0) {
       a.tokens[r] = f.top > -INFINITY ? (int32_t)f.first : -1;
@@ -345,6 +367,21 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   Cut cut{kBins, 0, 0};
   double target = 0.;
   if (cuts) {
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t b = bin_of(distance_of(f, v[c][j]));
+          const uint64_t its = mass_of(v[c][j]);
+          if (4 * (c * kThreads + tid) + j >= a.vocab) continue;
+          atomicAdd(&lds_bin_count[b], 1u);
+          if (f.by_mass) atomicAdd((unsigned long long*)&lds_bin_mass[b], (unsigned long long)its);
+        }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kBinsPer; ++i) count[i] = lds_bin_count[tid * kBinsPer + i], mass[i] = lds_bin_mass[tid * kBinsPer + i];
+    }
     uint64_t all = 0;
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) all += mass[i];
@@ -362,6 +399,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   };
 
   // this part
+  double kept = 0.;   // (of a whole row)
+  uint32_t all_listed = 0;
   if (!open) {
     const uint32_t part_first = part * kPart<CHUNKS>;
     double sum = 0.;
@@ -386,10 +425,10 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
       if (w < wave) at += lds_n[w];
       all_n += lds_n[w];
     }
-    if (tid == 0) {
-      double all = 0.;
-      for (uint32_t w = 0; w < kThreads / 64; ++w) all += lds_sum[w];
-      __hip_atomic_store((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + part], __builtin_bit_cast(uint64_t, all), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (WHOLE || tid == 0)
+      for (uint32_t w = 0; w < kThreads / 64; ++w) kept += lds_sum[w];
+    if (!WHOLE && tid == 0) {
+      __hip_atomic_store((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + part], __builtin_bit_cast(uint64_t, kept), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __hip_atomic_store(&a.notes.listed[(uint64_t)r * a.parts + part], all_n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     if (all_n) {
@@ -398,28 +437,37 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
-          if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin)
-            __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + part_first + at++], key_of(v[c][j], i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin) {
+            if (WHOLE && at < kListed) lds_keys[at] = key_of(v[c][j], i);
+            else __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + part_first + at], key_of(v[c][j], i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            ++at;
+          }
         }
     }
     // the stores have reached the level that the device shares; the last workgroup goes on with all of the row
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) lds_done = __hip_atomic_fetch_add(&a.notes.done[(uint64_t)r * kApart], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (lds_done != a.parts - 1) return;
+    if constexpr (WHOLE) {
+      all_listed = all_n;
+    } else {
+      if (tid == 0) lds_done = __hip_atomic_fetch_add(&a.notes.done[(uint64_t)r * kApart], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      if (lds_done != a.parts - 1) return;
+    }
   }
 
   // The cut within the bin: narrowed by a 256th of the bin, then by 8 bits of the key at a time, until few enough are left to compare all with each other.
   uint64_t last = 0;   // tokens of at least this key are kept
   constexpr int kPer = kMostParts / kThreads;
   double weights[kPer];
-  uint32_t listed[kPer], all_listed = 0;
+  uint32_t listed[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const uint32_t of = tid * kPer + i;
     weights[i] = 0., listed[i] = 0;
-    if (of < a.parts) {
+    if constexpr (WHOLE) {
+      if (of == 0) weights[i] = kept, lds_more[of] = 0;
+    } else if (of < a.parts) {
       weights[i] = __builtin_bit_cast(double, __hip_atomic_load((uint64_t*)&a.notes.kept[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
       if (open) weights[i] *= weight(logit_of_rank((uint32_t)(a.notes.keys[(uint64_t)r * a.parts + of] >> 32)));
       if (cuts) listed[i] = __hip_atomic_load(&a.notes.listed[(uint64_t)r * a.parts + of], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -428,6 +476,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   }
   // (keys in the order of the parts: lds_upto[part] of them up to and with a part)
   auto read_key = [&](uint32_t at) {
+    if constexpr (WHOLE) return __hip_atomic_load(&a.notes.list[(uint64_t)r * a.vocab + at], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     uint32_t low = 0, high = a.parts - 1;
     while (low < high) {
       const uint32_t middle = (low + high) / 2;
@@ -437,7 +486,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     const uint32_t in_part = at - (low ? lds_upto[low - 1] : 0);
     return __hip_atomic_load(&a.notes.list[(uint64_t)r * a.vocab + low * kPart<CHUNKS> + in_part], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   };
-  if (cuts) {
+  if (cuts && !WHOLE) {
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) mine += listed[i];
@@ -622,7 +671,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
 struct Layout {
   uint64_t keys, kept, mass, count, listed, list, done, bytes;   // offsets
   uint32_t parts;
-  bool many;
+  bool whole, many;   // whole: a row is one workgroup's
 };
 
 int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
@@ -635,8 +684,11 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
     l->bytes += (n + 255) / 256 * 256;
     return at;
   };
+  // a row of one workgroup needs no launches ahead, but its weights are all behind each other: 16 rows with filters of 2048 logits 11.0 us in place of 18.7, of 4096 15.4 in place of 19.1, of 8192 24.3 in place of
+  // 19.4; without filters 7.3 in place of 12.8, 9.2 and 12.8, 14.8 and 12.5
+  l->whole = a->vocab <= kPart<4>;
   l->many = (uint64_t)a->rows * ((a->vocab + kPart<kFew> - 1) / kPart<kFew>) > 1024;
-  const uint32_t part = l->many ? kPart<kMany> : kPart<kFew>;
+  const uint32_t part = l->whole ? kPart<4> : l->many ? kPart<kMany> : kPart<kFew>;
   l->parts = (a->vocab + part - 1) / part;
   l->bytes = 0;
   l->keys = place((uint64_t)a->rows * l->parts * 8);
@@ -678,9 +730,13 @@ int sample(const tq_sample_args* a, void* stream) {
       if ((uint64_t)small * a->rows <= 256) hipLaunchKernelGGL(k_sample_bins<2>, dim3(small, a->rows), dim3(kBinThreads), 0, st, v);
       else hipLaunchKernelGGL(k_sample_bins<8>, dim3(large, a->rows), dim3(kBinThreads), 0, st, v);
     }
-    hipLaunchKernelGGL(k_sample_draw<kChunks>, dim3(a->rows, l.parts), dim3(kThreads), 0, st, v);
+    hipLaunchKernelGGL((k_sample_draw<kChunks, false>), dim3(a->rows, l.parts), dim3(kThreads), 0, st, v);
   };
-  if (l.many) go(std::integral_constant<int, kMany>());
+  // (half as many tokens a thread where they are enough: 2048 logits 11.0 us, where 4096 take 15.4)
+  auto whole = [&](auto chunks) { hipLaunchKernelGGL((k_sample_draw<decltype(chunks)::value, true>), dim3(a->rows), dim3(kThreads), 0, st, v); };
+  if (l.whole && a->vocab <= kPart<2>) whole(std::integral_constant<int, 2>());
+  else if (l.whole) whole(std::integral_constant<int, 4>());
+  else if (l.many) go(std::integral_constant<int, kMany>());
   else go(std::integral_constant<int, kFew>());
   return launched("tq_sample");
 }

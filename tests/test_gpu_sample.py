@@ -164,7 +164,7 @@ def test_results_repeat_on_another_stream_with_a_workspace_of_other_calls():
             assert torch.equal(tokens, first[0]) and torch.equal(probs, first[1])
 
 
-@pytest.mark.parametrize("rows,vocab", [(48, 100000), (3, 70001), (300, 9000)])
+@pytest.mark.parametrize("rows,vocab", [(48, 100000), (3, 70001), (300, 9000), (7, 15000)])
 def test_rows_without_filters_beside_others(rows, vocab):
     """Their weights are summed relative to each part's own largest logit: parts of masked tokens, parts far below the others, parts with infinities."""
     inf = float("inf")
@@ -206,6 +206,21 @@ def test_graphs_that_share_a_workspace():
         torch.cuda.synchronize()
         for (_, tokens, probs), want in zip(made, wants):
             assert torch.equal(tokens, want[0]) and torch.equal(probs, want[1])
+
+
+@pytest.mark.parametrize("vocab", [1500, 2047, 2048, 2049, 4095, 4096, 4097, 8191, 12289])
+def test_around_the_sizes_of_parts(vocab):
+    """Rows of one workgroup and of several, more tokens of one bin than LDS has room for, and everything else that rows of a single workgroup have to themselves."""
+    inf, n = float("inf"), len(FILTERS)
+    g = np.random.default_rng(vocab)
+    t, k, p, m = zip(*FILTERS)
+    x = peaked(n, vocab, vocab)
+    check(x, t, k, p, m, g.random(n, dtype=np.float32).tolist())
+    x[:, : vocab - 40] = 1.25                                 # one bin, equal logits: the lowest tokens stay
+    check(x, [1.0] * n, [vocab - 60 + r for r in range(n)], [0.9, 1.0] * (n // 2) + [0.5], None, g.random(n, dtype=np.float32).tolist())
+    x = 1 + 1e-4 * torch.rand((n, vocab), generator=torch.Generator().manual_seed(vocab)).cuda()      # one bin, different ones
+    x[1, ::3], x[2, 5:9], x[3, :-1] = -inf, inf, float("nan")
+    check(x, [0.9] * n, [0, vocab // 2, 3] + [vocab // 3 + r for r in range(n - 3)], [0.7] * n, [0.0, 0.5] * (n // 2) + [0.0], g.random(n, dtype=np.float32).tolist())
 
 
 def test_how_often_tokens_are_drawn():
