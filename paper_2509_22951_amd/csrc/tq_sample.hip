@@ -685,7 +685,7 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
     return at;
   };
   // a row of one workgroup needs no launches ahead, but its weights are all behind each other: 16 rows with filters of 2048 logits 11.0 us in place of 18.7, of 4096 15.4 in place of 19.1, of 8192 24.3 in place of
-  // 19.4; without filters 7.3 in place of 12.8, 9.2 and 12.8, 14.8 and 12.5
+  // 19.4 (with 1024 threads 19.2); without filters 7.3 in place of 12.8, 9.2 and 12.8, 14.8 and 12.5
   l->whole = a->vocab <= kPart<4>;
   l->many = (uint64_t)a->rows * ((a->vocab + kPart<kFew> - 1) / kPart<kFew>) > 1024;
   const uint32_t part = l->whole ? kPart<4> : l->many ? kPart<kMany> : kPart<kFew>;
