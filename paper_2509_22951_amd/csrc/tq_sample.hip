@@ -319,6 +319,9 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   // of 32000 logits; of many, whose reading takes longer than the wait, after that: 64 open rows of 128256 9.5 us in place of 24.)
   constexpr int kBinsPer = kBins / kThreads;
   float v[CHUNKS][4];
+  double w[CHUNKS][4];
+  // (of a whole row neighbouring tokens, so that one sum over the threads is enough in the end)
+  auto token_of = [&](int c, int j) { return WHOLE ? 4 * CHUNKS * tid + 4 * c + j : part * kPart<CHUNKS> + 4 * (c * kThreads + tid) + j; };
   uint32_t count[kBinsPer];
   uint64_t mass[kBinsPer];
   auto ask = [&] {
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   Filter f;
   if constexpr (WHOLE) {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) four_of(row, 4 * (c * kThreads + tid), a.vocab, v[c]);
+    for (int c = 0; c < CHUNKS; ++c) four_of(row, token_of(c, 0), a.vocab, v[c]);
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) lds_bin_count[i * kThreads + tid] = 0, lds_bin_mass[i * kThreads + tid] = 0;
     uint64_t best = 0;
@@ -345,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t i = 4 * (c * kThreads + tid) + j;
+        const uint32_t i = token_of(c, j);
         if (i < a.vocab) best = max(best, key_of(v[c][j], i));
       }
     f = filter_from(asked, a.vocab, largest_of(best, slots));
@@ -363,6 +366,11 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
   const Weigher weight(f.top, f.temperature);
   const double unit = (double)(1ull << a.mass_bits), least = (double)f.least;
   auto mass_of = [&](float l) { return (uint64_t)(weight(l) * unit + 0.5); };
+  if constexpr (WHOLE)
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[c][j] = weight(v[c][j]);
   const bool cuts = f.by_rank || f.by_mass;
   Cut cut{kBins, 0, 0};
   double target = 0.;
@@ -373,8 +381,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t b = bin_of(distance_of(f, v[c][j]));
-          const uint64_t its = mass_of(v[c][j]);
-          if (4 * (c * kThreads + tid) + j >= a.vocab) continue;
+          const uint64_t its = (uint64_t)(w[c][j] * unit + 0.5);
+          if (token_of(c, j) >= a.vocab) continue;
           atomicAdd(&lds_bin_count[b], 1u);
           if (f.by_mass) atomicAdd((unsigned long long*)&lds_bin_mass[b], (unsigned long long)its);
         }
@@ -393,10 +401,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     target = (double)f.p * (double)all;
     cut = find_cut<kBinsPer>(count, mass, 0, 0, f.k, f.by_mass, target, lds_n, lds_m, &lds_cut);
   }
-  auto kept_weight = [&](float l, uint32_t i) {   // of a token that no cut leaves out
-    const double w = weight(l);
-    return ((i == f.first) | !(w < least)) ? w : 0.;
-  };
+  auto if_kept = [&](double w, uint32_t i) { return ((i == f.first) | !(w < least)) ? w : 0.; };   // of a token that no cut leaves out
+  auto kept_weight = [&](float l, uint32_t i) { return if_kept(weight(l), i); };
 
   // this part
   double kept = 0.;   // (of a whole row)
@@ -409,10 +415,11 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
+        const uint32_t i = token_of(c, j);
         const uint32_t b = i >= a.vocab ? kBins + 1 : cuts ? bin_of(distance_of(f, v[c][j])) : 0;
-        const double w = kept_weight(v[c][j], i);   // (beyond the row: none)
-        sum += b < cut.bin ? w : 0.;
+        if constexpr (WHOLE) w[c][j] = if_kept(w[c][j], i);   // (beyond the row: none)
+        else w[c][j] = kept_weight(v[c][j], i);
+        sum += b < cut.bin ? w[c][j] : 0.;
         n += b == cut.bin;
       }
     sum = wave_sum(sum);
@@ -436,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
       for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t i = part_first + 4 * (c * kThreads + tid) + j;
+          const uint32_t i = token_of(c, j);
           if (i < a.vocab && bin_of(distance_of(f, v[c][j])) == cut.bin) {
             if (WHOLE && at < kListed) lds_keys[at] = key_of(v[c][j], i);
             else __hip_atomic_store(&a.notes.list[(uint64_t)r * a.vocab + part_first + at], key_of(v[c][j], i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -603,46 +610,52 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     }
     return before + in_wave;
   };
-  double total;
-  const double upto = upto_of(mine, &total);
-  const double place = (double)a.uniform[r] * total;
-  if (tid == 0) lds_base = ~0u, lds_last = 0, lds_token = ~0u;
-  __syncthreads();
-  {
-    double reached = upto - mine;
-    uint32_t first_of = ~0u, last_of = 0;
+  double total, reached = 0.;
+  uint32_t of = 0;
+  bool beyond = false;   // beyond all: the last token
+  if constexpr (WHOLE) {
+    total = kept + (double)lds_more[0] / unit;
+    if (tid == 0) lds_last = 0, lds_token = ~0u;
+  }
+  const double upto = WHOLE ? 0. : upto_of(mine, &total), place = (double)a.uniform[r] * total;
+  if constexpr (!WHOLE) {
+    if (tid == 0) lds_base = ~0u, lds_last = 0, lds_token = ~0u;
+    __syncthreads();
+    {
+      double upto_here = upto - mine;
+      uint32_t first_of = ~0u, last_of = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const uint32_t of = tid * kPer + i;
-      reached += weights[i];
-      const bool has = of < a.parts && weights[i] > 0.;
-      last_of = has ? of : last_of;
-      first_of = has && reached > place ? min(first_of, of) : first_of;
+      for (int i = 0; i < kPer; ++i) {
+        const uint32_t one = tid * kPer + i;
+        upto_here += weights[i];
+        const bool has = one < a.parts && weights[i] > 0.;
+        last_of = has ? one : last_of;
+        first_of = has && upto_here > place ? min(first_of, one) : first_of;
+      }
+      first_of = wave_least(first_of), last_of = wave_most(last_of);
+      if (lane == 0) atomicMin(&lds_base, first_of), atomicMax(&lds_last, last_of);
     }
-    first_of = wave_least(first_of), last_of = wave_most(last_of);
-    if (lane == 0) atomicMin(&lds_base, first_of), atomicMax(&lds_last, last_of);
+    __syncthreads();
+    of = lds_base != ~0u ? lds_base : lds_last, beyond = lds_base == ~0u;
+    if (tid == of / kPer) {
+      double before = upto - mine;
+      for (int i = 0; i < kPer; ++i)
+        if ((uint32_t)(tid * kPer + i) < of) before += weights[i];
+      lds_share = before;
+    }
+    __syncthreads();
+    reached = lds_share;
   }
-  __syncthreads();
-  const uint32_t of = lds_base != ~0u ? lds_base : lds_last;
-  const bool beyond = lds_base == ~0u;   // beyond all: the last token
-  if (tid == of / kPer) {
-    double before = upto - mine;
-    for (int i = 0; i < kPer; ++i)
-      if ((uint32_t)(tid * kPer + i) < of) before += weights[i];
-    lds_share = before;
-  }
-  __syncthreads();
-  double reached = lds_share;
-  // (a thread takes neighbouring tokens here, so that one sum over the threads is enough; from the caches)
+  // (a thread takes neighbouring tokens here; from the caches, unless it has them)
   const uint32_t at0 = of * kPart<CHUNKS> + 4 * CHUNKS * tid;
-  double w[CHUNKS][4], own = 0.;
+  double own = 0.;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
-    four_of(row, at0 + 4 * c, a.vocab, v[c]);
+    if constexpr (!WHOLE) four_of(row, at0 + 4 * c, a.vocab, v[c]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t i = at0 + 4 * c + j;
-      const double one = kept_weight(v[c][j], i);
+      const double one = WHOLE ? w[c][j] : kept_weight(v[c][j], i);
       w[c][j] = ((i < a.vocab) & (key_of(v[c][j], i) >= last)) ? one : 0.;
       own += w[c][j];
     }
