@@ -697,8 +697,8 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
     l->bytes += (n + 255) / 256 * 256;
     return at;
   };
-  // a row of one workgroup needs no launches ahead, but its weights are all behind each other: 16 rows with filters of 2048 logits 11.0 us in place of 18.7, of 4096 15.4 in place of 19.1, of 8192 24.3 in place of
-  // 19.4 (with 1024 threads 19.2); without filters 7.3 in place of 12.8, 9.2 and 12.8, 14.8 and 12.5
+  // a row of one workgroup needs no launches ahead, but its weights are all behind each other: 16 rows with filters of 2048 logits 9.1 us in place of 18.7, of 4096 12.4 in place of 19.1, of 8192 19.7 in place of
+  // 19.4; without filters 6.4 in place of 12.8, 7.1 and 12.8, 11.6 and 12.5; 1024 rows of 8192, whose threads need too many registers, 76 and 67, without filters 44 and 32
   l->whole = a->vocab <= kPart<4>;
   l->many = (uint64_t)a->rows * ((a->vocab + kPart<kFew> - 1) / kPart<kFew>) > 1024;
   const uint32_t part = l->whole ? kPart<4> : l->many ? kPart<kMany> : kPart<kFew>;
@@ -745,7 +745,7 @@ int sample(const tq_sample_args* a, void* stream) {
     }
     hipLaunchKernelGGL((k_sample_draw<kChunks, false>), dim3(a->rows, l.parts), dim3(kThreads), 0, st, v);
   };
-  // (half as many tokens a thread where they are enough: 2048 logits 11.0 us, where 4096 take 15.4)
+  // (half as many tokens a thread where they are enough: 2048 logits 9.1 us, where 4096 take 12.4)
   auto whole = [&](auto chunks) { hipLaunchKernelGGL((k_sample_draw<decltype(chunks)::value, true>), dim3(a->rows), dim3(kThreads), 0, st, v); };
   if (l.whole && a->vocab <= kPart<2>) whole(std::integral_constant<int, 2>());
   else if (l.whole) whole(std::integral_constant<int, 4>());
