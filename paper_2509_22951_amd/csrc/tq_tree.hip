@@ -7,9 +7,10 @@
 //   out^T [dim][column] = V^T [dim][token] P^T: the lane that got the logits of tokens 4g..4g+3 of both 16-token blocks (g = l / 16) supplies the same tokens as its 8
 //   values of the contraction, so P is already where it is needed; V is transposed on its way out of LDS.
 // bf16: q (if fp32) and the weights enter as three bf16 parts each, all of fp32's 24 bits.  8 bits: q as a whole number of 24 bits, in units of a row's largest value / (127 * 2^16),
-// whose three digits of 8 bits meet the keys in integer products, which are exact; values become f16 in registers, which is exact too, and meet weights (times the
-// values' scales) of two f16 parts, 22 bits.  (q loses up to 2^-24 of its largest value in every dim: over 256 dims that is 2^-8 of what
-// the rounding of a key to 8 bits in the one dim of that value can be.)
+// whose three digits of 8 bits meet the keys in integer products, which are exact; values become bf16 in registers, which is exact too, and meet weights (times the
+// values' scales) of three bf16 parts.  (q loses up to 2^-24 of its largest value in every dim: over 256 dims that is 2^-8 of what
+// the rounding of a key to 8 bits in the one dim of that value can be.  Weights are never brought to one exponent like that: in a dim where the tokens
+// of the largest ones have values of zero, the small ones are all there is.)
 #include <algorithm>
 
 #include "tq_cache_view.h"
@@ -68,17 +69,7 @@ __device__ __forceinline__ void write_out(A& a, uint32_t size, uint32_t t, uint3
   *(u32x2_any*)to = u32x2_any{lo, hi};
 }
 
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-// Four int8 levels as f16: the bits of 1024 + (level + 128), less 1152.
-__device__ __forceinline__ uint2 levels_to_f16(uint32_t four) {
-  const uint32_t u = four ^ 0x80808080u;
-  const f16x2 less = {(_Float16)-1152.f, (_Float16)-1152.f};
-  const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + less, hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + less;
-  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-}
 
 template <int DIM, bool INT8>
 struct Shape {
@@ -126,8 +117,8 @@ __device__ __forceinline__ uint32_t rounded(uint32_t units, const Cutting& cut) 
 
 // Bound: reading the cache while there are few columns, the matrix and vector units from two or three column tiles on.  24 heads on 8, 128 dims, bf16, 16 x 16384 tokens (171 us at the
 // 6.3 TB/s of a read stream): 5 nodes, one tile, 201 us, 5.3 TB/s; 16 nodes, three, 255; 20 nodes, four, 287.  1 x 131000 tokens, 64 nodes, 12 tiles: 291 us, with q in bf16 229: three parts
-// of q and three of the weights are 6 products where 2 would be the least; the matrix units are busy 59 % of the time.  16 x 32700 tokens in 8 bits (176 us): 5 nodes 238, 16 nodes 364:
-// vector instructions are issued 82 % of the time, of which values' widening is a quarter.
+// of q and three of the weights are 6 products where 2 would be the least; the matrix units are busy 59 % of the time.  16 x 32700 tokens in 8 bits (176 us): 5 nodes 237, 16 nodes 365..371
+// (weights of two f16 parts, at one exponent for all of a column's: 236, 351; what is 2^-37 of the largest then begins to be lost).
 //
 // Why so: 12 wavefronts, because of the 168 registers that leaves each (8 of them with everything in registers and no LDS: 80 us for the ragged batch, 368, 462; 4 with three column tiles each and
 // 512 registers: 131, 420, 813; the sums' copies between the two halves of the register file cost more than the reads that were saved).  Two stages of 64 KB: what is on its way
@@ -136,16 +127,11 @@ __device__ __forceinline__ uint32_t rounded(uint32_t units, const Cutting& cut) 
 template <int DIM, bool INT8, bool Q16>
 __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
-  constexpr int kParts = Q16 && !INT8 ? 1 : 3, kWeightParts = INT8 ? 2 : 3;
+  constexpr int kParts = Q16 && !INT8 ? 1 : 3;
   typedef std::conditional_t<INT8, i32x4, bf16x8> key8;      // what a lane supplies of a row of keys or q
   typedef std::conditional_t<INT8, i32x4, f32x4> logits4;
-  typedef std::conditional_t<INT8, f16x8, bf16x8> value8;
   auto multiply_keys = [](key8 of_rows, key8 of_columns, logits4 sum) __attribute__((always_inline)) {
     if constexpr (INT8) return __builtin_amdgcn_mfma_i32_16x16x64_i8(of_rows, of_columns, sum, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(of_rows, of_columns, sum, 0, 0, 0);
-  };
-  auto multiply_values = [](value8 of_rows, value8 of_columns, f32x4 sum) __attribute__((always_inline)) {
-    if constexpr (INT8) return __builtin_amdgcn_mfma_f32_16x16x32_f16(of_rows, of_columns, sum, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(of_rows, of_columns, sum, 0, 0, 0);
   };
   constexpr uint32_t kT = S::kTokens, kBytes = kT * S::kRow, kAll = 64, kNobody = 65;
@@ -402,10 +388,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
 
   f32x4 o[S::kBlocks];
   float top = -INFINITY, total = 0.f;
-  // 8 bits: weights times their values' scales are two f16 parts each, 22 bits, and are multiplied by 2^raised for that: by as much as keeps a column's below 2^15.  So are the sums.
-  constexpr int kRaised = 126;
-  constexpr float kMostWeight = 32768.f, kMostScale = 0x1p80f;   // (sums of levels and digits are below 2^39)
-  int raised = kRaised;
+  constexpr float kMostScale = 0x1p80f;   // of an 8-bit key (sums of levels and digits are below 2^39)
   auto take_tile = [&](auto buffer, uint32_t tile, bool some) __attribute__((always_inline)) {
     constexpr int kBuffer = decltype(buffer)::value;
     const char* keys = stage(buffer) + tile * kTile * S::kRow;
@@ -456,23 +439,19 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
     const uint32_t value_row = INT8 ? 4 * g + n / 2 % 4 + n / 8 * 16 : 4 * g + n / 4;
     const uint32_t value_at0 = value_row * S::kRow + S::value_swizzle(value_row) * 16 + (INT8 ? n % 2 : n % 4) * 8;
-    std::conditional_t<INT8, i32x2, value8> asked[S::kBlocks];
+    std::conditional_t<INT8, i32x2, bf16x8> asked[S::kBlocks];
     auto ask = [&](int b) __attribute__((always_inline)) {
       const char* from = values + (value_at0 ^ (b * 16 * S::kSize));
       if constexpr (INT8) {
         asked[b] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)from);
       } else {
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 16 * S::kRow));
-        asked[b] = __builtin_bit_cast(value8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        asked[b] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       }
     };
     auto value_of = [&](int b) __attribute__((always_inline)) {
-      if constexpr (INT8) {
-        const uint2 lo = levels_to_f16((uint32_t)asked[b][0]), hi = levels_to_f16((uint32_t)asked[b][1]);
-        return __builtin_bit_cast(value8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-      } else {
-        return asked[b];
-      }
+      if constexpr (INT8) return i8x8_to_bf16x8(make_uint2((uint32_t)asked[b][0], (uint32_t)asked[b][1]));
+      else return asked[b];
     };
     constexpr int kEarly = INT8 ? 4 : 2;
 #pragma unroll
@@ -519,53 +498,27 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       m = fmaxf(m, top);
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
-      const float lower = top - (m == -INFINITY ? 0.f : m);
-      float shrink = __builtin_amdgcn_exp2f(lower);
+      const float shrink = __builtin_amdgcn_exp2f(top - (m == -INFINITY ? 0.f : m));
       top = m, total *= shrink;
-      if constexpr (INT8) {   // the sums are left about as they are, as far as that goes
-        const float more = fminf(floorf(-lower), (float)(kRaised - raised));
-        raised += (int)more, shrink = __builtin_amdgcn_exp2f(lower + more);
-      }
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) o[b] *= shrink;
     }
     const float base = top == -INFINITY ? 0.f : top;
-    float w[8], most_weight = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], scale, -base));
-      total += w[i];
-      if constexpr (INT8) w[i] *= (&vs[i / 4].x)[i % 4], most_weight = fmaxf(most_weight, fabsf(w[i]));
-    }
-    if constexpr (INT8) {
-      if (__any(most_weight * ldexpf(1.f, raised) > kMostWeight)) {
-        most_weight = fmaxf(most_weight, __shfl_xor(most_weight, 16));
-        most_weight = fmaxf(most_weight, __shfl_xor(most_weight, 32));
-        // to 2^12 .. 2^13 (what is infinite stays so)
-        const int to = most_weight * ldexpf(1.f, raised) > kMostWeight ? max(12 - (most_weight < INFINITY ? ilogbf(most_weight) : 128), -kRaised) : raised;
-        const float shrink = ldexpf(1.f, to - raised);
-        raised = to;
-#pragma unroll
-        for (int b = 0; b < S::kBlocks; ++b) o[b] *= shrink;
-      }
-      const float up = ldexpf(1.f, raised);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] *= up;
-    }
-    uint32_t part[kWeightParts][4];
+    uint32_t part[3][4];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
+      float w[2];
 #pragma unroll
-      for (int k = 0; k < kWeightParts; ++k) {
-        if constexpr (INT8) {   // 11 bits, the next 11
-          const f16x2 two = {(_Float16)w[i], (_Float16)w[i + 1]};
-          part[k][i / 2] = __builtin_bit_cast(uint32_t, two);
-          w[i] -= (float)two[0], w[i + 1] -= (float)two[1];
-        } else {   // the upper 8 bits of the mantissas, the next 8, the last 8
-          const uint32_t lo = __float_as_uint(w[i]), hi = __float_as_uint(w[i + 1]);
-          part[k][i / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-          w[i] -= __uint_as_float(lo & 0xFFFF0000u), w[i + 1] -= __uint_as_float(hi & 0xFFFF0000u);
-        }
+      for (int j = 0; j < 2; ++j) {
+        w[j] = __builtin_amdgcn_exp2f(fmaf(p[i + j], scale, -base));
+        total += w[j];
+        if constexpr (INT8) w[j] *= (&vs[i / 4].x)[i % 4 + j];
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {   // the upper 8 bits of the mantissas, the next 8, the last 8
+        const uint32_t lo = __float_as_uint(w[0]), hi = __float_as_uint(w[1]);
+        part[k][i / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+        w[0] -= __uint_as_float(lo & 0xFFFF0000u), w[1] -= __uint_as_float(hi & 0xFFFF0000u);
       }
     }
 #pragma unroll
@@ -573,14 +526,14 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
       if (first)
 #pragma unroll
         for (int b = 0; b < kEarly; ++b) ask(first + b);
-      value8 value[kEarly];
+      bf16x8 value[kEarly];
 #pragma unroll
       for (int b = 0; b < kEarly; ++b) value[b] = value_of(first + b);
 #pragma unroll
-      for (int k = 0; k < kWeightParts; ++k)
+      for (int k = 0; k < 3; ++k)
 #pragma unroll
         for (int b = 0; b < kEarly; ++b)
-          o[first + b] = multiply_values(value[b], __builtin_bit_cast(value8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), o[first + b]);
+          o[first + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[b], __builtin_bit_cast(bf16x8, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), o[first + b], 0, 0, 0);
     }
   };
 
@@ -666,11 +619,6 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     const uint32_t tid = anew(threadIdx.x), lane = tid & 63, g = lane / 16, n = lane % 16;
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
-    if constexpr (INT8) {
-      const float down = ldexpf(1.f, -raised);
-#pragma unroll
-      for (int b = 0; b < S::kBlocks; ++b) o[b] *= down;
-    }
     if (tid == 0) lds_odd = 0;
     if (tid < S::kWaves * 16) lds_odd_column[tid] = 0;
     __syncthreads();   // everyone is done with the stage
@@ -753,7 +701,7 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
   };
   auto step = [&](auto buffer, auto other) __attribute__((always_inline)) {
     if (now.unit == 0) {
-      top = -INFINITY, total = 0.f, raised = kRaised;
+      top = -INFINITY, total = 0.f;
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }

@@ -346,6 +346,36 @@ def test_values_scales_of_any_size(order, dim):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("far", [1, 650])
+@pytest.mark.parametrize("larger,gap", [(1.0, 0.36), (2.0 ** 13, 0.36), (2.0 ** 26, 0.36), (2.0 ** 34, 0.36), (2.0 ** 40, 0.36), (2.0 ** 100, 0.36), (1.0, 10.0), (1.0, 20.0), (1.0, 25.0), (1.0, 60.0),
+                                        (2.0 ** 30, 40.0)])
+def test_a_small_weight_where_the_larger_one_has_a_value_of_zero(larger, gap, far, dim, kind):
+    """Two tokens, in one tile or in two wavefronts' shares.  The first has the larger weight times scale, and zeros in every other dim: what the second gives there is as good as anywhere, 2^-14 of it.
+
+    Its logit, -gap, is off by six roundings to 24 bits: with a gap of 60, 87 in units of log 2, 2^7 * 6 * 2^-24 < 2^-14."""
+    nodes, heads = 3, 2
+    p = Paged(1, 44, kv_heads=1, dim=dim, kind=kind)
+    q = torch.zeros((1, nodes, heads, dim), device="cuda")
+    q[..., 0] = 1.0
+    p.k.zero_(), p.v.zero_()
+    p.k[..., 0] = -1 if kind == "int8" else -300.0     # the other tokens: a weight of e^-300, which is zero
+    if kind == "int8":
+        p.k_scale.fill_(300.0), p.v_scale.fill_(1.0)
+    first = torch.tensor([127.0, 0.0] * (dim // 2))
+    for slot, logit, size, values in ((0, 0.0, larger, first), (far, -gap, 1.0, torch.full((dim,), 101.0))):
+        page, at = int(p.tables[0, slot // 16]), slot % 16
+        if kind == "int8":
+            p.k[page, 0, at, 0], p.k_scale[page, 0, at] = -1 if logit else 0, gap
+            p.v[page, 0, at], p.v_scale[page, 0, at] = values.to(torch.int8).cuda(), size
+        else:
+            p.k[page, 0, at, 0], p.v[page, 0, at] = logit, (values * size).to(torch.bfloat16).cuda()
+    lengths, bits = ints([far + 1]), [[0] * nodes]
+    out, want = run(p, q, lengths, bits, scale=1.0).cpu().double(), tree_reference(p, q, lengths, bits, scale=1.0)
+    assert (want[..., 1::2] > 0).all() and ((out - want).abs() <= want * (2.0 ** -8 + 2.0 ** -14)).all()      # (no value is negative: the terms add up to the result)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_logits_that_rise_from_token_to_token(kind, dim):
     """The largest so far grows over and over, by 1 a token, in 8 bits with values' scales that fall as the weights rise."""
