@@ -557,7 +557,8 @@ int tq_attend_tree_workspace(const tq_cache *cache, const tq_tree_args *args, ui
  *   path: device, int32 [trees][nodes]: the accepted nodes, rising, -1 behind them.  accepted: device, int32 [trees]: how many.
  *   next: device, int32 [trees]: the token drawn at the last of them (-1 for a tree without nodes), the next tree's node 0.
  *   lengths_out: device, int32 [trees]: lengths[t] + accepted[t].  Not lengths itself; the outputs do not overlap each other or the inputs.
- * caches: host array of n (0..4096) caches that hold these sequences, the layers of a model, none of them twice.  In each of them the accepted nodes' keys, values, scales, scores and positions
+ * caches: host array of n (0..4096) caches that hold these sequences, the layers of a model, none of them twice, and with nothing in common but scores and
+ * positions, which move with the first cache that has them.  In each of them the accepted nodes' keys, values, scales, scores and positions
  * move to the slots lengths[t] + 0, 1, ..., in order; what lay in the slots behind them is not used any more and may be anything.  Nothing is moved
  * into or out of a slot beyond a cache's capacity, a page that is not there or a sequence that is not there.  n = 0: only the branches.
  */

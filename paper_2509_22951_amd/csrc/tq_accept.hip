@@ -129,6 +129,14 @@ int tree_accept(uint32_t n, const tq_cache* const* caches, const tq_accept_args*
     if (!aligned_to(p, 4)) return refuse(TQ_E_INVALID_ARG, who + ": a pointer is not aligned to its type");
   if (a->lengths_out == a->lengths) return refuse(TQ_E_INVALID_ARG, who + ": lengths_out is lengths, which other workgroups read");
   AcceptView v{a->masks, a->sizes, a->seqs, a->lengths, a->drafted, a->sampled, a->path, a->accepted, a->next, a->lengths_out, a->trees, a->nodes, 1};
+  // Scores or positions that several layers share move once, with the first of these: a move in place reads slots that a second one would find moved.
+  std::vector<const void*> moving;
+  auto first_of = [&](auto*& marks) {
+    if (!marks) return;
+    const auto at = std::lower_bound(moving.begin(), moving.end(), (const void*)marks);
+    if (at != moving.end() && *at == marks) marks = nullptr;
+    else moving.insert(at, marks);
+  };
   uint32_t done = 0;
   do {
     CacheList list{};
@@ -136,6 +144,7 @@ int tree_accept(uint32_t n, const tq_cache* const* caches, const tq_accept_args*
     uint32_t groups = 1;
     for (uint32_t i = 0; i < now; ++i) {
       if (int rc = view_cache(who, caches[done + i], &list.of[i])) return rc;
+      first_of(list.of[i].scores), first_of(list.of[i].positions);
       const bool int8 = caches[done + i]->type == TQ_INT8;
       list.int8 |= (uint32_t)int8 << i;
       const uint64_t pieces = 2ull * list.of[i].kv_heads * ((int8 ? 1 : 2) * list.of[i].head_dim / 16 + 2);

@@ -128,6 +128,28 @@ def test_layers_of_different_shapes_more_than_a_launch_takes():
     check(ps, random_parents(2, 16, 1), [20, 40], likely=1.0)
 
 
+@pytest.mark.parametrize("layers", [2, 7, 40])
+@pytest.mark.parametrize("shared", [("positions",), ("scores",), ("scores", "positions")])
+def test_layers_that_share_scores_or_positions(layers, shared):
+    """Without eviction the positions of all layers are alike, and one array holds them: it moves once."""
+    ps = [Paged(2, 8, kind=("bf16", "int8")[n % 2], marks=True, seed=n) for n in range(layers)]
+    for p in ps[1:]:
+        for name in shared:
+            setattr(p, name, getattr(ps[0], name))
+    nodes = [[-1, 0, 0] + [i - 2 for i in range(3, 64)]] * 2         # two chains in turn: a slot that is read is written, too
+    drafted = [[100 + i for i in range(64)]] * 2
+    drawn = [[drafted[0][2]] + [drafted[0][i + 2] if i + 2 < 64 else 5 for i in range(1, 64)]] * 2
+    lengths, before = ints([5, 30]), [everything(p) for p in ps]
+    made, *_ = accept([p.describe() for p in ps], bits_of(nodes), drafted, drawn, lengths)
+    made.launch(stream())
+    torch.cuda.synchronize()
+    branch = [0] + list(range(2, 64, 2))
+    for p, was in zip(ps, before):
+        want, got = moved(p, was, [(branch, 5)] * 2, lengths, None), everything(p)
+        for n in want:
+            assert torch.equal(got[n], want[n]), n
+
+
 def test_without_caches():
     check([], random_parents(200, 16, 2), [7] * 200, seed=3)
 
