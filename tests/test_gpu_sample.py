@@ -223,6 +223,37 @@ def test_around_the_sizes_of_parts(vocab):
     check(x, [0.9] * n, [0, vocab // 2, 3] + [vocab // 3 + r for r in range(n - 3)], [0.7] * n, [0.0, 0.5] * (n // 2) + [0.0], g.random(n, dtype=np.float32).tolist())
 
 
+@pytest.mark.parametrize("vocab", [700, 2500, 4096, 30000, 128256])
+@pytest.mark.parametrize("mask", [float("-inf"), float("nan"), torch.finfo(torch.float32).min, -1e4])
+def test_most_of_a_vocabulary_masked(vocab, mask):
+    """Ten tokens that are not: fewer than, as many as and more than top_k asks for, with the other filters."""
+    n, g = 12, np.random.default_rng(vocab)
+    x = torch.full((n, vocab), mask, device="cuda")
+    at = torch.stack([torch.randperm(vocab, generator=torch.Generator().manual_seed(r))[:10] for r in range(n)]).cuda()
+    x.scatter_(1, at, peaked(n, 10, vocab))
+    x[1, 5:], x[2] = mask, mask                       # (fewer still; none but, perhaps, a mask that is a number)
+    k = [50, 50, 50, 9, 10, 11, 0, 50, vocab - 1, 50, 0, 3]
+    p = [1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 0.9, 0.9, 0.999, 1.0, 0.9999999, 0.5]
+    m = [0.0] * 9 + [0.05, 0.0, 0.01]
+    check(x, [0.8] * n, k, p, m, g.random(n, dtype=np.float32).tolist())
+    check(x, [0.8] * n, k, None, m, [float(np.nextafter(np.float32(1), np.float32(0)))] * n)
+    check(x, [0.8] * n, None, p, m, [0.0] * n)
+
+
+@pytest.mark.parametrize("k,p", [(50, 1.0), (50, 0.9), (0, 0.95)])
+def test_masked_tokens_are_not_listed(k, p):
+    """Eight bytes a token that a cut could leave out or not: a cut beyond all tokens that have any weight lists none of the others, whose order nobody needs."""
+    vocab = 128256
+    x = torch.full((1, vocab), float("-inf"), device="cuda")
+    x[0, 1000:1010] = peaked(1, 10, 1)[0]
+    made, tokens, _ = call(x, [0.8], [k], [p], None, [0.4])
+    made.launch(stream())
+    torch.cuda.synchronize()
+    assert 1000 <= int(tokens[0]) < 1010
+    written = int((made.keep[-1] != 0xEE).sum())
+    assert written < 2 * vocab, written                # (bins and what the parts leave each other: some 30000 bytes)
+
+
 def test_how_often_tokens_are_drawn():
     """4096 evenly spaced numbers: every token is drawn as often as its share says, give or take the two ends."""
     x = torch.tensor([2.0, 1.0, 0.0, -1.0, 1.5, -30.0], device="cuda")
