@@ -699,8 +699,8 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
   if (a->rows > 65535) return refuse(TQ_E_UNSUPPORTED, who + ": more than 65535 rows");
   if (a->logits_stride && a->logits_stride < a->vocab) return refuse(TQ_E_INVALID_ARG, who + ": logits_stride is smaller than a row");
   auto place = [&](uint64_t n) {
-    const uint64_t at = l->bytes;
-    l->bytes += (n + 255) / 256 * 256;
+    const uint64_t at = (l->bytes + 255) / 256 * 256;
+    l->bytes = at + n;
     return at;
   };
   // a row of one workgroup needs no launches ahead, but its weights are all behind each other: 16 rows with filters of 2048 logits 9.1 us in place of 18.7, of 4096 12.4 in place of 19.1, of 8192 19.7 in place of
@@ -709,14 +709,20 @@ int check_sample(const std::string& who, const tq_sample_args* a, Layout* l) {
   l->many = (uint64_t)a->rows * ((a->vocab + kPart<kFew> - 1) / kPart<kFew>) > 1024;
   const uint32_t part = l->whole ? kPart<4> : l->many ? kPart<kMany> : kPart<kFew>;
   l->parts = (a->vocab + part - 1) / part;
-  l->bytes = 0;
+  l->bytes = 16;   // (a workspace is there in any case)
+  const bool lists = a->top_k || a->top_p;
+  if (l->whole) {
+    // (a row of one workgroup leaves itself nothing but the keys that LDS has no room for)
+    if (lists && a->vocab > kListed) l->list = place((uint64_t)a->rows * a->vocab * 8);
+    return TQ_OK;
+  }
   l->keys = place((uint64_t)a->rows * l->parts * 8);
   l->kept = place((uint64_t)a->rows * l->parts * 8);
   l->mass = place((uint64_t)a->rows * kBins * 8);
   l->count = place((uint64_t)a->rows * kBins * 4);
   l->listed = place((uint64_t)a->rows * l->parts * 4);
   l->done = place((uint64_t)a->rows * kApart * 4);
-  l->list = place((uint64_t)a->rows * a->vocab * 8);
+  if (lists) l->list = place((uint64_t)a->rows * a->vocab * 8);
   return TQ_OK;
 }
 

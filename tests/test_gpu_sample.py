@@ -254,6 +254,23 @@ def test_masked_tokens_are_not_listed(k, p):
     assert written < 2 * vocab, written                # (bins and what the parts leave each other: some 30000 bytes)
 
 
+@pytest.mark.parametrize("vocab", [100, 2048, 2049, 4096, 4097, 30000, 70001])
+@pytest.mark.parametrize("filters", ["all", "top_k", "top_p", "none"])
+def test_nothing_is_written_behind_the_room_that_is_asked_for(vocab, filters):
+    """Equal logits: as many keys are listed as there can be."""
+    rows = 3
+    k, p = ([vocab // 2] * rows if filters in ("all", "top_k") else None), ([0.5] * rows if filters in ("all", "top_p") else None)
+    x = torch.zeros((rows, vocab), device="cuda")
+    made, _, _ = call(x, [1.0] * rows, k, p, [0.5] * rows, [0.4] * rows)
+    need = made.keep[-1].numel()
+    room = torch.full((need + (1 << 22),), 0xEE, dtype=torch.uint8, device="cuda")
+    made.args.workspace = ptr(room)
+    made.launch(stream())
+    torch.cuda.synchronize()
+    assert (room[need:] == 0xEE).all()
+    check(x, [1.0] * rows, k, p, [0.5] * rows, [0.4] * rows, workspace=room[:need])
+
+
 def test_how_often_tokens_are_drawn():
     """4096 evenly spaced numbers: every token is drawn as often as its share says, give or take the two ends."""
     x = torch.tensor([2.0, 1.0, 0.0, -1.0, 1.5, -30.0], device="cuda")

@@ -92,3 +92,16 @@ def test_null_structures_no_work_and_the_workspaces():
     assert "needed" in refused(INVALID, lambda: tq.AttendTree(c, **{**TREE, "workspace_bytes": need - 1}).launch())
     need = tq.Sample.workspace_bytes(**SAMPLE)
     assert "needed" in refused(INVALID, lambda: tq.Sample(**{**SAMPLE, "workspace_bytes": need - 1}).launch())
+
+
+def test_drawing_asks_for_no_more_room_than_it_uses():
+    """Lists of keys, 8 bytes a logit, only where something can be cut off and LDS may be too small; of rows that one workgroup draws from nothing else."""
+    def need(rows, vocab, **more):
+        return tq.Sample.workspace_bytes(**{**SAMPLE, "rows": rows, "vocab": vocab, **more})
+
+    filters = dict(top_k=A, top_p=A)
+    assert need(65535, 100, **filters) <= 256 and need(65535, 2048, **filters) <= 256 and need(65535, 4096) <= 256
+    for only in (dict(top_k=A), dict(top_p=A), filters):
+        assert 8 * 1000 * 2049 <= need(1000, 2049, **only) <= 8 * 1000 * 2049 + 512 and 8 * 64 * 128256 <= need(64, 128256, **only) <= 8 * 64 * (128256 + 4096)
+    assert need(64, 128256, temperature=A, min_p=A) <= 8 * 64 * 4096
+    assert need(1, 1) >= 16 and need(0, 128256) >= 16 and all(need(r + 1, v, **filters) >= need(r, v, **filters) for r in (1, 7) for v in (100, 4096, 4097, 1 << 20))
