@@ -271,6 +271,18 @@ def test_nothing_is_written_behind_the_room_that_is_asked_for(vocab, filters):
     check(x, [1.0] * rows, k, p, [0.5] * rows, [0.4] * rows, workspace=room[:need])
 
 
+@pytest.mark.parametrize("rows,vocab", [(1, 1 << 20), (2, (1 << 20) - 1), (5, 1 << 20), (13, 1000003), (2, 600000)])
+def test_the_largest_vocabularies(rows, vocab):
+    """Up to 512 parts a row, two to a thread of the workgroup that draws; numbers that fall into the first ones, the middle and the last."""
+    f = [FILTERS[r % len(FILTERS)] for r in range(rows)]
+    t, k, p, m = zip(*f)
+    u = np.linspace(0.02, 0.999, rows, dtype=np.float32).tolist()
+    x = peaked(rows, vocab, vocab)
+    check(x, t, k, p, m, u)
+    check(x, None, None, None, None, u[::-1])
+    check(x, [1.2] * rows, [60000] * rows, [0.97] * rows, [1e-4] * rows, u)
+
+
 def test_how_often_tokens_are_drawn():
     """4096 evenly spaced numbers: every token is drawn as often as its share says, give or take the two ends."""
     x = torch.tensor([2.0, 1.0, 0.0, -1.0, 1.5, -30.0], device="cuda")

@@ -244,6 +244,34 @@ def test_how_trees_are_cut(trees, longest, nodes, heads, kv_heads, dim, kind):
         assert torch.equal(*got)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("trees,longest,nodes,heads,kv_heads,dim", [(70, 810, 5, 10, 5, 64), (131, 500, 3, 5, 5, 128), (200, 510, 4, 7, 7, 64), (67, 630, 17, 9, 3, 256)])
+def test_more_trees_than_a_wavefront_has_lanes(trees, longest, nodes, heads, kv_heads, dim, kind):
+    """Trees are looked at 64 at a time.  Sequences of several stages, and shares that begin in one 64 and end in the next, with parts that are joined behind them."""
+    p = Paged(trees, -(-(longest + nodes) // 16), kv_heads=kv_heads, dim=dim, kind=kind, seed=trees)
+    q = queries(trees, nodes, heads, dim, longest)
+    bits = bits_of(random_parents(trees, nodes, dim))
+    crossed = 0
+    for n in ([longest] * trees, [(r * 619 + 5) % (longest + 1) for r in range(trees)], [longest if r % 64 in (0, 63) else r * 37 % 150 for r in range(trees)]):
+        tokens = 32768 // (dim * (1 if kind == "int8" else 2))
+        units = [max(1, -(-(length + nodes) // tokens)) for length in n]
+        share = -(-sum(units) * kv_heads // 256)
+        assert max(units) > 1 and share > 1
+        crossed += bool(sum(units[:64]) * kv_heads % share or (trees > 128 and sum(units[:128]) * kv_heads % share))
+        lengths = ints(n)
+        call, out = tree_call(p.describe(), q, lengths, masks_of(bits))
+        want = tree_reference(p, q, lengths, bits)
+        got = []
+        for _ in range(2):
+            out.fill_(float("nan"))
+            call.launch(stream())
+            torch.cuda.synchronize()
+            close(out, want, p)
+            got.append(out.clone())
+        assert torch.equal(*got)
+    assert crossed      # (what the cut is made from: without a share across tree 64 or 128 this would show less)
+
+
 def test_every_token_counts_once():
     """One token has nearly all of the weight, in turn at edges of tiles and of shares: left out or taken twice, the result would be another."""
     n, nodes, dim = 2600, 5, 64
