@@ -261,6 +261,9 @@ def main():
     numbers = torch.Generator(device="cuda").manual_seed(0)
     if tree:
         texts, steps = [[i] for i in range(a.batch)], 0
+        dec.draft(torch.zeros((a.batch, a.draft), dtype=torch.int32), graph=True)      # captured, and forgotten
+        dec.lengths.zero_()
+        torch.cuda.synchronize()
         began = time.perf_counter()
         while min(len(t) for t in texts) <= a.tokens and int(dec.lengths.max()) + a.draft <= dec.context:
             dec.uniform.uniform_(generator=numbers)

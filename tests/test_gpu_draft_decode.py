@@ -6,6 +6,8 @@ the logits, taken as a 2-norm.  (An 8-bit cache rounds about as bf16 does; head 
 the decoder itself has."""
 import os
 import sys
+import time
+import types
 
 import numpy as np
 import pytest
@@ -13,6 +15,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+import decode
 from decode import Decoder, guesses, two_chains
 from drafts import sample_reference
 from test_gpu_decode import Plain
@@ -130,3 +133,21 @@ def test_guesses_are_what_came_behind_earlier_occurrences():
     assert guesses([7, 1, 2, 3, 7, 4, 5, 6, 9, 7], tree) == [7, 4, 5, 6, 9, 1, 2, 3]
     assert guesses([1, 2, 3], tree) == [3] + [-1] * 7
     assert guesses([5, 5], tree) == [5, 5, -1, -1, -1, -1, -1, -1]
+
+
+def test_the_clock_starts_behind_the_capture(monkeypatch, capsys):
+    """The program's steps are replays, as it says of the ones that it times; what it draws begins at the beginning."""
+    happened, launch = [], Decoder._launch
+
+    def recorded(self, graph):
+        happened.append(("step", self.graph is not None, int(self.lengths.max())))
+        return launch(self, graph)
+
+    monkeypatch.setattr(Decoder, "_launch", recorded)
+    monkeypatch.setattr(decode, "time", types.SimpleNamespace(perf_counter=lambda: happened.append(("clock",)) or time.perf_counter()))
+    monkeypatch.setattr(sys, "argv", "decode.py --layers 1 --hidden 128 --heads 4 --kv-heads 2 --inter 256 --vocab 500 --batch 2 --tokens 12 --draft 6".split())
+    decode.main()
+    began, ended = (i for i, what in enumerate(happened) if what[0] == "clock")
+    timed = happened[began + 1:ended]
+    assert began == 1 and len(timed) >= 1 and all(what[1] for what in timed) and timed[0][2] == 0
+    assert f"{len(timed)} steps" in capsys.readouterr().out
