@@ -534,6 +534,7 @@ int tq_cache_evict_workspace(const tq_cache *cache, const tq_evict_args *args, u
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_tree_workspace gives for the same arguments, with any contents; calls whose execution
  *   overlaps need one each.
  * Precision, what is not finite, and what lies in a cache where a row does not attend to it: as in tq_attend.  trees is at most 65535.
+ * No attention weights are added up: cache->scores stays as it is, and a cache that tq_cache_evict keeps at a budget has them from tq_attend only.
  */
 typedef struct tq_tree_args {
   const void *q;
@@ -578,7 +579,9 @@ int tq_tree_accept(uint32_t n, const tq_cache *const *caches, const tq_accept_ar
  *   min_p: the tokens with w >= min_p (0 or less: all).
  * tokens[r] is the first token, by number, at which the weight of the kept ones up to and with it exceeds uniform[r] times that of all kept ones (the last kept
  * one, if none does); probs[r] its share of that weight.  A temperature that is not above 0 takes the first token in order, with probability 1.
- * Weights and sums are held in 64 bits, so that what is drawn is what the formula draws; results repeat.
+ * top_p is of the weight of all tokens, beside a top_k, too: not of what top_k leaves.
+ * Weights and sums are held in 64 bits.  Sums whose order is not fixed, top_p's and those of the tokens next to a cut, are of whole numbers, in units of 2^-45 of the largest weight for a vocabulary
+ * of 128256 (2^-41 for 2^20): they are off by at most 2^-29 (2^-22) of all weight, and results repeat.
  * A logit of -infinity or NaN is a masked token and never drawn; a row of nothing else gives token -1 with probability 0.  If there are logits of +infinity, only they have
  * weight, equal shares of it.
  *   logits: device, fp32 [rows][vocab], logits_stride elements apart (0: vocab).

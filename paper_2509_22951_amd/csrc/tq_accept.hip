@@ -28,7 +28,7 @@ static_assert(sizeof(CacheList) + sizeof(AcceptView) <= 4096, "the arguments of 
 // of all of them, in order.  A token moves to a slot no higher than its own: what a thread has written no later token of the branch is read from, and within kBatch tokens
 // it reads before it writes.  So the move works in place, without a barrier.
 //
-// Bound: launch, and the chain masks -> branch -> page -> piece -> store: 16 layers of one tree of 8 nodes, 8 heads of 64, 2.0..4.1 us; 28 layers of 16 trees of 64 nodes, 8 heads of 128, 8.8 us.  A launch per
+// Bound: launch, and the chain masks -> branch -> page -> piece -> store: 16 layers of one tree of 8 nodes, 8 heads of 64, 4.2 us (least: 1.8); 28 layers of 16 trees of 64 nodes, 8 heads of 128, 9.0 us (8.6).  A launch per
 // layer would cost 28 times the first of these.
 __global__ __launch_bounds__(kAcceptThreads) void k_tree_accept(CacheList caches, AcceptView a) {
   const uint32_t lane = threadIdx.x & 63, t = blockIdx.z;

@@ -35,8 +35,8 @@ struct HeadNormView {
 // beside slot -> angles -> rotation.
 //
 // With a norm (NORM is HeadNormView) the mean of a query's or key's squares is a sum over the same group of lanes, taken before the rotation;
-// its weights are requested with the values, which hides all of it: 8192 rows of 24 + 16 heads of 128, bf16 pages, fp32 q in and out, 302 MB, 66..70 us, 4.5 TB/s; 16 rows
-// of 32 + 16 heads of 64 3.4..3.9 us.
+// its weights are requested with the values, which hides all of it: 8192 rows of 24 + 16 heads of 128, bf16 pages, fp32 q in and out, 302 MB, 68.8 us (least: 66.2), 4.4 TB/s; 8-bit
+// pages, 286 MB, 77.1 us (75.7); 16 rows of 32 + 16 heads of 64 3.7 us (3.3).
 template <int LANES, bool INT8, bool Q16, typename NORM>
 __global__ __launch_bounds__(kAppendThreads) void k_cache_append(CacheView c, AppendView a, NORM norm) {
   constexpr bool kNormed = std::is_same_v<NORM, HeadNormView>;

@@ -183,7 +183,8 @@ constexpr uint32_t kPart = 4 * CHUNKS * kThreads;
 
 // First launch: the first token of every part, and an open row's weights; bins and counters are cleared for the next ones.
 //
-// Bound: a launch and a wait for few rows (1.9..3.0 us); for many the reading, and of open rows the weights, which a part's largest logit has to be known for: 64 rows of 128256 8.2 us, 14.1..15.2 if open.
+// Bound: a launch and a wait for few rows (3.1 us, at the least 2.0); for many the reading, and of open rows the weights, which a part's largest logit has to be known for: 64 rows of 128256 7.9 us (7.6),
+// 16.4 (14.6) if open.
 template <int CHUNKS>
 __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
   __shared__ uint64_t slots[kThreads / 64];
@@ -224,8 +225,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_first(SampleView a) {
 
 // Second launch, for rows with top_k or top_p: tokens and weights of every bin.  PER tokens a thread.  Tokens without any weight, the masked ones, are left out: none of them is drawn
 // whether it is kept or not, and a cut among all that a grammar leaves of a vocabulary, one row of 128256 logits with ten that are not masked and top_k 50, took 3800 us to find, now 17.
-// Counts and weights are added up in LDS first, whole numbers both.  Bound: the parts' first keys -> weights -> additions in LDS -> additions in memory, behind each other: one row of 32000 logits 4.6..4.9 us with two
-// tokens a thread, 6.7 with eight, which is what the many rows take that fill the card anyway (16 of 128256 6.2..8.4).
+// Counts and weights are added up in LDS first, whole numbers both.  Bound: the parts' first keys -> weights -> additions in LDS -> additions in memory, behind each other: one row of 32000 logits 5.0 us (least: 4.5) with two
+// tokens a thread, 6.7 with eight, which is what the many rows take that fill the card anyway (16 of 128256 8.0, 7.6).
 template <int PER>
 __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleView a) {
   __shared__ uint64_t slots[kBinThreads / 64], lds_mass[kBins];
@@ -306,8 +307,9 @@ __device__ __forceinline__ Cut find_cut(const uint32_t (&count)[PER], const uint
 // are summed, the first one draws.  A whole row (WHOLE: no more than a part) needs no launch ahead: its first token, its bins and its list are the workgroup's own.
 //
 // Bound: a chain of waits.  One row: logits, bins and the parts' first keys 1.8 us -> the bin of the cut 1.3 -> weights, sums over the workgroup, the list's stores 2.3 -> count 0.5 -> the parts' sums and lists 2 ->
-// the cut within the bin 1 -> the part that has the token 0.9 -> its logits, weights once more 1.6: 11.5..11.9 us for 32000 tokens, beside 2.1..3.0 and 4.0..4.9 of the launches ahead.  16 rows of 128256 with filters:
-// 20.2 us, beside 4.1 and 6.2 (read: 8 MB, 1.3 us).  64 open rows: 7.6 us, beside 14.1 of the first launch (33 MB read, 5.2 us; weights, some 30 instructions of 64 bits each, 10) and 2.5.  Why three
+// the cut within the bin 1 -> the part that has the token 0.9 -> its logits, weights once more 1.6: 11.7 us (least: 11.0) for 32000 tokens, beside 3.1 (2.0) and 5.0 (4.5) of the launches ahead.  16 rows of 128256 with filters:
+// 20.2 us (19.8), beside 4.8 (4.2) and 8.0 (7.6) (read: 8 MB, 1.3 us).  64 open rows: 7.2 us (6.7), beside 16.4 (14.6) of the first launch (33 MB read, 5.2 us; weights, some 30 instructions of 64 bits
+// each, 10) and 4.5 (3.8).  Why three
 // launches: a row's largest logit is needed ahead of every weight that is compared with others, and the cut ahead of every sum; one workgroup per row, that needs no launch between, took 284 us for the first and 621 for the second.
 template <int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
@@ -469,7 +471,8 @@ __global__ __launch_bounds__(kThreads) void k_sample_draw(SampleView a) {
     }
   }
 
-  // The cut within the bin: narrowed by a 256th of the bin, then by 8 bits of the key at a time, until few enough are left to compare all with each other.
+  // The cut within the bin: narrowed by a 256th of the bin, then by 8 bits of the key at a time, until few enough are left to compare all with each other.  One workgroup goes through all that the bin has
+  // each time, keys beyond kListed from memory: a row of 128256 equal logits takes 4400 us with top_k and 5300 with top_p, one at a temperature of 100 455.
   uint64_t last = 0;   // tokens of at least this key are kept
   constexpr int kPer = kMostParts / kThreads;
   double weights[kPer];

@@ -116,9 +116,9 @@ __device__ __forceinline__ Cutting cutting_of(uint32_t all, uint32_t units, uint
 __device__ __forceinline__ uint32_t rounded(uint32_t units, const Cutting& cut) { return cut.whole ? (units + cut.share - 1) / cut.share * cut.share : units; }
 
 // Bound: reading the cache while there are few columns, the matrix and vector units from two or three column tiles on.  24 heads on 8, 128 dims, bf16, 16 x 16384 tokens (171 us at the
-// 6.3 TB/s of a read stream): 5 nodes, one tile, 201 us, 5.3 TB/s; 16 nodes, three, 255; 20 nodes, four, 287.  1 x 131000 tokens, 64 nodes, 12 tiles: 291 us, with q in bf16 229: three parts
-// of q and three of the weights are 6 products where 2 would be the least; the matrix units are busy 59 % of the time.  16 x 32700 tokens in 8 bits (176 us): 5 nodes 237, 16 nodes 365..371
-// (weights of two f16 parts, at one exponent for all of a column's: 236, 351; what is 2^-37 of the largest then begins to be lost).
+// 6.3 TB/s of a read stream): 5 nodes, one tile, 202 us, 5.3 TB/s; 16 nodes, three, 246; 20 nodes, four, 280.  1 x 131000 tokens, 64 nodes, 12 tiles: 280 us, with q in bf16 224: three parts
+// of q and three of the weights are 6 products where 2 would be the least; the matrix units are busy 62 % of the time.  16 x 32700 tokens in 8 bits (176 us): 5 nodes 235, 16 nodes 369: vector
+// instructions are issued 79 % of the time (weights of two f16 parts, at one exponent for all of a column's: 236, 351; what is 2^-37 of the largest then begins to be lost).
 //
 // Why so: 12 wavefronts, because of the 168 registers that leaves each (8 of them with everything in registers and no LDS: 80 us for the ragged batch, 368, 462; 4 with three column tiles each and
 // 512 registers: 131, 420, 813; the sums' copies between the two halves of the register file cost more than the reads that were saved).  Two stages of 64 KB: what is on its way
@@ -277,7 +277,8 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
     uint64_t mark_of_lane = 0;
 #pragma unroll
     for (int b = 0; b < S::kOwnBlocks; ++b) {
-      // In place of rows that are not there the block's first one comes again, so that what is beside a weight of zero is a number.
+      // In place of rows that are not there the block's first one comes again, so that beside a weight of zero lies what is attended to anyway; in place of a page that is not there, page 0: if that
+      // holds something that is not finite, the tokens are taken again.
       const uint32_t newest = max(p.s.of.end, 1u) - 1, slot = first + 16 * b, from = min(slot, newest & ~(uint32_t)(S::kOwnRows < 16 ? S::kOwnRows - 1 : 15)), id = scalar(ids[b]);
       const uint32_t page = id < c.n_pages ? id : 0, in_page = from & page_mask, limit = id < c.n_pages && slot < p.s.of.end ? min(p.s.of.end - slot, 16u) : 0u;
       some |= id >= c.n_pages;
@@ -722,8 +723,8 @@ __global__ __launch_bounds__((Shape<DIM, INT8>::kThreads)) void k_attend_tree(Ca
 #undef ARGUMENTS_ANEW
 
 // The parts of what lies in more than one share, joined in the order of the line: a wavefront per 16 columns and 16 dims.  A launch of its own, which a sequence that can not be longer than a stage
-// does without: the last workgroup to arrive would join alone what all of them share here.  Bound: its launch and three waits behind each other, 4.9 us for the ragged batch of 8 x 15 nodes; the parts, 25 MB written and
-// read, 9.8 us for 64 nodes over 131000 tokens.
+// does without: the last workgroup to arrive would join alone what all of them share here.  Bound: its launch and three waits behind each other, 5.1 us (least: 4.8) for the ragged batch of 8 x 15 nodes; the parts, 25 MB written and
+// read, 11.4 us (9.6) for 64 nodes over 131000 tokens.
 template <int DIM, bool INT8>
 __global__ __launch_bounds__(256) void k_join_tree(CacheView c, TreeView a) {
   using S = Shape<DIM, INT8>;
@@ -746,7 +747,7 @@ __global__ __launch_bounds__(256) void k_join_tree(CacheView c, TreeView a) {
     auto part_of = [&](uint32_t group) { return a.partials + ((uint64_t)(2 * group + (group * share >= first ? 0 : 1)) * a.tiles + tile) * S::kPartial; };
     float m = -INFINITY, sum_p = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr uint32_t kAhead = 8;   // (four, sixteen: ragged batch 5.4, 6.4 us in place of 4.9; 64 nodes over 131000 tokens 14.2, 11.0 in place of 9.8)
+    constexpr uint32_t kAhead = 8;   // (four, sixteen: ragged batch 5.4, 6.4 us at the least in place of 4.9; 64 nodes over 131000 tokens 14.2, 11.0 in place of 9.8)
     for (uint32_t group = group0; group <= group1; group += kAhead) {
       float4 v[kAhead];
       float2 st[kAhead];
