@@ -529,7 +529,7 @@ int tq_cache_evict_workspace(const tq_cache *cache, const tq_evict_args *args, u
  *   masks[t][i]; keys and values of head h / (heads / kv_heads).
  * Slots beyond the capacity and pages that are not there are masked.  A row with nothing to attend to, of a sequence that is not there, and one that is padding, are zero.
  *   q: device, TQ_FP32 or TQ_BF16 (q_type) [trees * nodes][heads * head_dim]; an fp32 q is used unrounded over a TQ_BF16 cache, over a TQ_INT8 one
- *   to 2^-24 of its head's largest value.  out: device, bf16 [trees * nodes][heads * head_dim].
+ *   to 2^-24 of its head's largest value, and weights times values' scales to 2^-133.  out: device, bf16 [trees * nodes][heads * head_dim].
  *   Neither lengths, sizes, seqs, masks nor q are written while the call runs.
  *   workspace: device, 16-byte aligned, of at least the size tq_attend_tree_workspace gives for the same arguments, with any contents; calls whose execution
  *   overlaps need one each.

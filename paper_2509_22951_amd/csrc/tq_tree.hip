@@ -10,7 +10,7 @@
 // whose three digits of 8 bits meet the keys in integer products, which are exact; values become bf16 in registers, which is exact too, and meet weights (times the
 // values' scales) of three bf16 parts.  (q loses up to 2^-24 of its largest value in every dim: over 256 dims that is 2^-8 of what
 // the rounding of a key to 8 bits in the one dim of that value can be.  Weights are never brought to one exponent like that: in a dim where the tokens
-// of the largest ones have values of zero, the small ones are all there is.)
+// of the largest ones have values of zero, the small ones are all there is.  Parts end at 2^-133, bf16's last step: a weight times a scale has all 24 bits from 2^-110 on.)
 #include <algorithm>
 
 #include "tq_cache_view.h"

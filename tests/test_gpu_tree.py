@@ -403,6 +403,18 @@ def test_a_small_weight_where_the_larger_one_has_a_value_of_zero(larger, gap, fa
     assert (want[..., 1::2] > 0).all() and ((out - want).abs() <= want * (2.0 ** -8 + 2.0 ** -14)).all()      # (no value is negative: the terms add up to the result)
 
 
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -60, 2.0 ** -110])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_values_scales_that_are_all_small(size, dim):
+    """8 bits.  Weights times scales end at 2^-133, half a step of which is 2^-24 of 2^-110: of 105 tokens, the largest with a weight of 1, 105 * 2^-24 of it, below 2^-17."""
+    p = Paged(2, 8, dim=dim, kind="int8", seed=dim)
+    p.v_scale.fill_(size)
+    q, bits, lengths = queries(2, 5, 6, dim, 1), bits_of(random_parents(2, 5)), ints([100, 60])
+    out, want = run(p, q, lengths, bits).cpu().double(), tree_reference(p, q, lengths, bits)
+    p.v = p.v.abs()
+    assert ((out - want).abs() <= want.abs() * 2.0 ** -8 + tree_reference(p, q, lengths, bits) * 2.0 ** -14 + 127 * size * 2.0 ** -17).all()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_logits_that_rise_from_token_to_token(kind, dim):
